@@ -1,0 +1,133 @@
+/*
+ * cudallm_layers.h -- C ABI of the operators around the matrix products of a
+ * transformer block, for its training step and for single tokens:
+ *
+ *   cudallm_layernorm_rows       LayerNorm over the rows of a matrix, with the rows'
+ *   cudallm_layernorm_rows_bwd   statistics, and its gradient
+ *   cudallm_grad_norm            the norm of all gradients of a model together,
+ *   cudallm_grad_clip            and scaling them down to a limit
+ *   cudallm_grad_clip_norm
+ *
+ * The general conventions of cudallm_gemm.h hold (device pointers owned by the
+ * caller, pitches in elements, calls enqueue on `stream` and return without
+ * synchronising, negative CUDALLM_ERR_* status codes, argument errors found
+ * before any CUDA call, compute capability 10.0 only, no CPU fallback).  All
+ * pointers must belong to the device that is current at the call, and `stream`
+ * to that device.
+ *
+ * What a call needs beside its operands it takes as `scratch` from the caller
+ * (16-byte aligned, at least what the matching _scratch_bytes function says; its
+ * contents before the call do not matter and are not kept).  Nothing else is
+ * shared between calls: calls with different scratch and outputs may run at the
+ * same time on several streams, and every call can be captured into a CUDA graph
+ * (a graph keeps using the scratch of the captured call).  Given the same inputs
+ * on the same kind of device, a call returns the same bits each time.
+ */
+#ifndef CUDALLM_LAYERS_H
+#define CUDALLM_LAYERS_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "cudallm_gemm.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element types of these operators: CUDALLM_F32, CUDALLM_BF16 and */
+#define CUDALLM_F16 2
+
+/*
+ * LayerNorm of every row of a matrix.
+ *     mean_r = (1/n) sum_i x[r][i]
+ *     var_r  = (1/n) sum_i (x[r][i] - mean_r)^2              (biased estimate)
+ *     rstd_r = 1 / sqrt(var_r + eps)
+ *     y[r][i] = (x[r][i] - mean_r) * rstd_r * gamma[i] + beta[i]
+ *   x, y        : dtype, rows x n, row pitches ldx, ldy >= n; padding columns of y
+ *                 are left untouched; y may be x itself (with ldy == ldx), else the
+ *                 two must not overlap
+ *   gamma, beta : param_dtype, n elements each, or NULL for all ones / all zeros
+ *   mean, rstd  : fp32, rows elements each, written; either may be NULL
+ *   dtype       : CUDALLM_F32, _BF16 or _F16; param_dtype: dtype or CUDALLM_F32
+ * Statistics and arithmetic are in fp32 (mean and variance from differences to a
+ * first mean, so a mean far above the spread costs no accuracy of y); y is
+ * rounded once.  A row that holds an infinity or a NaN gives NaN in that row only.
+ * rows == 0 or n == 0: success, nothing written.
+ * Errors: INVALID_DIM (negative, rows or n >= 2^31 - 1024, eps negative or not
+ * finite), INVALID_LD, INVALID_DTYPE, INVALID_POINTER (x or y NULL), MISALIGNED
+ * (a pointer off its element size), UNSUPPORTED_DEVICE, CUDA.
+ */
+int cudallm_layernorm_rows(const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd,
+                           int64_t rows, int64_t n, int64_t ldx, int64_t ldy, int dtype, int param_dtype,
+                           float eps, void *stream);
+
+/*
+ * Gradient of cudallm_layernorm_rows.  With xhat = (x - mean) * rstd, g = dy * gamma:
+ *     dx     = rstd * (g - (1/n) sum_i g_i - xhat * (1/n) sum_i g_i xhat_i)
+ *     dgamma = sum_rows dy * xhat,   dbeta = sum_rows dy
+ *   dy, x, dx     : dtype, rows x n, pitches lddy, ldx, lddx >= n; dx may be dy or x
+ *                   itself (with the same pitch), else must not overlap them
+ *   gamma         : param_dtype, or NULL for all ones
+ *   mean, rstd    : fp32, rows elements, as the forward call wrote them
+ *   dgamma, dbeta : param_dtype, n elements each, overwritten (no accumulation)
+ * Any of dx, dgamma and dbeta may be NULL: that gradient is not computed.
+ * Sums are in fp32 in a fixed order; every result is rounded once.  rows == 0
+ * gives dgamma = dbeta = 0; n == 0 is a no-op.
+ * Errors: as the forward call; WORKSPACE (scratch NULL, misaligned or smaller than
+ * cudallm_layernorm_rows_bwd_scratch_bytes; not needed when dgamma and dbeta are NULL).
+ */
+int cudallm_layernorm_rows_bwd(const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd,
+                               void *dx, void *dgamma, void *dbeta, int64_t rows, int64_t n,
+                               int64_t lddy, int64_t ldx, int64_t lddx, int dtype, int param_dtype,
+                               void *scratch, size_t scratch_bytes, void *stream);
+/* 0 for sizes that the call refuses */
+size_t cudallm_layernorm_rows_bwd_scratch_bytes(int64_t rows, int64_t n);
+
+/* One gradient of a model: n contiguous elements of `dtype` at `data` (device).
+ * `out` is where the scaled gradient goes: `data` itself (in place) or a buffer of
+ * the same size and type that overlaps no other one of the list. */
+typedef struct cudallm_tensor {
+    void *data;
+    void *out;
+    int64_t n;
+    int32_t dtype;
+    int32_t reserved;     /* 0 */
+} cudallm_tensor;
+
+/*
+ * norm[0] = sqrt(sum over all tensors and elements of g^2), fp32 on the DEVICE.
+ *   tensors : HOST array of `count` entries, read during the call only (the
+ *             entries travel in the kernels' parameters); `out` is not used
+ * Squares are summed in fp32 in groups of eight and from there in double; a group
+ * whose sum leaves the middle of the fp32 range is summed in double, so the norm is
+ * right for gradients of any size as long as it fits into fp32 itself.  An infinity
+ * gives inf, a NaN gives NaN.  No tensors, or only empty ones, give 0.  Entries with
+ * n == 0 are skipped (their pointers may be NULL).
+ * Errors: INVALID_DIM (count or an n negative, count > 2^24, n > 2^40, more than 2^44
+ * elements), INVALID_POINTER, INVALID_DTYPE, MISALIGNED, WORKSPACE,
+ * UNSUPPORTED_DEVICE, CUDA.
+ */
+int cudallm_grad_norm(const cudallm_tensor *tensors, int64_t count, float *norm, void *scratch, size_t scratch_bytes,
+                      void *stream);
+/*
+ * out = g * c for every tensor, with c = min(1, max_norm / (norm[0] + eps)), the
+ * product rounded once.  `norm` is on the device, from cudallm_grad_norm or, for
+ * gradients spread over several devices, combined by the caller.  A NaN norm makes
+ * all gradients NaN, an infinite one makes the finite ones zero.  Tensors that are
+ * scaled in place stay untouched (no bit changes) where c is 1.
+ * Errors: as cudallm_grad_norm; INVALID_DIM also for max_norm or eps negative or NaN.
+ */
+int cudallm_grad_clip(const cudallm_tensor *tensors, int64_t count, const float *norm, float max_norm, float eps,
+                      void *stream);
+/* Both, in fewer launches: norm[0] is written, then the gradients are scaled. */
+int cudallm_grad_clip_norm(const cudallm_tensor *tensors, int64_t count, float max_norm, float eps, float *norm,
+                           void *scratch, size_t scratch_bytes, void *stream);
+/* Scratch of cudallm_grad_norm and cudallm_grad_clip_norm for lists of up to `count` tensors. */
+size_t cudallm_grad_norm_scratch_bytes(int64_t count);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* CUDALLM_LAYERS_H */

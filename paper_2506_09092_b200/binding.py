@@ -11,7 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 
-F32, BF16 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 VARIANT_AUTO = -1
 
 OK = 0
@@ -38,7 +38,15 @@ _vp = ctypes.c_void_p
 _int = ctypes.c_int
 _sz = ctypes.c_size_t
 
-# name -> (restype, argtypes); mirrors include/cudallm_gemm.h and include/cudallm_tasks.h
+_f32 = ctypes.c_float
+
+
+class CTensor(ctypes.Structure):
+    """``cudallm_tensor`` of include/cudallm_layers.h."""
+    _fields_ = [("data", _vp), ("out", _vp), ("n", _i64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+# name -> (restype, argtypes); mirrors include/cudallm_gemm.h, cudallm_tasks.h and cudallm_layers.h
 SIGNATURES = {
     "cudallm_gemm_bf16": (_int, [_vp, _vp, _vp] + [_i64] * 6 + [_int, _vp]),
     "cudallm_gemm_f32": (_int, [_vp, _vp, _vp] + [_i64] * 6 + [_int, _vp]),
@@ -73,6 +81,13 @@ SIGNATURES = {
     "cudallm_sum_f32": (_int, [_vp, _i64, _vp, _vp]),
     "cudallm_dot_f32": (_int, [_vp, _vp, _i64, _vp, _vp]),
     "cudallm_layernorm_f32": (_int, [_vp, _vp, _vp, _vp, _i64, _i64, ctypes.c_float, _vp]),
+    "cudallm_layernorm_rows": (_int, [_vp] * 6 + [_i64] * 4 + [_int, _int, _f32, _vp]),
+    "cudallm_layernorm_rows_bwd": (_int, [_vp] * 8 + [_i64] * 5 + [_int, _int, _vp, _sz, _vp]),
+    "cudallm_layernorm_rows_bwd_scratch_bytes": (_sz, [_i64, _i64]),
+    "cudallm_grad_norm": (_int, [ctypes.POINTER(CTensor), _i64, _vp, _vp, _sz, _vp]),
+    "cudallm_grad_clip": (_int, [ctypes.POINTER(CTensor), _i64, _vp, _f32, _f32, _vp]),
+    "cudallm_grad_clip_norm": (_int, [ctypes.POINTER(CTensor), _i64, _f32, _f32, _vp, _vp, _sz, _vp]),
+    "cudallm_grad_norm_scratch_bytes": (_sz, [_i64]),
 }
 
 
@@ -110,6 +125,25 @@ def _p(x):
     if hasattr(x, "ctypes"):
         return x.ctypes.data
     raise TypeError(type(x))
+
+
+_torch = None
+
+
+def _d(x):
+    """Address of a device buffer: int, None, or a CUDA tensor on the current device."""
+    if x is None or isinstance(x, int):
+        return x
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    dev = x.get_device()
+    if dev < 0:
+        raise TypeError("a CUDA tensor is needed, not one in host memory")
+    if dev != _torch.cuda.current_device():
+        raise ValueError(f"the tensor is on device {dev}, the current device is {_torch.cuda.current_device()}")
+    return x.data_ptr()
 
 
 def _s(stream):
@@ -172,6 +206,95 @@ def layernorm_f32(x, gamma, beta, y, batch, m, eps=1e-5, stream=None, check=True
     """Task 4: LayerNorm of ``batch`` samples of ``m`` fp32 elements; gamma / beta may be None."""
     st = lib().cudallm_layernorm_f32(_p(x), _p(gamma), _p(beta), _p(y), batch, m, ctypes.c_float(eps), _s(stream))
     return _check(st, "cudallm_layernorm_f32", check)
+
+
+def layernorm_rows(x, gamma, beta, y, mean, rstd, rows, n, ldx, ldy, dtype, param_dtype, eps=1e-5, stream=None,
+                   check=True):
+    """LayerNorm of every row of x (rows x n); gamma, beta, mean and rstd may be None."""
+    st = lib().cudallm_layernorm_rows(_d(x), _d(gamma), _d(beta), _d(y), _d(mean), _d(rstd), rows, n, ldx, ldy,
+                                      dtype, param_dtype, eps, _s(stream))
+    return _check(st, "cudallm_layernorm_rows", check)
+
+
+def layernorm_rows_bwd_scratch_bytes(rows, n) -> int:
+    return int(lib().cudallm_layernorm_rows_bwd_scratch_bytes(rows, n))
+
+
+def layernorm_rows_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, rows, n, lddy, ldx, lddx, dtype, param_dtype,
+                       scratch, scratch_bytes, stream=None, check=True):
+    """Gradient of ``layernorm_rows``; dx, dgamma and dbeta may each be None."""
+    st = lib().cudallm_layernorm_rows_bwd(_d(dy), _d(x), _d(gamma), _d(mean), _d(rstd), _d(dx), _d(dgamma), _d(dbeta),
+                                          rows, n, lddy, ldx, lddx, dtype, param_dtype, _d(scratch), scratch_bytes,
+                                          _s(stream))
+    return _check(st, "cudallm_layernorm_rows_bwd", check)
+
+
+class TensorTable:
+    """The gradients of a model as the C calls take them: a host array of ``cudallm_tensor``.
+    Built once for gradients that stay where they are; holds references to the tensors."""
+
+    def __init__(self, tensors, outs=None):
+        tensors = list(tensors)
+        outs = tensors if outs is None else list(outs)
+        if len(outs) != len(tensors):
+            raise ValueError("as many outputs as tensors are needed")
+        codes = {"torch.float32": F32, "torch.bfloat16": BF16, "torch.float16": F16}
+        self.count = len(tensors)
+        self.array = (CTensor * max(self.count, 1))()
+        self._keep = (tensors, outs)
+        spans, inputs = [], []
+        for e, t, o in zip(self.array, tensors, outs):
+            if t.dtype != o.dtype or t.numel() != o.numel():
+                raise ValueError("an output has the size and type of its tensor")
+            if str(t.dtype) not in codes:
+                raise TypeError(f"fp32, bf16 or fp16 gradients, not {t.dtype}")
+            if not (t.is_contiguous() and o.is_contiguous()):
+                raise ValueError("contiguous tensors are needed")
+            e.data, e.out, e.n, e.dtype = _d(t), _d(o), t.numel(), codes[str(t.dtype)]
+            if e.n:
+                nbytes = e.n * t.element_size()
+                spans.append((e.out, e.out + nbytes, e.data != e.out))
+                inputs.append((e.data, e.data + nbytes, False))
+        spans.sort()
+        for (_, end, _a), (begin, _, _b) in zip(spans, spans[1:]):
+            if begin < end:
+                raise ValueError("two outputs overlap (a gradient that is scaled in place may be listed once)")
+        # an output beside its tensor must not lie over any other input either
+        merged = sorted([(b, e, 1) for b, e, apart in spans if apart] + [(b, e, 0) for b, e, _ in inputs])
+        end = [0, 0]
+        for b, e, kind in merged:
+            if b < end[1 - kind]:
+                raise ValueError("an output overlaps a gradient of the list")
+            end[kind] = max(end[kind], e)
+
+
+def tensor_table(tensors, outs=None) -> TensorTable:
+    """Table of contiguous CUDA tensors for the grad_* calls; ``outs`` where the scaled ones go
+    (None: in place)."""
+    return TensorTable(tensors, outs)
+
+
+def grad_norm_scratch_bytes(table) -> int:
+    return int(lib().cudallm_grad_norm_scratch_bytes(table if isinstance(table, int) else table.count))
+
+
+def grad_norm(table, norm, scratch, scratch_bytes, stream=None, check=True):
+    """norm[0] (device fp32) = the norm of all tensors of the table together."""
+    st = lib().cudallm_grad_norm(table.array, table.count, _d(norm), _d(scratch), scratch_bytes, _s(stream))
+    return _check(st, "cudallm_grad_norm", check)
+
+
+def grad_clip(table, norm, max_norm, eps=1e-6, stream=None, check=True):
+    """Scale the table's tensors by min(1, max_norm / (norm[0] + eps))."""
+    st = lib().cudallm_grad_clip(table.array, table.count, _d(norm), max_norm, eps, _s(stream))
+    return _check(st, "cudallm_grad_clip", check)
+
+
+def grad_clip_norm(table, max_norm, eps, norm, scratch, scratch_bytes, stream=None, check=True):
+    """``grad_norm`` and ``grad_clip`` together."""
+    st = lib().cudallm_grad_clip_norm(table.array, table.count, max_norm, eps, _d(norm), _d(scratch), scratch_bytes,
+                                      _s(stream))
+    return _check(st, "cudallm_grad_clip_norm", check)
 
 
 def gemm_bf16_batched(A, B, C, M, N, K, lda, ldb, ldc, strideA, strideB, strideC, batch,

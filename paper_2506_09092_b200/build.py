@@ -19,6 +19,7 @@ NVCC_FLAGS = [
     "-O3", "-std=c++17", "-lineinfo",
     "-shared", "-Xcompiler", "-fPIC",
     "-cudart", "static",
+    "--threads", "0",               # the translation units at the same time
 ]
 
 
@@ -54,7 +55,7 @@ def sources():
 
 
 def _deps():
-    return sources() + sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + HEADERS + [TABLE_INC]
+    return sources() + sorted(glob.glob(os.path.join(CSRC, "*.cuh")) + glob.glob(os.path.join(CSRC, "*.h"))) + HEADERS + [TABLE_INC]
 
 
 def up_to_date() -> bool:

@@ -21,6 +21,7 @@
 #include "umma_tf32.cuh"
 #include "mhsa.cuh"
 #include "hbm_tasks.cuh"
+#include "runtime.h"
 
 using namespace cudallm;
 
@@ -1765,7 +1766,7 @@ const char *cudallm_strerror(int status)
     case CUDALLM_ERR_INVALID_POINTER: return "null operand pointer for a non-empty problem";
     case CUDALLM_ERR_INVALID_DIM: return "negative or too large dimension";
     case CUDALLM_ERR_INVALID_LD: return "leading dimension smaller than the row length, or overlapping batch items of C";
-    case CUDALLM_ERR_INVALID_DTYPE: return "out_dtype must be 0 (fp32) or 1 (bf16)";
+    case CUDALLM_ERR_INVALID_DTYPE: return "an element type that this entry point does not take";
     case CUDALLM_ERR_INVALID_VARIANT: return "variant id out of range";
     case CUDALLM_ERR_UNSUPPORTED_SHAPE: return "the requested variant cannot run this problem";
     case CUDALLM_ERR_UNSUPPORTED_DEVICE: return "the current device is not compute capability 10.0";
@@ -1786,3 +1787,18 @@ int cudallm_version(void)
 }  // extern "C"
 
 #include "hbm_tasks_host.cuh"
+
+// ------------------------------------ what the other translation units use --
+namespace cudallm {
+
+int rt_cuda_fail(cudaError_t e, const char *where) { return cuda_fail(e, where); }
+
+int rt_current_device(int *dev_out, int *sm_count)
+{
+    std::lock_guard<std::mutex> lock(g_mutex);
+    const int st = task_device(dev_out);
+    if (st == CUDALLM_OK) *sm_count = g_dev[*dev_out].sm_count;
+    return st;
+}
+
+}  // namespace cudallm

@@ -1,0 +1,377 @@
+// Entry points of include/cudallm_layers.h that are bound by memory bandwidth: LayerNorm over
+// rows (forward, backward), and the norm and clipping of a list of gradients.
+#include "../../include/cudallm_layers.h"
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "runtime.h"
+#include "layernorm_rows.cuh"
+#include "grad_norm.cuh"
+
+using namespace cudallm;
+
+namespace {
+
+constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
+constexpr int64_t kMaxElems = int64_t(1) << 46;
+
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int elem_size(int dtype) { return dtype == CUDALLM_F32 ? 4 : 2; }
+inline bool valid_dtype(int d) { return d == CUDALLM_F32 || d == CUDALLM_BF16 || d == CUDALLM_F16; }
+inline bool off(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+
+// --------------------------------------------------------------- LayerNorm --
+// What both directions check; dtype-sized operands first.
+int check_ln(int64_t rows, int64_t n, int dtype, int param_dtype)
+{
+    if (!valid_dtype(dtype) || (param_dtype != dtype && param_dtype != CUDALLM_F32)) return CUDALLM_ERR_INVALID_DTYPE;
+    if (rows < 0 || n < 0 || rows > kMaxDim || n > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
+    return CUDALLM_OK;
+}
+int check_ld(int64_t rows, int64_t n, int64_t ld)
+{
+    if (ld < n) return CUDALLM_ERR_INVALID_LD;
+    if (ld > kMaxElems || (long double)rows * ld > (long double)kMaxElems) return CUDALLM_ERR_INVALID_DIM;
+    return CUDALLM_OK;
+}
+
+// CTAs of `kernel` that one SM holds (asked once per kernel).
+template <typename Kernel>
+int resident(Kernel kernel, int threads, std::atomic<int> &cache, int *out)
+{
+    int v = cache.load(std::memory_order_relaxed);
+    if (v == 0) {
+        RT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&v, kernel, threads, 0));
+        if (v < 1) v = 1;
+        cache.store(v, std::memory_order_relaxed);
+    }
+    *out = v;
+    return CUDALLM_OK;
+}
+
+template <typename T, int VEC, int TPR, int E>
+int launch_ln(const LnRowsParams &p, int sms, cudaStream_t stream)
+{
+    static std::atomic<int> occ{0};
+    auto kernel = layernorm_rows_kernel<T, VEC, TPR, E / VEC>;
+    int per_sm = 0;
+    const int st = resident(kernel, ln_threads(TPR), occ, &per_sm);
+    if (st != CUDALLM_OK) return st;
+    const int64_t grid = std::min<int64_t>(cdiv(p.rows, ln_threads(TPR) / TPR), (int64_t)sms * per_sm);
+    return rt_launch(kernel, dim3((unsigned)grid), ln_threads(TPR), 0, stream, p);
+}
+
+// Threads per row and elements per thread by the row's length.  16 elements a thread keep a row,
+// the next one, gamma and beta in registers with two CTAs or more on an SM; short rows are a
+// warp's, which needs no barrier.
+template <typename T, int VEC>
+int launch_ln_by_length(const LnRowsParams &p, int sms, cudaStream_t stream)
+{
+    if (p.n <= 256) return launch_ln<T, VEC, 32, 8>(p, sms, stream);
+    if (p.n <= 1024) return launch_ln<T, VEC, 32, 32>(p, sms, stream);
+    if (p.n <= 2048) return launch_ln<T, VEC, 128, 16>(p, sms, stream);
+    if (p.n <= 4096) return launch_ln<T, VEC, 256, 16>(p, sms, stream);
+    if (p.n <= 8192) return launch_ln<T, VEC, 512, 16>(p, sms, stream);
+    if (p.n <= 16384) return launch_ln<T, VEC, 1024, 16>(p, sms, stream);
+    const int64_t grid = std::min<int64_t>(p.rows, (int64_t)sms * 2);
+    return rt_launch(layernorm_long_kernel<T>, dim3((unsigned)grid), kLnLongThreads, 0, stream, p);
+}
+
+// Partial rows of dgamma and dbeta at most: enough CTAs for eight per SM where rows are short,
+// one per SM where a CTA's partial rows are long (they are written once and read once).
+int64_t ln_max_parts(int64_t n)
+{
+    return std::min<int64_t>(1184, std::max<int64_t>(148, int64_t(148) * 8192 / std::max<int64_t>(n, 1)));
+}
+
+template <typename T, int VEC, int TPR, int E>
+int launch_ln_bwd(const LnRowsParams &p, int sms, cudaStream_t stream, int *parts)
+{
+    static std::atomic<int> occ{0};
+    auto kernel = layernorm_rows_bwd_kernel<T, VEC, TPR, E / VEC>;
+    int per_sm = 0;
+    const int st = resident(kernel, ln_threads(TPR), occ, &per_sm);
+    if (st != CUDALLM_OK) return st;
+    int64_t grid = std::min<int64_t>(cdiv(p.rows, ln_threads(TPR) / TPR), (int64_t)sms * per_sm);
+    grid = std::min(grid, ln_max_parts(p.n));
+    *parts = (int)grid;
+    return rt_launch(kernel, dim3((unsigned)grid), ln_threads(TPR), 0, stream, p);
+}
+
+template <typename T, int VEC>
+int launch_ln_bwd_by_length(const LnRowsParams &p, int sms, cudaStream_t stream, int *parts)
+{
+    if (p.n <= 256) return launch_ln_bwd<T, VEC, 32, 8>(p, sms, stream, parts);
+    if (p.n <= 1024) return launch_ln_bwd<T, VEC, 128, 8>(p, sms, stream, parts);
+    if (p.n <= 2048) return launch_ln_bwd<T, VEC, 256, 8>(p, sms, stream, parts);
+    if (p.n <= 4096) return launch_ln_bwd<T, VEC, 512, 8>(p, sms, stream, parts);
+    if (p.n <= 8192) return launch_ln_bwd<T, VEC, 512, 16>(p, sms, stream, parts);
+    if (p.n <= 16384) return launch_ln_bwd<T, VEC, 1024, 16>(p, sms, stream, parts);
+    // long rows: the column sums first (dx may lie over x or dy), then dx
+    if (p.partials) {
+        const int64_t g = std::min<int64_t>({int64_t(148), int64_t(p.rows), std::max<int64_t>(1, 148 * 8 / cdiv(p.n, 256))});
+        *parts = (int)g;
+        const int st = rt_launch(layernorm_long_columns_kernel<T>, dim3((unsigned)cdiv(p.n, 256), (unsigned)g), 256, 0,
+                                 stream, p);
+        if (st != CUDALLM_OK) return st;
+    }
+    if (!p.y) return CUDALLM_OK;
+    const int64_t grid = std::min<int64_t>(p.rows, (int64_t)sms * 2);
+    return rt_launch(layernorm_long_dx_kernel<T>, dim3((unsigned)grid), kLnLongThreads, 0, stream, p);
+}
+
+// 16-byte accesses need bases and pitches on 16-byte boundaries and whole pieces per row.
+template <typename T, typename... Ptrs>
+bool pieces_ok(int64_t n, std::initializer_list<int64_t> lds, Ptrs... ptrs)
+{
+    uintptr_t all = 0;
+    for (const void *q : {static_cast<const void *>(ptrs)...}) all |= reinterpret_cast<uintptr_t>(q);
+    int64_t m = n;
+    for (int64_t ld : lds) m |= ld;
+    return (all & 15) == 0 && m % ElemVec<T>::kN == 0;
+}
+
+template <typename T>
+int run_ln(const LnRowsParams &p, int sms, cudaStream_t stream)
+{
+    if (pieces_ok<T>(p.n, {p.ldx, p.ldy}, p.x, p.y))
+        return launch_ln_by_length<T, ElemVec<T>::kN>(p, sms, stream);
+    return launch_ln_by_length<T, 1>(p, sms, stream);
+}
+template <typename T>
+int run_ln_bwd(const LnRowsParams &p, int sms, cudaStream_t stream, int *parts)
+{
+    if (pieces_ok<T>(p.n, {p.ldx, p.lddy, p.y ? p.ldy : p.ldx}, p.x, p.dy, p.y))
+        return launch_ln_bwd_by_length<T, ElemVec<T>::kN>(p, sms, stream, parts);
+    return launch_ln_bwd_by_length<T, 1>(p, sms, stream, parts);
+}
+
+// -------------------------------------------------------------- gradients --
+constexpr int64_t kGradMaxTensors = int64_t(1) << 24;
+constexpr int64_t kGradMaxElems = int64_t(1) << 44;
+constexpr int kGradSmallCap = 64;          // entries of the two parameter blocks: 2 KB and 30 KB (a
+constexpr int kGradLargeCap = 1024;        // kernel's parameters end at 32,764 bytes)
+static_assert(sizeof(GradList<kGradLargeCap>) + 64 <= 32764, "kernel parameters");
+
+int check_grads(const cudallm_tensor *t, int64_t count, bool scaled, int64_t *total, int64_t *live)
+{
+    if (count < 0 || count > kGradMaxTensors) return CUDALLM_ERR_INVALID_DIM;
+    if (count > 0 && !t) return CUDALLM_ERR_INVALID_POINTER;
+    *total = *live = 0;
+    for (int64_t i = 0; i < count; ++i) {
+        if (t[i].n < 0 || t[i].n > (int64_t(1) << 40)) return CUDALLM_ERR_INVALID_DIM;
+        if (!valid_dtype(t[i].dtype)) return CUDALLM_ERR_INVALID_DTYPE;
+        if (t[i].n == 0) continue;
+        if (!t[i].data || (scaled && !t[i].out)) return CUDALLM_ERR_INVALID_POINTER;
+        if (off(t[i].data, elem_size(t[i].dtype)) || (scaled && off(t[i].out, elem_size(t[i].dtype))))
+            return CUDALLM_ERR_MISALIGNED;
+        *total += t[i].n;
+        ++*live;
+        if (*total > kGradMaxElems) return CUDALLM_ERR_INVALID_DIM;
+    }
+    return CUDALLM_OK;
+}
+
+// Elements per chunk: about eight chunks per SM, within 2048 (eight elements a thread) and
+// 16384 (enough 16-byte loads in a row to pay for finding the chunk).
+unsigned grad_chunk_elems(int64_t total, int sms)
+{
+    const int64_t c = cdiv(cdiv(total, (int64_t)sms * 8), 2048) * 2048;
+    return (unsigned)std::min<int64_t>(16384, std::max<int64_t>(2048, c));
+}
+
+// Fills `l` with entries from t[*next] on; returns the CTAs that its chunks occupy (0: no entry left).
+template <int CAP>
+unsigned fill_list(GradList<CAP> &l, const cudallm_tensor *t, int64_t count, int64_t *next, unsigned chunk, int sms)
+{
+    l.count = 0;
+    l.chunk = chunk;
+    uint64_t chunks = 0;                                  // <= 2^44 / 16384 + 2^24: fits 32 bits
+    int64_t i = *next;
+    for (; i < count && l.count < CAP; ++i) {
+        if (t[i].n == 0) continue;
+        const uint64_t c = (uint64_t)cdiv(t[i].n, chunk);
+        l.data[l.count] = t[i].data;
+        l.out[l.count] = t[i].out;
+        l.n[l.count] = t[i].n;
+        l.dtype[l.count] = (unsigned char)t[i].dtype;
+        l.first[l.count] = (unsigned)chunks;
+        ++l.count;
+        chunks += c;
+    }
+    l.first[l.count] = (unsigned)chunks;
+    *next = i;
+    return (unsigned)std::min<uint64_t>(chunks, (uint64_t)std::min(kGradMaxBlocks, 8 * sms));
+}
+
+// Launches that write at most CAP entries' partial sums each, then either the join (norm only)
+// or the scaling launches.
+template <int CAP>
+int run_grads(const cudallm_tensor *t, int64_t count, int64_t total, int sms, bool want_norm, bool want_scale,
+              float max_norm, float eps, float *norm, double *partials, size_t max_partials, cudaStream_t stream)
+{
+    GradList<CAP> l;
+    const unsigned chunk = grad_chunk_elems(total, sms);
+    int64_t next = 0;
+    int nparts = 0, st = CUDALLM_OK;
+    bool one = false;
+    unsigned grid = 0;
+    if (want_norm) {
+        while (next < count && (grid = fill_list(l, t, count, &next, chunk, sms)) != 0) {
+            if ((size_t)nparts + grid > max_partials) return CUDALLM_ERR_WORKSPACE;
+            st = rt_launch(grad_norm_kernel<CAP>, dim3(grid), kGradThreads, 0, stream, l, partials + nparts);
+            if (st != CUDALLM_OK) return st;
+            one = nparts == 0;
+            nparts += (int)grid;
+        }
+        // one list: the scaling launch joins the partial sums itself
+        one = one && want_scale;
+        if (!one) {
+            st = rt_launch(grad_norm_join_kernel, dim3(1), kGradThreads, 0, stream, (const double *)partials, nparts, norm);
+            if (st != CUDALLM_OK) return st;
+        }
+    }
+    if (!want_scale) return CUDALLM_OK;
+    next = 0;
+    while (next < count && (grid = fill_list(l, t, count, &next, chunk, sms)) != 0) {
+        st = rt_launch(grad_scale_kernel<CAP>, dim3(grid), kGradThreads, 0, stream, l,
+                       one ? (const double *)partials : (const double *)nullptr, nparts, norm, max_norm, eps);
+        if (st != CUDALLM_OK) return st;
+    }
+    return CUDALLM_OK;
+}
+
+int grads(const cudallm_tensor *t, int64_t count, bool want_norm, bool want_scale, float max_norm, float eps,
+          float *norm, void *scratch, size_t scratch_bytes, void *stream_v)
+{
+    int64_t total = 0, live = 0;
+    int st = check_grads(t, count, want_scale, &total, &live);
+    if (st != CUDALLM_OK) return st;
+    if (want_scale && (!(max_norm >= 0.f) || !(eps >= 0.f))) return CUDALLM_ERR_INVALID_DIM;
+    if (!norm) return CUDALLM_ERR_INVALID_POINTER;
+    if (off(norm, 4)) return CUDALLM_ERR_MISALIGNED;
+    if (want_norm && (!scratch || off(scratch, 16) || scratch_bytes < cudallm_grad_norm_scratch_bytes(live)))
+        return CUDALLM_ERR_WORKSPACE;
+    if (live == 0 && !want_norm) return CUDALLM_OK;
+    int dev = 0, sms = 0;
+    st = rt_current_device(&dev, &sms);
+    if (st != CUDALLM_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    double *partials = static_cast<double *>(scratch);
+    const size_t cap = scratch_bytes / sizeof(double);
+    if (live <= kGradSmallCap)
+        return run_grads<kGradSmallCap>(t, count, total, sms, want_norm, want_scale, max_norm, eps, norm, partials, cap, stream);
+    return run_grads<kGradLargeCap>(t, count, total, sms, want_norm, want_scale, max_norm, eps, norm, partials, cap, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int cudallm_layernorm_rows(const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd,
+                           int64_t rows, int64_t n, int64_t ldx, int64_t ldy, int dtype, int param_dtype, float eps,
+                           void *stream_v)
+{
+    int st = check_ln(rows, n, dtype, param_dtype);
+    if (st != CUDALLM_OK) return st;
+    if (!(eps >= 0.f) || !(eps <= 3.0e38f)) return CUDALLM_ERR_INVALID_DIM;
+    if (rows == 0 || n == 0) return CUDALLM_OK;
+    if ((st = check_ld(rows, n, ldx)) != CUDALLM_OK || (st = check_ld(rows, n, ldy)) != CUDALLM_OK) return st;
+    if (!x || !y) return CUDALLM_ERR_INVALID_POINTER;
+    const int es = elem_size(dtype), ps = elem_size(param_dtype);
+    if (off(x, es) || off(y, es) || off(gamma, ps) || off(beta, ps) || off(mean, 4) || off(rstd, 4))
+        return CUDALLM_ERR_MISALIGNED;
+    int dev = 0, sms = 0;
+    if ((st = rt_current_device(&dev, &sms)) != CUDALLM_OK) return st;
+    LnRowsParams p{};
+    p.x = x; p.gamma = gamma; p.beta = beta; p.y = y; p.mean = mean; p.rstd = rstd;
+    p.ldx = ldx; p.ldy = ldy;
+    p.rows = (int)rows; p.n = (int)n; p.param_dtype = param_dtype;
+    p.eps = eps;
+    p.inv_n = 1.f / (float)n;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    if (dtype == CUDALLM_F32) return run_ln<float>(p, sms, stream);
+    if (dtype == CUDALLM_BF16) return run_ln<__nv_bfloat16>(p, sms, stream);
+    return run_ln<__half>(p, sms, stream);
+}
+
+size_t cudallm_layernorm_rows_bwd_scratch_bytes(int64_t rows, int64_t n)
+{
+    if (rows < 0 || n < 0 || rows > kMaxDim || n > kMaxDim) return 0;
+    return (size_t)(std::min<int64_t>(std::max<int64_t>(rows, 1), ln_max_parts(n)) * n * 8);
+}
+
+int cudallm_layernorm_rows_bwd(const void *dy, const void *x, const void *gamma, const float *mean, const float *rstd,
+                               void *dx, void *dgamma, void *dbeta, int64_t rows, int64_t n, int64_t lddy, int64_t ldx,
+                               int64_t lddx, int dtype, int param_dtype, void *scratch, size_t scratch_bytes,
+                               void *stream_v)
+{
+    int st = check_ln(rows, n, dtype, param_dtype);
+    if (st != CUDALLM_OK) return st;
+    if (n == 0 || (!dx && !dgamma && !dbeta)) return CUDALLM_OK;
+    const int es = elem_size(dtype), ps = elem_size(param_dtype);
+    if (rows > 0) {
+        if ((st = check_ld(rows, n, lddy)) != CUDALLM_OK || (st = check_ld(rows, n, ldx)) != CUDALLM_OK) return st;
+        if (dx && (st = check_ld(rows, n, lddx)) != CUDALLM_OK) return st;
+        if (!dy || !x || !mean || !rstd) return CUDALLM_ERR_INVALID_POINTER;
+    }
+    if (off(dy, es) || off(x, es) || off(dx, es) || off(gamma, ps) || off(dgamma, ps) || off(dbeta, ps) || off(mean, 4)
+        || off(rstd, 4))
+        return CUDALLM_ERR_MISALIGNED;
+    const bool sums = dgamma || dbeta;
+    if (sums && (!scratch || off(scratch, 16) || scratch_bytes < cudallm_layernorm_rows_bwd_scratch_bytes(rows, n)))
+        return CUDALLM_ERR_WORKSPACE;
+    if (rows == 0 && !sums) return CUDALLM_OK;
+    int dev = 0, sms = 0;
+    if ((st = rt_current_device(&dev, &sms)) != CUDALLM_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    int parts = 0;
+    if (rows > 0) {
+        LnRowsParams p{};
+        p.x = x; p.dy = dy; p.gamma = gamma; p.y = dx;
+        p.mean = const_cast<float *>(mean); p.rstd = const_cast<float *>(rstd);
+        p.partials = sums ? static_cast<float *>(scratch) : nullptr;
+        p.ldx = ldx; p.lddy = lddy; p.ldy = lddx;
+        p.rows = (int)rows; p.n = (int)n; p.param_dtype = param_dtype;
+        p.inv_n = 1.f / (float)n;
+        if (dtype == CUDALLM_F32) st = run_ln_bwd<float>(p, sms, stream, &parts);
+        else if (dtype == CUDALLM_BF16) st = run_ln_bwd<__nv_bfloat16>(p, sms, stream, &parts);
+        else st = run_ln_bwd<__half>(p, sms, stream, &parts);
+        if (st != CUDALLM_OK) return st;
+    }
+    if (!sums) return CUDALLM_OK;
+    LnJoinParams j{};
+    j.partials = static_cast<const float *>(scratch);
+    j.dgamma = dgamma; j.dbeta = dbeta;
+    j.n = (int)n; j.parts = parts; j.param_dtype = param_dtype;
+    return rt_launch(layernorm_join_kernel, dim3((unsigned)cdiv(n, 32), 2), 1024, 0, stream, j);
+}
+
+size_t cudallm_grad_norm_scratch_bytes(int64_t count)
+{
+    if (count < 0 || count > kGradMaxTensors) return 0;
+    const int64_t launches = std::max<int64_t>(1, cdiv(count, kGradLargeCap));     // of up to kGradLargeCap tensors
+    return (size_t)(launches * kGradMaxBlocks) * sizeof(double);
+}
+
+int cudallm_grad_norm(const cudallm_tensor *tensors, int64_t count, float *norm, void *scratch, size_t scratch_bytes,
+                      void *stream)
+{
+    return grads(tensors, count, true, false, 0.f, 0.f, norm, scratch, scratch_bytes, stream);
+}
+
+int cudallm_grad_clip(const cudallm_tensor *tensors, int64_t count, const float *norm, float max_norm, float eps,
+                      void *stream)
+{
+    return grads(tensors, count, false, true, max_norm, eps, const_cast<float *>(norm), nullptr, 0, stream);
+}
+
+int cudallm_grad_clip_norm(const cudallm_tensor *tensors, int64_t count, float max_norm, float eps, float *norm,
+                           void *scratch, size_t scratch_bytes, void *stream)
+{
+    return grads(tensors, count, true, true, max_norm, eps, norm, scratch, scratch_bytes, stream);
+}
+
+}  // extern "C"
