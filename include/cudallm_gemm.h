@@ -376,16 +376,22 @@ int cudallm_shutdown(void);
  *   CUDALLM_DEBUG_LAYERNORM_PATH         value = 0: cudallm_layernorm_f32 picks its
  *       kernel by size; 1: always the two-kernel path; 2: the one-pass kernel
  *       whenever the samples fit in shared memory, however small.
+ *   CUDALLM_DEBUG_SKIP_NEXT_XATTN_LOADS  value != 0: the next cudallm_xattn_fwd or
+ *       cudallm_xattn_bwd kernel with in-kernel waits (not the one for single tokens)
+ *       loads nothing, so its waits run out after the limit; as above it returns
+ *       normally with unspecified output, and the status says so.  One launch only.
  * Returns CUDALLM_ERR_INVALID_VARIANT for an unknown `what` or value.
  */
 #define CUDALLM_DEBUG_WAIT_LIMIT_NS          1
 #define CUDALLM_DEBUG_MISS_NEXT_SPLIT_FLAGS  2
 #define CUDALLM_DEBUG_LAYERNORM_PATH         3
+#define CUDALLM_DEBUG_SKIP_NEXT_XATTN_LOADS  4
 int cudallm_debug_set(int what, unsigned long long value);
 
 /*
  * Synchronises `stream`, then reads and clears the device status word that
- * kernels set when one of their bounded waits ran out.  *code is CUDALLM_OK or
+ * kernels set when one of their bounded waits ran out (the cross-attention
+ * kernels' word is one per device, whatever their stream).  *code is CUDALLM_OK or
  * CUDALLM_ERR_DEVICE_TIMEOUT, *detail identifies the wait (role and barrier).
  * Returns *code (or CUDALLM_ERR_CUDA if the synchronisation failed).
  */

@@ -7,6 +7,8 @@
  *   cudallm_grad_norm            the norm of all gradients of a model together,
  *   cudallm_grad_clip            and scaling them down to a limit
  *   cudallm_grad_clip_norm
+ *   cudallm_xattn_fwd            attention of one sequence's queries to the states of
+ *   cudallm_xattn_bwd            another, of another length, and its gradient
  *
  * The general conventions of cudallm_gemm.h hold (device pointers owned by the
  * caller, pitches in elements, calls enqueue on `stream` and return without
@@ -125,6 +127,60 @@ int cudallm_grad_clip_norm(const cudallm_tensor *tensors, int64_t count, float m
                            void *scratch, size_t scratch_bytes, void *stream);
 /* Scratch of cudallm_grad_norm and cudallm_grad_clip_norm for lists of up to `count` tensors. */
 size_t cudallm_grad_norm_scratch_bytes(int64_t count);
+
+/*
+ * Cross attention: batch items of q_rows queries attend to kv_rows states of their
+ * own.  For batch item b, query head h and key head g = h / (q_heads / kv_heads):
+ *     S = scale * Q[b, :, h] K[b, :, g]^T,  P = softmax(S) over the keys < kv_lens[b]
+ *     O[b, :, h] = P V[b, :, g],   lse[b][h][i] = log(sum_j exp(S_ij))
+ * Sizes, strides (ELEMENTS; order: batch item, row, head; the head_dim values of a
+ * row and head are contiguous) and scale come in a struct, which a program fills in
+ * once for a layer.  Q and O (and their gradients) use q_stride and o_stride; K, V
+ * and their gradients k_stride and v_stride, so rows x heads and heads x rows
+ * layouts, and keys and values side by side in one tensor, are all taken as they lie.
+ *   dtype    : CUDALLM_BF16 or CUDALLM_F16, of all operands and results but lse (fp32,
+ *              contiguous [batch][q_heads][q_rows])
+ *   head_dim : a multiple of 8, at most 128; kv_heads divides q_heads
+ *   strides  : multiples of 8 for dimensions larger than 1, and such that no two
+ *              elements share a place (the stride of a dimension of size 1 is not used)
+ *   scale    : finite, >= 0 (usually 1 / sqrt(head_dim))
+ */
+typedef struct cudallm_xattn_shape {
+    int64_t batch, q_rows, kv_rows, q_heads, kv_heads, head_dim;
+    int64_t q_stride[3], k_stride[3], v_stride[3], o_stride[3];
+    int32_t dtype;
+    float scale;
+} cudallm_xattn_shape;
+
+/*
+ * Forward.
+ *   q, k, v : read only, 16-byte aligned;  o : written, must not overlap them
+ *   kv_lens : int32, `batch` elements on the device, the states of each item that
+ *             exist (values outside 0..kv_rows are taken as the nearer end), or NULL:
+ *             all.  States from kv_lens[b] on are never used, whatever they hold
+ *             (NaN and infinities too).
+ *   lse     : written unless NULL (the backward call needs it)
+ * An item without states (kv_lens[b] == 0, or kv_rows == 0) gives O = 0 and
+ * lse = -inf.  A query, key or value that is not finite makes the rows that see it
+ * not finite, and no others.
+ * Products are taken on the tensor cores with fp32 accumulation; maxima and sums in
+ * fp32; the probabilities are rounded to dtype for the second product (relative to a
+ * maximum: at most 2^-8 (bf16) or 2^-11 (fp16) of themselves each), O once.
+ * Kernels: (q_heads / kv_heads) * q_rows <= 16 rows per key head (single tokens) take
+ * a kernel that reads every K and V once and splits the keys over the GPU; longer
+ * queries one that owns 256 query rows of a head per CTA, split over the keys where
+ * there are too few of those.  Split calls join in a second launch.
+ * batch, q_rows or q_heads == 0 or head_dim == 0: success, nothing written.
+ * Errors: INVALID_POINTER (shape, q or o NULL; k or v NULL with kv_rows > 0),
+ * INVALID_DTYPE, INVALID_DIM (negative or too large sizes, kv_heads not a divisor of
+ * q_heads, scale), INVALID_LD (strides), UNSUPPORTED_SHAPE (head_dim, strides or
+ * pointers off 16 bytes), MISALIGNED (kv_lens, lse), WORKSPACE, UNSUPPORTED_DEVICE,
+ * CUDA.
+ */
+int cudallm_xattn_fwd(const cudallm_xattn_shape *shape, const void *q, const void *k, const void *v,
+                      const int32_t *kv_lens, void *o, float *lse, void *scratch, size_t scratch_bytes, void *stream);
+/* 0 where no scratch is needed (it may be NULL then), and for shapes that the call refuses */
+size_t cudallm_xattn_fwd_scratch_bytes(const cudallm_xattn_shape *shape);
 
 #ifdef __cplusplus
 }

@@ -46,6 +46,34 @@ class CTensor(ctypes.Structure):
     _fields_ = [("data", _vp), ("out", _vp), ("n", _i64), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class XattnShape(ctypes.Structure):
+    """``cudallm_xattn_shape`` of include/cudallm_layers.h: sizes, strides and scale of a layer."""
+    _fields_ = [(n, _i64) for n in ("batch", "q_rows", "kv_rows", "q_heads", "kv_heads", "head_dim")] + [
+        (n, _i64 * 3) for n in ("q_stride", "k_stride", "v_stride", "o_stride")] + [
+        ("dtype", ctypes.c_int32), ("scale", _f32)]
+
+    @classmethod
+    def of(cls, q, k, v, o, scale=None):
+        """From tensors (batch, rows, heads, head_dim) of any strides with a contiguous last dimension;
+        scale defaults to 1 / sqrt(head_dim)."""
+        if not (q.shape == o.shape and k.shape == v.shape and q.dim() == k.dim() == 4
+                and q.shape[0] == k.shape[0] and q.shape[3] == k.shape[3]):
+            raise ValueError("q and o (batch, q_rows, q_heads, head_dim), k and v (batch, kv_rows, kv_heads, head_dim)")
+        if not (q.dtype == k.dtype == v.dtype == o.dtype):
+            raise TypeError("operands of one type are needed")
+        code = {"torch.bfloat16": BF16, "torch.float16": F16}.get(str(q.dtype))
+        if code is None:
+            raise TypeError(f"bf16 or fp16 operands, not {q.dtype}")
+        if any(t.shape[3] > 1 and t.stride(3) != 1 for t in (q, k, v, o)):
+            raise ValueError("the last dimension must be contiguous")
+        s = cls(batch=q.shape[0], q_rows=q.shape[1], kv_rows=k.shape[1], q_heads=q.shape[2], kv_heads=k.shape[2],
+                head_dim=q.shape[3], dtype=code,
+                scale=(q.shape[3] ** -0.5 if q.shape[3] else 1.0) if scale is None else scale)
+        for field, t in (("q_stride", q), ("k_stride", k), ("v_stride", v), ("o_stride", o)):
+            setattr(s, field, (_i64 * 3)(*t.stride()[:3]))
+        return s
+
+
 # name -> (restype, argtypes); mirrors include/cudallm_gemm.h, cudallm_tasks.h and cudallm_layers.h
 SIGNATURES = {
     "cudallm_gemm_bf16": (_int, [_vp, _vp, _vp] + [_i64] * 6 + [_int, _vp]),
@@ -88,6 +116,8 @@ SIGNATURES = {
     "cudallm_grad_clip": (_int, [ctypes.POINTER(CTensor), _i64, _vp, _f32, _f32, _vp]),
     "cudallm_grad_clip_norm": (_int, [ctypes.POINTER(CTensor), _i64, _f32, _f32, _vp, _vp, _sz, _vp]),
     "cudallm_grad_norm_scratch_bytes": (_sz, [_i64]),
+    "cudallm_xattn_fwd": (_int, [ctypes.POINTER(XattnShape)] + [_vp] * 7 + [_sz, _vp]),
+    "cudallm_xattn_fwd_scratch_bytes": (_sz, [ctypes.POINTER(XattnShape)]),
 }
 
 
@@ -297,6 +327,18 @@ def grad_clip_norm(table, max_norm, eps, norm, scratch, scratch_bytes, stream=No
     return _check(st, "cudallm_grad_clip_norm", check)
 
 
+def xattn_fwd_scratch_bytes(shape) -> int:
+    return int(lib().cudallm_xattn_fwd_scratch_bytes(shape))
+
+
+def xattn_fwd(shape, q, k, v, kv_lens, o, lse, scratch, scratch_bytes, stream=None, check=True):
+    """Cross attention: o = softmax(scale q k^T) v over the first kv_lens[b] states of each batch item
+    (``shape``: an XattnShape); kv_lens, lse and scratch may be None."""
+    st = lib().cudallm_xattn_fwd(shape, _d(q), _d(k), _d(v), _d(kv_lens), _d(o), _d(lse), _d(scratch), scratch_bytes,
+                                 _s(stream))
+    return _check(st, "cudallm_xattn_fwd", check)
+
+
 def gemm_bf16_batched(A, B, C, M, N, K, lda, ldb, ldc, strideA, strideB, strideC, batch,
                       out_dtype, stream=None, check=True):
     st = lib().cudallm_gemm_bf16_batched(_p(A), _p(B), _p(C), M, N, K, lda, ldb, ldc,
@@ -425,7 +467,7 @@ def shutdown(check=True):
     return _check(lib().cudallm_shutdown(), "cudallm_shutdown", check)
 
 
-DEBUG_WAIT_LIMIT_NS, DEBUG_MISS_NEXT_SPLIT_FLAGS, DEBUG_LAYERNORM_PATH = 1, 2, 3
+DEBUG_WAIT_LIMIT_NS, DEBUG_MISS_NEXT_SPLIT_FLAGS, DEBUG_LAYERNORM_PATH, DEBUG_SKIP_NEXT_XATTN_LOADS = 1, 2, 3, 4
 
 
 def debug_set(what: int, value: int, check=True):

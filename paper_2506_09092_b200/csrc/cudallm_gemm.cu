@@ -429,6 +429,7 @@ std::mutex g_mutex;
 // waits for, so that every such wait runs out (the self-test of the timeout path).
 std::atomic<unsigned long long> g_wait_limit_ns{kWaitLimitNs};
 std::atomic<int> g_skew_next_flags{0};
+std::atomic<int> g_skip_next_loads{0};     // the next cross-attention launch loads nothing
 std::atomic<int> g_layernorm_path{0};      // 0 = by size, 1 = always the two-kernel path, 2 = one-pass whenever it fits
 
 // The workspace calls on `stream` use: the one attached to the stream, else the device's.
@@ -1730,6 +1731,9 @@ int cudallm_debug_set(int what, unsigned long long value)
         if (value > 2) return CUDALLM_ERR_INVALID_VARIANT;
         g_layernorm_path.store((int)value);
         return CUDALLM_OK;
+    case CUDALLM_DEBUG_SKIP_NEXT_XATTN_LOADS:
+        g_skip_next_loads.store(value ? 1 : 0);
+        return CUDALLM_OK;
     default:
         return CUDALLM_ERR_INVALID_VARIANT;
     }
@@ -1747,8 +1751,17 @@ int cudallm_device_status(void *stream_v, int *code, int *detail)
     std::lock_guard<std::mutex> lock(g_mutex);
     DeviceState &d = g_dev[dev];
     Workspace &w = workspace_for(d, stream);
-    if (!w.ptr) return CUDALLM_OK;                     // no kernel of ours has run yet
     int host[2] = {0, 0};
+    if (d.probed && d.supported) {                     // the attention kernels' word is not in a workspace
+        const int st = rt_xattn_status(host);
+        if (st != CUDALLM_OK) return st;
+        if (host[0] != 0) {
+            if (code) *code = host[0];
+            if (detail) *detail = host[1];
+            return host[0];
+        }
+    }
+    if (!w.ptr) return CUDALLM_OK;                     // no kernel with a workspace has run yet
     CUDA_TRY(cudaMemcpy(host, w.ptr, sizeof host, cudaMemcpyDeviceToHost));
     if (host[0] != 0) {
         // a kernel gave up: flags and counters may be stale; clear the whole header
@@ -1800,5 +1813,24 @@ int rt_current_device(int *dev_out, int *sm_count)
     if (st == CUDALLM_OK) *sm_count = g_dev[*dev_out].sm_count;
     return st;
 }
+
+int rt_encode_rows(CUtensorMap *tm, const void *base, bool f16, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
+                   int rows)
+{
+    cuuint64_t d[4], st[3];
+    for (int i = 0; i < 4; ++i) d[i] = dims[i];
+    for (int i = 0; i < 3; ++i) st[i] = strides[i];
+    const cuuint32_t box[4] = {64, 1, (cuuint32_t)rows, 1}, one[4] = {1, 1, 1, 1};
+    const CUresult r = g_encode(tm, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4,
+                                const_cast<void *>(base), d, st, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return CUDALLM_OK;
+    snprintf(g_cuda_err, sizeof g_cuda_err, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+    return CUDALLM_ERR_CUDA;
+}
+
+unsigned long long rt_wait_limit_ns() { return g_wait_limit_ns.load(); }
+bool rt_take_skip_loads() { return g_skip_next_loads.exchange(0) != 0; }
 
 }  // namespace cudallm

@@ -17,6 +17,20 @@ int rt_cuda_fail(cudaError_t e, const char *where);
 // The current device, if it can run the kernels: its index and SM count.
 int rt_current_device(int *dev, int *sm_count);
 
+// 4-D tensor map of 16-bit values (fp16 if `f16`, else bf16): inner dimension first, strides of the
+// outer three in bytes, boxes of 64 x 1 x rows x 1 values in the 128-byte swizzle, zero fill.
+// Call rt_current_device first.
+int rt_encode_rows(CUtensorMap *tm, const void *base, bool f16, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
+                   int rows);
+
+// Host-side knobs of the kernels' bounded waits (cudallm_debug_set).
+unsigned long long rt_wait_limit_ns();
+bool rt_take_skip_loads();             // one-shot: the next attention launch loads nothing
+
+// Status word of the attention kernels on device `dev` (current): read, and cleared if it was set.
+// Defined in xattn.cu.
+int rt_xattn_status(int (&host)[2]);
+
 #define RT_CUDA_TRY(expr)                                              \
     do {                                                               \
         cudaError_t e__ = (expr);                                      \

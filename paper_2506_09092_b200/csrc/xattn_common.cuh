@@ -1,0 +1,166 @@
+// What the cross-attention kernels share: parameters, 4-D TMA loads, tcgen05 wrappers with the A
+// operand in shared or tensor memory, and the tile layout.
+//
+// A tile is 128 rows of one head in shared memory, its head dimension padded with zeros to DP =
+// 64 or 128 (by TMA, which fills what lies outside the tensor): DP / 64 chunks of 64 columns, each
+// 128 rows x 128 bytes in the 128-byte swizzle.  The same bytes serve the tensor core as a K-major
+// operand (contraction over the head dimension) and as an MN-major one (contraction over the rows).
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "ptx.cuh"
+
+namespace cudallm {
+
+constexpr int kXaRows = 128;                   // rows of a tile
+constexpr int kXaChunkBytes = kXaRows * 128;   // one 64-column chunk of a tile
+
+struct XaStrides { long long b, r, h; };       // elements between batch items, rows, heads
+
+// status detail codes of the attention kernels' bounded waits: (role << 8) | barrier
+enum : int { kXaRoleLoad = 0x10, kXaRoleMma = 0x11, kXaRoleSoftmax = 0x12, kXaRoleBwd = 0x20 };
+
+__device__ __forceinline__ void xa_report(int *status, int role, int what)
+{
+    if (atomicCAS(status, 0, -9 /* CUDALLM_ERR_DEVICE_TIMEOUT */) == 0) status[1] = (role << 8) | what;
+}
+
+// One 64-column chunk of a tile: columns 64 c .., head h, rows row .. row + 127, batch item b.
+__device__ __forceinline__ void xa_load_chunk(const CUtensorMap *tm, uint32_t dst, uint32_t bar, int c, int h, int row, int b)
+{
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(c * 64), "r"(h), "r"(row), "r"(b), "r"(bar) : "memory");
+}
+template <int DP>
+__device__ __forceinline__ void xa_load_tile(const CUtensorMap *tm, uint32_t dst, uint32_t bar, int h, int row, int b)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) xa_load_chunk(tm, dst + c * kXaChunkBytes, bar, c, h, row, b);
+}
+__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+// D (tensor memory) (+)= A B with A and B in shared memory, or with A in tensor memory.
+__device__ __forceinline__ void xa_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void xa_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+
+// 128 x 128 products over the head dimension: D = A B^T, both tiles K-major.
+template <int DP>
+__device__ __forceinline__ void xa_product_nt(uint32_t d, uint32_t a_tile, uint32_t b_tile, uint32_t idesc)
+{
+    const uint64_t a0 = make_smem_desc_sw128(a_tile, 16, 1024), b0 = make_smem_desc_sw128(b_tile, 16, 1024);
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const uint64_t o = (k / 4) * (kXaChunkBytes >> 4) + (k % 4) * 2;
+        xa_mma_ss(d, a0 + o, b0 + o, idesc, k > 0);
+    }
+}
+// 128 x DP product over `ROWS` rows: D (+)= P T, P (128 x ROWS, 16-bit) in tensor memory, tile T MN-major.
+template <int ROWS>
+__device__ __forceinline__ void xa_product_tn(uint32_t d, uint32_t p_tmem, uint32_t tile, uint32_t idesc, bool accumulate)
+{
+    const uint64_t b0 = make_smem_desc_sw128(tile, kXaChunkBytes, 1024);
+#pragma unroll
+    for (int k = 0; k < ROWS / 16; ++k) xa_mma_ts(d, p_tmem + k * 8, b0 + k * (2048 >> 4), idesc, accumulate || k > 0);
+}
+
+// Instruction descriptor: kind::f16, both operands T, fp32 accumulator, A K-major, M = 128.
+template <typename T> struct XaElem;
+template <> struct XaElem<__nv_bfloat16> {
+    static constexpr uint32_t kFormat = 1;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16x2(lo, hi); }
+};
+template <> struct XaElem<__half> {
+    static constexpr uint32_t kFormat = 0;
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi)
+    {
+        uint32_t r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+};
+template <typename T>
+__host__ __device__ constexpr uint32_t xa_idesc(int n, int b_mn_major)
+{
+    return (1u << 4) | (XaElem<T>::kFormat << 7) | (XaElem<T>::kFormat << 10) | ((uint32_t)b_mn_major << 16)
+         | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(kXaRows >> 4) << 24);
+}
+
+// 32 lanes x 16 consecutive columns, registers -> tensor memory and back.
+__device__ __forceinline__ void tmem_st_32x32b_x16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+                   "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_32x32b_x16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait()
+{
+    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+// 2^x by the special-function unit (relative error ~2^-22); -inf gives 0.
+__device__ __forceinline__ float xa_exp2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Valid keys of batch item b.
+__device__ __forceinline__ int xa_keys(const int *lens, int b, int kv_rows)
+{
+    if (!lens) return kv_rows;
+    const int n = lens[b];
+    return n < 0 ? 0 : (n < kv_rows ? n : kv_rows);
+}
+
+// Zero the rows from `valid` on of a tile that TMA has written (thread t of 128 takes row t): a
+// padded row may hold anything, and 0 x NaN would reach the product's sums.  The writes must be
+// followed by fence_proxy_async_smem() before the tensor core may read them.
+template <int DP>
+__device__ __forceinline__ void xa_zero_rows(uint32_t tile, int t, int valid)
+{
+    if (t >= valid)
+#pragma unroll
+        for (int c = 0; c < DP / 64; ++c)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                st_shared_v4_b32(tile + c * kXaChunkBytes + t * 128 + k * 16, 0, 0, 0, 0);
+}
+
+// DP fp32 values of a row, scaled and rounded to T, to `dst` (D of them exist, a multiple of 8).
+template <typename T>
+__device__ __forceinline__ void xa_store_32(T *dst, const float (&v)[32], int left)
+{
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        if (g * 8 < left)
+            *reinterpret_cast<uint4 *>(dst + g * 8) =
+                make_uint4(XaElem<T>::pack(v[8 * g], v[8 * g + 1]), XaElem<T>::pack(v[8 * g + 2], v[8 * g + 3]),
+                           XaElem<T>::pack(v[8 * g + 4], v[8 * g + 5]), XaElem<T>::pack(v[8 * g + 6], v[8 * g + 7]));
+}
+
+}  // namespace cudallm
