@@ -182,6 +182,25 @@ int cudallm_xattn_fwd(const cudallm_xattn_shape *shape, const void *q, const voi
 /* 0 where no scratch is needed (it may be NULL then), and for shapes that the call refuses */
 size_t cudallm_xattn_fwd_scratch_bytes(const cudallm_xattn_shape *shape);
 
+/*
+ * Gradient of cudallm_xattn_fwd.  With P = exp(S - lse), delta_i = sum_c dO_ic O_ic:
+ *     dV = P^T dO,  dS = P * (dO V^T - delta),  dQ = scale * dS K,  dK = scale * dS^T Q
+ * with dK and dV summed over the query heads that share a key head.
+ *   o, lse      : as the forward call wrote them;  d_o : laid out like o (o_stride)
+ *   dq          : written, q_stride;  dk, dv : written, k_stride and v_stride; both or
+ *                 neither may be NULL (the states' gradients are not computed then)
+ * Results must not overlap any operand.  States from kv_lens[b] on get zero
+ * gradients; an item without states gives dQ = 0; q_rows == 0 gives dK = dV = 0.
+ * P and dS are rounded to dtype for the tensor cores (as P is in the forward call);
+ * sums are in fp32, without atomics.  For fp16 that means that a dS below 2^-14 loses
+ * relative precision and one beyond 65504 overflows: scale the loss accordingly.
+ * Errors: as the forward call.
+ */
+int cudallm_xattn_bwd(const cudallm_xattn_shape *shape, const void *q, const void *k, const void *v,
+                      const int32_t *kv_lens, const void *o, const float *lse, const void *d_o,
+                      void *dq, void *dk, void *dv, void *scratch, size_t scratch_bytes, void *stream);
+size_t cudallm_xattn_bwd_scratch_bytes(const cudallm_xattn_shape *shape);
+
 #ifdef __cplusplus
 }
 #endif

@@ -118,6 +118,8 @@ SIGNATURES = {
     "cudallm_grad_norm_scratch_bytes": (_sz, [_i64]),
     "cudallm_xattn_fwd": (_int, [ctypes.POINTER(XattnShape)] + [_vp] * 7 + [_sz, _vp]),
     "cudallm_xattn_fwd_scratch_bytes": (_sz, [ctypes.POINTER(XattnShape)]),
+    "cudallm_xattn_bwd": (_int, [ctypes.POINTER(XattnShape)] + [_vp] * 11 + [_sz, _vp]),
+    "cudallm_xattn_bwd_scratch_bytes": (_sz, [ctypes.POINTER(XattnShape)]),
 }
 
 
@@ -337,6 +339,18 @@ def xattn_fwd(shape, q, k, v, kv_lens, o, lse, scratch, scratch_bytes, stream=No
     st = lib().cudallm_xattn_fwd(shape, _d(q), _d(k), _d(v), _d(kv_lens), _d(o), _d(lse), _d(scratch), scratch_bytes,
                                  _s(stream))
     return _check(st, "cudallm_xattn_fwd", check)
+
+
+def xattn_bwd_scratch_bytes(shape) -> int:
+    return int(lib().cudallm_xattn_bwd_scratch_bytes(shape))
+
+
+def xattn_bwd(shape, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch, scratch_bytes, stream=None, check=True):
+    """Gradients of ``xattn_fwd`` (d_o laid out like o, dq like q, dk like k, dv like v); dk and dv may
+    both be None."""
+    st = lib().cudallm_xattn_bwd(shape, _d(q), _d(k), _d(v), _d(kv_lens), _d(o), _d(lse), _d(d_o), _d(dq), _d(dk), _d(dv),
+                                 _d(scratch), scratch_bytes, _s(stream))
+    return _check(st, "cudallm_xattn_bwd", check)
 
 
 def gemm_bf16_batched(A, B, C, M, N, K, lda, ldb, ldc, strideA, strideB, strideC, batch,

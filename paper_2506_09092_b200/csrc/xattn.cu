@@ -9,6 +9,7 @@
 #include "runtime.h"
 #include "xattn_fwd.cuh"
 #include "xattn_token.cuh"
+#include "xattn_bwd.cuh"
 
 using namespace cudallm;
 
@@ -24,7 +25,9 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t round_up(int64_t a, int64_t b) { return cdiv(a, b) * b; }
 inline bool off(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 
-bool is_empty(const cudallm_xattn_shape &s) { return s.batch == 0 || s.q_rows == 0 || s.q_heads == 0 || s.head_dim == 0; }
+// Nothing to read or write at all; no queries.
+bool is_void(const cudallm_xattn_shape &s) { return s.batch == 0 || s.q_heads == 0 || s.head_dim == 0; }
+bool is_empty(const cudallm_xattn_shape &s) { return is_void(s) || s.q_rows == 0; }
 
 // Strides of a (batch, rows, heads, head_dim) operand: multiples of 8, no two elements in one place.
 int check_strides(const int64_t (&st)[3], int64_t batch, int64_t rows, int64_t heads, int64_t dim)
@@ -56,15 +59,18 @@ int check_shape(const cudallm_xattn_shape *sp)
     for (int64_t v : {s.batch, s.q_rows, s.kv_rows, s.q_heads, s.kv_heads, s.head_dim})
         if (v < 0 || v > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
     if (!(s.scale >= 0.f) || !(s.scale <= 3.0e38f)) return CUDALLM_ERR_INVALID_DIM;
-    if (is_empty(s)) return CUDALLM_OK;
+    if (is_void(s)) return CUDALLM_OK;
     if (s.kv_heads == 0 || s.q_heads % s.kv_heads) return CUDALLM_ERR_INVALID_DIM;
     if (s.head_dim % 8 || s.head_dim > 128) return CUDALLM_ERR_UNSUPPORTED_SHAPE;
     if ((long double)s.batch * s.q_heads * cdiv(s.q_rows, kXaRows) > (long double)kMaxDim
         || (long double)s.batch * s.kv_heads * cdiv(s.kv_rows, kXaRows) > (long double)kMaxDim)
         return CUDALLM_ERR_INVALID_DIM;
     if ((long double)s.batch * s.q_heads * s.q_rows * s.head_dim > (long double)kMaxElems) return CUDALLM_ERR_INVALID_DIM;
-    int st = check_strides(s.q_stride, s.batch, s.q_rows, s.q_heads, s.head_dim);
-    if (st == CUDALLM_OK) st = check_strides(s.o_stride, s.batch, s.q_rows, s.q_heads, s.head_dim);
+    int st = CUDALLM_OK;
+    if (s.q_rows > 0) {
+        st = check_strides(s.q_stride, s.batch, s.q_rows, s.q_heads, s.head_dim);
+        if (st == CUDALLM_OK) st = check_strides(s.o_stride, s.batch, s.q_rows, s.q_heads, s.head_dim);
+    }
     if (s.kv_rows > 0) {
         if (st == CUDALLM_OK) st = check_strides(s.k_stride, s.batch, s.kv_rows, s.kv_heads, s.head_dim);
         if (st == CUDALLM_OK) st = check_strides(s.v_stride, s.batch, s.kv_rows, s.kv_heads, s.head_dim);
@@ -206,6 +212,42 @@ int run_fwd(const cudallm_xattn_shape &s, const FwdPlan &f, const void *q, const
     return join<T>(s, f, o_part, lse_part, o, lse, stream);
 }
 
+template <int DP, typename T>
+int run_bwd(const cudallm_xattn_shape &s, const void *q, const void *k, const void *v, const int32_t *lens, const void *o,
+            const float *lse, const void *d_o, void *dq, void *dk, void *dv, float *delta, int dev, cudaStream_t stream)
+{
+    using L = XaBwdSmem<DP>;
+    static std::atomic<bool> done_dq[kRtMaxDevices] = {}, done_dkv[kRtMaxDevices] = {};
+    int st;
+    if ((st = allow_smem(xattn_dq_kernel<DP, T>, L::kBytes, done_dq, dev)) != CUDALLM_OK
+        || (st = allow_smem(xattn_dkv_kernel<DP, T>, L::kBytes, done_dkv, dev)) != CUDALLM_OK)
+        return st;
+    const bool f16 = s.dtype == CUDALLM_F16;
+    CUtensorMap tq, tk, tv, tdo;
+    if ((st = encode(&tq, q, k, f16, s.q_stride, s.batch, s.q_rows, s.q_heads, s.head_dim)) != CUDALLM_OK
+        || (st = encode(&tk, k, q, f16, s.k_stride, s.batch, s.kv_rows, s.kv_heads, s.head_dim)) != CUDALLM_OK
+        || (st = encode(&tv, v, q, f16, s.v_stride, s.batch, s.kv_rows, s.kv_heads, s.head_dim)) != CUDALLM_OK
+        || (st = encode(&tdo, d_o, k, f16, s.o_stride, s.batch, s.q_rows, s.q_heads, s.head_dim)) != CUDALLM_OK)
+        return st;
+    XaBwdParams p{};
+    p.o = o; p.d_o = d_o; p.dq = dq; p.dk = dk; p.dv = dv; p.lse = lse; p.delta = delta; p.lens = lens;
+    p.sq = strides(s.q_stride); p.sk = strides(s.k_stride); p.sv = strides(s.v_stride); p.so = strides(s.o_stride);
+    p.q_rows = (int)s.q_rows; p.kv_rows = (int)s.kv_rows; p.q_heads = (int)s.q_heads; p.kv_heads = (int)s.kv_heads;
+    p.group = (int)(s.q_heads / s.kv_heads); p.batch = (int)s.batch; p.head_dim = (int)s.head_dim;
+    p.q_tiles = (int)cdiv(s.q_rows, kXaRows); p.kv_tiles = (int)cdiv(s.kv_rows, kXaRows);
+    p.scale = s.scale; p.scale_log2 = scale_log2(s);
+    if ((st = status_word(dev, &p.status)) != CUDALLM_OK) return st;
+    p.wait_limit_ns = rt_wait_limit_ns();
+    p.skip_loads = rt_take_skip_loads();
+    if (s.q_rows > 0)
+        st = rt_launch(xattn_dq_kernel<DP, T>, dim3((unsigned)((int64_t)p.q_tiles * s.q_heads * s.batch)), kXaBwdThreads,
+                       (size_t)L::kBytes, stream, tq, tk, tv, tdo, p);
+    if (st != CUDALLM_OK || !dk || s.kv_rows == 0) return st;
+    p.skip_loads = 0;
+    return rt_launch(xattn_dkv_kernel<DP, T>, dim3((unsigned)((int64_t)p.kv_tiles * s.kv_heads * s.batch)), kXaBwdThreads,
+                     (size_t)L::kBytes, stream, tq, tk, tv, tdo, p);
+}
+
 }  // namespace
 
 namespace cudallm {
@@ -254,6 +296,41 @@ int cudallm_xattn_fwd(const cudallm_xattn_shape *shape, const void *q, const voi
                     : run_fwd<64, __nv_bfloat16>(s, f, q, k, v, kv_lens, o, lse, scr, dev, stream);
     return wide ? run_fwd<128, __half>(s, f, q, k, v, kv_lens, o, lse, scr, dev, stream)
                 : run_fwd<64, __half>(s, f, q, k, v, kv_lens, o, lse, scr, dev, stream);
+}
+
+size_t cudallm_xattn_bwd_scratch_bytes(const cudallm_xattn_shape *shape)
+{
+    if (check_shape(shape) != CUDALLM_OK || is_empty(*shape)) return 0;
+    return (size_t)(shape->batch * shape->q_heads * shape->q_rows) * sizeof(float);
+}
+
+int cudallm_xattn_bwd(const cudallm_xattn_shape *shape, const void *q, const void *k, const void *v, const int32_t *kv_lens,
+                      const void *o, const float *lse, const void *d_o, void *dq, void *dk, void *dv, void *scratch,
+                      size_t scratch_bytes, void *stream_v)
+{
+    int st = check_shape(shape);
+    if (st != CUDALLM_OK) return st;
+    const cudallm_xattn_shape &s = *shape;
+    const bool queries = s.q_rows > 0, kv = s.kv_rows > 0;
+    if (is_void(s) || (!queries && !kv)) return CUDALLM_OK;
+    if ((queries && (!q || !o || !lse || !d_o || !dq)) || (kv && (!k || !v || !dk != !dv))) return CUDALLM_ERR_INVALID_POINTER;
+    if (off(kv_lens, 4) || off(lse, 4)) return CUDALLM_ERR_MISALIGNED;
+    if ((queries && (off(q, 16) || off(o, 16) || off(d_o, 16) || off(dq, 16)))
+        || (kv && (off(k, 16) || off(v, 16) || off(dk, 16) || off(dv, 16))))
+        return CUDALLM_ERR_UNSUPPORTED_SHAPE;
+    if (queries && (!scratch || off(scratch, 16) || scratch_bytes < cudallm_xattn_bwd_scratch_bytes(shape)))
+        return CUDALLM_ERR_WORKSPACE;
+    if (!queries && !dk) return CUDALLM_OK;
+    int dev = 0, sms = 0;
+    if ((st = rt_current_device(&dev, &sms)) != CUDALLM_OK) return st;
+    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
+    float *delta = static_cast<float *>(scratch);
+    const bool wide = s.head_dim > 64;
+    if (s.dtype == CUDALLM_BF16)
+        return wide ? run_bwd<128, __nv_bfloat16>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream)
+                    : run_bwd<64, __nv_bfloat16>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream);
+    return wide ? run_bwd<128, __half>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream)
+                : run_bwd<64, __half>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,511 @@
+// Cross attention, backward.  With P = exp(S - lse) and delta = rowsum(dO * O):
+//     dP = dO V^T,  dS = P * (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+//
+// Two kernels, each with its result stationary in tensor memory, so nothing is added by atomics
+// and equal inputs give equal bits: one owns 128 query rows of a head and walks the keys (S, dP,
+// dQ: three products per block, and delta on the way), one owns 128 keys of a key head and walks
+// the queries of all heads that share it (S^T, dP^T, dV, dK: four).  Seven products where five
+// would do with dQ added up through memory; the two extra ones cost less than writing and reading
+// dS or ordered fp32 additions into dQ.
+//
+// Both run the same roles: 256 threads on the 128 x 128 blocks (a thread is a row and a half of the
+// columns), a TMA warp, a warp that issues the products, and (keys) a warp that brings the
+// queries' lse and delta.  S and P, dP and dS lie over each other in tensor memory; P and dS, 16
+// bits each, are the A operand of the second products straight from there.
+//
+// Bound: the tensor core at DP = 128 (3 and 4 products of 512 clocks per block) with the
+// special-function unit (1024 clocks per block) beside it; the exponentials at DP = 64.
+// P and dS are rounded to the operands' type: that is what the tensor core multiplies.
+#pragma once
+#include "xattn_common.cuh"
+
+namespace cudallm {
+
+constexpr int kXaBwdThreads = 352;             // 8 warps on the blocks, TMA, products, lse / delta
+constexpr int kXaBwdWorkers = 256;
+
+struct XaBwdParams {
+    const void *o, *d_o;
+    void *dq, *dk, *dv;
+    const float *lse;
+    float *delta;               // [batch][q_heads][q_rows]
+    const int *lens;
+    XaStrides sq, sk, sv, so;
+    int q_rows, kv_rows, q_heads, kv_heads, group, batch, head_dim;
+    int q_tiles, kv_tiles;      // of 128 rows
+    float scale, scale_log2;
+    int *status;
+    int skip_loads;
+    unsigned long long wait_limit_ns;
+};
+
+// Shared memory: the two stationary tiles, a ring of three tiles (the operand that serves two
+// products: K or Q), a ring of two (V or dO), lse and delta of two blocks.
+template <int DP> struct XaBwdSmem {
+    static constexpr int kTile = DP / 64 * kXaChunkBytes;
+    static constexpr int kLong = 3, kShort = 2;
+    static constexpr int kRingL = 2 * kTile, kRingS = kRingL + kLong * kTile;
+    static constexpr int kRows = kRingS + kShort * kTile;          // floats: [2][lse 128, delta 128]
+    static constexpr int kBars = kRows + 2 * 2 * kXaRows * 4;
+    static constexpr int kNumBars = 24;
+    static constexpr int kMisc = kBars + kNumBars * 8;
+    static constexpr int kBytes = kMisc + 16;
+};
+static_assert(XaBwdSmem<128>::kBytes <= 232448, "shared memory budget");
+static_assert(XaBwdSmem<64>::kBytes > 114 * 1024, "one CTA per SM (each takes all of tensor memory)");
+
+// Barriers, 8 bytes each from XaBwdSmem::kBars.
+enum : int { kBwStat = 0, kBwS = 1 /* 2 */, kBwDp = 3, kBwP = 4, kBwDs = 5, kBwDone = 6, kBwLFull = 7 /* 3 */,
+             kBwLEmpty = 10 /* 3 */, kBwSFull = 13 /* 2 */, kBwSEmpty = 15 /* 2 */, kBwRowsFull = 17 /* 2 */,
+             kBwRowsEmpty = 19 /* 2 */ };
+
+// The TMA warp of both kernels: the stationary tiles, then `n` pairs of tiles.  coords(i, h, row) gives
+// the head and first row of pair i.  Returns false if a wait ran out.
+template <int DP, typename Coords>
+__device__ __forceinline__ bool xa_bwd_load(uint32_t sbase, const CUtensorMap *stat_a, const CUtensorMap *stat_b, int stat_h,
+                                            int stat_row, const CUtensorMap *ring_l, const CUtensorMap *ring_s, int b, int n,
+                                            Coords coords, volatile int *abort_flag, unsigned long long limit)
+{
+    using L = XaBwdSmem<DP>;
+    const uint32_t bars = sbase + L::kBars;
+    mbar_expect_tx(bars + 8 * kBwStat, 2 * L::kTile);
+    xa_load_tile<DP>(stat_a, sbase, bars + 8 * kBwStat, stat_h, stat_row, b);
+    xa_load_tile<DP>(stat_b, sbase + L::kTile, bars + 8 * kBwStat, stat_h, stat_row, b);
+    bool ok = true;
+    int nl = 0, ns = 0;
+    for (int i = 0; i < n && ok; ++i) {
+        int h, row;
+        coords(i, h, row);
+        const int sl = i % L::kLong, ss = i % L::kShort;
+        if (i >= L::kLong) ok = mbar_wait(bars + 8 * (kBwLEmpty + sl), (i / L::kLong - 1) & 1, abort_flag, limit);
+        if (!ok) break;
+        mbar_expect_tx(bars + 8 * (kBwLFull + sl), L::kTile);
+        xa_load_tile<DP>(ring_l, sbase + L::kRingL + sl * L::kTile, bars + 8 * (kBwLFull + sl), h, row, b);
+        ++nl;
+        if (i >= L::kShort) ok = mbar_wait(bars + 8 * (kBwSEmpty + ss), (i / L::kShort - 1) & 1, abort_flag, limit);
+        if (!ok) break;
+        mbar_expect_tx(bars + 8 * (kBwSFull + ss), L::kTile);
+        xa_load_tile<DP>(ring_s, sbase + L::kRingS + ss * L::kTile, bars + 8 * (kBwSFull + ss), h, row, b);
+        ++ns;
+    }
+    if (!ok) {
+        // the copies in flight must land before the CTA ends
+        volatile int never = 0;
+        mbar_wait(bars + 8 * kBwStat, 0, &never, limit);
+        for (int s = 0; s < L::kLong; ++s) {
+            const int uses = (nl - s + L::kLong - 1) / L::kLong;
+            if (uses > 0) mbar_wait(bars + 8 * (kBwLFull + s), (uses - 1) & 1, &never, limit);
+        }
+        for (int s = 0; s < L::kShort; ++s) {
+            const int uses = (ns - s + L::kShort - 1) / L::kShort;
+            if (uses > 0) mbar_wait(bars + 8 * (kBwSFull + s), (uses - 1) & 1, &never, limit);
+        }
+    }
+    return ok;
+}
+
+template <int DP>
+__device__ __forceinline__ void xa_bwd_init(uint32_t bars, volatile int *abort_flag)
+{
+    *abort_flag = 0;
+    for (int i = 0; i < XaBwdSmem<DP>::kNumBars; ++i) {
+        const bool workers = i == kBwP || i == kBwDs || i == kBwRowsEmpty || i == kBwRowsEmpty + 1;
+        mbar_init(bars + 8 * i, workers ? kXaBwdWorkers : 1);
+    }
+    fence_mbar_init();
+}
+
+// End of both kernels, by all threads: after a failed wait the products in flight are waited for,
+// then tensor memory is released by warp 9.
+__device__ __forceinline__ void xa_bwd_finish(uint32_t bars, uint32_t tmem, volatile int *abort_flag, unsigned long long limit)
+{
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x >> 5 == 9) {
+        tc_fence_after();
+        if (*abort_flag) {
+            if ((threadIdx.x & 31) == 0) {
+                volatile int never = 0;
+                mbar_init(bars + 8 * kBwDone, 1);
+                fence_mbar_init();
+                umma_commit(bars + 8 * kBwDone);
+                mbar_wait(bars + 8 * kBwDone, 0, &never, limit);
+            }
+            __syncwarp();
+        }
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// A worker's half of a row of a DP-column result in tensor memory, times `f`, to `dst` (NULL: not stored).
+template <int DP, typename T>
+__device__ __forceinline__ void xa_bwd_store(uint32_t t_addr, int half, float f, T *dst, int head_dim)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) {
+        const int col = half * (DP / 2) + c * 32;
+        uint32_t r[32];
+        tmem_ld_32x32b_x32(t_addr + col, r);
+        tmem_ld_wait();
+        float v[32];
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * f;
+        if (dst) xa_store_32(dst + col, v, head_dim - col);
+    }
+}
+template <int DP, typename T>
+__device__ __forceinline__ void xa_bwd_zero(int half, T *dst, int head_dim)
+{
+    for (int col = half * (DP / 2); col < (half + 1) * (DP / 2) && col < head_dim; col += 8)
+        *reinterpret_cast<uint4 *>(dst + col) = make_uint4(0, 0, 0, 0);
+}
+
+// ---------------------------------------------------------------- dQ --
+// Tensor memory: S of even and odd blocks at 0 and 128 (dS over them), dP at 256, dQ at 384.
+// When a block's dS is there, three products follow: dP of the next block, this block's part of
+// dQ, and S of the block after next, into the place that dS leaves.
+template <int DP, typename T>
+__global__ void __launch_bounds__(kXaBwdThreads, 1)
+xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do, const XaBwdParams p)
+{
+    using L = XaBwdSmem<DP>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t sbase = smem_u32(smem), bars = sbase + L::kBars;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kMisc);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMisc + 4);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int qt = blockIdx.x % p.q_tiles, bh = blockIdx.x / p.q_tiles;
+    const int h = bh % p.q_heads, b = bh / p.q_heads, kvh = h / p.group;
+    const int row0 = qt * kXaRows;
+
+    if (tid == 0) xa_bwd_init<DP>(bars, abort_flag);
+    if (warp == 9) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int keys = xa_keys(p.lens, b, p.kv_rows);
+    const int nblk = (keys + kXaRows - 1) / kXaRows;
+    const unsigned long long limit = p.wait_limit_ns;
+
+    if (warp == 8) {
+        if (lane == 0 && nblk > 0 && !p.skip_loads) {
+            const bool ok = xa_bwd_load<DP>(sbase, &tm_q, &tm_do, h, row0, &tm_k, &tm_v, b, nblk,
+                                            [&](int i, int &hh, int &row) { hh = kvh; row = i * kXaRows; }, abort_flag, limit);
+            if (!ok) xa_report(p.status, kXaRoleDq, 1);
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && nblk > 0) {
+            constexpr uint32_t idesc_s = xa_idesc<T>(128, 0), idesc_o = xa_idesc<T>(DP, 1);
+            auto wait = [&](int bar, int parity) { return mbar_wait(bars + 8 * bar, parity & 1, abort_flag, limit); };
+            auto k_tile = [&](int i) { return sbase + L::kRingL + (i % L::kLong) * L::kTile; };
+            auto issue_s = [&](int i) {
+                if (!wait(kBwLFull + i % L::kLong, i / L::kLong)) return false;
+                tc_fence_after();
+                xa_product_nt<DP>(tmem + (i & 1) * 128, sbase, k_tile(i), idesc_s);
+                umma_commit(bars + 8 * (kBwS + (i & 1)));
+                return true;
+            };
+            auto issue_dp = [&](int i) {
+                const int ss = i % L::kShort;
+                if (!wait(kBwSFull + ss, i / L::kShort)) return false;
+                tc_fence_after();
+                xa_product_nt<DP>(tmem + 256, sbase + L::kTile, sbase + L::kRingS + ss * L::kTile, idesc_s);
+                umma_commit(bars + 8 * kBwDp);
+                umma_commit(bars + 8 * (kBwSEmpty + ss));
+                return true;
+            };
+            bool ok = wait(kBwStat, 0) && issue_s(0) && issue_dp(0) && (nblk < 2 || issue_s(1));
+            for (int i = 0; i < nblk && ok; ++i) {
+                ok = wait(kBwDs, i);
+                if (!ok) break;
+                tc_fence_after();
+                if (i + 1 < nblk) ok = issue_dp(i + 1);
+                if (!ok) break;
+                xa_product_tn<64>(tmem + 384, tmem + (i & 1) * 128, k_tile(i), idesc_o, i > 0);
+                umma_commit(bars + 8 * (kBwLEmpty + i % L::kLong));
+                if (i + 1 == nblk) umma_commit(bars + 8 * kBwDone);
+                if (i + 2 < nblk) ok = issue_s(i + 2);
+            }
+            if (!ok) xa_report(p.status, kXaRoleDq, 2);
+        }
+    } else if (warp < 8) {
+        const int t = tid & (kXaRows - 1), half = tid >> 7;
+        const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const int row = row0 + t;
+        const bool live = row < p.q_rows;
+        const long long bhr = (long long)bh * p.q_rows + row;
+        // delta = rowsum(dO * O): half of the columns each, exchanged through shared memory
+        float part = 0.f;
+        if (live) {
+            const long long at = b * p.so.b + row * p.so.r + h * p.so.h;
+            const T *o = static_cast<const T *>(p.o) + at, *d = static_cast<const T *>(p.d_o) + at;
+#pragma unroll
+            for (int c = 0; c < DP / 16; ++c) {
+                const int col = half * (DP / 2) + c * 8;
+                if (col < p.head_dim) {
+                    const uint4 a = *reinterpret_cast<const uint4 *>(o + col), g = *reinterpret_cast<const uint4 *>(d + col);
+                    const T *ae = reinterpret_cast<const T *>(&a), *ge = reinterpret_cast<const T *>(&g);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) part = fmaf(float(ae[e]), float(ge[e]), part);
+                }
+            }
+        }
+        float *xch = reinterpret_cast<float *>(smem + L::kRows);
+        xch[half * kXaRows + t] = part;
+        named_bar_sync(1, kXaBwdWorkers);
+        const float delta = xch[t] + xch[kXaRows + t];
+        if (live && half == 0) p.delta[bhr] = delta;
+        const float lse2 = live ? p.lse[bhr] * 1.4426950408889634f : INFINITY;      // rows that do not exist: P = 0
+        bool ok = true;
+        for (int i = 0; i < nblk; ++i) {
+            ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (kBwS + (i & 1)), (i >> 1) & 1, abort_flag, limit));
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t t_s = tmem + (i & 1) * 128 + half * 64 + t_lane, t_dp = tmem + 256 + half * 64 + t_lane;
+            const int valid = keys - i * kXaRows - half * 64;            // of this thread's 64 columns
+            uint32_t s[2][32];
+            tmem_ld_32x32b_x32(t_s, s[0]);
+            tmem_ld_32x32b_x32(t_s + 32, s[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int k = 0; k < 32; ++k)
+                    s[c][k] = __float_as_uint(xa_exp2(fmaf(__uint_as_float(s[c][k]), p.scale_log2, -lse2)));
+            ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDp, i & 1, abort_flag, limit));
+            if (!ok) break;
+            tc_fence_after();
+            if (keys - i * kXaRows < kXaRows && keys < p.kv_rows && half == 0) {
+                xa_zero_rows<DP>(sbase + L::kRingL + (i % L::kLong) * L::kTile, t, keys - i * kXaRows);
+                fence_proxy_async_smem();
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t r[32], w[16];
+                tmem_ld_32x32b_x32(t_dp + 32 * c, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(s[c][k]) * (__uint_as_float(r[k]) - delta));
+                if (valid < 64) {
+#pragma unroll
+                    for (int k = 0; k < 32; ++k)
+                        if (c * 32 + k >= valid) r[k] = 0;
+                }
+#pragma unroll
+                for (int k = 0; k < 16; ++k) w[k] = XaElem<T>::pack(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+                tmem_st_32x32b_x16(t_s + 16 * c, w);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(bars + 8 * kBwDs);
+        }
+        if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
+        if (ok) {
+            T *dst = live ? static_cast<T *>(p.dq) + b * p.sq.b + row * p.sq.r + h * p.sq.h : nullptr;
+            if (nblk > 0) {
+                tc_fence_after();
+                xa_bwd_store<DP, T>(tmem + 384 + t_lane, half, p.scale, dst, p.head_dim);
+            } else if (live) {
+                xa_bwd_zero<DP, T>(half, dst, p.head_dim);
+            }
+        } else if (lane == 0) {
+            xa_report(p.status, kXaRoleDq, 3);
+        }
+    }
+    xa_bwd_finish(bars, tmem, abort_flag, limit);
+}
+
+// ------------------------------------------------------------- dK, dV --
+// Tensor memory: S^T at 0 (P^T over it), dP^T at 128 (dS^T over it), dV at 256, dK at 384.  While
+// the exponentials of a block run, the tensor core adds the last block's dK and computes dP^T;
+// while dS^T is formed, it adds dV and computes the next S^T.
+template <int DP, typename T>
+__global__ void __launch_bounds__(kXaBwdThreads, 1)
+xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                 const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_do, const XaBwdParams p)
+{
+    using L = XaBwdSmem<DP>;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const uint32_t sbase = smem_u32(smem), bars = sbase + L::kBars;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kMisc);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMisc + 4);
+    float *rows_buf = reinterpret_cast<float *>(smem + L::kRows);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int kt = blockIdx.x % p.kv_tiles, bk = blockIdx.x / p.kv_tiles;
+    const int kvh = bk % p.kv_heads, b = bk / p.kv_heads;
+    const int key0 = kt * kXaRows;
+
+    if (tid == 0) xa_bwd_init<DP>(bars, abort_flag);
+    if (warp == 9) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int keys = xa_keys(p.lens, b, p.kv_rows);
+    const int nblk = key0 < keys ? p.group * p.q_tiles : 0;          // block i: head i / q_tiles of the group
+    const unsigned long long limit = p.wait_limit_ns;
+
+    if (warp == 8) {
+        if (lane == 0 && nblk > 0 && !p.skip_loads) {
+            const bool ok = xa_bwd_load<DP>(sbase, &tm_k, &tm_v, kvh, key0, &tm_q, &tm_do, b, nblk,
+                                            [&](int i, int &hh, int &row) {
+                                                hh = kvh * p.group + i / p.q_tiles;
+                                                row = (i % p.q_tiles) * kXaRows;
+                                            }, abort_flag, limit);
+            if (!ok) xa_report(p.status, kXaRoleDkv, 1);
+        }
+    } else if (warp == 9) {
+        if (lane == 0 && nblk > 0) {
+            constexpr uint32_t idesc_s = xa_idesc<T>(128, 0), idesc_o = xa_idesc<T>(DP, 1);
+            auto wait = [&](int bar, int parity) { return mbar_wait(bars + 8 * bar, parity & 1, abort_flag, limit); };
+            auto q_tile = [&](int i) { return sbase + L::kRingL + (i % L::kLong) * L::kTile; };
+            auto do_tile = [&](int i) { return sbase + L::kRingS + (i % L::kShort) * L::kTile; };
+            auto issue_s = [&](int i) {
+                if (!wait(kBwLFull + i % L::kLong, i / L::kLong)) return false;
+                tc_fence_after();
+                xa_product_nt<DP>(tmem, sbase, q_tile(i), idesc_s);
+                umma_commit(bars + 8 * kBwS);
+                return true;
+            };
+            auto issue_dp = [&](int i) {
+                if (!wait(kBwSFull + i % L::kShort, i / L::kShort)) return false;
+                tc_fence_after();
+                xa_product_nt<DP>(tmem + 128, sbase + L::kTile, do_tile(i), idesc_s);
+                umma_commit(bars + 8 * kBwDp);
+                return true;
+            };
+            bool ok = wait(kBwStat, 0) && issue_s(0) && issue_dp(0);
+            for (int i = 0; i < nblk && ok; ++i) {
+                ok = wait(kBwP, i);
+                if (!ok) break;
+                tc_fence_after();
+                xa_product_tn<64>(tmem + 256, tmem, do_tile(i), idesc_o, i > 0);
+                umma_commit(bars + 8 * (kBwSEmpty + i % L::kShort));
+                if (i + 1 < nblk) ok = issue_s(i + 1);
+                ok = ok && wait(kBwDs, i);
+                if (!ok) break;
+                tc_fence_after();
+                xa_product_tn<64>(tmem + 384, tmem + 128, q_tile(i), idesc_o, i > 0);
+                umma_commit(bars + 8 * (kBwLEmpty + i % L::kLong));
+                if (i + 1 < nblk) ok = issue_dp(i + 1);
+                else umma_commit(bars + 8 * kBwDone);
+            }
+            if (!ok) xa_report(p.status, kXaRoleDkv, 2);
+        }
+    } else if (warp == 10) {
+        // lse (in units of log2) and delta of each block's queries; a query that does not exist has P = 0
+        bool ok = true;
+        for (int i = 0; i < nblk && ok; ++i) {
+            const int j = i & 1;
+            if (i >= 2) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (kBwRowsEmpty + j), ((i >> 1) - 1) & 1, abort_flag, limit));
+            if (!ok) break;
+            const int row0 = (i % p.q_tiles) * kXaRows;
+            const long long base = ((long long)b * p.q_heads + kvh * p.group + i / p.q_tiles) * p.q_rows;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int r = lane + 32 * u, row = row0 + r;
+                rows_buf[j * 256 + r] = row < p.q_rows ? p.lse[base + row] * 1.4426950408889634f : INFINITY;
+                rows_buf[j * 256 + 128 + r] = row < p.q_rows ? p.delta[base + row] : 0.f;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + 8 * (kBwRowsFull + j));
+        }
+    } else {
+        const int t = tid & (kXaRows - 1), half = tid >> 7;
+        const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const uint32_t t_s = tmem + half * 64 + t_lane, t_dp = tmem + 128 + half * 64 + t_lane;
+        bool ok = true;
+        for (int i = 0; i < nblk; ++i) {
+            const int j = i & 1;
+            const float4 *lse4 = reinterpret_cast<const float4 *>(rows_buf + j * 256 + half * 64);
+            const float4 *delta4 = lse4 + 32;
+            ok = mbar_wait(bars + 8 * (kBwRowsFull + j), (i >> 1) & 1, abort_flag, limit)
+                 && mbar_wait(bars + 8 * kBwS, i & 1, abort_flag, limit);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t s[2][32];
+            tmem_ld_32x32b_x32(t_s, s[0]);
+            tmem_ld_32x32b_x32(t_s + 32, s[1]);
+            tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t w[16];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float4 l4 = lse4[c * 8 + k];
+                    const float e0 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k]), p.scale_log2, -l4.x));
+                    const float e1 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k + 1]), p.scale_log2, -l4.y));
+                    const float e2 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k + 2]), p.scale_log2, -l4.z));
+                    const float e3 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k + 3]), p.scale_log2, -l4.w));
+                    s[c][4 * k] = __float_as_uint(e0);
+                    s[c][4 * k + 1] = __float_as_uint(e1);
+                    s[c][4 * k + 2] = __float_as_uint(e2);
+                    s[c][4 * k + 3] = __float_as_uint(e3);
+                    w[2 * k] = XaElem<T>::pack(e0, e1);
+                    w[2 * k + 1] = XaElem<T>::pack(e2, e3);
+                }
+                tmem_st_32x32b_x16(t_s + 16 * c, w);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(bars + 8 * kBwP);
+            ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDp, i & 1, abort_flag, limit));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                uint32_t r[32], w[16];
+                tmem_ld_32x32b_x32(t_dp + 32 * c, r);
+                tmem_ld_wait();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float4 d4 = delta4[c * 8 + k];
+                    w[2 * k] = XaElem<T>::pack(__uint_as_float(s[c][4 * k]) * (__uint_as_float(r[4 * k]) - d4.x),
+                                               __uint_as_float(s[c][4 * k + 1]) * (__uint_as_float(r[4 * k + 1]) - d4.y));
+                    w[2 * k + 1] = XaElem<T>::pack(__uint_as_float(s[c][4 * k + 2]) * (__uint_as_float(r[4 * k + 2]) - d4.z),
+                                                   __uint_as_float(s[c][4 * k + 3]) * (__uint_as_float(r[4 * k + 3]) - d4.w));
+                }
+                tmem_st_32x32b_x16(t_dp + 16 * c, w);
+            }
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(bars + 8 * (kBwRowsEmpty + j));
+            mbar_arrive(bars + 8 * kBwDs);
+        }
+        if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
+        if (ok) {
+            const int key = key0 + t;
+            const bool row_live = key < p.kv_rows, valid = key < keys;
+            T *dk = static_cast<T *>(p.dk) + b * p.sk.b + key * p.sk.r + kvh * p.sk.h;
+            T *dv = static_cast<T *>(p.dv) + b * p.sv.b + key * p.sv.r + kvh * p.sv.h;
+            if (nblk > 0) {
+                tc_fence_after();
+                xa_bwd_store<DP, T>(tmem + 256 + t_lane, half, 1.f, valid ? dv : nullptr, p.head_dim);
+                xa_bwd_store<DP, T>(tmem + 384 + t_lane, half, p.scale, valid ? dk : nullptr, p.head_dim);
+            }
+            if (row_live && (!valid || nblk == 0)) {                 // padded states, or no queries: no gradient
+                xa_bwd_zero<DP, T>(half, dk, p.head_dim);
+                xa_bwd_zero<DP, T>(half, dv, p.head_dim);
+            }
+        } else if (lane == 0) {
+            xa_report(p.status, kXaRoleDkv, 3);
+        }
+    }
+    xa_bwd_finish(bars, tmem, abort_flag, limit);
+}
+
+}  // namespace cudallm

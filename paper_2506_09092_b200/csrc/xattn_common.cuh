@@ -19,7 +19,7 @@ constexpr int kXaChunkBytes = kXaRows * 128;   // one 64-column chunk of a tile
 struct XaStrides { long long b, r, h; };       // elements between batch items, rows, heads
 
 // status detail codes of the attention kernels' bounded waits: (role << 8) | barrier
-enum : int { kXaRoleLoad = 0x10, kXaRoleMma = 0x11, kXaRoleSoftmax = 0x12, kXaRoleBwd = 0x20 };
+enum : int { kXaRoleLoad = 0x10, kXaRoleMma = 0x11, kXaRoleSoftmax = 0x12, kXaRoleDq = 0x20, kXaRoleDkv = 0x30 };
 
 __device__ __forceinline__ void xa_report(int *status, int role, int what)
 {
@@ -69,13 +69,15 @@ __device__ __forceinline__ void xa_product_nt(uint32_t d, uint32_t a_tile, uint3
         xa_mma_ss(d, a0 + o, b0 + o, idesc, k > 0);
     }
 }
-// 128 x DP product over `ROWS` rows: D (+)= P T, P (128 x ROWS, 16-bit) in tensor memory, tile T MN-major.
-template <int ROWS>
+// 128 x DP product over a tile's rows: D (+)= P T, P (128 x 128, 16-bit) in tensor memory, tile T
+// MN-major.  The second half of P's columns lies `HALF` tensor-memory columns after the first.
+template <int HALF>
 __device__ __forceinline__ void xa_product_tn(uint32_t d, uint32_t p_tmem, uint32_t tile, uint32_t idesc, bool accumulate)
 {
     const uint64_t b0 = make_smem_desc_sw128(tile, kXaChunkBytes, 1024);
 #pragma unroll
-    for (int k = 0; k < ROWS / 16; ++k) xa_mma_ts(d, p_tmem + k * 8, b0 + k * (2048 >> 4), idesc, accumulate || k > 0);
+    for (int k = 0; k < kXaRows / 16; ++k)
+        xa_mma_ts(d, p_tmem + (k / 4) * HALF + (k % 4) * 8, b0 + k * (2048 >> 4), idesc, accumulate || k > 0);
 }
 
 // Instruction descriptor: kind::f16, both operands T, fp32 accumulator, A K-major, M = 128.

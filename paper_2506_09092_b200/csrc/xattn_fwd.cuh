@@ -151,7 +151,7 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     tc_fence_after();
                     // (products of one issuing thread run in order: S_j of the next block, which
                     // overwrites P_j, starts after this product has read it)
-                    xa_product_tn<128>(t_o + DP * j, t_s + 128 * j, sbase + L::kRing + sv * L::kTile, idesc_o, i > 0);
+                    xa_product_tn<32>(t_o + DP * j, t_s + 128 * j, sbase + L::kRing + sv * L::kTile, idesc_o, i > 0);
                     umma_commit(pv_done + 8 * j);
                     if (more) {
                         if (j == 0) ok = mbar_wait(full + 8 * sk, (ik / L::kStages) & 1, abort_flag, p.wait_limit_ns);

@@ -250,3 +250,191 @@ def test_waits_that_run_out_end_the_kernel():
         B.debug_set(B.DEBUG_SKIP_NEXT_XATTN_LOADS, 0)
     run_forward(q, k, v, None, out)
     assert torch.equal(out, ref)
+
+
+# ------------------------------------------------------------------ backward --
+def exact_backward(q, k, v, lens, o, lse, do, scale, dtype):
+    """(value, tolerance) of dQ, dK, dV in 64 bits from the operands as they are.  An entry of dS is off by
+    P (W (dim + 4) u + |dP - delta| (rho + 2 u)), W = sum |dO||V| + sum |dO||O|, and by its rounding; then the
+    products' sums as in the forward direction."""
+    h = torch.finfo(TYPES[dtype]).eps / 2
+    small = 2.0 ** -25 if dtype == "fp16" else 0.0
+    batch, q_rows, hq, dim = q.shape
+    kv_rows, hk = k.shape[1], k.shape[2]
+    zeros = lambda t: torch.zeros(t.shape, dtype=torch.float64, device="cuda")
+    (dq, dk, dv), (tq, tk, tv) = (zeros(q), zeros(k), zeros(v)), (zeros(q), zeros(k), zeros(v))
+    for b in range(batch):
+        n = kv_rows if lens is None else min(max(lens[b], 0), kv_rows)
+        if n == 0:
+            continue
+        for hh in range(hq):
+            kh = hh // (hq // hk)
+            qq, kk, vv = q[b, :, hh].double(), k[b, :n, kh].double(), v[b, :n, kh].double()
+            oo, dd, ll = o[b, :, hh].double(), do[b, :, hh].double(), lse[b, hh].double()[:, None]
+            z = scale * (qq @ kk.T)
+            p = torch.exp(z - ll)
+            delta = (dd * oo).sum(1, keepdim=True)
+            diff = dd @ vv.T - delta
+            ds = p * diff
+            dq[b, :, hh] = scale * (ds @ kk)
+            dk[b, :n, kh] += scale * (ds.T @ qq)
+            dv[b, :n, kh] += p.T @ dd
+            w = dd.abs() @ vv.abs().T + (dd.abs() * oo.abs()).sum(1, keepdim=True)
+            rho = (dim + 4) * U * scale * (qq.abs() @ kk.abs().T) + 4 * U * (z.abs() + ll.abs()) + 2.0 ** -21
+            e = p * (w * (dim + 4) * U + diff.abs() * (rho + 2 * U))
+            e = e + h * (ds.abs() + e) + small
+            rows = (max(n, q_rows * (hq // hk)) / 8 + 32) * 2 * U
+            tq[b, :, hh] = scale * ((e + rows * ds.abs()) @ kk.abs())
+            tk[b, :n, kh] += scale * ((e + rows * ds.abs()).T @ qq.abs())
+            tv[b, :n, kh] += (p * (rho + h * (1 + rho) + rows) + small).T @ dd.abs()
+    return [(g, (t + h * (g.abs() + t)) * 1.01 + 1e-30 + small) for g, t in ((dq, tq), (dk, tk), (dv, tv))]
+
+
+def check_backward(batch, q_rows, kv_rows, hq, hk, dim, dtype, lens=None, kind="rows", scale=None, spread=1.5, keys_too=True,
+                   seed=0):
+    t = TYPES[dtype]
+    q, k, v, lens_t = operands(batch, q_rows, kv_rows, hq, hk, dim, dtype, lens, kind, seed, spread)
+    sc = float(torch.tensor(dim ** -0.5 if scale is None else scale, dtype=torch.float32))
+    o64, lse64, _, _, _ = exact(q, k, v, lens, sc)
+    _, o = layout(kind, batch, q_rows, hq, dim, t)
+    _, do = layout(kind, batch, q_rows, hq, dim, t)
+    o.copy_(o64.to(t))
+    do.copy_((torch.randn(batch, q_rows, hq, dim, generator=torch.Generator(device="cuda").manual_seed(seed + 1),
+                          device="cuda")).to(t))
+    lse = lse64.float()
+    bufs = [layout(kind, batch, r, hh, dim, t, 7.0) for r, hh in ((q_rows, hq), (kv_rows, hk), (kv_rows, hk))]
+    shape = B.XattnShape.of(q, k, v, o, scale)
+    n = B.xattn_bwd_scratch_bytes(shape)
+    scratch = torch.full((n + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+    grads = [g for _, g in bufs]
+    B.xattn_bwd(shape, q, k, v, lens_t, o, lse, do, grads[0], *(grads[1:] if keys_too else (None, None)), scratch, n,
+                torch.cuda.current_stream())
+    code, detail = B.device_status(torch.cuda.current_stream())
+    assert code == B.OK, hex(detail)
+    assert bool((scratch[n:] == 0xFF).all())
+    if not keys_too:
+        assert all(bool((b == 7.0).all()) for b, _ in bufs[1:])
+    ref = exact_backward(q, k, v, lens, o, lse, do, sc, dtype)
+    for name, got, (want, tol) in list(zip(("dq", "dk", "dv"), grads, ref))[:3 if keys_too else 1]:
+        err = (got.double() - want).abs()
+        assert bool((err <= tol).all()), (name, float((err / tol).nan_to_num(nan=1e9).max()))
+    if lens is not None and keys_too:
+        for b, m in enumerate(lens):
+            m = min(max(m, 0), kv_rows)
+            assert bool((grads[1][b, m:] == 0).all()) and bool((grads[2][b, m:] == 0).all())
+    if kind == "padded":
+        for (buf, _), (r, hh) in zip(bufs, ((q_rows, hq), (kv_rows, hk), (kv_rows, hk))):
+            around = buf.clone()
+            around[:, :r, 1:hh + 1, :dim] = 7.0
+            assert bool((around == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("dim", [64, 128, 8, 32, 40, 72, 80])
+def test_backward_one_block(dtype, dim):
+    check_backward(1, 128, 128, 1, 1, dim, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("q_rows,kv_rows", [(1, 1), (1, 700), (700, 1), (128, 129), (129, 127), (256, 256), (257, 1000),
+                                            (500, 333), (2000, 400)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_backward_sizes(q_rows, kv_rows, dim, dtype):
+    check_backward(2, q_rows, kv_rows, 2, 2, dim, dtype)
+
+
+@pytest.mark.parametrize("kind", ["rows", "heads", "rows first", "padded"])
+def test_backward_layouts_shared_heads_and_lengths(kind):
+    check_backward(6, 150, 300, 8, 2, 64, "bf16", lens=[0, 1, 128, 129, 300, 299], kind=kind)
+    check_backward(3, 150, 300, 4, 1, 96, "fp16", lens=[-5, 1000, 257], kind=kind)
+
+
+def test_backward_many_blocks_and_optional_gradients():
+    check_backward(1, 1500, 3000, 1, 1, 128, "bf16")
+    check_backward(1, 1500, 1000, 6, 2, 64, "fp16", lens=[901])
+    check_backward(2, 300, 300, 2, 2, 64, "bf16", keys_too=False)
+    check_backward(1, 200, 300, 2, 2, 64, "bf16", scale=0.0)
+    check_backward(1, 200, 300, 2, 2, 64, "bf16", spread=10.0)
+
+
+def test_backward_without_queries_or_states():
+    empty = torch.empty(2, 0, 3, 64, device="cuda", dtype=torch.bfloat16)
+    some = torch.randn(2, 200, 3, 64, device="cuda").bfloat16()
+    lse = torch.full((2, 3, 200), float("-inf"), device="cuda")
+    scratch = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream()
+    dk, dv = torch.full_like(some, 5.0), torch.full_like(some, 5.0)
+    B.xattn_bwd(B.XattnShape.of(empty, some, some, empty), None, some, some, None, None, None, None, None, dk, dv, None, 0, stream)
+    assert bool((dk == 0).all()) and bool((dv == 0).all())
+    dq = torch.full_like(some, 5.0)
+    B.xattn_bwd(B.XattnShape.of(some, empty, empty, some), some, None, None, None, some, lse, some, dq, None, None, scratch,
+                1 << 16, stream)
+    assert bool((dq == 0).all())
+
+
+def test_backward_formula_against_differences():
+    """The 64-bit gradients that the kernels are compared with, against central differences of the forward
+    definition (step 1e-6: differences are exact to about 1e-8) with unrounded O and lse."""
+    q, k, v, _ = operands(1, 5, 7, 2, 1, 8, "bf16")
+    q, k, v = q.double(), k.double(), v.double()
+    sc, w = 0.35, torch.randn(1, 5, 2, 8, device="cuda", dtype=torch.float64)
+    o, lse, _, _, _ = exact(q, k, v, [6], sc)
+    ref = exact_backward(q, k, v, [6], o, lse, w, sc, "bf16")
+    for i, x in enumerate((q, k, v)):
+        for at in ((0, 0, 0, 0), (0, 3, x.shape[2] - 1, 5), (0, x.shape[1] - 1, 0, 7)):
+            up, down = [t.clone() for t in (q, k, v)], [t.clone() for t in (q, k, v)]
+            up[i][at] += 1e-6
+            down[i][at] -= 1e-6
+            slope = float(((exact(*up, [6], sc)[0] - exact(*down, [6], sc)[0]) * w).sum() / 2e-6)
+            assert abs(slope - float(ref[i][0][at])) < 1e-6
+
+
+def test_backward_replay_streams_and_repeatability():
+    q, k, v, lens = operands(2, 300, 500, 4, 2, 64, "bf16", [500, 377], poison=False)
+    o = torch.empty_like(q)
+    lse = run_forward(q, k, v, lens, o)
+    do = torch.randn_like(q)
+    shape = B.XattnShape.of(q, k, v, o)
+    n = B.xattn_bwd_scratch_bytes(shape)
+
+    def grads():
+        return [torch.empty_like(q), torch.empty_like(k), torch.empty_like(v), torch.empty(n, dtype=torch.uint8, device="cuda")]
+
+    def call(g, stream):
+        B.xattn_bwd(shape, q, k, v, lens, o, lse, do, g[0], g[1], g[2], g[3], n, stream)
+
+    first, replayed, other = grads(), grads(), grads()
+    call(first, torch.cuda.current_stream())
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        call(replayed, torch.cuda.current_stream())
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        graph.replay()
+        call(other, side)
+    torch.cuda.synchronize()
+    for a, b, c in zip(first[:3], replayed, other):
+        assert torch.equal(a, b) and torch.equal(a, c)
+
+
+def test_backward_waits_that_run_out_end_the_kernel():
+    q, k, v, _ = operands(1, 300, 500, 2, 2, 64, "bf16")
+    o = torch.empty_like(q)
+    lse = run_forward(q, k, v, None, o)
+    shape = B.XattnShape.of(q, k, v, o)
+    n = B.xattn_bwd_scratch_bytes(shape)
+    scratch = torch.empty(n, dtype=torch.uint8, device="cuda")
+    out = [[torch.empty_like(t) for t in (q, k, v)] for _ in range(2)]
+    stream = torch.cuda.current_stream()
+    B.xattn_bwd(shape, q, k, v, None, o, lse, q, *out[0], scratch, n, stream)
+    try:
+        B.debug_set(B.DEBUG_WAIT_LIMIT_NS, 1_000_000)
+        B.debug_set(B.DEBUG_SKIP_NEXT_XATTN_LOADS, 1)
+        B.xattn_bwd(shape, q, k, v, None, o, lse, q, *out[1], scratch, n, stream)
+        assert B.device_status(stream)[0] == B.ERR_DEVICE_TIMEOUT
+    finally:
+        B.debug_set(B.DEBUG_WAIT_LIMIT_NS, 0)
+        B.debug_set(B.DEBUG_SKIP_NEXT_XATTN_LOADS, 0)
+    B.xattn_bwd(shape, q, k, v, None, o, lse, q, *out[1], scratch, n, stream)
+    assert B.device_status(stream)[0] == B.OK
+    assert all(torch.equal(a, b) for a, b in zip(*out))

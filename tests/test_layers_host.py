@@ -122,3 +122,90 @@ def test_host_tensors_are_refused_by_the_binding():
 
 def test_struct_layout():
     assert ctypes.sizeof(B.CTensor) == 32
+
+
+def xshape(**k):
+    a = dict(batch=2, q_rows=5, kv_rows=7, q_heads=4, kv_heads=2, head_dim=64, dtype=B.BF16, scale=0.125,
+             q_stride=(5 * 4 * 64, 4 * 64, 64), k_stride=(7 * 2 * 64, 2 * 64, 64), v_stride=(7 * 2 * 64, 2 * 64, 64),
+             o_stride=(5 * 4 * 64, 4 * 64, 64))
+    a.update(k)
+    for f in ("q_stride", "k_stride", "v_stride", "o_stride"):
+        a[f] = (ctypes.c_int64 * 3)(*a[f])
+    return B.XattnShape(**a)
+
+
+def fwd(shape, **k):
+    a = dict(q=P, k=P, v=P, kv_lens=P, o=P, lse=P, scratch=P, scratch_bytes=1 << 40)
+    a.update(k)
+    return B.xattn_fwd(shape, check=False, **a)
+
+
+def bwd(shape, **k):
+    a = dict(q=P, k=P, v=P, kv_lens=P, o=P, lse=P, d_o=P, dq=P, dk=P, dv=P, scratch=P, scratch_bytes=1 << 40)
+    a.update(k)
+    return B.xattn_bwd(shape, check=False, **a)
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(dtype=B.F32), B.ERR_INVALID_DTYPE), (dict(dtype=3), B.ERR_INVALID_DTYPE),
+    (dict(batch=-1), B.ERR_INVALID_DIM), (dict(q_rows=-1), B.ERR_INVALID_DIM), (dict(kv_rows=1 << 31), B.ERR_INVALID_DIM),
+    (dict(kv_heads=3), B.ERR_INVALID_DIM), (dict(kv_heads=0), B.ERR_INVALID_DIM),
+    (dict(scale=-1.0), B.ERR_INVALID_DIM), (dict(scale=float("nan")), B.ERR_INVALID_DIM),
+    (dict(scale=float("inf")), B.ERR_INVALID_DIM),
+    (dict(head_dim=60), B.ERR_UNSUPPORTED_SHAPE), (dict(head_dim=136), B.ERR_UNSUPPORTED_SHAPE),
+    (dict(q_stride=(1280, 256, 0)), B.ERR_INVALID_LD), (dict(q_stride=(1280, -256, 64)), B.ERR_INVALID_LD),
+    (dict(k_stride=(896, 128, 56)), B.ERR_INVALID_LD),          # heads overlap
+    (dict(v_stride=(840, 128, 64)), B.ERR_INVALID_LD),          # batch items overlap
+    (dict(o_stride=(1284, 256, 64)), B.ERR_UNSUPPORTED_SHAPE),  # not a multiple of 8
+    (dict(o_stride=(1 << 45, 256, 64)), B.ERR_INVALID_DIM),
+    (dict(batch=0), B.OK), (dict(q_heads=0), B.OK), (dict(head_dim=0), B.OK),
+])
+def test_attention_shape_refusals(change, status):
+    s = xshape(**change)
+    assert fwd(s) == status and bwd(s) == status
+    if status != B.OK:
+        assert B.xattn_fwd_scratch_bytes(s) == B.xattn_bwd_scratch_bytes(s) == 0
+
+
+def test_attention_operand_refusals():
+    s = xshape()
+    assert B.lib().cudallm_xattn_fwd(None, P, P, P, P, P, P, P, 1 << 30, None) == B.ERR_INVALID_POINTER
+    for name in ("q", "k", "v", "o"):
+        assert fwd(s, **{name: None}) == B.ERR_INVALID_POINTER
+        assert fwd(s, **{name: P + 8}) == B.ERR_UNSUPPORTED_SHAPE
+        assert bwd(s, **{name: None}) == B.ERR_INVALID_POINTER
+        assert bwd(s, **{name: P + 8}) == B.ERR_UNSUPPORTED_SHAPE
+    for name in ("kv_lens", "lse"):
+        assert fwd(s, **{name: P + 2}) == B.ERR_MISALIGNED
+        assert bwd(s, **{name: P + 2}) == B.ERR_MISALIGNED
+    for name in ("lse", "d_o", "dq", "dk", "dv"):
+        assert bwd(s, **{name: None}) == B.ERR_INVALID_POINTER
+    for name in ("d_o", "dq", "dk", "dv"):
+        assert bwd(s, **{name: P + 8}) == B.ERR_UNSUPPORTED_SHAPE
+    need = B.xattn_bwd_scratch_bytes(s)
+    assert need >= 2 * 4 * 5 * 4
+    for scratch, size in ((None, need), (P + 8, need), (P, need - 1)):
+        assert bwd(s, scratch=scratch, scratch_bytes=size) == B.ERR_WORKSPACE
+    long = xshape(batch=1, q_rows=1, kv_rows=1 << 16, k_stride=(0, 128, 64), v_stride=(0, 128, 64))
+    need = B.xattn_fwd_scratch_bytes(long)
+    assert need > 0
+    for scratch, size in ((None, need), (P + 8, need), (P, need - 1)):
+        assert fwd(long, scratch=scratch, scratch_bytes=size) == B.ERR_WORKSPACE
+    assert fwd(xshape(q_rows=0), q=None, k=None, v=None, o=None) == B.OK
+    assert bwd(xshape(q_rows=0), q=None, o=None, lse=None, d_o=None, dq=None, dk=None, dv=None, scratch=None) == B.OK
+    assert bwd(xshape(q_rows=0, kv_rows=0), q=None, k=None, v=None) == B.OK
+
+
+def test_attention_shape_from_tensors():
+    q = torch.zeros(2, 5, 4, 64, dtype=torch.bfloat16)
+    kv = torch.zeros(2, 7, 2, 2, 64, dtype=torch.bfloat16)
+    s = B.XattnShape.of(q, kv[:, :, 0], kv[:, :, 1], q)
+    assert (s.batch, s.q_rows, s.kv_rows, s.q_heads, s.kv_heads, s.head_dim) == (2, 5, 7, 4, 2, 64)
+    assert list(s.k_stride) == [7 * 4 * 64, 4 * 64, 64] and s.scale == 0.125 and s.dtype == B.BF16
+    for bad in ((q.float(), kv[:, :, 0], kv[:, :, 1], q), (q.float(),) * 4):
+        with pytest.raises(TypeError):
+            B.XattnShape.of(*bad)
+    for bad in ((q, kv[:, :, 0], kv[:, :1, 1], q), (q, kv[:, :, 0], kv[:, :, 1], q[:, :4]), (q.transpose(2, 3),) * 4):
+        with pytest.raises(ValueError):
+            B.XattnShape.of(*bad)
+    assert ctypes.sizeof(B.XattnShape) == 152
