@@ -159,23 +159,29 @@ def _p(x):
     raise TypeError(type(x))
 
 
-_torch = None
+_get_device = None
 
 
-def _d(x):
-    """Address of a device buffer: int, None, or a CUDA tensor on the current device."""
-    if x is None or isinstance(x, int):
-        return x
-    global _torch
-    if _torch is None:
+def _d(*xs):
+    """Addresses of device buffers: ints, Nones, or CUDA tensors on the current device."""
+    global _get_device
+    if _get_device is None:
         import torch
-        _torch = torch
-    dev = x.get_device()
-    if dev < 0:
-        raise TypeError("a CUDA tensor is needed, not one in host memory")
-    if dev != _torch.cuda.current_device():
-        raise ValueError(f"the tensor is on device {dev}, the current device is {_torch.cuda.current_device()}")
-    return x.data_ptr()
+        _get_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+    cur, out = -2, []
+    for x in xs:
+        if x is None or isinstance(x, int):
+            out.append(x)
+            continue
+        dev = x.get_device()
+        if dev != cur:
+            if dev < 0:
+                raise TypeError("a CUDA tensor is needed, not one in host memory")
+            cur = _get_device()
+            if dev != cur:
+                raise ValueError(f"the tensor is on device {dev}, the current device is {cur}")
+        out.append(x.data_ptr())
+    return out
 
 
 def _s(stream):
@@ -243,8 +249,8 @@ def layernorm_f32(x, gamma, beta, y, batch, m, eps=1e-5, stream=None, check=True
 def layernorm_rows(x, gamma, beta, y, mean, rstd, rows, n, ldx, ldy, dtype, param_dtype, eps=1e-5, stream=None,
                    check=True):
     """LayerNorm of every row of x (rows x n); gamma, beta, mean and rstd may be None."""
-    st = lib().cudallm_layernorm_rows(_d(x), _d(gamma), _d(beta), _d(y), _d(mean), _d(rstd), rows, n, ldx, ldy,
-                                      dtype, param_dtype, eps, _s(stream))
+    st = lib().cudallm_layernorm_rows(*_d(x, gamma, beta, y, mean, rstd), rows, n, ldx, ldy, dtype,
+                                      param_dtype, eps, _s(stream))
     return _check(st, "cudallm_layernorm_rows", check)
 
 
@@ -255,8 +261,8 @@ def layernorm_rows_bwd_scratch_bytes(rows, n) -> int:
 def layernorm_rows_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, rows, n, lddy, ldx, lddx, dtype, param_dtype,
                        scratch, scratch_bytes, stream=None, check=True):
     """Gradient of ``layernorm_rows``; dx, dgamma and dbeta may each be None."""
-    st = lib().cudallm_layernorm_rows_bwd(_d(dy), _d(x), _d(gamma), _d(mean), _d(rstd), _d(dx), _d(dgamma), _d(dbeta),
-                                          rows, n, lddy, ldx, lddx, dtype, param_dtype, _d(scratch), scratch_bytes,
+    *ptrs, scr = _d(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, scratch)
+    st = lib().cudallm_layernorm_rows_bwd(*ptrs, rows, n, lddy, ldx, lddx, dtype, param_dtype, scr, scratch_bytes,
                                           _s(stream))
     return _check(st, "cudallm_layernorm_rows_bwd", check)
 
@@ -282,7 +288,7 @@ class TensorTable:
                 raise TypeError(f"fp32, bf16 or fp16 gradients, not {t.dtype}")
             if not (t.is_contiguous() and o.is_contiguous()):
                 raise ValueError("contiguous tensors are needed")
-            e.data, e.out, e.n, e.dtype = _d(t), _d(o), t.numel(), codes[str(t.dtype)]
+            (e.data, e.out), e.n, e.dtype = _d(t, o), t.numel(), codes[str(t.dtype)]
             if e.n:
                 nbytes = e.n * t.element_size()
                 spans.append((e.out, e.out + nbytes, e.data != e.out))
@@ -312,19 +318,19 @@ def grad_norm_scratch_bytes(table) -> int:
 
 def grad_norm(table, norm, scratch, scratch_bytes, stream=None, check=True):
     """norm[0] (device fp32) = the norm of all tensors of the table together."""
-    st = lib().cudallm_grad_norm(table.array, table.count, _d(norm), _d(scratch), scratch_bytes, _s(stream))
+    st = lib().cudallm_grad_norm(table.array, table.count, *_d(norm, scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_grad_norm", check)
 
 
 def grad_clip(table, norm, max_norm, eps=1e-6, stream=None, check=True):
     """Scale the table's tensors by min(1, max_norm / (norm[0] + eps))."""
-    st = lib().cudallm_grad_clip(table.array, table.count, _d(norm), max_norm, eps, _s(stream))
+    st = lib().cudallm_grad_clip(table.array, table.count, *_d(norm), max_norm, eps, _s(stream))
     return _check(st, "cudallm_grad_clip", check)
 
 
 def grad_clip_norm(table, max_norm, eps, norm, scratch, scratch_bytes, stream=None, check=True):
     """``grad_norm`` and ``grad_clip`` together."""
-    st = lib().cudallm_grad_clip_norm(table.array, table.count, max_norm, eps, _d(norm), _d(scratch), scratch_bytes,
+    st = lib().cudallm_grad_clip_norm(table.array, table.count, max_norm, eps, *_d(norm, scratch), scratch_bytes,
                                       _s(stream))
     return _check(st, "cudallm_grad_clip_norm", check)
 
@@ -336,8 +342,7 @@ def xattn_fwd_scratch_bytes(shape) -> int:
 def xattn_fwd(shape, q, k, v, kv_lens, o, lse, scratch, scratch_bytes, stream=None, check=True):
     """Cross attention: o = softmax(scale q k^T) v over the first kv_lens[b] states of each batch item
     (``shape``: an XattnShape); kv_lens, lse and scratch may be None."""
-    st = lib().cudallm_xattn_fwd(shape, _d(q), _d(k), _d(v), _d(kv_lens), _d(o), _d(lse), _d(scratch), scratch_bytes,
-                                 _s(stream))
+    st = lib().cudallm_xattn_fwd(shape, *_d(q, k, v, kv_lens, o, lse, scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_xattn_fwd", check)
 
 
@@ -348,8 +353,7 @@ def xattn_bwd_scratch_bytes(shape) -> int:
 def xattn_bwd(shape, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch, scratch_bytes, stream=None, check=True):
     """Gradients of ``xattn_fwd`` (d_o laid out like o, dq like q, dk like k, dv like v); dk and dv may
     both be None."""
-    st = lib().cudallm_xattn_bwd(shape, _d(q), _d(k), _d(v), _d(kv_lens), _d(o), _d(lse), _d(d_o), _d(dq), _d(dk), _d(dv),
-                                 _d(scratch), scratch_bytes, _s(stream))
+    st = lib().cudallm_xattn_bwd(shape, *_d(q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_xattn_bwd", check)
 
 

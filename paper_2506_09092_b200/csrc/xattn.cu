@@ -200,7 +200,7 @@ int run_fwd(const cudallm_xattn_shape &s, const FwdPlan &f, const void *q, const
         p.q_rows = (int)s.q_rows; p.kv_rows = (int)s.kv_rows; p.q_heads = (int)s.q_heads;
         p.group = (int)(s.q_heads / s.kv_heads); p.batch = (int)s.batch; p.head_dim = (int)s.head_dim;
         p.q_tiles = (int)cdiv(s.q_rows, 2 * kXaRows);
-        p.splits = f.splits; p.blocks_per_split = (int)f.per_split;
+        p.splits = f.splits; p.tiles_per_split = (int)f.per_split;
         p.scale = s.scale; p.scale_log2 = scale_log2(s);
         if ((st = status_word(dev, &p.status)) != CUDALLM_OK) return st;
         p.skip_loads = rt_take_skip_loads();

@@ -110,7 +110,7 @@ __device__ __forceinline__ void xa_bwd_init(uint32_t bars, volatile int *abort_f
     *abort_flag = 0;
     for (int i = 0; i < XaBwdSmem<DP>::kNumBars; ++i) {
         const bool workers = i == kBwP || i == kBwDs || i == kBwRowsEmpty || i == kBwRowsEmpty + 1;
-        mbar_init(bars + 8 * i, workers ? kXaBwdWorkers : 1);
+        mbar_init(bars + 8 * i, workers ? kXaBwdWorkers / 32 : 1);      // (one arrival per warp)
     }
     fence_mbar_init();
 }
@@ -147,7 +147,7 @@ __device__ __forceinline__ void xa_bwd_store(uint32_t t_addr, int half, float f,
         const int col = half * (DP / 2) + c * 32;
         uint32_t r[32];
         tmem_ld_32x32b_x32(t_addr + col, r);
-        tmem_ld_wait();
+        tmem_ld_wait_for(r);
         float v[32];
 #pragma unroll
         for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * f;
@@ -175,7 +175,7 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const uint32_t sbase = smem_u32(smem), bars = sbase + L::kBars;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMisc + 4);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int qt = blockIdx.x % p.q_tiles, bh = blockIdx.x / p.q_tiles;
     const int h = bh % p.q_heads, b = bh / p.q_heads, kvh = h / p.group;
     const int row0 = qt * kXaRows;
@@ -202,39 +202,55 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             if (!ok) xa_report(p.status, kXaRoleDq, 1);
         }
     } else if (warp == 9) {
-        if (lane == 0 && nblk > 0) {
+        if (nblk > 0) {
             constexpr uint32_t idesc_s = xa_idesc<T>(128, 0), idesc_o = xa_idesc<T>(DP, 1);
-            auto wait = [&](int bar, int parity) { return mbar_wait(bars + 8 * bar, parity & 1, abort_flag, limit); };
-            auto k_tile = [&](int i) { return sbase + L::kRingL + (i % L::kLong) * L::kTile; };
-            auto issue_s = [&](int i) {
-                if (!wait(kBwLFull + i % L::kLong, i / L::kLong)) return false;
-                tc_fence_after();
-                xa_product_nt<DP>(tmem + (i & 1) * 128, sbase, k_tile(i), idesc_s);
-                umma_commit(bars + 8 * (kBwS + (i & 1)));
-                return true;
+            const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0), s0 = sbase, bar0 = s0 + L::kBars;
+            auto wait = [&](int bar, int parity) {
+                return __all_sync(0xffffffffu, mbar_wait(bar0 + 8 * bar, parity & 1, abort_flag, limit)) != 0;
+            };
+            auto k_tile = [&](int i) { return s0 + L::kRingL + (i % L::kLong) * L::kTile; };
+            auto wait_k = [&](int i) { return wait(kBwLFull + i % L::kLong, i / L::kLong); };
+            auto wait_v = [&](int i) { return wait(kBwSFull + i % L::kShort, i / L::kShort); };
+            auto issue_s = [&](int i) {                                  // (by one lane, like the next)
+                xa_product_nt<DP>(t0 + (i & 1) * 128, s0, k_tile(i), idesc_s);
+                umma_commit(bar0 + 8 * (kBwS + (i & 1)));
             };
             auto issue_dp = [&](int i) {
                 const int ss = i % L::kShort;
-                if (!wait(kBwSFull + ss, i / L::kShort)) return false;
-                tc_fence_after();
-                xa_product_nt<DP>(tmem + 256, sbase + L::kTile, sbase + L::kRingS + ss * L::kTile, idesc_s);
-                umma_commit(bars + 8 * kBwDp);
-                umma_commit(bars + 8 * (kBwSEmpty + ss));
-                return true;
+                xa_product_nt<DP>(t0 + 256, s0 + L::kTile, s0 + L::kRingS + ss * L::kTile, idesc_s);
+                umma_commit(bar0 + 8 * kBwDp);
+                umma_commit(bar0 + 8 * (kBwSEmpty + ss));
             };
-            bool ok = wait(kBwStat, 0) && issue_s(0) && issue_dp(0) && (nblk < 2 || issue_s(1));
+            bool ok = wait(kBwStat, 0) && wait_k(0) && wait_v(0) && (nblk < 2 || wait_k(1));
+            if (ok) {
+                tc_fence_after();
+                if (elect_one()) {
+                    issue_s(0);
+                    issue_dp(0);
+                    if (nblk > 1) issue_s(1);
+                }
+                __syncwarp();
+            }
             for (int i = 0; i < nblk && ok; ++i) {
-                ok = wait(kBwDs, i);
+                ok = (i + 1 >= nblk || wait_v(i + 1)) && wait(kBwDs, i);
                 if (!ok) break;
                 tc_fence_after();
-                if (i + 1 < nblk) ok = issue_dp(i + 1);
-                if (!ok) break;
-                xa_product_tn<64>(tmem + 384, tmem + (i & 1) * 128, k_tile(i), idesc_o, i > 0);
-                umma_commit(bars + 8 * (kBwLEmpty + i % L::kLong));
-                if (i + 1 == nblk) umma_commit(bars + 8 * kBwDone);
-                if (i + 2 < nblk) ok = issue_s(i + 2);
+                if (elect_one()) {
+                    if (i + 1 < nblk) issue_dp(i + 1);
+                    xa_product_tn<64>(t0 + 384, t0 + (i & 1) * 128, k_tile(i), idesc_o, i > 0);
+                    umma_commit(bar0 + 8 * (kBwLEmpty + i % L::kLong));
+                    if (i + 1 == nblk) umma_commit(bar0 + 8 * kBwDone);
+                }
+                __syncwarp();
+                if (i + 2 < nblk) {
+                    ok = wait_k(i + 2);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) issue_s(i + 2);
+                    __syncwarp();
+                }
             }
-            if (!ok) xa_report(p.status, kXaRoleDq, 2);
+            if (!ok && lane == 0) xa_report(p.status, kXaRoleDq, 2);
         }
     } else if (warp < 8) {
         const int t = tid & (kXaRows - 1), half = tid >> 7;
@@ -274,7 +290,8 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             uint32_t s[2][32];
             tmem_ld_32x32b_x32(t_s, s[0]);
             tmem_ld_32x32b_x32(t_s + 32, s[1]);
-            tmem_ld_wait();
+            tmem_ld_wait_for(s[0]);
+            tmem_ld_wait_for(s[1]);
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -284,14 +301,14 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             if (!ok) break;
             tc_fence_after();
             if (keys - i * kXaRows < kXaRows && keys < p.kv_rows && half == 0) {
-                xa_zero_rows<DP>(sbase + L::kRingL + (i % L::kLong) * L::kTile, t, keys - i * kXaRows);
+                if (t >= keys - i * kXaRows) xa_zero_row<DP>(sbase + L::kRingL + (i % L::kLong) * L::kTile, t);
                 fence_proxy_async_smem();
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 uint32_t r[32], w[16];
                 tmem_ld_32x32b_x32(t_dp + 32 * c, r);
-                tmem_ld_wait();
+                tmem_ld_wait_for(r);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(s[c][k]) * (__uint_as_float(r[k]) - delta));
                 if (valid < 64) {
@@ -305,7 +322,8 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             tmem_st_wait();
             tc_fence_before();
-            mbar_arrive(bars + 8 * kBwDs);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + 8 * kBwDs);
         }
         if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
         if (ok) {
@@ -338,7 +356,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMisc + 4);
     float *rows_buf = reinterpret_cast<float *>(smem + L::kRows);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int kt = blockIdx.x % p.kv_tiles, bk = blockIdx.x / p.kv_tiles;
     const int kvh = bk % p.kv_heads, b = bk / p.kv_heads;
     const int key0 = kt * kXaRows;
@@ -368,42 +386,56 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (!ok) xa_report(p.status, kXaRoleDkv, 1);
         }
     } else if (warp == 9) {
-        if (lane == 0 && nblk > 0) {
+        if (nblk > 0) {
             constexpr uint32_t idesc_s = xa_idesc<T>(128, 0), idesc_o = xa_idesc<T>(DP, 1);
-            auto wait = [&](int bar, int parity) { return mbar_wait(bars + 8 * bar, parity & 1, abort_flag, limit); };
-            auto q_tile = [&](int i) { return sbase + L::kRingL + (i % L::kLong) * L::kTile; };
-            auto do_tile = [&](int i) { return sbase + L::kRingS + (i % L::kShort) * L::kTile; };
-            auto issue_s = [&](int i) {
-                if (!wait(kBwLFull + i % L::kLong, i / L::kLong)) return false;
-                tc_fence_after();
-                xa_product_nt<DP>(tmem, sbase, q_tile(i), idesc_s);
-                umma_commit(bars + 8 * kBwS);
-                return true;
+            const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0), s0 = sbase, bar0 = s0 + L::kBars;
+            auto wait = [&](int bar, int parity) {
+                return __all_sync(0xffffffffu, mbar_wait(bar0 + 8 * bar, parity & 1, abort_flag, limit)) != 0;
+            };
+            auto q_tile = [&](int i) { return s0 + L::kRingL + (i % L::kLong) * L::kTile; };
+            auto do_tile = [&](int i) { return s0 + L::kRingS + (i % L::kShort) * L::kTile; };
+            auto wait_q = [&](int i) { return wait(kBwLFull + i % L::kLong, i / L::kLong); };
+            auto wait_do = [&](int i) { return wait(kBwSFull + i % L::kShort, i / L::kShort); };
+            auto issue_s = [&](int i) {                                  // (by one lane, like the next)
+                xa_product_nt<DP>(t0, s0, q_tile(i), idesc_s);
+                umma_commit(bar0 + 8 * kBwS);
             };
             auto issue_dp = [&](int i) {
-                if (!wait(kBwSFull + i % L::kShort, i / L::kShort)) return false;
-                tc_fence_after();
-                xa_product_nt<DP>(tmem + 128, sbase + L::kTile, do_tile(i), idesc_s);
-                umma_commit(bars + 8 * kBwDp);
-                return true;
+                xa_product_nt<DP>(t0 + 128, s0 + L::kTile, do_tile(i), idesc_s);
+                umma_commit(bar0 + 8 * kBwDp);
             };
-            bool ok = wait(kBwStat, 0) && issue_s(0) && issue_dp(0);
-            for (int i = 0; i < nblk && ok; ++i) {
-                ok = wait(kBwP, i);
-                if (!ok) break;
+            bool ok = wait(kBwStat, 0) && wait_q(0) && wait_do(0);
+            if (ok) {
                 tc_fence_after();
-                xa_product_tn<64>(tmem + 256, tmem, do_tile(i), idesc_o, i > 0);
-                umma_commit(bars + 8 * (kBwSEmpty + i % L::kShort));
-                if (i + 1 < nblk) ok = issue_s(i + 1);
-                ok = ok && wait(kBwDs, i);
-                if (!ok) break;
-                tc_fence_after();
-                xa_product_tn<64>(tmem + 384, tmem + 128, q_tile(i), idesc_o, i > 0);
-                umma_commit(bars + 8 * (kBwLEmpty + i % L::kLong));
-                if (i + 1 < nblk) ok = issue_dp(i + 1);
-                else umma_commit(bars + 8 * kBwDone);
+                if (elect_one()) {
+                    issue_s(0);
+                    issue_dp(0);
+                }
+                __syncwarp();
             }
-            if (!ok) xa_report(p.status, kXaRoleDkv, 2);
+            for (int i = 0; i < nblk && ok; ++i) {
+                const bool more = i + 1 < nblk;
+                ok = (!more || wait_q(i + 1)) && wait(kBwP, i);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    xa_product_tn<64>(t0 + 256, t0, do_tile(i), idesc_o, i > 0);
+                    umma_commit(bar0 + 8 * (kBwSEmpty + i % L::kShort));
+                    if (more) issue_s(i + 1);
+                }
+                __syncwarp();
+                ok = (!more || wait_do(i + 1)) && wait(kBwDs, i);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    xa_product_tn<64>(t0 + 384, t0 + 128, q_tile(i), idesc_o, i > 0);
+                    umma_commit(bar0 + 8 * (kBwLEmpty + i % L::kLong));
+                    if (more) issue_dp(i + 1);
+                    else umma_commit(bar0 + 8 * kBwDone);
+                }
+                __syncwarp();
+            }
+            if (!ok && lane == 0) xa_report(p.status, kXaRoleDkv, 2);
         }
     } else if (warp == 10) {
         // lse (in units of log2) and delta of each block's queries; a query that does not exist has P = 0
@@ -440,7 +472,8 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             uint32_t s[2][32];
             tmem_ld_32x32b_x32(t_s, s[0]);
             tmem_ld_32x32b_x32(t_s + 32, s[1]);
-            tmem_ld_wait();
+            tmem_ld_wait_for(s[0]);
+            tmem_ld_wait_for(s[1]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 uint32_t w[16];
@@ -462,7 +495,8 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
             tmem_st_wait();
             tc_fence_before();
-            mbar_arrive(bars + 8 * kBwP);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bars + 8 * kBwP);
             ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDp, i & 1, abort_flag, limit));
             if (!ok) break;
             tc_fence_after();
@@ -470,7 +504,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             for (int c = 0; c < 2; ++c) {
                 uint32_t r[32], w[16];
                 tmem_ld_32x32b_x32(t_dp + 32 * c, r);
-                tmem_ld_wait();
+                tmem_ld_wait_for(r);
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const float4 d4 = delta4[c * 8 + k];
@@ -483,8 +517,11 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
             tmem_st_wait();
             tc_fence_before();
-            mbar_arrive(bars + 8 * (kBwRowsEmpty + j));
-            mbar_arrive(bars + 8 * kBwDs);
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(bars + 8 * (kBwRowsEmpty + j));
+                mbar_arrive(bars + 8 * kBwDs);
+            }
         }
         if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
         if (ok) {

@@ -58,7 +58,16 @@ __device__ __forceinline__ void xa_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
 }
 
-// 128 x 128 products over the head dimension: D = A B^T, both tiles K-major.
+// One lane of a converged warp.  The warp that issues products runs its loop as a whole, so that
+// descriptors and addresses are uniform values, and only the instructions themselves are one lane's.
+__device__ __forceinline__ bool elect_one()
+{
+    int one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.s32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+
+// Product over the head dimension: D = A B^T, both tiles K-major (idesc says how many rows of B).
 template <int DP>
 __device__ __forceinline__ void xa_product_nt(uint32_t d, uint32_t a_tile, uint32_t b_tile, uint32_t idesc)
 {
@@ -69,15 +78,18 @@ __device__ __forceinline__ void xa_product_nt(uint32_t d, uint32_t a_tile, uint3
         xa_mma_ss(d, a0 + o, b0 + o, idesc, k > 0);
     }
 }
-// 128 x DP product over a tile's rows: D (+)= P T, P (128 x 128, 16-bit) in tensor memory, tile T
-// MN-major.  The second half of P's columns lies `HALF` tensor-memory columns after the first.
-template <int HALF>
+// Product over a tile's rows: D (+)= P T, P (128 x 128, 16-bit) in tensor memory, tile T MN-major.  P's
+// second 64 values lie STEP tensor-memory columns after its first.  QUARTERS says which 32 of each 64
+// rows take part: 1 the first, 2 the second, 3 all.
+template <int STEP, int QUARTERS = 3>
 __device__ __forceinline__ void xa_product_tn(uint32_t d, uint32_t p_tmem, uint32_t tile, uint32_t idesc, bool accumulate)
 {
     const uint64_t b0 = make_smem_desc_sw128(tile, kXaChunkBytes, 1024);
 #pragma unroll
     for (int k = 0; k < kXaRows / 16; ++k)
-        xa_mma_ts(d, p_tmem + (k / 4) * HALF + (k % 4) * 8, b0 + k * (2048 >> 4), idesc, accumulate || k > 0);
+        if ((k % 4 < 2 ? 1 : 2) & QUARTERS)
+            xa_mma_ts(d, p_tmem + (k / 4) * STEP + (k % 4) * 8, b0 + k * (2048 >> 4), idesc,
+                      accumulate || k > (QUARTERS == 2 ? 2 : 0));
 }
 
 // Instruction descriptor: kind::f16, both operands T, fp32 accumulator, A K-major, M = 128.
@@ -123,12 +135,62 @@ __device__ __forceinline__ void tmem_st_wait()
     asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
+// Waits for the warp's loads from tensor memory; the registers are tied to the wait, so that no use
+// of theirs can be moved ahead of it.
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&r)[N])
+{
+    tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i]));
+}
+
+// Two fp32 values in one register pair: packed arithmetic issues half the instructions.
+__device__ __forceinline__ uint64_t f32x2(float lo, float hi)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ void f32x2_split(uint64_t v, float &lo, float &hi)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t f32x2_fma(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// Maximum of three values; a NaN among them is the result.
+__device__ __forceinline__ float max3_nan(float a, float b, float c)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // 2^x by the special-function unit (relative error ~2^-22); -inf gives 0.
 __device__ __forceinline__ float xa_exp2(float x)
 {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// Named barrier over `threads` threads that also tells each whether `ok` held for all of them.
+__device__ __forceinline__ bool named_bar_all(int id, int threads, bool ok)
+{
+    int all;
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %3, 0;\n\tbar.red.and.pred q, %1, %2, p;\n\t"
+                 "selp.s32 %0, 1, 0, q;\n\t}" : "=r"(all) : "r"(id), "r"(threads), "r"((int)ok) : "memory");
+    return all != 0;
 }
 
 // Valid keys of batch item b.
@@ -139,18 +201,16 @@ __device__ __forceinline__ int xa_keys(const int *lens, int b, int kv_rows)
     return n < 0 ? 0 : (n < kv_rows ? n : kv_rows);
 }
 
-// Zero the rows from `valid` on of a tile that TMA has written (thread t of 128 takes row t): a
-// padded row may hold anything, and 0 x NaN would reach the product's sums.  The writes must be
-// followed by fence_proxy_async_smem() before the tensor core may read them.
+// Zero a row of a tile that TMA has written: a padded row may hold anything, and 0 x NaN would reach
+// the product's sums.  The writes must be followed by fence_proxy_async_smem() before the tensor core
+// may read them.
 template <int DP>
-__device__ __forceinline__ void xa_zero_rows(uint32_t tile, int t, int valid)
+__device__ __forceinline__ void xa_zero_row(uint32_t tile, int row)
 {
-    if (t >= valid)
 #pragma unroll
-        for (int c = 0; c < DP / 64; ++c)
+    for (int c = 0; c < DP / 64; ++c)
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                st_shared_v4_b32(tile + c * kXaChunkBytes + t * 128 + k * 16, 0, 0, 0, 0);
+        for (int k = 0; k < 8; ++k) st_shared_v4_b32(tile + c * kXaChunkBytes + row * 128 + k * 16, 0, 0, 0, 0);
 }
 
 // DP fp32 values of a row, scaled and rounded to T, to `dst` (D of them exist, a multiple of 8).

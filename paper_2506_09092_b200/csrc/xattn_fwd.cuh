@@ -1,25 +1,26 @@
 // Cross attention, forward: O = softmax(scale Q K^T) V per head, keys from kv_len on masked.
 //
 // A CTA owns two tiles of 128 query rows of one head and walks the keys in blocks of 128.
-//   warps 0-3, 4-7  softmax of the first and second tile: a thread is a row (a lane of tensor
-//                   memory), so the row's maximum and sum need no exchange between threads
-//   warp 8          TMA: the queries once, then K and V tiles through a ring
-//   warp 9          the tensor core: S_j = Q_j K^T into tensor memory, O_j += P_j V with P_j read
-//                   from tensor memory (it lies over S_j, as 16-bit values)
+//   warps 0-15      softmax: eight warps per tile; a row is a lane of tensor memory, its 128 scores
+//                   are shared by two threads (of warps w and w + 4) with 64 in registers each
+//   warp 16         TMA: the queries once, then K and V tiles through a ring
+//   warp 17         the tensor core: S = Q K^T into tensor memory, O += P V with P read from tensor
+//                   memory
 // While one tile's softmax runs, the tensor core works for the other.  One pass over the keys: the
-// row's reference maximum is only moved (and O_j rescaled in tensor memory) when a block's maximum
+// row's reference maximum is only moved (and O rescaled in tensor memory) when a block's maximum
 // passes it by more than 2^8, since any reference gives the same quotient; probabilities stay
 // below 2^8, far inside every type's range.
 //
-// Bound: the tensor core (two products of 2 x 128 x 128 x DP multiply-adds per block and pair of
-// tiles) and, close behind it at DP = 64, the special-function unit (16 exponentials per clock).
-// Tensor memory: S_0 and S_1 128 columns each, O_0 and O_1 DP columns each: all 512 at DP = 128.
+// Bound: at DP = 128 the chain softmax -> P V -> next S of a tile, which only the other tile's
+// chain covers: tensor memory (S 2 x 128 columns, O 2 x 128) has no room for a second S, and P lies
+// over S.  At DP = 64 P has columns of its own, the next S starts as soon as this one is in
+// registers, and the special-function unit (16 exponentials per clock) is the bound.
 #pragma once
 #include "xattn_common.cuh"
 
 namespace cudallm {
 
-constexpr int kXaFwdThreads = 320;
+constexpr int kXaFwdThreads = 576;
 
 struct XaFwdParams {
     void *o;
@@ -29,23 +30,42 @@ struct XaFwdParams {
     XaStrides so;
     int q_rows, kv_rows, q_heads, group, batch, head_dim;
     int q_tiles;                // pairs of query tiles per head
-    int splits, blocks_per_split;
+    int splits, tiles_per_split;
     float scale, scale_log2;    // scale, and scale * log2(e)
     int *status;
     int skip_loads;             // self-test of the bounded waits: nothing is loaded, every wait runs out
     unsigned long long wait_limit_ns;
 };
 
+__device__ __forceinline__ float xa_max32(const uint32_t (&r)[32])
+{
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = max3_nan(__uint_as_float(r[i]), __uint_as_float(r[i + 4]), __uint_as_float(r[i + 8]));
+#pragma unroll
+    for (int k = 12; k < 28; k += 8)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = max3_nan(m[i], __uint_as_float(r[k + i]), __uint_as_float(r[k + 4 + i]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = max3_nan(m[i], __uint_as_float(r[28 + i]), __uint_as_float(r[28 + i]));
+    return max3_nan(max3_nan(m[0], m[1], m[2]), m[3], m[3]);
+}
+
 template <int DP> struct XaFwdSmem {
     static constexpr int kTile = DP / 64 * kXaChunkBytes;
-    static constexpr int kStages = DP == 128 ? 5 : 10;
+    static constexpr int kStages = DP == 128 ? 4 : 10;
     static constexpr int kRing = 2 * kTile;
     static constexpr int kBars = kRing + kStages * kTile;
-    // q_full, s_full[2], p_full[2], pv_done[2], full[kStages], empty[kStages]
-    static constexpr int kNumBars = 7 + 2 * kStages;
+    // q_full, s_full[2], p_full[2], pv_done[2], s_read[2], p_half[2], turn[2], full[kStages], empty[kStages]
+    static constexpr int kNumBars = 13 + 2 * kStages;
     static constexpr int kMisc = kBars + kNumBars * 8;
-    static constexpr int kBytes = kMisc + 16;
+    static constexpr int kXch = kMisc + 16 + 8 * (kNumBars & 1);   // floats: [tile][parity][half][row]
+    static constexpr int kBytes = kXch + 2 * 2 * 2 * kXaRows * 4;
+    // tensor memory: S of tile j, P of tile j, O of tile j
+    static constexpr bool kOwnP = DP == 64;
+    static constexpr int kTmemS = 0, kTmemP = kOwnP ? 256 : 0, kStepP = kOwnP ? 64 : 128, kTmemO = kOwnP ? 384 : 256;
 };
+static_assert(XaFwdSmem<128>::kBytes <= 232448 && XaFwdSmem<64>::kBytes > 114 * 1024, "one CTA per SM");
 
 template <int DP, typename T>
 __global__ void __launch_bounds__(kXaFwdThreads, 1)
@@ -56,12 +76,12 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t sbase = smem_u32(smem);
     const uint32_t bars = sbase + L::kBars;
-    const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, pv_done = bars + 40, full = bars + 56,
-                   empty = full + 8 * L::kStages;
+    const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, pv_done = bars + 40, s_read = bars + 56,
+                   p_half = bars + 72, turn = bars + 88, full = bars + 104, empty = full + 8 * L::kStages;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMisc + 4);
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     const int qt = blockIdx.x % p.q_tiles;
     const int bh = blockIdx.x / p.q_tiles;
     const int h = bh % p.q_heads, b = bh / p.q_heads;
@@ -74,8 +94,11 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         mbar_init(q_full, 1);
         for (int j = 0; j < 2; ++j) {
             mbar_init(s_full + 8 * j, 1);
-            mbar_init(p_full + 8 * j, kXaRows);
+            mbar_init(p_full + 8 * j, 8);                                // (one arrival per warp)
             mbar_init(pv_done + 8 * j, 1);
+            mbar_init(s_read + 8 * j, 8);
+            mbar_init(p_half + 8 * j, 8);
+            mbar_init(turn + 8 * j, 8);
         }
         for (int s = 0; s < L::kStages; ++s) {
             mbar_init(full + 8 * s, 1);
@@ -83,7 +106,7 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         }
         fence_mbar_init();
     }
-    if (warp == 9) {
+    if (warp == 17) {
         tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
         tmem_relinquish();
     }
@@ -96,10 +119,11 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     grid_dependency_wait();
 
     const int keys = xa_keys(p.lens, b, p.kv_rows);
-    const int blk0 = blockIdx.y * p.blocks_per_split;
-    const int nblk = min(p.blocks_per_split, (keys + kXaRows - 1) / kXaRows - blk0);      // <= 0: no keys here
+    const int key0 = blockIdx.y * p.tiles_per_split * kXaRows;
+    const int nkeys = min(p.tiles_per_split * kXaRows, keys - key0);                      // <= 0: no keys here
+    const int nblk = (nkeys + kXaRows - 1) / kXaRows;
 
-    if (warp == 8) {
+    if (warp == 16) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
             mbar_expect_tx(q_full, tiles * L::kTile);
             for (int j = 0; j < tiles; ++j) xa_load_tile<DP>(&tm_q, sbase + j * L::kTile, q_full, h, row0 + j * kXaRows, b);
@@ -112,7 +136,7 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                     if (!ok) break;
                     mbar_expect_tx(full + 8 * s, L::kTile);
                     xa_load_tile<DP>(w ? &tm_v : &tm_k, sbase + L::kRing + s * L::kTile, full + 8 * s, kvh,
-                                     (blk0 + i) * kXaRows, b);
+                                     key0 + i * kXaRows, b);
                 }
             }
             if (!ok) {
@@ -126,164 +150,230 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 }
             }
         }
-    } else if (warp == 9) {
-        if (lane == 0 && nblk > 0) {
-            constexpr uint32_t idesc_s = xa_idesc<T>(128, 0), idesc_o = xa_idesc<T>(DP, 1);
-            const uint32_t t_s = tmem, t_o = tmem + 256;
-            bool ok = mbar_wait(q_full, 0, abort_flag, p.wait_limit_ns);
-            ok = ok && mbar_wait(full, 0, abort_flag, p.wait_limit_ns);
+    } else if (warp == 17) {
+        if (nblk > 0) {
+            constexpr uint32_t idesc_s = xa_idesc<T>(kXaRows, 0), idesc_o = xa_idesc<T>(DP, 1);
+            const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0), s0 = sbase, ring = s0 + L::kRing;
+            const uint32_t b0 = s0 + L::kBars, b_s = b0 + 8, b_p = b0 + 24, b_pv = b0 + 40, b_read = b0 + 56, b_half = b0 + 72, b_full = b0 + 104,
+                           b_empty = b_full + 8 * L::kStages;
+            auto wait = [&](uint32_t bar, int parity) {
+                return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, abort_flag, p.wait_limit_ns)) != 0;
+            };
+            // ring position of K of block i: 2 i, of V: 2 i + 1
+            auto stage = [&](int pos) { return pos % L::kStages; };
+            auto wait_tile = [&](int pos) { return wait(b_full + 8 * stage(pos), pos / L::kStages); };
+            auto tile_at = [&](int pos) { return ring + stage(pos) * L::kTile; };
+            auto issue_s = [&](int j, int i) {                            // (by one lane, like the next)
+                xa_product_nt<DP>(t0 + L::kTmemS + 128 * j, s0 + j * L::kTile, tile_at(2 * i), idesc_s);
+                umma_commit(b_s + 8 * j);
+                if (j + 1 == tiles) umma_commit(b_empty + 8 * stage(2 * i));
+            };
+            auto issue_pv_half = [&](int j, int i) {
+                xa_product_tn<64, 1>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, i > 0);
+            };
+            auto issue_pv = [&](int j, int i) {
+                if (L::kOwnP)
+                    xa_product_tn<32>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, i > 0);
+                else
+                    xa_product_tn<64, 2>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, true);
+                umma_commit(b_pv + 8 * j);
+                if (j + 1 == tiles) umma_commit(b_empty + 8 * stage(2 * i + 1));
+            };
+            bool ok = wait(b0, 0) && wait_tile(0);
             if (ok) {
                 tc_fence_after();
-                for (int j = 0; j < tiles; ++j) {
-                    xa_product_nt<DP>(t_s + 128 * j, sbase + j * L::kTile, sbase + L::kRing, idesc_s);
-                    umma_commit(s_full + 8 * j);
-                }
-                umma_commit(empty);
+                if (elect_one())
+                    for (int j = 0; j < tiles; ++j) issue_s(j, 0);
+                __syncwarp();
             }
             for (int i = 0; i < nblk && ok; ++i) {
-                const int iv = 2 * i + 1, ik = 2 * i + 2;                 // ring positions of V(i) and K(i + 1)
-                const int sv = iv % L::kStages, sk = ik % L::kStages;
                 const bool more = i + 1 < nblk;
-                for (int j = 0; j < tiles && ok; ++j) {
-                    if (j == 0) ok = mbar_wait(full + 8 * sv, (iv / L::kStages) & 1, abort_flag, p.wait_limit_ns);
-                    ok = ok && mbar_wait(p_full + 8 * j, i & 1, abort_flag, p.wait_limit_ns);
-                    if (!ok) break;
-                    tc_fence_after();
-                    // (products of one issuing thread run in order: S_j of the next block, which
-                    // overwrites P_j, starts after this product has read it)
-                    xa_product_tn<32>(t_o + DP * j, t_s + 128 * j, sbase + L::kRing + sv * L::kTile, idesc_o, i > 0);
-                    umma_commit(pv_done + 8 * j);
-                    if (more) {
-                        if (j == 0) ok = mbar_wait(full + 8 * sk, (ik / L::kStages) & 1, abort_flag, p.wait_limit_ns);
-                        if (!ok) break;
-                        xa_product_nt<DP>(t_s + 128 * j, sbase + j * L::kTile, sbase + L::kRing + sk * L::kTile, idesc_s);
-                        umma_commit(s_full + 8 * j);
-                    }
-                }
-                if (ok) {
-                    umma_commit(empty + 8 * sv);
-                    if (more) umma_commit(empty + 8 * sk);
-                }
-            }
-            if (!ok) xa_report(p.status, kXaRoleMma, 1);
-        }
-    } else {
-        const int j = warp >> 2;
-        if (j < tiles && nblk > 0) {
-            const int t = tid & (kXaRows - 1);                           // row of the tile = lane of tensor memory
-            const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16;
-            const uint32_t t_s = tmem + 128 * j + t_lane, t_o = tmem + 256 + DP * j + t_lane;
-            float m = -INFINITY, l = 0.f;
-            bool ok = true;
-            for (int i = 0; i < nblk; ++i) {
-                ok = __all_sync(0xffffffffu, mbar_wait(s_full + 8 * j, i & 1, abort_flag, p.wait_limit_ns));
-                if (!ok) break;
-                tc_fence_after();
-                uint32_t r[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(t_s + 32 * c, r[c]);
-                tmem_ld_wait();
-                const int valid = keys - (blk0 + i) * kXaRows;            // keys of this block that exist
-                if (valid < kXaRows) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int k = 0; k < 32; ++k)
-                            if (c * 32 + k >= valid) r[c][k] = 0xFF800000u;                 // -inf
-                    if (j == 0 && keys < p.kv_rows) {
-                        // rows of V that are padding, not beyond the tensor's end
-                        const int iv = 2 * i + 1, sv = iv % L::kStages;
-                        ok = __all_sync(0xffffffffu, mbar_wait(full + 8 * sv, (iv / L::kStages) & 1, abort_flag, p.wait_limit_ns));
-                        if (!ok) break;
-                        xa_zero_rows<DP>(sbase + L::kRing + sv * L::kTile, t, valid);
-                        fence_proxy_async_smem();
-                    }
-                }
-                float mx[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    mx[c] = __uint_as_float(r[c][0]);
-#pragma unroll
-                    for (int k = 1; k < 32; ++k) mx[c] = fmaxf(mx[c], __uint_as_float(r[c][k]));
-                }
-                const float bm = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-                if (i == 0) {
-                    m = bm;
-                } else {
-                    const bool move = (bm - m) * p.scale_log2 > 8.f;
-                    if (__any_sync(0xffffffffu, move)) {
-                        const float alpha = move ? xa_exp2((m - bm) * p.scale_log2) : 1.f;
-                        if (move) m = bm;
-                        l *= alpha;
-                        ok = __all_sync(0xffffffffu, mbar_wait(pv_done + 8 * j, (i - 1) & 1, abort_flag, p.wait_limit_ns));
+                ok = wait_tile(2 * i + 1) && (!more || wait_tile(2 * i + 2));
+                if (L::kOwnP) {
+                    // the next scores of each tile as soon as these have been read
+                    for (int j = 0; j < tiles && ok && more; ++j) {
+                        ok = wait(b_read + 8 * j, i);
                         if (!ok) break;
                         tc_fence_after();
+                        if (elect_one()) issue_s(j, i + 1);
+                        __syncwarp();
+                    }
+                }
+                for (int j = 0; j < tiles && ok; ++j) {
+                    if (!L::kOwnP) {
+                        // the first half of P is multiplied while the exponentials of the second run
+                        ok = wait(b_half + 8 * j, i);
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) issue_pv_half(j, i);
+                        __syncwarp();
+                    }
+                    ok = wait(b_p + 8 * j, i);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        // (products of one issuing thread run in order: the next S, which overwrites P where
+                        // they share their place, starts after this product has read it)
+                        issue_pv(j, i);
+                        if (!L::kOwnP && more) issue_s(j, i + 1);
+                    }
+                    __syncwarp();
+                }
+            }
+            if (!ok && lane == 0) xa_report(p.status, kXaRoleMma, 1);
+        }
+    } else {
+        const int j = warp >> 3, half = (warp >> 2) & 1;                 // tile, half of the block's keys
+        const int t = (warp & 3) * 32 + lane;                            // row of the tile = lane of tensor memory
+        if (j < tiles && nblk > 0) {
+            const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16;
+            const uint32_t t_s = tmem + L::kTmemS + 128 * j + 64 * half + t_lane, t_o = tmem + L::kTmemO + DP * j + t_lane;
+            const uint32_t t_p = tmem + L::kTmemP + L::kStepP * j + (L::kOwnP ? 32 : 64) * half + t_lane;
+            float *xch = reinterpret_cast<float *>(smem + L::kXch) + j * 4 * kXaRows;     // [parity][half][row]
+            float m = -INFINITY, l = 0.f;
+            bool ok = true;
+            auto wait = [&](uint32_t bar, int parity) {
+                return __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, abort_flag, p.wait_limit_ns)) != 0;
+            };
+            for (int i = 0; i < nblk; ++i) {
+                ok = ok && wait(s_full + 8 * j, i);
+                tc_fence_after();
+                uint32_t r[2][32];
+                float bm = -INFINITY;
+                if (ok) {
+                    tmem_ld_32x32b_x32(t_s, r[0]);
+                    tmem_ld_32x32b_x32(t_s + 32, r[1]);
+                    tmem_ld_wait_for(r[0]);
+                    tmem_ld_wait_for(r[1]);
+                    if (L::kOwnP) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(s_read + 8 * j);
+                    }
+                    const int valid = nkeys - i * kXaRows;                // keys of this block that exist
+                    if (valid < kXaRows) {
 #pragma unroll
-                        for (int c = 0; c < DP / 16; ++c) {               // (16 at a time: the block's scores
-                            uint32_t o[16];                               // stay in registers meanwhile)
-                            tmem_ld_32x32b_x16(t_o + 16 * c, o);
-                            tmem_ld_wait();
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int k = 0; k < 32; ++k)
+                                if (half * 64 + c * 32 + k >= valid) r[c][k] = 0xFF800000u;         // -inf
+                        if (j == 0 && half == 0 && key0 + nkeys < p.kv_rows) {
+                            // rows of V that are padding, not beyond the tensor's end
+                            const int sv = (2 * i + 1) % L::kStages;
+                            ok = wait(full + 8 * sv, (2 * i + 1) / L::kStages);
+                            if (ok && t >= valid) xa_zero_row<DP>(sbase + L::kRing + sv * L::kTile, t);
+                            fence_proxy_async_smem();
+                        }
+                    }
+                    bm = max3_nan(xa_max32(r[0]), xa_max32(r[1]), -INFINITY);
+                }
+                // the other half of the row; a wait that failed for one warp ends the loop for all of the
+                // tile's, so that none is missing at a later barrier
+                xch[((i & 1) * 2 + half) * kXaRows + t] = bm;
+                ok = named_bar_all(1 + j, 2 * kXaRows, ok);
+                if (!ok) break;
+                bm = max3_nan(bm, xch[((i & 1) * 2 + (half ^ 1)) * kXaRows + t], bm);
+                const bool move = !((bm - m) * p.scale_log2 <= 8.f);      // (always for the first block, and with a NaN)
+                if (i == 0) {
+                    m = bm;
+                } else if (__any_sync(0xffffffffu, move)) {
+                    const float alpha = move ? xa_exp2((m - bm) * p.scale_log2) : 1.f;
+                    if (move) m = bm;
+                    l *= alpha;
+                    // (block i - 2's product is complete: its P was read before block i - 1's was formed)
+                    ok = wait(pv_done + 8 * j, i - 1);
+                    tc_fence_after();
+                    if (ok) {
+#pragma unroll
+                        for (int c = 0; c < DP / 32; ++c) {               // half of O's columns
+                            uint32_t o[16];
+                            tmem_ld_32x32b_x16(t_o + half * (DP / 2) + 16 * c, o);
+                            tmem_ld_wait_for(o);
 #pragma unroll
                             for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * alpha);
-                            tmem_st_32x32b_x16(t_o + 16 * c, o);
+                            tmem_st_32x32b_x16(t_o + half * (DP / 2) + 16 * c, o);
                         }
                     }
                 }
+                if (L::kOwnP && i > 0) {                                  // the last block's P has been read
+                    ok = ok && wait(pv_done + 8 * j, i - 1);
+                    tc_fence_after();
+                }
+                if (L::kOwnP && tiles == 2 && (i > 0 || j > 0)) ok = ok && wait(turn + 8 * j, j ? i : i - 1);
                 const float neg = -m * p.scale_log2;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2), neg2 = f32x2(neg, neg);
+                uint64_t sum[2] = {0, 0};
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
+                for (int c = 0; c < 2; ++c) {
                     uint32_t w[16];
 #pragma unroll
-                    for (int k = 0; k < 32; k += 2) {
-                        const float e0 = xa_exp2(fmaf(__uint_as_float(r[c][k]), p.scale_log2, neg));
-                        const float e1 = xa_exp2(fmaf(__uint_as_float(r[c][k + 1]), p.scale_log2, neg));
-                        sum[k & 2] += e0;
-                        sum[(k & 2) + 1] += e1;
-                        w[k >> 1] = XaElem<T>::pack(e0, e1);
+                    for (int k = 0; k < 16; ++k) {
+                        float lo, hi;
+                        f32x2_split(f32x2_fma(f32x2(__uint_as_float(r[c][2 * k]), __uint_as_float(r[c][2 * k + 1])), scale2, neg2),
+                                    lo, hi);
+                        lo = xa_exp2(lo);
+                        hi = xa_exp2(hi);
+                        sum[k & 1] = f32x2_add(sum[k & 1], f32x2(lo, hi));
+                        w[k] = XaElem<T>::pack(lo, hi);
                     }
-                    tmem_st_32x32b_x16(t_s + 16 * c, w);                  // over S, which is in registers
+                    tmem_st_32x32b_x16(t_p + 16 * c, w);                  // (over S it is this thread's own half)
+                    if (c == 0) {
+                        if (!L::kOwnP) {
+                            tmem_st_wait();
+                            tc_fence_before();
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(L::kOwnP ? turn + 8 * (j ^ 1) : p_half + 8 * j);
+                    }
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                float s0, s1;
+                f32x2_split(f32x2_add(sum[0], sum[1]), s0, s1);
+                l += s0 + s1;
                 tmem_st_wait();
                 tc_fence_before();
-                mbar_arrive(p_full + 8 * j);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full + 8 * j);
             }
-            // the row's output
-            if (ok) ok = __all_sync(0xffffffffu, mbar_wait(pv_done + 8 * j, (nblk - 1) & 1, abort_flag, p.wait_limit_ns));
+            // the row's output: the halves' sums join, each thread stores half of the columns
+            // (block nblk - 2's product is complete: see above)
+            ok = ok && wait(pv_done + 8 * j, nblk - 1);
+            xch[((nblk & 1) * 2 + half) * kXaRows + t] = l;
+            ok = named_bar_all(1 + j, 2 * kXaRows, ok);
             if (ok) {
                 tc_fence_after();
+                l += xch[((nblk & 1) * 2 + (half ^ 1)) * kXaRows + t];
                 const int row = row0 + j * kXaRows + t;
                 const bool live = row < p.q_rows;
                 const float inv = 1.f / l;
-                const float lse = fmaf(m, p.scale, logf(l));
                 const long long bhr = (long long)bh * p.q_rows + row;
                 const long long rows_all = (long long)p.batch * p.q_heads * p.q_rows;
                 const long long part = (long long)blockIdx.y * rows_all + bhr;
                 T *dst = static_cast<T *>(p.o) + b * p.so.b + row * p.so.r + h * p.so.h;
                 float *dst_part = p.o_part + part * p.head_dim;
 #pragma unroll
-                for (int c = 0; c < DP / 32; ++c) {
+                for (int c = 0; c < DP / 64; ++c) {
+                    const int col = half * (DP / 2) + c * 32;
                     uint32_t o[32];
-                    tmem_ld_32x32b_x32(t_o + 32 * c, o);
-                    tmem_ld_wait();
+                    tmem_ld_32x32b_x32(t_o + col, o);
+                    tmem_ld_wait_for(o);
                     float v[32];
 #pragma unroll
                     for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(o[k]) * inv;
-                    const int left = p.head_dim - c * 32;
+                    const int left = p.head_dim - col;
                     if (live) {
                         if (p.splits == 1) {
-                            xa_store_32(dst + c * 32, v, left);
+                            xa_store_32(dst + col, v, left);
                         } else {
 #pragma unroll
                             for (int g = 0; g < 8; ++g)
                                 if (g * 4 < left)
-                                    *reinterpret_cast<float4 *>(dst_part + c * 32 + g * 4) =
+                                    *reinterpret_cast<float4 *>(dst_part + col + g * 4) =
                                         make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
                         }
                     }
                 }
-                if (live) {
+                if (live && half == 0) {
+                    const float lse = fmaf(m, p.scale, logf(l));
                     if (p.splits > 1) p.lse_part[part] = lse;
                     else if (p.lse) p.lse[bhr] = lse;
                 }
@@ -292,8 +382,8 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
         } else if (j < tiles) {
             // no keys: the output is zero, the sum of no exponentials is zero
-            const int row = row0 + j * kXaRows + (tid & (kXaRows - 1));
-            if (row < p.q_rows) {
+            const int row = row0 + j * kXaRows + t;
+            if (row < p.q_rows && half == 0) {
                 const long long bhr = (long long)bh * p.q_rows + row;
                 if (p.splits > 1) {
                     p.lse_part[(long long)blockIdx.y * p.batch * p.q_heads * p.q_rows + bhr] = -INFINITY;
@@ -306,11 +396,11 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         }
     }
     __syncwarp();
-    // all products have been waited for (the last pv_done), or the kernel gave up after a failed wait;
+    // all products have been waited for (o_done), or the kernel gave up after a failed wait;
     // then the tensor core's queue is drained before tensor memory is released
     tc_fence_before();
     __syncthreads();
-    if (warp == 9) {
+    if (warp == 17) {
         tc_fence_after();
         if (*abort_flag) {
             if (lane == 0) {
