@@ -9,6 +9,43 @@
 
 namespace cudallm {
 
+// Two fp32 values in one register pair: packed arithmetic issues half the instructions.
+__device__ __forceinline__ uint64_t f32x2(float lo, float hi)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ void f32x2_split(uint64_t v, float &lo, float &hi)
+{
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
+}
+__device__ __forceinline__ uint64_t f32x2_fma(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t f32x2_mul(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t f32x2_both(float v) { return f32x2(v, v); }
+__device__ __forceinline__ float f32x2_sum(uint64_t v)
+{
+    float lo, hi;
+    f32x2_split(v, lo, hi);
+    return lo + hi;
+}
+
 __device__ __forceinline__ float elem_to_float(float v) { return v; }
 __device__ __forceinline__ float elem_to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float elem_to_float(__half v) { return __half2float(v); }

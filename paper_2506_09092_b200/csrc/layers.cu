@@ -37,46 +37,87 @@ int check_ld(int64_t rows, int64_t n, int64_t ld)
     return CUDALLM_OK;
 }
 
-// CTAs of `kernel` that one SM holds (asked once per kernel).
+// CTAs of `kernel` that one SM holds (asked once per kernel, device and size of shared memory).
+struct Residency {
+    std::atomic<int> ctas[kRtMaxDevices];
+    std::atomic<int> smem[kRtMaxDevices];
+};
 template <typename Kernel>
-int resident(Kernel kernel, int threads, std::atomic<int> &cache, int *out)
+int resident(Kernel kernel, int threads, int smem, int dev, Residency &cache, int *out)
 {
-    int v = cache.load(std::memory_order_relaxed);
-    if (v == 0) {
-        RT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&v, kernel, threads, 0));
+    int v = cache.ctas[dev].load(std::memory_order_relaxed);
+    if (v == 0 || cache.smem[dev].load(std::memory_order_relaxed) != smem) {
+        if (smem > 48 * 1024)
+            RT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+        RT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&v, kernel, threads, smem));
         if (v < 1) v = 1;
-        cache.store(v, std::memory_order_relaxed);
+        cache.ctas[dev].store(v, std::memory_order_relaxed);
+        cache.smem[dev].store(smem, std::memory_order_relaxed);
     }
     *out = v;
     return CUDALLM_OK;
 }
 
-template <typename T, int VEC, int TPR, int E>
-int launch_ln(const LnRowsParams &p, int sms, cudaStream_t stream)
+struct LnLaunch {
+    int dev, sms;
+    cudaStream_t stream;
+};
+
+template <typename T, int VEC, int TPR, int E, int R>
+int launch_warp(const LnRowsParams &p, const LnLaunch &at)
 {
-    static std::atomic<int> occ{0};
-    auto kernel = layernorm_rows_kernel<T, VEC, TPR, E / VEC>;
+    static Residency occ = {};
+    auto kernel = layernorm_warp_kernel<T, VEC, TPR, E / kUnit<VEC>, R>;
+    const int smem = 2 * p.n * (int)sizeof(float);
     int per_sm = 0;
-    const int st = resident(kernel, ln_threads(TPR), occ, &per_sm);
+    const int st = resident(kernel, kLnWarpThreads, smem, at.dev, occ, &per_sm);
     if (st != CUDALLM_OK) return st;
-    const int64_t grid = std::min<int64_t>(cdiv(p.rows, ln_threads(TPR) / TPR), (int64_t)sms * per_sm);
-    return rt_launch(kernel, dim3((unsigned)grid), ln_threads(TPR), 0, stream, p);
+    const int64_t grid = std::min<int64_t>(cdiv(p.rows, R * (kLnWarpThreads / TPR)), (int64_t)at.sms * per_sm);
+    return rt_launch(kernel, dim3((unsigned)grid), kLnWarpThreads, (size_t)smem, at.stream, p);
+}
+template <typename T, int VEC, int TPR, int E, int R>
+int launch_block(const LnRowsParams &p, const LnLaunch &at)
+{
+    static Residency occ = {};
+    auto kernel = layernorm_block_kernel<T, VEC, TPR, E / kUnit<VEC>, R>;
+    constexpr int smem = ln_slot_bytes(VEC, TPR, E / kUnit<VEC>, R, 1);
+    static_assert(smem <= 200 * 1024, "slots of the rows read and of those on their way");
+    int per_sm = 0;
+    const int st = resident(kernel, TPR, smem, at.dev, occ, &per_sm);
+    if (st != CUDALLM_OK) return st;
+    const int64_t grid = std::min<int64_t>(p.rows, (int64_t)at.sms * per_sm);
+    return rt_launch(kernel, dim3((unsigned)grid), TPR, (size_t)smem, at.stream, p);
 }
 
-// Threads per row and elements per thread by the row's length.  16 elements a thread keep a row,
-// the next one, gamma and beta in registers with two CTAs or more on an SM; short rows are a
-// warp's, which needs no barrier.
+// Lanes or threads per row, values per thread and rows at a time by the row's length.  Where there are rows
+// for every SM's warps, 32 values a thread: the shuffles and addresses of a row are then shared by
+// enough of them (16384 x 4096 bf16: 48.3 us; with 16 values 56, with 8 60; 262144 x 256 on 8 lanes 48.3 us,
+// on 32 lanes 61).  With few rows a row's latency counts and it is spread over more threads.  Rows
+// that are not whole 16-byte pieces carry the next row in registers and take 16 values.
 template <typename T, int VEC>
-int launch_ln_by_length(const LnRowsParams &p, int sms, cudaStream_t stream)
+int launch_ln_by_length(const LnRowsParams &p, const LnLaunch &at)
 {
-    if (p.n <= 256) return launch_ln<T, VEC, 32, 8>(p, sms, stream);
-    if (p.n <= 1024) return launch_ln<T, VEC, 32, 32>(p, sms, stream);
-    if (p.n <= 2048) return launch_ln<T, VEC, 128, 16>(p, sms, stream);
-    if (p.n <= 4096) return launch_ln<T, VEC, 256, 16>(p, sms, stream);
-    if (p.n <= 8192) return launch_ln<T, VEC, 512, 16>(p, sms, stream);
-    if (p.n <= 16384) return launch_ln<T, VEC, 1024, 16>(p, sms, stream);
-    const int64_t grid = std::min<int64_t>(p.rows, (int64_t)sms * 2);
-    return rt_launch(layernorm_long_kernel<T>, dim3((unsigned)grid), kLnLongThreads, 0, stream, p);
+    if (p.n <= 32) return launch_warp<T, VEC, 4, 8, 2>(p, at);
+    if (p.n <= 64) return launch_warp<T, VEC, 4, 16, 2>(p, at);
+    if (p.rows >= 32 * at.sms) {
+        if (p.n <= 128) return launch_warp<T, VEC, 4, 32, 2>(p, at);
+        if (p.n <= 256) return launch_warp<T, VEC, 8, 32, 2>(p, at);
+        if (p.n <= 512) return launch_warp<T, VEC, 16, 32, 2>(p, at);
+        if (p.n <= 1024) return launch_warp<T, VEC, 32, 32, 1>(p, at);
+    }
+    if (p.n <= 256) return launch_warp<T, VEC, 32, 8, 2>(p, at);
+    if (VEC > 1 && p.rows >= 4 * at.sms) {
+        if (p.n <= 2048) return launch_block<T, VEC, 64, 32, 1>(p, at);
+        if (p.n <= 4096) return launch_block<T, VEC, 128, 32, 1>(p, at);
+        if (p.n <= 8192) return launch_block<T, VEC, 256, 32, 1>(p, at);
+    }
+    if (p.n <= 1024) return launch_block<T, VEC, 128, 8, 1>(p, at);
+    if (VEC == 1 && p.n <= 2048) return launch_block<T, VEC, 128, 16, 1>(p, at);
+    if (VEC == 1 && p.n <= 4096) return launch_block<T, VEC, 256, 16, 1>(p, at);
+    if (p.n <= 4096) return launch_block<T, VEC, 512, 8, 1>(p, at);
+    if (p.n <= 16384) return launch_block<T, VEC, 512, 32, 1>(p, at);
+    const int64_t grid = std::min<int64_t>(p.rows, (int64_t)at.sms * 2);
+    return rt_launch(layernorm_long_kernel<T>, dim3((unsigned)grid), kLnLongThreads, 0, at.stream, p);
 }
 
 // Partial rows of dgamma and dbeta at most: enough CTAs for eight per SM where rows are short,
@@ -86,40 +127,71 @@ int64_t ln_max_parts(int64_t n)
     return std::min<int64_t>(1184, std::max<int64_t>(148, int64_t(148) * 8192 / std::max<int64_t>(n, 1)));
 }
 
-template <typename T, int VEC, int TPR, int E>
-int launch_ln_bwd(const LnRowsParams &p, int sms, cudaStream_t stream, int *parts)
+template <typename T, int VEC, int TPR, int E, int R>
+int launch_warp_bwd(const LnRowsParams &p, const LnLaunch &at, int *parts)
 {
-    static std::atomic<int> occ{0};
-    auto kernel = layernorm_rows_bwd_kernel<T, VEC, TPR, E / VEC>;
+    static Residency occ = {};
+    auto kernel = layernorm_warp_bwd_kernel<T, VEC, TPR, E / kUnit<VEC>, R>;
+    constexpr int kRows = kLnWarpThreads / TPR;
+    const int smem = kRows * p.n * (int)sizeof(float);
     int per_sm = 0;
-    const int st = resident(kernel, ln_threads(TPR), occ, &per_sm);
+    const int st = resident(kernel, kLnWarpThreads, smem, at.dev, occ, &per_sm);
     if (st != CUDALLM_OK) return st;
-    int64_t grid = std::min<int64_t>(cdiv(p.rows, ln_threads(TPR) / TPR), (int64_t)sms * per_sm);
-    grid = std::min(grid, ln_max_parts(p.n));
+    const int64_t grid = std::min<int64_t>({cdiv(p.rows, R * kRows), (int64_t)at.sms * per_sm, ln_max_parts(p.n)});
     *parts = (int)grid;
-    return rt_launch(kernel, dim3((unsigned)grid), ln_threads(TPR), 0, stream, p);
+    return rt_launch(kernel, dim3((unsigned)grid), kLnWarpThreads, (size_t)smem, at.stream, p);
+}
+template <typename T, int VEC, int TPR, int E, int R>
+int launch_block_bwd(const LnRowsParams &p, const LnLaunch &at, int *parts)
+{
+    static Residency occ = {};
+    auto kernel = layernorm_block_bwd_kernel<T, VEC, TPR, E / kUnit<VEC>, R>;
+    constexpr int smem = ln_slot_bytes(VEC, TPR, E / kUnit<VEC>, R, 2);
+    static_assert(smem <= 200 * 1024, "slots of the rows read and of those on their way");
+    int per_sm = 0;
+    const int st = resident(kernel, TPR, smem, at.dev, occ, &per_sm);
+    if (st != CUDALLM_OK) return st;
+    const int64_t grid = std::min<int64_t>({(int64_t)p.rows, (int64_t)at.sms * per_sm, ln_max_parts(p.n)});
+    *parts = (int)grid;
+    return rt_launch(kernel, dim3((unsigned)grid), TPR, (size_t)smem, at.stream, p);
 }
 
+// The same for the gradient, whose column sums take registers too: 8 values a thread and two or four rows at
+// a time (16384 x 4096 bf16: 82.5 us; 16 values 85.8, one row at a time 97 to 112).
 template <typename T, int VEC>
-int launch_ln_bwd_by_length(const LnRowsParams &p, int sms, cudaStream_t stream, int *parts)
+int launch_ln_bwd_by_length(const LnRowsParams &p, const LnLaunch &at, int *parts)
 {
-    if (p.n <= 256) return launch_ln_bwd<T, VEC, 32, 8>(p, sms, stream, parts);
-    if (p.n <= 1024) return launch_ln_bwd<T, VEC, 128, 8>(p, sms, stream, parts);
-    if (p.n <= 2048) return launch_ln_bwd<T, VEC, 256, 8>(p, sms, stream, parts);
-    if (p.n <= 4096) return launch_ln_bwd<T, VEC, 512, 8>(p, sms, stream, parts);
-    if (p.n <= 8192) return launch_ln_bwd<T, VEC, 512, 16>(p, sms, stream, parts);
-    if (p.n <= 16384) return launch_ln_bwd<T, VEC, 1024, 16>(p, sms, stream, parts);
+    if (p.n <= 32) return launch_warp_bwd<T, VEC, 4, 8, 2>(p, at, parts);
+    if (p.rows >= 32 * at.sms) {
+        if (p.n <= 64) return launch_warp_bwd<T, VEC, 4, 16, 2>(p, at, parts);
+        if (p.n <= 128) return launch_warp_bwd<T, VEC, 8, 16, 2>(p, at, parts);
+        if (p.n <= 256) return launch_warp_bwd<T, VEC, 16, 16, 2>(p, at, parts);
+        if (p.n <= 512) return launch_warp_bwd<T, VEC, 32, 16, 2>(p, at, parts);
+    }
+    if (p.n <= 256) return launch_warp_bwd<T, VEC, 32, 8, 1>(p, at, parts);
+    if (VEC > 1 && p.rows >= 4 * at.sms) {
+        if (p.n <= 1024) return launch_block_bwd<T, VEC, 128, 8, 4>(p, at, parts);
+        if (p.n <= 2048) return launch_block_bwd<T, VEC, 256, 8, 2>(p, at, parts);
+        if (p.n <= 4096) return launch_block_bwd<T, VEC, 512, 8, 2>(p, at, parts);
+    }
+    if (p.n <= 1024) return launch_block_bwd<T, VEC, 128, 8, 1>(p, at, parts);
+    if (p.n <= 2048) return launch_block_bwd<T, VEC, 256, 8, 1>(p, at, parts);
+    if (p.n <= 4096) return launch_block_bwd<T, VEC, 512, 8, 1>(p, at, parts);
+    if (p.n <= 8192) return launch_block_bwd<T, VEC, 512, 16, 1>(p, at, parts);
+    // (two rows of 16384 fp32 values and the next two take more than an SM's shared memory)
+    if constexpr (sizeof(T) == 2)
+        if (p.n <= 16384) return launch_block_bwd<T, VEC, 1024, 16, 1>(p, at, parts);
     // long rows: the column sums first (dx may lie over x or dy), then dx
     if (p.partials) {
         const int64_t g = std::min<int64_t>({int64_t(148), int64_t(p.rows), std::max<int64_t>(1, 148 * 8 / cdiv(p.n, 256))});
         *parts = (int)g;
         const int st = rt_launch(layernorm_long_columns_kernel<T>, dim3((unsigned)cdiv(p.n, 256), (unsigned)g), 256, 0,
-                                 stream, p);
+                                 at.stream, p);
         if (st != CUDALLM_OK) return st;
     }
     if (!p.y) return CUDALLM_OK;
-    const int64_t grid = std::min<int64_t>(p.rows, (int64_t)sms * 2);
-    return rt_launch(layernorm_long_dx_kernel<T>, dim3((unsigned)grid), kLnLongThreads, 0, stream, p);
+    const int64_t grid = std::min<int64_t>(p.rows, (int64_t)at.sms * 2);
+    return rt_launch(layernorm_long_dx_kernel<T>, dim3((unsigned)grid), kLnLongThreads, 0, at.stream, p);
 }
 
 // 16-byte accesses need bases and pitches on 16-byte boundaries and whole pieces per row.
@@ -134,18 +206,18 @@ bool pieces_ok(int64_t n, std::initializer_list<int64_t> lds, Ptrs... ptrs)
 }
 
 template <typename T>
-int run_ln(const LnRowsParams &p, int sms, cudaStream_t stream)
+int run_ln(const LnRowsParams &p, const LnLaunch &at)
 {
     if (pieces_ok<T>(p.n, {p.ldx, p.ldy}, p.x, p.y))
-        return launch_ln_by_length<T, ElemVec<T>::kN>(p, sms, stream);
-    return launch_ln_by_length<T, 1>(p, sms, stream);
+        return launch_ln_by_length<T, ElemVec<T>::kN>(p, at);
+    return launch_ln_by_length<T, 1>(p, at);
 }
 template <typename T>
-int run_ln_bwd(const LnRowsParams &p, int sms, cudaStream_t stream, int *parts)
+int run_ln_bwd(const LnRowsParams &p, const LnLaunch &at, int *parts)
 {
     if (pieces_ok<T>(p.n, {p.ldx, p.lddy, p.y ? p.ldy : p.ldx}, p.x, p.dy, p.y))
-        return launch_ln_bwd_by_length<T, ElemVec<T>::kN>(p, sms, stream, parts);
-    return launch_ln_bwd_by_length<T, 1>(p, sms, stream, parts);
+        return launch_ln_bwd_by_length<T, ElemVec<T>::kN>(p, at, parts);
+    return launch_ln_bwd_by_length<T, 1>(p, at, parts);
 }
 
 // -------------------------------------------------------------- gradients --
@@ -291,10 +363,10 @@ int cudallm_layernorm_rows(const void *x, const void *gamma, const void *beta, v
     p.rows = (int)rows; p.n = (int)n; p.param_dtype = param_dtype;
     p.eps = eps;
     p.inv_n = 1.f / (float)n;
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    if (dtype == CUDALLM_F32) return run_ln<float>(p, sms, stream);
-    if (dtype == CUDALLM_BF16) return run_ln<__nv_bfloat16>(p, sms, stream);
-    return run_ln<__half>(p, sms, stream);
+    const LnLaunch at{dev, sms, static_cast<cudaStream_t>(stream_v)};
+    if (dtype == CUDALLM_F32) return run_ln<float>(p, at);
+    if (dtype == CUDALLM_BF16) return run_ln<__nv_bfloat16>(p, at);
+    return run_ln<__half>(p, at);
 }
 
 size_t cudallm_layernorm_rows_bwd_scratch_bytes(int64_t rows, int64_t n)
@@ -336,9 +408,10 @@ int cudallm_layernorm_rows_bwd(const void *dy, const void *x, const void *gamma,
         p.ldx = ldx; p.lddy = lddy; p.ldy = lddx;
         p.rows = (int)rows; p.n = (int)n; p.param_dtype = param_dtype;
         p.inv_n = 1.f / (float)n;
-        if (dtype == CUDALLM_F32) st = run_ln_bwd<float>(p, sms, stream, &parts);
-        else if (dtype == CUDALLM_BF16) st = run_ln_bwd<__nv_bfloat16>(p, sms, stream, &parts);
-        else st = run_ln_bwd<__half>(p, sms, stream, &parts);
+        const LnLaunch at{dev, sms, stream};
+        if (dtype == CUDALLM_F32) st = run_ln_bwd<float>(p, at, &parts);
+        else if (dtype == CUDALLM_BF16) st = run_ln_bwd<__nv_bfloat16>(p, at, &parts);
+        else st = run_ln_bwd<__half>(p, at, &parts);
         if (st != CUDALLM_OK) return st;
     }
     if (!sums) return CUDALLM_OK;

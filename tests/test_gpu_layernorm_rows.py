@@ -240,6 +240,14 @@ def test_gradient_against_differences():
         assert abs((loss(x, gamma.double() + e[i]) - loss(x, gamma.double() - e[i])) / (2 * h) - float(dg[j])) < 1e-4
 
 
+@pytest.mark.parametrize("n", [24, 40, 64, 99, 128, 200, 256, 333, 512, 1000, 1001, 1024])
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16, B.F16])
+def test_short_rows_by_the_thousand(n, dtype):
+    """Rows enough for the kernels that give a row to a part of a warp, the last round of rows not full."""
+    check_forward(4999, n, dtype, dtype, in_place=n == 200)
+    check_backward(4999, n, dtype, dtype)
+
+
 def test_graph_replay_side_stream_and_repeatability():
     rows, n = 700, 1537
     _, x = matrix(rows, n, n, B.BF16, 31)
