@@ -113,6 +113,34 @@ FwdPlan plan_fwd(const cudallm_xattn_shape &s)
 // scale of 0 enters as 1e-30: every finite score then gives exp2(0) = 1 all the same.
 inline float scale_log2(const cudallm_xattn_shape &s) { return std::max(s.scale, 1e-30f) * 1.4426950408889634f; }
 
+// The backward call's parts (see xattn_bwd.cuh), planned for kPlanSms SMs, and where they lie in the scratch.
+struct BwdPlan {
+    int dq_parts, dkv_parts, dq_blocks, dkv_blocks;
+    int64_t q_elems, kv_elems;                  // of one part of dQ; of dK and of dV
+    size_t off_dq, off_dk, off_dv, scratch;     // in floats; bytes
+};
+int parts_for(int64_t ctas, int64_t blocks, int *per_part)
+{
+    // at least two blocks a part: one costs about as much as starting a CTA
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({int64_t(32), kPlanSms / std::max<int64_t>(ctas, 1), blocks / 2}));
+    *per_part = (int)cdiv(std::max<int64_t>(blocks, 1), want);
+    return (int)std::max<int64_t>(1, cdiv(blocks, *per_part));
+}
+BwdPlan plan_bwd(const cudallm_xattn_shape &s)
+{
+    BwdPlan f{};
+    const int64_t q_tiles = cdiv(s.q_rows, kXaRows), kv_tiles = cdiv(s.kv_rows, kXaRows), group = s.q_heads / s.kv_heads;
+    f.dq_parts = parts_for(s.batch * s.q_heads * q_tiles, kv_tiles, &f.dq_blocks);
+    f.dkv_parts = parts_for(s.batch * s.kv_heads * kv_tiles, group * q_tiles, &f.dkv_blocks);
+    f.q_elems = s.batch * s.q_heads * s.q_rows * s.head_dim;
+    f.kv_elems = s.batch * s.kv_heads * s.kv_rows * s.head_dim;
+    f.off_dq = (size_t)round_up(s.batch * s.q_heads * s.q_rows, 4);             // behind delta
+    f.off_dk = f.off_dq + (f.dq_parts > 1 ? (size_t)f.dq_parts * f.q_elems : 0);
+    f.off_dv = f.off_dk + (f.dkv_parts > 1 ? (size_t)f.dkv_parts * f.kv_elems : 0);
+    f.scratch = (f.off_dv + (f.dkv_parts > 1 ? (size_t)f.dkv_parts * f.kv_elems : 0)) * sizeof(float);
+    return f;
+}
+
 inline XaStrides strides(const int64_t (&s)[3]) { return XaStrides{(long long)s[0], (long long)s[1], (long long)s[2]}; }
 
 // Tensor map of an operand; an absent one (no rows) gets a map of `other` that no kernel uses.
@@ -214,8 +242,9 @@ int run_fwd(const cudallm_xattn_shape &s, const FwdPlan &f, const void *q, const
 
 template <int DP, typename T>
 int run_bwd(const cudallm_xattn_shape &s, const void *q, const void *k, const void *v, const int32_t *lens, const void *o,
-            const float *lse, const void *d_o, void *dq, void *dk, void *dv, float *delta, int dev, cudaStream_t stream)
+            const float *lse, const void *d_o, void *dq, void *dk, void *dv, float *scratch, int dev, cudaStream_t stream)
 {
+    const BwdPlan f = plan_bwd(s);
     using L = XaBwdSmem<DP>;
     static std::atomic<bool> done_dq[kRtMaxDevices] = {}, done_dkv[kRtMaxDevices] = {};
     int st;
@@ -230,7 +259,10 @@ int run_bwd(const cudallm_xattn_shape &s, const void *q, const void *k, const vo
         || (st = encode(&tdo, d_o, k, f16, s.o_stride, s.batch, s.q_rows, s.q_heads, s.head_dim)) != CUDALLM_OK)
         return st;
     XaBwdParams p{};
-    p.o = o; p.d_o = d_o; p.dq = dq; p.dk = dk; p.dv = dv; p.lse = lse; p.delta = delta; p.lens = lens;
+    p.o = o; p.d_o = d_o; p.dq = dq; p.dk = dk; p.dv = dv; p.lse = lse; p.delta = scratch; p.lens = lens;
+    if (scratch && f.dq_parts > 1) p.dq_part = scratch + f.off_dq;
+    if (scratch && f.dkv_parts > 1) { p.dk_part = scratch + f.off_dk; p.dv_part = scratch + f.off_dv; }
+    p.dq_blocks = f.dq_blocks; p.dkv_blocks = f.dkv_blocks;
     p.sq = strides(s.q_stride); p.sk = strides(s.k_stride); p.sv = strides(s.v_stride); p.so = strides(s.o_stride);
     p.q_rows = (int)s.q_rows; p.kv_rows = (int)s.kv_rows; p.q_heads = (int)s.q_heads; p.kv_heads = (int)s.kv_heads;
     p.group = (int)(s.q_heads / s.kv_heads); p.batch = (int)s.batch; p.head_dim = (int)s.head_dim;
@@ -239,13 +271,31 @@ int run_bwd(const cudallm_xattn_shape &s, const void *q, const void *k, const vo
     if ((st = status_word(dev, &p.status)) != CUDALLM_OK) return st;
     p.wait_limit_ns = rt_wait_limit_ns();
     p.skip_loads = rt_take_skip_loads();
-    if (s.q_rows > 0)
-        st = rt_launch(xattn_dq_kernel<DP, T>, dim3((unsigned)((int64_t)p.q_tiles * s.q_heads * s.batch)), kXaBwdThreads,
-                       (size_t)L::kBytes, stream, tq, tk, tv, tdo, p);
-    if (st != CUDALLM_OK || !dk || s.kv_rows == 0) return st;
-    p.skip_loads = 0;
-    return rt_launch(xattn_dkv_kernel<DP, T>, dim3((unsigned)((int64_t)p.kv_tiles * s.kv_heads * s.batch)), kXaBwdThreads,
-                     (size_t)L::kBytes, stream, tq, tk, tv, tdo, p);
+    if (s.q_rows > 0) {
+        st = rt_launch(xattn_dq_kernel<DP, T>, dim3((unsigned)((int64_t)p.q_tiles * s.q_heads * s.batch), (unsigned)f.dq_parts),
+                       kXaBwdThreads, (size_t)L::kBytes, stream, tq, tk, tv, tdo, p);
+        p.skip_loads = 0;
+    }
+    if (st == CUDALLM_OK && dk && s.kv_rows > 0)
+        st = rt_launch(xattn_dkv_kernel<DP, T>, dim3((unsigned)((int64_t)p.kv_tiles * s.kv_heads * s.batch), (unsigned)f.dkv_parts),
+                       kXaBwdThreads, (size_t)L::kBytes, stream, tq, tk, tv, tdo, p);
+    // the parts' sums
+    if (st == CUDALLM_OK && s.q_rows > 0 && f.dq_parts > 1) {
+        XaGradJoinParams j{};
+        j.part[0] = p.dq_part; j.out[0] = dq; j.st[0] = p.sq; j.f[0] = s.scale;
+        j.parts = f.dq_parts; j.rows = p.q_rows; j.heads = p.q_heads; j.head_dim = p.head_dim;
+        j.rows_all = s.batch * s.q_heads * s.q_rows;
+        st = rt_launch(xattn_grad_join_kernel<T>, dim3((unsigned)cdiv(f.q_elems / 4, 256)), 256, 0, stream, j);
+    }
+    if (st == CUDALLM_OK && dk && s.kv_rows > 0 && f.dkv_parts > 1) {
+        XaGradJoinParams j{};
+        j.part[0] = p.dk_part; j.out[0] = dk; j.st[0] = p.sk; j.f[0] = s.scale;
+        j.part[1] = p.dv_part; j.out[1] = dv; j.st[1] = p.sv; j.f[1] = 1.f;
+        j.parts = f.dkv_parts; j.rows = p.kv_rows; j.heads = p.kv_heads; j.head_dim = p.head_dim;
+        j.rows_all = s.batch * s.kv_heads * s.kv_rows;
+        st = rt_launch(xattn_grad_join_kernel<T>, dim3((unsigned)cdiv(f.kv_elems / 4, 256), 2), 256, 0, stream, j);
+    }
+    return st;
 }
 
 }  // namespace
@@ -301,7 +351,7 @@ int cudallm_xattn_fwd(const cudallm_xattn_shape *shape, const void *q, const voi
 size_t cudallm_xattn_bwd_scratch_bytes(const cudallm_xattn_shape *shape)
 {
     if (check_shape(shape) != CUDALLM_OK || is_empty(*shape)) return 0;
-    return (size_t)(shape->batch * shape->q_heads * shape->q_rows) * sizeof(float);
+    return plan_bwd(*shape).scratch;
 }
 
 int cudallm_xattn_bwd(const cudallm_xattn_shape *shape, const void *q, const void *k, const void *v, const int32_t *kv_lens,
@@ -324,13 +374,13 @@ int cudallm_xattn_bwd(const cudallm_xattn_shape *shape, const void *q, const voi
     int dev = 0, sms = 0;
     if ((st = rt_current_device(&dev, &sms)) != CUDALLM_OK) return st;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    float *delta = static_cast<float *>(scratch);
+    float *scr = queries ? static_cast<float *>(scratch) : nullptr;
     const bool wide = s.head_dim > 64;
     if (s.dtype == CUDALLM_BF16)
-        return wide ? run_bwd<128, __nv_bfloat16>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream)
-                    : run_bwd<64, __nv_bfloat16>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream);
-    return wide ? run_bwd<128, __half>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream)
-                : run_bwd<64, __half>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, delta, dev, stream);
+        return wide ? run_bwd<128, __nv_bfloat16>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scr, dev, stream)
+                    : run_bwd<64, __nv_bfloat16>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scr, dev, stream);
+    return wide ? run_bwd<128, __half>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scr, dev, stream)
+                : run_bwd<64, __half>(s, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scr, dev, stream);
 }
 
 }  // extern "C"

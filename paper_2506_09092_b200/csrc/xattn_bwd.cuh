@@ -33,6 +33,11 @@ struct XaBwdParams {
     XaStrides sq, sk, sv, so;
     int q_rows, kv_rows, q_heads, kv_heads, group, batch, head_dim;
     int q_tiles, kv_tiles;      // of 128 rows
+    // Where one kernel's CTAs are too few to fill the GPU, the axis that they walk is cut into parts
+    // (gridDim.y), whose fp32 results are added in order by xattn_grad_join_kernel.
+    float *dq_part;             // [part][batch][q_heads][q_rows][head_dim], or NULL: one part
+    float *dk_part, *dv_part;   // [part][batch][kv_heads][kv_rows][head_dim], or NULL
+    int dq_blocks, dkv_blocks;  // blocks per part
     float scale, scale_log2;
     int *status;
     int skip_loads;
@@ -154,6 +159,28 @@ __device__ __forceinline__ void xa_bwd_store(uint32_t t_addr, int half, float f,
         if (dst) xa_store_32(dst + col, v, head_dim - col);
     }
 }
+template <int DP>
+__device__ __forceinline__ void xa_bwd_store_part(uint32_t t_addr, int half, float *dst, int head_dim)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 64; ++c) {
+        const int col = half * (DP / 2) + c * 32;
+        uint32_t r[32];
+        tmem_ld_32x32b_x32(t_addr + col, r);
+        tmem_ld_wait_for(r);
+        if (dst)
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+                if (col + g * 4 < head_dim)
+                    *reinterpret_cast<uint4 *>(dst + col + g * 4) = make_uint4(r[4 * g], r[4 * g + 1], r[4 * g + 2], r[4 * g + 3]);
+    }
+}
+template <int DP>
+__device__ __forceinline__ void xa_bwd_zero_part(int half, float *dst, int head_dim)
+{
+    for (int col = half * (DP / 2); col < (half + 1) * (DP / 2) && col < head_dim; col += 4)
+        *reinterpret_cast<float4 *>(dst + col) = make_float4(0.f, 0.f, 0.f, 0.f);
+}
 template <int DP, typename T>
 __device__ __forceinline__ void xa_bwd_zero(int half, T *dst, int head_dim)
 {
@@ -192,13 +219,14 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     grid_launch_dependents();
     grid_dependency_wait();
     const int keys = xa_keys(p.lens, b, p.kv_rows);
-    const int nblk = (keys + kXaRows - 1) / kXaRows;
+    const int blk0 = blockIdx.y * p.dq_blocks;                       // (the first of this part's blocks)
+    const int nblk = min(p.dq_blocks, (keys + kXaRows - 1) / kXaRows - blk0);
     const unsigned long long limit = p.wait_limit_ns;
 
     if (warp == 8) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
             const bool ok = xa_bwd_load<DP>(sbase, &tm_q, &tm_do, h, row0, &tm_k, &tm_v, b, nblk,
-                                            [&](int i, int &hh, int &row) { hh = kvh; row = i * kXaRows; }, abort_flag, limit);
+                                            [&](int i, int &hh, int &row) { hh = kvh; row = (blk0 + i) * kXaRows; }, abort_flag, limit);
             if (!ok) xa_report(p.status, kXaRoleDq, 1);
         }
     } else if (warp == 9) {
@@ -278,7 +306,7 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         xch[half * kXaRows + t] = part;
         named_bar_sync(1, kXaBwdWorkers);
         const float delta = xch[t] + xch[kXaRows + t];
-        if (live && half == 0) p.delta[bhr] = delta;
+        if (live && half == 0 && blockIdx.y == 0) p.delta[bhr] = delta;
         const float lse2 = live ? p.lse[bhr] * 1.4426950408889634f : INFINITY;      // rows that do not exist: P = 0
         bool ok = true;
         for (int i = 0; i < nblk; ++i) {
@@ -286,7 +314,7 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             if (!ok) break;
             tc_fence_after();
             const uint32_t t_s = tmem + (i & 1) * 128 + half * 64 + t_lane, t_dp = tmem + 256 + half * 64 + t_lane;
-            const int valid = keys - i * kXaRows - half * 64;            // of this thread's 64 columns
+            const int valid = keys - (blk0 + i) * kXaRows - half * 64;            // of this thread's 64 columns
             uint32_t s[2][32];
             tmem_ld_32x32b_x32(t_s, s[0]);
             tmem_ld_32x32b_x32(t_s + 32, s[1]);
@@ -300,8 +328,8 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDp, i & 1, abort_flag, limit));
             if (!ok) break;
             tc_fence_after();
-            if (keys - i * kXaRows < kXaRows && keys < p.kv_rows && half == 0) {
-                if (t >= keys - i * kXaRows) xa_zero_row<DP>(sbase + L::kRingL + (i % L::kLong) * L::kTile, t);
+            if (keys - (blk0 + i) * kXaRows < kXaRows && keys < p.kv_rows && half == 0) {
+                if (t >= keys - (blk0 + i) * kXaRows) xa_zero_row<DP>(sbase + L::kRingL + (i % L::kLong) * L::kTile, t);
                 fence_proxy_async_smem();
             }
 #pragma unroll
@@ -326,7 +354,15 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             if (lane == 0) mbar_arrive(bars + 8 * kBwDs);
         }
         if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
-        if (ok) {
+        if (ok && p.dq_part) {
+            float *dst = live ? p.dq_part + ((long long)blockIdx.y * p.batch * p.q_heads * p.q_rows + bhr) * p.head_dim : nullptr;
+            if (nblk > 0) {
+                tc_fence_after();
+                xa_bwd_store_part<DP>(tmem + 384 + t_lane, half, dst, p.head_dim);
+            } else if (live) {
+                xa_bwd_zero_part<DP>(half, dst, p.head_dim);
+            }
+        } else if (ok) {
             T *dst = live ? static_cast<T *>(p.dq) + b * p.sq.b + row * p.sq.r + h * p.sq.h : nullptr;
             if (nblk > 0) {
                 tc_fence_after();
@@ -373,15 +409,17 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     grid_launch_dependents();
     grid_dependency_wait();
     const int keys = xa_keys(p.lens, b, p.kv_rows);
-    const int nblk = key0 < keys ? p.group * p.q_tiles : 0;          // block i: head i / q_tiles of the group
+    // block i: head i / q_tiles of the group; blk0: the first of this part's blocks
+    const int blk0 = blockIdx.y * p.dkv_blocks;
+    const int nblk = key0 < keys ? min(p.dkv_blocks, p.group * p.q_tiles - blk0) : 0;
     const unsigned long long limit = p.wait_limit_ns;
 
     if (warp == 8) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
             const bool ok = xa_bwd_load<DP>(sbase, &tm_k, &tm_v, kvh, key0, &tm_q, &tm_do, b, nblk,
                                             [&](int i, int &hh, int &row) {
-                                                hh = kvh * p.group + i / p.q_tiles;
-                                                row = (i % p.q_tiles) * kXaRows;
+                                                hh = kvh * p.group + (blk0 + i) / p.q_tiles;
+                                                row = ((blk0 + i) % p.q_tiles) * kXaRows;
                                             }, abort_flag, limit);
             if (!ok) xa_report(p.status, kXaRoleDkv, 1);
         }
@@ -444,8 +482,8 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             const int j = i & 1;
             if (i >= 2) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (kBwRowsEmpty + j), ((i >> 1) - 1) & 1, abort_flag, limit));
             if (!ok) break;
-            const int row0 = (i % p.q_tiles) * kXaRows;
-            const long long base = ((long long)b * p.q_heads + kvh * p.group + i / p.q_tiles) * p.q_rows;
+            const int row0 = ((blk0 + i) % p.q_tiles) * kXaRows;
+            const long long base = ((long long)b * p.q_heads + kvh * p.group + (blk0 + i) / p.q_tiles) * p.q_rows;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int r = lane + 32 * u, row = row0 + r;
@@ -527,6 +565,18 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         if (ok) {
             const int key = key0 + t;
             const bool row_live = key < p.kv_rows, valid = key < keys;
+            if (p.dk_part) {
+                const long long at = (((long long)blockIdx.y * p.batch * p.kv_heads + bk) * p.kv_rows + key) * p.head_dim;
+                if (nblk > 0) {
+                    tc_fence_after();
+                    xa_bwd_store_part<DP>(tmem + 256 + t_lane, half, valid ? p.dv_part + at : nullptr, p.head_dim);
+                    xa_bwd_store_part<DP>(tmem + 384 + t_lane, half, valid ? p.dk_part + at : nullptr, p.head_dim);
+                }
+                if (row_live && (!valid || nblk <= 0)) {
+                    xa_bwd_zero_part<DP>(half, p.dv_part + at, p.head_dim);
+                    xa_bwd_zero_part<DP>(half, p.dk_part + at, p.head_dim);
+                }
+            } else {
             T *dk = static_cast<T *>(p.dk) + b * p.sk.b + key * p.sk.r + kvh * p.sk.h;
             T *dv = static_cast<T *>(p.dv) + b * p.sv.b + key * p.sv.r + kvh * p.sv.h;
             if (nblk > 0) {
@@ -538,11 +588,44 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 xa_bwd_zero<DP, T>(half, dk, p.head_dim);
                 xa_bwd_zero<DP, T>(half, dv, p.head_dim);
             }
+            }
         } else if (lane == 0) {
             xa_report(p.status, kXaRoleDkv, 3);
         }
     }
     xa_bwd_finish(bars, tmem, abort_flag, limit);
+}
+
+// Adds the parts of one or two gradients in order and rounds the sums, times f0 and f1.  A thread takes four
+// columns of a row.
+struct XaGradJoinParams {
+    const float *part[2];
+    void *out[2];
+    XaStrides st[2];
+    float f[2];
+    int parts, rows, heads, head_dim;
+    long long rows_all;             // batch * heads * rows
+};
+template <typename T>
+__global__ void __launch_bounds__(256)
+xattn_grad_join_kernel(const XaGradJoinParams p)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int per_row = p.head_dim / 4, a = blockIdx.y;
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= p.rows_all * per_row) return;
+    const long long row = i / per_row;
+    const int col = (int)(i % per_row) * 4;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = 0; s < p.parts; ++s) {
+        const float4 v = *reinterpret_cast<const float4 *>(p.part[a] + (s * p.rows_all + row) * p.head_dim + col);
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+    }
+    const float f = p.f[a];
+    const long long r = row % p.rows, bh = row / p.rows, h = bh % p.heads, b = bh / p.heads;
+    *reinterpret_cast<uint2 *>(static_cast<T *>(p.out[a]) + b * p.st[a].b + r * p.st[a].r + h * p.st[a].h + col) =
+        make_uint2(XaElem<T>::pack(sum.x * f, sum.y * f), XaElem<T>::pack(sum.z * f, sum.w * f));
 }
 
 }  // namespace cudallm

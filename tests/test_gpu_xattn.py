@@ -357,6 +357,17 @@ def test_backward_many_blocks_and_optional_gradients():
     check_backward(1, 200, 300, 2, 2, 64, "bf16", spread=10.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_backward_split_over_the_long_axis(dtype):
+    """Few queries against many states and the other way round: parts that are added afterwards, some of them
+    without states or queries of their own."""
+    check_backward(1, 20, 3000, 2, 1, 64, dtype)
+    check_backward(1, 2500, 30, 2, 1, 64, dtype)
+    check_backward(3, 70, 2000, 2, 2, 128, dtype, lens=[2000, 1, 700], kind="padded")
+    check_backward(2, 1800, 130, 4, 2, 80, dtype, lens=[130, 0], kind="heads")
+    check_backward(1, 40, 1500, 1, 1, 32, dtype, keys_too=False)
+
+
 def test_backward_without_queries_or_states():
     empty = torch.empty(2, 0, 3, 64, device="cuda", dtype=torch.bfloat16)
     some = torch.randn(2, 200, 3, 64, device="cuda").bfloat16()
