@@ -109,14 +109,13 @@ __device__ __forceinline__ bool xa_bwd_load(uint32_t sbase, const CUtensorMap *s
     return ok;
 }
 
+// By warp 0: one barrier per lane.
 template <int DP>
-__device__ __forceinline__ void xa_bwd_init(uint32_t bars, volatile int *abort_flag)
+__device__ __forceinline__ void xa_bwd_init(uint32_t bars, int lane, volatile int *abort_flag)
 {
-    *abort_flag = 0;
-    for (int i = 0; i < XaBwdSmem<DP>::kNumBars; ++i) {
-        const bool workers = i == kBwP || i == kBwDs || i == kBwRowsEmpty || i == kBwRowsEmpty + 1;
-        mbar_init(bars + 8 * i, workers ? kXaBwdWorkers / 32 : 1);      // (one arrival per warp)
-    }
+    const bool workers = lane == kBwP || lane == kBwDs || lane == kBwRowsEmpty || lane == kBwRowsEmpty + 1;
+    if (lane == 0) *abort_flag = 0;
+    if (lane < XaBwdSmem<DP>::kNumBars) mbar_init(bars + 8 * lane, workers ? kXaBwdWorkers / 32 : 1);   // (one arrival per warp)
     fence_mbar_init();
 }
 
@@ -143,38 +142,6 @@ __device__ __forceinline__ void xa_bwd_finish(uint32_t bars, uint32_t tmem, vola
     }
 }
 
-// A worker's half of a row of a DP-column result in tensor memory, times `f`, to `dst` (NULL: not stored).
-template <int DP, typename T>
-__device__ __forceinline__ void xa_bwd_store(uint32_t t_addr, int half, float f, T *dst, int head_dim)
-{
-#pragma unroll
-    for (int c = 0; c < DP / 64; ++c) {
-        const int col = half * (DP / 2) + c * 32;
-        uint32_t r[32];
-        tmem_ld_32x32b_x32(t_addr + col, r);
-        tmem_ld_wait_for(r);
-        float v[32];
-#pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(r[k]) * f;
-        if (dst) xa_store_32(dst + col, v, head_dim - col);
-    }
-}
-template <int DP>
-__device__ __forceinline__ void xa_bwd_store_part(uint32_t t_addr, int half, float *dst, int head_dim)
-{
-#pragma unroll
-    for (int c = 0; c < DP / 64; ++c) {
-        const int col = half * (DP / 2) + c * 32;
-        uint32_t r[32];
-        tmem_ld_32x32b_x32(t_addr + col, r);
-        tmem_ld_wait_for(r);
-        if (dst)
-#pragma unroll
-            for (int g = 0; g < 8; ++g)
-                if (col + g * 4 < head_dim)
-                    *reinterpret_cast<uint4 *>(dst + col + g * 4) = make_uint4(r[4 * g], r[4 * g + 1], r[4 * g + 2], r[4 * g + 3]);
-    }
-}
 template <int DP>
 __device__ __forceinline__ void xa_bwd_zero_part(int half, float *dst, int head_dim)
 {
@@ -207,7 +174,7 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const int h = bh % p.q_heads, b = bh / p.q_heads, kvh = h / p.group;
     const int row0 = qt * kXaRows;
 
-    if (tid == 0) xa_bwd_init<DP>(bars, abort_flag);
+    if (warp == 0) xa_bwd_init<DP>(bars, lane, abort_flag);
     if (warp == 9) {
         tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
         tmem_relinquish();
@@ -286,26 +253,30 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         const int row = row0 + t;
         const bool live = row < p.q_rows;
         const long long bhr = (long long)bh * p.q_rows + row;
-        // delta = rowsum(dO * O): half of the columns each, exchanged through shared memory
-        float part = 0.f;
-        if (live) {
-            const long long at = b * p.so.b + row * p.so.r + h * p.so.h;
-            const T *o = static_cast<const T *>(p.o) + at, *d = static_cast<const T *>(p.d_o) + at;
+        // delta = rowsum(dO * O): DP / 8 neighbouring lanes a row (16 bytes each), the sums by way of shared memory
+        float *delta_s = reinterpret_cast<float *>(smem + L::kRows);
+        {
+            constexpr int kLanes = DP / 8;
+            const int piece = lane % kLanes;
 #pragma unroll
-            for (int c = 0; c < DP / 16; ++c) {
-                const int col = half * (DP / 2) + c * 8;
-                if (col < p.head_dim) {
-                    const uint4 a = *reinterpret_cast<const uint4 *>(o + col), g = *reinterpret_cast<const uint4 *>(d + col);
-                    const T *ae = reinterpret_cast<const T *>(&a), *ge = reinterpret_cast<const T *>(&g);
+            for (int k = 0; k < 16 * kLanes / 32; ++k) {
+                const int r = warp * 16 + k * (32 / kLanes) + lane / kLanes;
+                float part = 0.f;
+                if (row0 + r < p.q_rows && piece * 8 < p.head_dim) {
+                    const long long at = b * p.so.b + (row0 + r) * p.so.r + h * p.so.h + piece * 8;
+                    const uint4 ov = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.o) + at);
+                    const uint4 gv = *reinterpret_cast<const uint4 *>(static_cast<const T *>(p.d_o) + at);
+                    const T *oe = reinterpret_cast<const T *>(&ov), *ge = reinterpret_cast<const T *>(&gv);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) part = fmaf(float(ae[e]), float(ge[e]), part);
+                    for (int e = 0; e < 8; ++e) part = fmaf(float(oe[e]), float(ge[e]), part);
                 }
+#pragma unroll
+                for (int o = kLanes / 2; o; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+                if (piece == 0) delta_s[r] = part;
             }
         }
-        float *xch = reinterpret_cast<float *>(smem + L::kRows);
-        xch[half * kXaRows + t] = part;
         named_bar_sync(1, kXaBwdWorkers);
-        const float delta = xch[t] + xch[kXaRows + t];
+        const float delta = delta_s[t];
         if (live && half == 0 && blockIdx.y == 0) p.delta[bhr] = delta;
         const float lse2 = live ? p.lse[bhr] * 1.4426950408889634f : INFINITY;      // rows that do not exist: P = 0
         bool ok = true;
@@ -354,21 +325,19 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             if (lane == 0) mbar_arrive(bars + 8 * kBwDs);
         }
         if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
-        if (ok && p.dq_part) {
-            float *dst = live ? p.dq_part + ((long long)blockIdx.y * p.batch * p.q_heads * p.q_rows + bhr) * p.head_dim : nullptr;
+        if (ok) {
+            // this warp's rows: half of the columns, staged where the queries were
+            const int first = row0 + (warp & 3) * 32, rows = p.q_rows - first, col = half * (DP / 2), left = p.head_dim - col;
+            const uint32_t stage = sbase + warp * 4096, t_dq = tmem + 384 + t_lane + col;
+            float *part = p.dq_part + ((long long)blockIdx.y * p.batch * p.q_heads * p.q_rows + (long long)bh * p.q_rows + first) * p.head_dim;
+            T *dst = static_cast<T *>(p.dq) + b * p.sq.b + first * p.sq.r + h * p.sq.h;
             if (nblk > 0) {
                 tc_fence_after();
-                xa_bwd_store_part<DP>(tmem + 384 + t_lane, half, dst, p.head_dim);
+                if (p.dq_part) xa_store_part<DP / 2>(t_dq, stage, lane, 1.f, part + col, p.head_dim, rows, left);
+                else xa_store_result<DP / 2, T>(t_dq, stage, lane, p.scale, dst + col, p.sq.r, rows, left);
             } else if (live) {
-                xa_bwd_zero_part<DP>(half, dst, p.head_dim);
-            }
-        } else if (ok) {
-            T *dst = live ? static_cast<T *>(p.dq) + b * p.sq.b + row * p.sq.r + h * p.sq.h : nullptr;
-            if (nblk > 0) {
-                tc_fence_after();
-                xa_bwd_store<DP, T>(tmem + 384 + t_lane, half, p.scale, dst, p.head_dim);
-            } else if (live) {
-                xa_bwd_zero<DP, T>(half, dst, p.head_dim);
+                if (p.dq_part) xa_bwd_zero_part<DP>(half, part + lane * p.head_dim, p.head_dim);
+                else xa_bwd_zero<DP, T>(half, dst + lane * p.sq.r, p.head_dim);
             }
         } else if (lane == 0) {
             xa_report(p.status, kXaRoleDq, 3);
@@ -397,7 +366,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const int kvh = bk % p.kv_heads, b = bk / p.kv_heads;
     const int key0 = kt * kXaRows;
 
-    if (tid == 0) xa_bwd_init<DP>(bars, abort_flag);
+    if (warp == 0) xa_bwd_init<DP>(bars, lane, abort_flag);
     if (warp == 9) {
         tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
         tmem_relinquish();
@@ -494,7 +463,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (lane == 0) mbar_arrive(bars + 8 * (kBwRowsFull + j));
         }
     } else {
-        const int t = tid & (kXaRows - 1), half = tid >> 7;
+        const int half = tid >> 7;
         const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t t_s = tmem + half * 64 + t_lane, t_dp = tmem + 128 + half * 64 + t_lane;
         bool ok = true;
@@ -563,31 +532,31 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         }
         if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
         if (ok) {
-            const int key = key0 + t;
-            const bool row_live = key < p.kv_rows, valid = key < keys;
-            if (p.dk_part) {
-                const long long at = (((long long)blockIdx.y * p.batch * p.kv_heads + bk) * p.kv_rows + key) * p.head_dim;
-                if (nblk > 0) {
-                    tc_fence_after();
-                    xa_bwd_store_part<DP>(tmem + 256 + t_lane, half, valid ? p.dv_part + at : nullptr, p.head_dim);
-                    xa_bwd_store_part<DP>(tmem + 384 + t_lane, half, valid ? p.dk_part + at : nullptr, p.head_dim);
-                }
-                if (row_live && (!valid || nblk <= 0)) {
-                    xa_bwd_zero_part<DP>(half, p.dv_part + at, p.head_dim);
-                    xa_bwd_zero_part<DP>(half, p.dk_part + at, p.head_dim);
-                }
-            } else {
-            T *dk = static_cast<T *>(p.dk) + b * p.sk.b + key * p.sk.r + kvh * p.sk.h;
-            T *dv = static_cast<T *>(p.dv) + b * p.sv.b + key * p.sv.r + kvh * p.sv.h;
+            // this warp's states: half of the columns, staged where K and V were; rows from `keys` on are
+            // padding, and get no gradient
+            const int first = key0 + (warp & 3) * 32, rows = keys - first, col = half * (DP / 2), left = p.head_dim - col;
+            const uint32_t stage = sbase + warp * 4096, t_dv = tmem + 256 + t_lane + col, t_dk = tmem + 384 + t_lane + col;
+            const long long at = (((long long)blockIdx.y * p.batch * p.kv_heads + bk) * p.kv_rows + first) * p.head_dim;
+            T *dk = static_cast<T *>(p.dk) + b * p.sk.b + first * p.sk.r + kvh * p.sk.h;
+            T *dv = static_cast<T *>(p.dv) + b * p.sv.b + first * p.sv.r + kvh * p.sv.h;
             if (nblk > 0) {
                 tc_fence_after();
-                xa_bwd_store<DP, T>(tmem + 256 + t_lane, half, 1.f, valid ? dv : nullptr, p.head_dim);
-                xa_bwd_store<DP, T>(tmem + 384 + t_lane, half, p.scale, valid ? dk : nullptr, p.head_dim);
+                if (p.dk_part) {
+                    xa_store_part<DP / 2>(t_dv, stage, lane, 1.f, p.dv_part + at + col, p.head_dim, rows, left);
+                    xa_store_part<DP / 2>(t_dk, stage, lane, 1.f, p.dk_part + at + col, p.head_dim, rows, left);
+                } else {
+                    xa_store_result<DP / 2, T>(t_dv, stage, lane, 1.f, dv + col, p.sv.r, rows, left);
+                    xa_store_result<DP / 2, T>(t_dk, stage, lane, p.scale, dk + col, p.sk.r, rows, left);
+                }
             }
-            if (row_live && (!valid || nblk == 0)) {                 // padded states, or no queries: no gradient
-                xa_bwd_zero<DP, T>(half, dk, p.head_dim);
-                xa_bwd_zero<DP, T>(half, dv, p.head_dim);
-            }
+            if (first + lane < p.kv_rows && (lane >= rows || nblk <= 0)) {
+                if (p.dk_part) {
+                    xa_bwd_zero_part<DP>(half, p.dv_part + at + lane * p.head_dim, p.head_dim);
+                    xa_bwd_zero_part<DP>(half, p.dk_part + at + lane * p.head_dim, p.head_dim);
+                } else {
+                    xa_bwd_zero<DP, T>(half, dk + lane * p.sk.r, p.head_dim);
+                    xa_bwd_zero<DP, T>(half, dv + lane * p.sv.r, p.head_dim);
+                }
             }
         } else if (lane == 0) {
             xa_report(p.status, kXaRoleDkv, 3);

@@ -191,16 +191,70 @@ __device__ __forceinline__ void xa_zero_row(uint32_t tile, int row)
         for (int k = 0; k < 8; ++k) st_shared_v4_b32(tile + c * kXaChunkBytes + row * 128 + k * 16, 0, 0, 0, 0);
 }
 
-// DP fp32 values of a row, scaled and rounded to T, to `dst` (D of them exist, a multiple of 8).
-template <typename T>
-__device__ __forceinline__ void xa_store_32(T *dst, const float (&v)[32], int left)
+// Rows that a warp's lanes hold (lane t row t, PIECES x 16 bytes of it) to memory.  A store instruction whose
+// lanes write 32 different rows takes as long as 32 lines do, so the rows pass through `stage` (32 x
+// PIECES x 16 bytes of shared memory that only this warp uses; pieces of a row exchanged so that no two
+// lanes meet in a bank) and leave as whole rows, PIECES lanes each.  Of the rows `rows` exist, of their
+// pieces `pieces`.
+template <int PIECES>
+__device__ __forceinline__ void xa_store_rows(uint32_t stage, int lane, const uint4 (&v)[PIECES], uint8_t *dst, long long pitch,
+                                              int rows, int pieces)
+{
+    static_assert(PIECES == 4 || PIECES == 8, "64 or 128 bytes");
+    auto at = [&](int row, int i) {
+        return stage + row * (PIECES * 16) + ((i ^ ((PIECES == 8 ? row : row >> 1) & (PIECES - 1))) << 4);
+    };
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) st_shared_v4_b32(at(lane, i), v[i].x, v[i].y, v[i].z, v[i].w);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) {
+        const int row = (k * 32 + lane) / PIECES, i = lane % PIECES;
+        uint4 w;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(at(row, i)) : "memory");
+        if (row < rows && i < pieces) *reinterpret_cast<uint4 *>(dst + row * pitch + i * 16) = w;
+    }
+    __syncwarp();
+}
+
+// A warp's 32 rows x NC (32 or 64) columns of an fp32 result in tensor memory (from column `t_addr` on), row t times
+// f, to rows of T (`dst`: row 0, first of the columns; `pitch` in elements; `left` columns exist).
+template <int NC, typename T>
+__device__ __forceinline__ void xa_store_result(uint32_t t_addr, uint32_t stage, int lane, float f, T *dst, long long pitch, int rows, int left)
+{
+    uint4 v[NC / 8];
+#pragma unroll
+    for (int c = 0; c < NC / 32; ++c) {
+        uint32_t r[32];
+        tmem_ld_32x32b_x32(t_addr + 32 * c, r);
+        tmem_ld_wait_for(r);
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                w[k] = XaElem<T>::pack(__uint_as_float(r[8 * g + 2 * k]) * f, __uint_as_float(r[8 * g + 2 * k + 1]) * f);
+            v[4 * c + g] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    xa_store_rows<NC / 8>(stage, lane, v, reinterpret_cast<uint8_t *>(dst), pitch * (long long)sizeof(T), rows, left / 8);
+}
+// The same to rows of fp32.
+template <int NC>
+__device__ __forceinline__ void xa_store_part(uint32_t t_addr, uint32_t stage, int lane, float f, float *dst, long long pitch, int rows, int left)
 {
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
-        if (g * 8 < left)
-            *reinterpret_cast<uint4 *>(dst + g * 8) =
-                make_uint4(XaElem<T>::pack(v[8 * g], v[8 * g + 1]), XaElem<T>::pack(v[8 * g + 2], v[8 * g + 3]),
-                           XaElem<T>::pack(v[8 * g + 4], v[8 * g + 5]), XaElem<T>::pack(v[8 * g + 6], v[8 * g + 7]));
+    for (int c = 0; c < NC / 32; ++c) {
+        uint32_t r[32];
+        tmem_ld_32x32b_x32(t_addr + 32 * c, r);
+        tmem_ld_wait_for(r);
+        uint4 v[8];
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            v[g] = make_uint4(__float_as_uint(__uint_as_float(r[4 * g]) * f), __float_as_uint(__uint_as_float(r[4 * g + 1]) * f),
+                              __float_as_uint(__uint_as_float(r[4 * g + 2]) * f), __float_as_uint(__uint_as_float(r[4 * g + 3]) * f));
+        xa_store_rows<8>(stage, lane, v, reinterpret_cast<uint8_t *>(dst + 32 * c), pitch * 4, rows, (left - 32 * c) / 4);
+    }
 }
 
 }  // namespace cudallm

@@ -53,14 +53,17 @@ __device__ __forceinline__ float xa_max32(const uint32_t (&r)[32])
 
 template <int DP> struct XaFwdSmem {
     static constexpr int kTile = DP / 64 * kXaChunkBytes;
-    static constexpr int kStages = DP == 128 ? 4 : 10;
+    static constexpr int kStages = DP == 128 ? 4 : 7;
     static constexpr int kRing = 2 * kTile;
     static constexpr int kBars = kRing + kStages * kTile;
     // q_full, s_full[2], p_full[2], pv_done[2], s_read[2], p_half[2], turn[2], full[kStages], empty[kStages]
     static constexpr int kNumBars = 13 + 2 * kStages;
     static constexpr int kMisc = kBars + kNumBars * 8;
     static constexpr int kXch = kMisc + 16 + 8 * (kNumBars & 1);   // floats: [tile][parity][half][row]
-    static constexpr int kBytes = kXch + 2 * 2 * 2 * kXaRows * 4;
+    // 4 KiB per softmax warp for the output's rows: where the queries were (two tiles of 32 KiB), or behind
+    static constexpr int kEnd = kXch + 2 * 2 * 2 * kXaRows * 4;
+    static constexpr int kStore = DP == 128 ? 0 : (kEnd + 127) / 128 * 128;
+    static constexpr int kBytes = DP == 128 ? kEnd : kStore + 16 * 4096;
     // tensor memory: S of tile j, P of tile j, O of tile j
     static constexpr bool kOwnP = DP == 64;
     static constexpr int kTmemS = 0, kTmemP = kOwnP ? 256 : 0, kStepP = kOwnP ? 64 : 128, kTmemO = kOwnP ? 384 : 256;
@@ -89,21 +92,11 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const int row0 = qt * 2 * kXaRows;
     const int tiles = p.q_rows - row0 > kXaRows ? 2 : 1;
 
-    if (tid == 0) {
-        *abort_flag = 0;
-        mbar_init(q_full, 1);
-        for (int j = 0; j < 2; ++j) {
-            mbar_init(s_full + 8 * j, 1);
-            mbar_init(p_full + 8 * j, 8);                                // (one arrival per warp)
-            mbar_init(pv_done + 8 * j, 1);
-            mbar_init(s_read + 8 * j, 8);
-            mbar_init(p_half + 8 * j, 8);
-            mbar_init(turn + 8 * j, 8);
-        }
-        for (int s = 0; s < L::kStages; ++s) {
-            mbar_init(full + 8 * s, 1);
-            mbar_init(empty + 8 * s, 1);
-        }
+    if (tid == 0) *abort_flag = 0;
+    if (warp == 0) {
+        // one barrier per lane: p_full, s_read, p_half, turn take one arrival per warp of a tile, the others one
+        static_assert(L::kNumBars <= 32, "barriers");
+        if (lane < L::kNumBars) mbar_init(bars + 8 * lane, (lane == 3 || lane == 4 || (lane >= 7 && lane < 13)) ? 8 : 1);
         fence_mbar_init();
     }
     if (warp == 17) {
@@ -342,40 +335,21 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (ok) {
                 tc_fence_after();
                 l += xch[((nblk & 1) * 2 + (half ^ 1)) * kXaRows + t];
-                const int row = row0 + j * kXaRows + t;
-                const bool live = row < p.q_rows;
                 const float inv = 1.f / l;
-                const long long bhr = (long long)bh * p.q_rows + row;
-                const long long rows_all = (long long)p.batch * p.q_heads * p.q_rows;
-                const long long part = (long long)blockIdx.y * rows_all + bhr;
-                T *dst = static_cast<T *>(p.o) + b * p.so.b + row * p.so.r + h * p.so.h;
-                float *dst_part = p.o_part + part * p.head_dim;
-#pragma unroll
-                for (int c = 0; c < DP / 64; ++c) {
-                    const int col = half * (DP / 2) + c * 32;
-                    uint32_t o[32];
-                    tmem_ld_32x32b_x32(t_o + col, o);
-                    tmem_ld_wait_for(o);
-                    float v[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(o[k]) * inv;
-                    const int left = p.head_dim - col;
-                    if (live) {
-                        if (p.splits == 1) {
-                            xa_store_32(dst + col, v, left);
-                        } else {
-#pragma unroll
-                            for (int g = 0; g < 8; ++g)
-                                if (g * 4 < left)
-                                    *reinterpret_cast<float4 *>(dst_part + col + g * 4) =
-                                        make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
-                        }
-                    }
-                }
-                if (live && half == 0) {
+                const int first = row0 + j * kXaRows + (warp & 3) * 32, rows = p.q_rows - first;    // this warp's rows
+                const int col = half * (DP / 2), left = p.head_dim - col;
+                const long long bhr = (long long)bh * p.q_rows + first;
+                const long long part = (long long)blockIdx.y * p.batch * p.q_heads * p.q_rows + bhr;
+                const uint32_t stage = sbase + L::kStore + ((j * 2 + half) * 4 + (warp & 3)) * 4096;
+                if (p.splits == 1)
+                    xa_store_result<DP / 2, T>(t_o + col, stage, lane, inv,
+                                               static_cast<T *>(p.o) + b * p.so.b + first * p.so.r + h * p.so.h + col, p.so.r, rows, left);
+                else
+                    xa_store_part<DP / 2>(t_o + col, stage, lane, inv, p.o_part + part * p.head_dim + col, p.head_dim, rows, left);
+                if (lane < rows && half == 0) {
                     const float lse = fmaf(m, p.scale, logf(l));
-                    if (p.splits > 1) p.lse_part[part] = lse;
-                    else if (p.lse) p.lse[bhr] = lse;
+                    if (p.splits > 1) p.lse_part[part + lane] = lse;
+                    else if (p.lse) p.lse[bhr + lane] = lse;
                 }
             } else if (lane == 0) {
                 xa_report(p.status, kXaRoleSoftmax, 1);
