@@ -39,21 +39,32 @@ int rt_xattn_status(int (&host)[2]);
 
 // Launch with programmatic stream serialisation (the kernel calls griddepcontrol.wait before it
 // touches global memory): its launch latency hides behind the previous kernel of the stream.
+// rt_launch_cluster: the same in clusters of `cluster` CTAs along x.
 template <typename... KArgs, typename... Args>
-int rt_launch(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream, const Args &...args)
+int rt_launch_cluster(void (*kernel)(KArgs...), dim3 grid, unsigned cluster, unsigned block, size_t smem, cudaStream_t stream,
+                      const Args &...args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(block);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     RT_CUDA_TRY(cudaLaunchKernelEx(&cfg, kernel, args...));
     return CUDALLM_OK;
+}
+template <typename... KArgs, typename... Args>
+int rt_launch(void (*kernel)(KArgs...), dim3 grid, unsigned block, size_t smem, cudaStream_t stream, const Args &...args)
+{
+    return rt_launch_cluster(kernel, grid, 1, block, smem, stream, args...);
 }
 
 }  // namespace cudallm

@@ -94,18 +94,19 @@ FwdPlan plan_fwd(const cudallm_xattn_shape &s)
     const int64_t kv = std::max<int64_t>(s.kv_rows, 1);
     int64_t want;
     if (f.token) {
-        // two CTAs per SM; at least 256 keys each, below which the join costs more than it gives
+        // one wave of two CTAs per SM (two waves: 23.5 instead of 18.2 us on 16 x 16 heads of 64 x 1500 states);
+        // at least 256 keys each
         want = std::min<int64_t>({int64_t(32), 2 * kPlanSms / (s.batch * s.kv_heads), kv / 256});
-        f.per_split = round_up(cdiv(kv, std::max<int64_t>(want, 1)), kXaTokKeys);
+        f.per_split = round_up(cdiv(kv, std::max<int64_t>(want, 1)), 32);
         f.splits = (int)cdiv(kv, f.per_split);
     } else {
-        // one CTA per SM; at least four blocks each
+        // one CTA per SM; at least two blocks each
         const int64_t blocks = cdiv(kv, kXaRows), ctas = s.batch * s.q_heads * cdiv(s.q_rows, 2 * kXaRows);
-        want = std::min<int64_t>({int64_t(32), kPlanSms / ctas, blocks / 4});
+        want = std::min<int64_t>({int64_t(32), kPlanSms / ctas, blocks / 2});
         f.per_split = cdiv(blocks, std::max<int64_t>(want, 1));
         f.splits = (int)cdiv(blocks, f.per_split);
     }
-    f.scratch = f.splits > 1 ? (size_t)f.splits * (size_t)f.rows_all * (size_t)(s.head_dim + 1) * sizeof(float) : 0;
+    f.scratch = f.splits > (f.token ? kXaTokCluster : 1) ? (size_t)f.splits * (size_t)f.rows_all * (size_t)(s.head_dim + 1) * sizeof(float) : 0;
     return f;
 }
 
@@ -210,8 +211,10 @@ int run_fwd(const cudallm_xattn_shape &s, const FwdPlan &f, const void *q, const
         p.group = (int)(s.q_heads / s.kv_heads); p.batch = (int)s.batch; p.head_dim = (int)s.head_dim;
         p.splits = f.splits; p.keys_per_split = (int)f.per_split;
         p.scale = s.scale; p.scale_log2 = scale_log2(s);
-        st = rt_launch(xattn_token_kernel<DP, T>, dim3((unsigned)(s.batch * s.kv_heads * f.splits)), kXaTokThreads,
-                       (size_t)L::kBytes, stream, p);
+        p.cluster = f.splits > 1 && f.splits <= kXaTokCluster;
+        st = rt_launch_cluster(xattn_token_kernel<DP, T>, dim3((unsigned)(s.batch * s.kv_heads * f.splits)),
+                               p.cluster ? (unsigned)f.splits : 1u, kXaTokThreads, (size_t)L::kBytes, stream, p);
+        if (p.cluster) return st;
     } else {
         using L = XaFwdSmem<DP>;
         static std::atomic<bool> done[kRtMaxDevices] = {};
