@@ -8,8 +8,9 @@
 // would do with dQ added up through memory; the two extra ones cost less than writing and reading
 // dS or ordered fp32 additions into dQ.
 //
-// Both run the same roles: 256 threads on the 128 x 128 blocks (a thread is a row and a half of the
-// columns), a TMA warp, a warp that issues the products, and (keys) a warp that brings the
+// Both run the same roles: 512 threads on the 128 x 128 blocks (a thread is a row and a quarter of the
+// columns; with half of the columns each, 256 threads, the blocks' exponentials alone took 1250 clocks, for
+// want of warps to cover their latency), a TMA warp, a warp that issues the products, and (keys) a warp that brings the
 // queries' lse and delta.  S and P, dP and dS lie over each other in tensor memory; P and dS, 16
 // bits each, are the A operand of the second products straight from there.
 //
@@ -21,8 +22,8 @@
 
 namespace cudallm {
 
-constexpr int kXaBwdThreads = 352;             // 8 warps on the blocks, TMA, products, lse / delta
-constexpr int kXaBwdWorkers = 256;
+constexpr int kXaBwdThreads = 608;             // 16 warps on the blocks, TMA, products, lse / delta
+constexpr int kXaBwdWorkers = 512;
 
 struct XaBwdParams {
     const void *o, *d_o;
@@ -120,13 +121,13 @@ __device__ __forceinline__ void xa_bwd_init(uint32_t bars, int lane, volatile in
 }
 
 // End of both kernels, by all threads: after a failed wait the products in flight are waited for,
-// then tensor memory is released by warp 9.
+// then tensor memory is released by warp 17.
 __device__ __forceinline__ void xa_bwd_finish(uint32_t bars, uint32_t tmem, volatile int *abort_flag, unsigned long long limit)
 {
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if (threadIdx.x >> 5 == 9) {
+    if (threadIdx.x >> 5 == 17) {
         tc_fence_after();
         if (*abort_flag) {
             if ((threadIdx.x & 31) == 0) {
@@ -142,17 +143,11 @@ __device__ __forceinline__ void xa_bwd_finish(uint32_t bars, uint32_t tmem, vola
     }
 }
 
-template <int DP>
-__device__ __forceinline__ void xa_bwd_zero_part(int half, float *dst, int head_dim)
+// Columns [col, end) of a row of zeros.
+template <typename T>
+__device__ __forceinline__ void xa_bwd_zero(T *row, int col, int end)
 {
-    for (int col = half * (DP / 2); col < (half + 1) * (DP / 2) && col < head_dim; col += 4)
-        *reinterpret_cast<float4 *>(dst + col) = make_float4(0.f, 0.f, 0.f, 0.f);
-}
-template <int DP, typename T>
-__device__ __forceinline__ void xa_bwd_zero(int half, T *dst, int head_dim)
-{
-    for (int col = half * (DP / 2); col < (half + 1) * (DP / 2) && col < head_dim; col += 8)
-        *reinterpret_cast<uint4 *>(dst + col) = make_uint4(0, 0, 0, 0);
+    for (; col < end; col += 16 / (int)sizeof(T)) *reinterpret_cast<uint4 *>(row + col) = make_uint4(0, 0, 0, 0);
 }
 
 // ---------------------------------------------------------------- dQ --
@@ -175,7 +170,7 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const int row0 = qt * kXaRows;
 
     if (warp == 0) xa_bwd_init<DP>(bars, lane, abort_flag);
-    if (warp == 9) {
+    if (warp == 17) {
         tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
         tmem_relinquish();
     }
@@ -190,13 +185,13 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const int nblk = min(p.dq_blocks, (keys + kXaRows - 1) / kXaRows - blk0);
     const unsigned long long limit = p.wait_limit_ns;
 
-    if (warp == 8) {
+    if (warp == 16) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
             const bool ok = xa_bwd_load<DP>(sbase, &tm_q, &tm_do, h, row0, &tm_k, &tm_v, b, nblk,
                                             [&](int i, int &hh, int &row) { hh = kvh; row = (blk0 + i) * kXaRows; }, abort_flag, limit);
             if (!ok) xa_report(p.status, kXaRoleDq, 1);
         }
-    } else if (warp == 9) {
+    } else if (warp == 17) {
         if (nblk > 0) {
             constexpr uint32_t idesc_s = xa_idesc<T>(128, 0), idesc_o = xa_idesc<T>(DP, 1);
             const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0), s0 = sbase, bar0 = s0 + L::kBars;
@@ -232,7 +227,7 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 tc_fence_after();
                 if (elect_one()) {
                     if (i + 1 < nblk) issue_dp(i + 1);
-                    xa_product_tn<64>(t0 + 384, t0 + (i & 1) * 128, k_tile(i), idesc_o, i > 0);
+                    xa_product_tn<2, 32>(t0 + 384, t0 + (i & 1) * 128, k_tile(i), idesc_o, i > 0);
                     umma_commit(bar0 + 8 * (kBwLEmpty + i % L::kLong));
                     if (i + 1 == nblk) umma_commit(bar0 + 8 * kBwDone);
                 }
@@ -247,8 +242,8 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
             if (!ok && lane == 0) xa_report(p.status, kXaRoleDq, 2);
         }
-    } else if (warp < 8) {
-        const int t = tid & (kXaRows - 1), half = tid >> 7;
+    } else if (warp < 16) {
+        const int quarter = warp >> 2, t = (warp & 3) * 32 + lane;        // 32 columns of the block; its row
         const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const int row = row0 + t;
         const bool live = row < p.q_rows;
@@ -259,8 +254,8 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             constexpr int kLanes = DP / 8;
             const int piece = lane % kLanes;
 #pragma unroll
-            for (int k = 0; k < 16 * kLanes / 32; ++k) {
-                const int r = warp * 16 + k * (32 / kLanes) + lane / kLanes;
+            for (int k = 0; k < 8 * kLanes / 32; ++k) {
+                const int r = warp * 8 + k * (32 / kLanes) + lane / kLanes;
                 float part = 0.f;
                 if (row0 + r < p.q_rows && piece * 8 < p.head_dim) {
                     const long long at = b * p.so.b + (row0 + r) * p.so.r + h * p.so.h + piece * 8;
@@ -277,48 +272,40 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         }
         named_bar_sync(1, kXaBwdWorkers);
         const float delta = delta_s[t];
-        if (live && half == 0 && blockIdx.y == 0) p.delta[bhr] = delta;
+        if (live && quarter == 0 && blockIdx.y == 0) p.delta[bhr] = delta;
         const float lse2 = live ? p.lse[bhr] * 1.4426950408889634f : INFINITY;      // rows that do not exist: P = 0
         bool ok = true;
         for (int i = 0; i < nblk; ++i) {
             ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * (kBwS + (i & 1)), (i >> 1) & 1, abort_flag, limit));
             if (!ok) break;
             tc_fence_after();
-            const uint32_t t_s = tmem + (i & 1) * 128 + half * 64 + t_lane, t_dp = tmem + 256 + half * 64 + t_lane;
-            const int valid = keys - (blk0 + i) * kXaRows - half * 64;            // of this thread's 64 columns
-            uint32_t s[2][32];
-            tmem_ld_32x32b_x32(t_s, s[0]);
-            tmem_ld_32x32b_x32(t_s + 32, s[1]);
-            tmem_ld_wait_for(s[0]);
-            tmem_ld_wait_for(s[1]);
+            const uint32_t t_s = tmem + (i & 1) * 128 + quarter * 32 + t_lane, t_dp = tmem + 256 + quarter * 32 + t_lane;
+            const int valid = keys - (blk0 + i) * kXaRows - quarter * 32;        // of this thread's 32 columns
+            uint32_t s[32], r[32], w[16];
+            tmem_ld_32x32b_x32(t_s, s);
+            tmem_ld_wait_for(s);
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int k = 0; k < 32; ++k)
-                    s[c][k] = __float_as_uint(xa_exp2(fmaf(__uint_as_float(s[c][k]), p.scale_log2, -lse2)));
+            for (int k = 0; k < 32; ++k)
+                s[k] = __float_as_uint(xa_exp2(fmaf(__uint_as_float(s[k]), p.scale_log2, -lse2)));
             ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDp, i & 1, abort_flag, limit));
             if (!ok) break;
             tc_fence_after();
-            if (keys - (blk0 + i) * kXaRows < kXaRows && keys < p.kv_rows && half == 0) {
+            if (quarter == 0 && keys - (blk0 + i) * kXaRows < kXaRows && keys < p.kv_rows) {
                 if (t >= keys - (blk0 + i) * kXaRows) xa_zero_row<DP>(sbase + L::kRingL + (i % L::kLong) * L::kTile, t);
                 fence_proxy_async_smem();
             }
+            tmem_ld_32x32b_x32(t_dp, r);
+            tmem_ld_wait_for(r);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t r[32], w[16];
-                tmem_ld_32x32b_x32(t_dp + 32 * c, r);
-                tmem_ld_wait_for(r);
+            for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(s[k]) * (__uint_as_float(r[k]) - delta));
+            if (valid < 32) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) r[k] = __float_as_uint(__uint_as_float(s[c][k]) * (__uint_as_float(r[k]) - delta));
-                if (valid < 64) {
-#pragma unroll
-                    for (int k = 0; k < 32; ++k)
-                        if (c * 32 + k >= valid) r[k] = 0;
-                }
-#pragma unroll
-                for (int k = 0; k < 16; ++k) w[k] = XaElem<T>::pack(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
-                tmem_st_32x32b_x16(t_s + 16 * c, w);
+                for (int k = 0; k < 32; ++k)
+                    if (k >= valid) r[k] = 0;
             }
+#pragma unroll
+            for (int k = 0; k < 16; ++k) w[k] = XaElem<T>::pack(__uint_as_float(r[2 * k]), __uint_as_float(r[2 * k + 1]));
+            tmem_st_32x32b_x16(t_s, w);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -326,18 +313,19 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
         }
         if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
         if (ok) {
-            // this warp's rows: half of the columns, staged where the queries were
-            const int first = row0 + (warp & 3) * 32, rows = p.q_rows - first, col = half * (DP / 2), left = p.head_dim - col;
+            // this warp's rows, 32 columns, staged where the tiles were
+            const int first = row0 + (warp & 3) * 32, rows = p.q_rows - first, col = quarter * 32, left = p.head_dim - col;
             const uint32_t stage = sbase + warp * 4096, t_dq = tmem + 384 + t_lane + col;
             float *part = p.dq_part + ((long long)blockIdx.y * p.batch * p.q_heads * p.q_rows + (long long)bh * p.q_rows + first) * p.head_dim;
             T *dst = static_cast<T *>(p.dq) + b * p.sq.b + first * p.sq.r + h * p.sq.h;
-            if (nblk > 0) {
+            if (nblk > 0 && col < DP) {
                 tc_fence_after();
-                if (p.dq_part) xa_store_part<DP / 2>(t_dq, stage, lane, 1.f, part + col, p.head_dim, rows, left);
-                else xa_store_result<DP / 2, T>(t_dq, stage, lane, p.scale, dst + col, p.sq.r, rows, left);
-            } else if (live) {
-                if (p.dq_part) xa_bwd_zero_part<DP>(half, part + lane * p.head_dim, p.head_dim);
-                else xa_bwd_zero<DP, T>(half, dst + lane * p.sq.r, p.head_dim);
+                if (p.dq_part) xa_store_part<32>(t_dq, stage, lane, 1.f, part + col, p.head_dim, rows, left);
+                else xa_store_result<32, T>(t_dq, stage, lane, p.scale, dst + col, p.sq.r, rows, left);
+            } else if (nblk <= 0 && live) {
+                const int end = min(col + 32, p.head_dim);
+                if (p.dq_part) xa_bwd_zero(part + lane * p.head_dim, col, end);
+                else xa_bwd_zero(dst + lane * p.sq.r, col, end);
             }
         } else if (lane == 0) {
             xa_report(p.status, kXaRoleDq, 3);
@@ -367,7 +355,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const int key0 = kt * kXaRows;
 
     if (warp == 0) xa_bwd_init<DP>(bars, lane, abort_flag);
-    if (warp == 9) {
+    if (warp == 17) {
         tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
         tmem_relinquish();
     }
@@ -383,7 +371,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const int nblk = key0 < keys ? min(p.dkv_blocks, p.group * p.q_tiles - blk0) : 0;
     const unsigned long long limit = p.wait_limit_ns;
 
-    if (warp == 8) {
+    if (warp == 16) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
             const bool ok = xa_bwd_load<DP>(sbase, &tm_k, &tm_v, kvh, key0, &tm_q, &tm_do, b, nblk,
                                             [&](int i, int &hh, int &row) {
@@ -392,7 +380,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                                             }, abort_flag, limit);
             if (!ok) xa_report(p.status, kXaRoleDkv, 1);
         }
-    } else if (warp == 9) {
+    } else if (warp == 17) {
         if (nblk > 0) {
             constexpr uint32_t idesc_s = xa_idesc<T>(128, 0), idesc_o = xa_idesc<T>(DP, 1);
             const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0), s0 = sbase, bar0 = s0 + L::kBars;
@@ -426,7 +414,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    xa_product_tn<64>(t0 + 256, t0, do_tile(i), idesc_o, i > 0);
+                    xa_product_tn<2, 32>(t0 + 256, t0, do_tile(i), idesc_o, i > 0);
                     umma_commit(bar0 + 8 * (kBwSEmpty + i % L::kShort));
                     if (more) issue_s(i + 1);
                 }
@@ -435,7 +423,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
-                    xa_product_tn<64>(t0 + 384, t0 + 128, q_tile(i), idesc_o, i > 0);
+                    xa_product_tn<2, 32>(t0 + 384, t0 + 128, q_tile(i), idesc_o, i > 0);
                     umma_commit(bar0 + 8 * (kBwLEmpty + i % L::kLong));
                     if (more) issue_dp(i + 1);
                     else umma_commit(bar0 + 8 * kBwDone);
@@ -444,7 +432,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             }
             if (!ok && lane == 0) xa_report(p.status, kXaRoleDkv, 2);
         }
-    } else if (warp == 10) {
+    } else if (warp == 18) {
         // lse (in units of log2) and delta of each block's queries; a query that does not exist has P = 0
         bool ok = true;
         for (int i = 0; i < nblk && ok; ++i) {
@@ -463,43 +451,37 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             if (lane == 0) mbar_arrive(bars + 8 * (kBwRowsFull + j));
         }
     } else {
-        const int half = tid >> 7;
+        const int quarter = warp >> 2;                               // 32 columns (queries) of the block
         const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t t_s = tmem + half * 64 + t_lane, t_dp = tmem + 128 + half * 64 + t_lane;
+        const uint32_t t_s = tmem + quarter * 32 + t_lane, t_dp = tmem + 128 + quarter * 32 + t_lane;
         bool ok = true;
         for (int i = 0; i < nblk; ++i) {
             const int j = i & 1;
-            const float4 *lse4 = reinterpret_cast<const float4 *>(rows_buf + j * 256 + half * 64);
+            const float4 *lse4 = reinterpret_cast<const float4 *>(rows_buf + j * 256 + quarter * 32);
             const float4 *delta4 = lse4 + 32;
             ok = mbar_wait(bars + 8 * (kBwRowsFull + j), (i >> 1) & 1, abort_flag, limit)
                  && mbar_wait(bars + 8 * kBwS, i & 1, abort_flag, limit);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
-            uint32_t s[2][32];
-            tmem_ld_32x32b_x32(t_s, s[0]);
-            tmem_ld_32x32b_x32(t_s + 32, s[1]);
-            tmem_ld_wait_for(s[0]);
-            tmem_ld_wait_for(s[1]);
+            uint32_t s[32], w[16];
+            tmem_ld_32x32b_x32(t_s, s);
+            tmem_ld_wait_for(s);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t w[16];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float4 l4 = lse4[c * 8 + k];
-                    const float e0 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k]), p.scale_log2, -l4.x));
-                    const float e1 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k + 1]), p.scale_log2, -l4.y));
-                    const float e2 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k + 2]), p.scale_log2, -l4.z));
-                    const float e3 = xa_exp2(fmaf(__uint_as_float(s[c][4 * k + 3]), p.scale_log2, -l4.w));
-                    s[c][4 * k] = __float_as_uint(e0);
-                    s[c][4 * k + 1] = __float_as_uint(e1);
-                    s[c][4 * k + 2] = __float_as_uint(e2);
-                    s[c][4 * k + 3] = __float_as_uint(e3);
-                    w[2 * k] = XaElem<T>::pack(e0, e1);
-                    w[2 * k + 1] = XaElem<T>::pack(e2, e3);
-                }
-                tmem_st_32x32b_x16(t_s + 16 * c, w);
+            for (int k = 0; k < 8; ++k) {
+                const float4 l4 = lse4[k];
+                const float e0 = xa_exp2(fmaf(__uint_as_float(s[4 * k]), p.scale_log2, -l4.x));
+                const float e1 = xa_exp2(fmaf(__uint_as_float(s[4 * k + 1]), p.scale_log2, -l4.y));
+                const float e2 = xa_exp2(fmaf(__uint_as_float(s[4 * k + 2]), p.scale_log2, -l4.z));
+                const float e3 = xa_exp2(fmaf(__uint_as_float(s[4 * k + 3]), p.scale_log2, -l4.w));
+                s[4 * k] = __float_as_uint(e0);
+                s[4 * k + 1] = __float_as_uint(e1);
+                s[4 * k + 2] = __float_as_uint(e2);
+                s[4 * k + 3] = __float_as_uint(e3);
+                w[2 * k] = XaElem<T>::pack(e0, e1);
+                w[2 * k + 1] = XaElem<T>::pack(e2, e3);
             }
+            tmem_st_32x32b_x16(t_s, w);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -507,21 +489,18 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDp, i & 1, abort_flag, limit));
             if (!ok) break;
             tc_fence_after();
+            uint32_t r[32];
+            tmem_ld_32x32b_x32(t_dp, r);
+            tmem_ld_wait_for(r);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t r[32], w[16];
-                tmem_ld_32x32b_x32(t_dp + 32 * c, r);
-                tmem_ld_wait_for(r);
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float4 d4 = delta4[c * 8 + k];
-                    w[2 * k] = XaElem<T>::pack(__uint_as_float(s[c][4 * k]) * (__uint_as_float(r[4 * k]) - d4.x),
-                                               __uint_as_float(s[c][4 * k + 1]) * (__uint_as_float(r[4 * k + 1]) - d4.y));
-                    w[2 * k + 1] = XaElem<T>::pack(__uint_as_float(s[c][4 * k + 2]) * (__uint_as_float(r[4 * k + 2]) - d4.z),
-                                                   __uint_as_float(s[c][4 * k + 3]) * (__uint_as_float(r[4 * k + 3]) - d4.w));
-                }
-                tmem_st_32x32b_x16(t_dp + 16 * c, w);
+            for (int k = 0; k < 8; ++k) {
+                const float4 d4 = delta4[k];
+                w[2 * k] = XaElem<T>::pack(__uint_as_float(s[4 * k]) * (__uint_as_float(r[4 * k]) - d4.x),
+                                           __uint_as_float(s[4 * k + 1]) * (__uint_as_float(r[4 * k + 1]) - d4.y));
+                w[2 * k + 1] = XaElem<T>::pack(__uint_as_float(s[4 * k + 2]) * (__uint_as_float(r[4 * k + 2]) - d4.z),
+                                               __uint_as_float(s[4 * k + 3]) * (__uint_as_float(r[4 * k + 3]) - d4.w));
             }
+            tmem_st_32x32b_x16(t_dp, w);
             tmem_st_wait();
             tc_fence_before();
             __syncwarp();
@@ -532,31 +511,24 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         }
         if (ok && nblk > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * kBwDone, 0, abort_flag, limit));
         if (ok) {
-            // this warp's states: half of the columns, staged where K and V were; rows from `keys` on are
-            // padding, and get no gradient
-            const int first = key0 + (warp & 3) * 32, rows = keys - first, col = half * (DP / 2), left = p.head_dim - col;
-            const uint32_t stage = sbase + warp * 4096, t_dv = tmem + 256 + t_lane + col, t_dk = tmem + 384 + t_lane + col;
+            // this warp's states: half of the columns of dV (quarters 0, 1) or of dK, staged where the tiles were;
+            // rows from `keys` on are padding, and get no gradient
+            const bool is_k = quarter >= 2;
+            const int first = key0 + (warp & 3) * 32, rows = keys - first, col = (quarter & 1) * (DP / 2), left = p.head_dim - col;
+            const uint32_t stage = sbase + warp * 4096, t_g = tmem + (is_k ? 384 : 256) + t_lane + col;
             const long long at = (((long long)blockIdx.y * p.batch * p.kv_heads + bk) * p.kv_rows + first) * p.head_dim;
-            T *dk = static_cast<T *>(p.dk) + b * p.sk.b + first * p.sk.r + kvh * p.sk.h;
-            T *dv = static_cast<T *>(p.dv) + b * p.sv.b + first * p.sv.r + kvh * p.sv.h;
+            float *part = (is_k ? p.dk_part : p.dv_part) + at;
+            const XaStrides st = is_k ? p.sk : p.sv;
+            T *dst = static_cast<T *>(is_k ? p.dk : p.dv) + b * st.b + first * st.r + kvh * st.h;
             if (nblk > 0) {
                 tc_fence_after();
-                if (p.dk_part) {
-                    xa_store_part<DP / 2>(t_dv, stage, lane, 1.f, p.dv_part + at + col, p.head_dim, rows, left);
-                    xa_store_part<DP / 2>(t_dk, stage, lane, 1.f, p.dk_part + at + col, p.head_dim, rows, left);
-                } else {
-                    xa_store_result<DP / 2, T>(t_dv, stage, lane, 1.f, dv + col, p.sv.r, rows, left);
-                    xa_store_result<DP / 2, T>(t_dk, stage, lane, p.scale, dk + col, p.sk.r, rows, left);
-                }
+                if (p.dk_part) xa_store_part<DP / 2>(t_g, stage, lane, 1.f, part + col, p.head_dim, rows, left);
+                else xa_store_result<DP / 2, T>(t_g, stage, lane, is_k ? p.scale : 1.f, dst + col, st.r, rows, left);
             }
             if (first + lane < p.kv_rows && (lane >= rows || nblk <= 0)) {
-                if (p.dk_part) {
-                    xa_bwd_zero_part<DP>(half, p.dv_part + at + lane * p.head_dim, p.head_dim);
-                    xa_bwd_zero_part<DP>(half, p.dk_part + at + lane * p.head_dim, p.head_dim);
-                } else {
-                    xa_bwd_zero<DP, T>(half, dk + lane * p.sk.r, p.head_dim);
-                    xa_bwd_zero<DP, T>(half, dv + lane * p.sv.r, p.head_dim);
-                }
+                const int end = min(col + DP / 2, p.head_dim);
+                if (p.dk_part) xa_bwd_zero(part + lane * p.head_dim, col, end);
+                else xa_bwd_zero(dst + lane * st.r, col, end);
             }
         } else if (lane == 0) {
             xa_report(p.status, kXaRoleDkv, 3);

@@ -79,18 +79,18 @@ __device__ __forceinline__ void xa_product_nt(uint32_t d, uint32_t a_tile, uint3
         xa_mma_ss(d, a0 + o, b0 + o, idesc, k > 0);
     }
 }
-// Product over a tile's rows: D (+)= P T, P (128 x 128, 16-bit) in tensor memory, tile T MN-major.  P's
-// second 64 values lie STEP tensor-memory columns after its first.  QUARTERS says which 32 of each 64
-// rows take part: 1 the first, 2 the second, 3 all.
-template <int STEP, int QUARTERS = 3>
+// Product over a tile's rows: D (+)= P T, P (128 x 128, 16-bit) in tensor memory, tile T MN-major.  P lies in
+// groups of 16 GROUP values, each STEP tensor-memory columns after the last.  HALVES says which half of each
+// four steps of 16 takes part: 1 the first, 2 the second, 3 both.
+template <int GROUP, int STEP, int HALVES = 3>
 __device__ __forceinline__ void xa_product_tn(uint32_t d, uint32_t p_tmem, uint32_t tile, uint32_t idesc, bool accumulate)
 {
     const uint64_t b0 = make_smem_desc_sw128(tile, kXaChunkBytes, 1024);
 #pragma unroll
     for (int k = 0; k < kXaRows / 16; ++k)
-        if ((k % 4 < 2 ? 1 : 2) & QUARTERS)
-            xa_mma_ts(d, p_tmem + (k / 4) * STEP + (k % 4) * 8, b0 + k * (2048 >> 4), idesc,
-                      accumulate || k > (QUARTERS == 2 ? 2 : 0));
+        if ((k % 4 < 2 ? 1 : 2) & HALVES)
+            xa_mma_ts(d, p_tmem + (k / GROUP) * STEP + (k % GROUP) * 8, b0 + k * (2048 >> 4), idesc,
+                      accumulate || k > (HALVES == 2 ? 2 : 0));
 }
 
 // Instruction descriptor: kind::f16, both operands T, fp32 accumulator, A K-major, M = 128.

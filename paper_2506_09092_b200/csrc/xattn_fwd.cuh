@@ -162,13 +162,13 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                 if (j + 1 == tiles) umma_commit(b_empty + 8 * stage(2 * i));
             };
             auto issue_pv_half = [&](int j, int i) {
-                xa_product_tn<64, 1>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, i > 0);
+                xa_product_tn<4, 64, 1>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, i > 0);
             };
             auto issue_pv = [&](int j, int i) {
                 if (L::kOwnP)
-                    xa_product_tn<32>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, i > 0);
+                    xa_product_tn<4, 32>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, i > 0);
                 else
-                    xa_product_tn<64, 2>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, true);
+                    xa_product_tn<4, 64, 2>(t0 + L::kTmemO + DP * j, t0 + L::kTmemP + L::kStepP * j, tile_at(2 * i + 1), idesc_o, true);
                 umma_commit(b_pv + 8 * j);
                 if (j + 1 == tiles) umma_commit(b_empty + 8 * stage(2 * i + 1));
             };
