@@ -517,12 +517,15 @@ def _main(argv=None):
     ap.add_argument("--table", default=None, help="with --search: JSON file to record the winner in")
     ap.add_argument("--dispatch", default=None,
                     help="a table file, or 'packaged': enter its records into the library's dispatch table first")
-    ap.add_argument("--task", default=None, choices=["transpose", "sum", "dot", "layernorm", "attention", "tf32", "f32"],
+    ap.add_argument("--task", default=None, choices=["transpose", "sum", "dot", "layernorm", "attention", "tf32", "f32", *LAYER_TASKS],
                     help="time one of the other tasks (8, 14, 15, 4, 6; tf32 / f32: Task 2 with float32 operands "
-                         "through cudallm_gemm_tf32 / cudallm_gemm_f32) instead of a GEMM configuration")
+                         "through cudallm_gemm_tf32 / cudallm_gemm_f32; ln-rows ... xattn-bwd: the layer operators) "
+                         "instead of a GEMM configuration")
     ap.add_argument("--size", type=int, default=None,
                     help="with --task: N (transpose: N x N; sum, dot: N elements; layernorm: (16, 4, N, N); "
-                         "attention: N queries and keys; tf32, f32: A (N x 4096) x B (4096 x 2048))")
+                         "attention: N queries and keys; tf32, f32: A (N x 4096) x B (4096 x 2048); ln-rows, ln-rows-bwd: "
+                         "bf16 N x 4096; grad-clip: N bf16 gradients in 48 tensors; xattn, xattn-bwd: N queries x 2 N "
+                         "states, 16 heads of 128; xattn-token: 8 tokens x N states, 32 heads on 8 key heads of 128)")
     ap.add_argument("--layernorm-kernels", default="auto", choices=["auto", "two", "persistent"],
                     help="with --task layernorm: let the library choose by size, or force the two plain "
                          "kernels / the persistent kernel (cudallm_debug_set)")
@@ -568,6 +571,71 @@ def _main(argv=None):
                           "us_min": t["min_s"] * 1e6, "us_median": t["median_s"] * 1e6,
                           "tflops": cfg.flops / t["median_s"] / 1e12,
                           "gbs": cfg.algorithmic_bytes / t["median_s"] / 1e9}), flush=True)
+
+
+LAYER_TASKS = ("ln-rows", "ln-rows-bwd", "grad-clip", "xattn", "xattn-token", "xattn-bwd")
+
+
+def layer_problem(task: str, size: int, nsets: int | None = None):
+    """The same for the operators of include/cudallm_layers.h (``LAYER_TASKS``)."""
+    import torch
+    from . import binding as B
+
+    st = torch.cuda.current_stream()
+    bf = torch.bfloat16
+    gen = torch.Generator(device="cuda").manual_seed(900)
+
+    def normal(*shape):
+        return torch.randn(*shape, device="cuda", generator=gen).to(bf)
+
+    def sets(bytes_):
+        return nsets or max(1, min(8, (400 << 20) // max(bytes_, 1) + 1))
+
+    if task in ("ln-rows", "ln-rows-bwd"):
+        cols = 4096
+        bytes_ = (2 if task == "ln-rows" else 3) * 2 * size * cols
+        n = sets(bytes_)
+        x, dy = [normal(size, cols) for _ in range(n)], [normal(size, cols) for _ in range(n)]
+        out = [torch.empty_like(t) for t in x]
+        gamma, beta, dg, db = (torch.ones(cols, device="cuda") for _ in range(4))
+        mean, rstd = torch.empty(size, device="cuda"), torch.empty(size, device="cuda")
+
+        def forward(i):
+            return B.layernorm_rows(x[i % n], gamma, beta, out[i % n], mean, rstd, size, cols, cols, cols, B.BF16, B.F32, 1e-5, st)
+
+        if task == "ln-rows":
+            return forward, bytes_, f"{size} x {cols} bf16"
+        forward(0)
+        need = B.layernorm_rows_bwd_scratch_bytes(size, cols)
+        scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+        return (lambda i: B.layernorm_rows_bwd(dy[i % n], x[i % n], gamma, mean, rstd, out[i % n], dg, db, size, cols, cols, cols,
+                                               cols, B.BF16, B.F32, scratch, need, st)), bytes_, f"{size} x {cols} bf16"
+    if task == "grad-clip":
+        n = sets(4 * size)
+        tables = [B.tensor_table(list(normal(size).chunk(48))) for _ in range(n)]
+        norm, need = torch.empty(1, device="cuda"), B.grad_norm_scratch_bytes(48)
+        scratch = torch.empty(need, dtype=torch.uint8, device="cuda")
+        return (lambda i: B.grad_clip_norm(tables[i % n], 1e-3, 1e-6, norm, scratch, need, st)), 4 * size, \
+            f"{size} bf16 gradients in 48 tensors, in place"
+    batch, rows, states, heads, kv_heads = ((8, 1, size, 32, 8) if task == "xattn-token" else (1, size, 2 * size, 16, 16))
+    bytes_ = 2 * 128 * batch * (2 * rows * heads + 2 * states * kv_heads)
+    n = sets(bytes_)
+    q, o, do, dq = ([normal(batch, rows, heads, 128) for _ in range(n)] for _ in range(4))
+    k, v, dk, dv = ([normal(batch, states, kv_heads, 128) for _ in range(n)] for _ in range(4))
+    lse = torch.empty(batch, heads, rows, device="cuda")
+    shape = B.XattnShape.of(q[0], k[0], v[0], o[0])
+    need = max(B.xattn_fwd_scratch_bytes(shape), B.xattn_bwd_scratch_bytes(shape))
+    scratch = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    what = f"{batch} x {rows} queries x {states} states, {heads} heads on {kv_heads} key heads of 128, bf16"
+
+    def attend(i):
+        return B.xattn_fwd(shape, q[i % n], k[i % n], v[i % n], None, o[i % n], lse, scratch, need, st)
+
+    if task != "xattn-bwd":
+        return attend, bytes_, what
+    attend(0)
+    return (lambda i: B.xattn_bwd(shape, q[i % n], k[i % n], v[i % n], None, o[i % n], lse, do[i % n], dq[i % n], dk[i % n],
+                                  dv[i % n], scratch, need, st)), 2 * bytes_, what
 
 
 def task_problem(task: str, size: int, nsets: int | None = None):
@@ -636,17 +704,21 @@ def _task_main(args):
     from . import binding as B
 
     default = {"transpose": 8192, "sum": 1 << 28, "dot": 1 << 27, "layernorm": 512, "attention": 512,
-               "tf32": 1 << 14, "f32": 1 << 14}
+               "tf32": 1 << 14, "f32": 1 << 14, "ln-rows": 16384, "ln-rows-bwd": 16384, "grad-clip": 1 << 28, "xattn": 2048,
+               "xattn-token": 16384, "xattn-bwd": 2048}
     size = args.size or default[args.task]
     if args.task == "layernorm":
         B.debug_set(B.DEBUG_LAYERNORM_PATH, {"auto": 0, "two": 1, "persistent": 2}[args.layernorm_kernels])
-    launch, bytes_, what = task_problem(args.task, size, args.sets)
+    problem = layer_problem if args.task in LAYER_TASKS else task_problem
+    launch, bytes_, what = problem(args.task, size, args.sets)
     t = performance_profiler(launch, iters=args.iters, warmup=args.warmup)
     code, detail = B.device_status(torch.cuda.current_stream())
     rec = {"task": args.task, "input": what, "status": code, "us_min": t["min_s"] * 1e6,
            "us_median": t["median_s"] * 1e6, "gbs": bytes_ / t["median_s"] / 1e9}
     if args.task in ("tf32", "f32"):
         rec["tflops"] = 2.0 * size * 4096 * 2048 / t["median_s"] / 1e12
+    if args.task in ("xattn", "xattn-bwd"):
+        rec["tflops"] = (4 if args.task == "xattn" else 10) * size * 2.0 * size * 16 * 128 / t["median_s"] / 1e12
     print(json.dumps(rec), flush=True)
 
 

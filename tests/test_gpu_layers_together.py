@@ -176,3 +176,13 @@ def test_single_tokens_answer_like_the_whole_sequence():
         # each of the two within 2^-8 (|O| + sum p |v|) of the exact value, sum p |v| <= max |v| of the item
         top = v.float().abs().amax((1, 3)).repeat_interleave(HEADS // KV_HEADS, 1)[:, None, :, None]
         assert bool(((o.float() - whole).abs() <= 2 * 2.0 ** -8 * (whole.abs() + top)).all())
+
+
+@pytest.mark.parametrize("task,size", [("ln-rows", 50), ("ln-rows-bwd", 50), ("grad-clip", 10000), ("xattn", 64), ("xattn-token", 100),
+                                       ("xattn-bwd", 64)])
+def test_harness_layer_commands_run(task, size, capsys):
+    import json
+    from paper_2506_09092_b200 import harness as H
+    H._main(["--task", task, "--size", str(size), "--iters", "2", "--warmup", "1"])
+    line = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    assert line["task"] == task and line["status"] == 0 and line["us_median"] > 0
