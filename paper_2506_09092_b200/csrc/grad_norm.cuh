@@ -6,7 +6,7 @@
 // chunk's tensor by bisection.  Bound: HBM; the second kernel visits the chunks in reverse, so
 // that it starts with what the first one left in L2.
 // Measured (one B200): 403 M bf16 values in 291 tensors, scaled into other buffers: 414 us, the norm alone 130
-// us = 6.2 TB/s, the scaling 267 us = 6.1 TB/s; 6.8 M in 27 tensors: 10 us.  Eviction priorities for
+// us = 6.2 TB/s, the scaling 280 us = 5.8 TB/s; 6.8 M in 27 tensors: 10 us.  Eviction priorities for
 // the chunks that the second pass meets first: 407 to 410 us whatever was kept, so none are given.
 #pragma once
 #include "elem.cuh"

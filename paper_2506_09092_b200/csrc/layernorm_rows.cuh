@@ -16,8 +16,8 @@
 // few to occupy the warps, are a CTA's.
 //
 // Measured (one B200; bytes read and written once): 16384 x 4096 bf16 forward 48.4 us = 5.5 TB/s (0.85 of the
-// measured copy bandwidth), backward 82.2 us = 4.9 TB/s; the same in fp32 96 us = 5.6 and 132 us =
-// 6.1 TB/s; 262144 x 256 bf16 forward 48.3 us = 5.6 TB/s; 2999 x 1537 fp32 (no 16-byte rows) 9.6 and
+// measured copy bandwidth), backward 82.2 us = 4.9 TB/s; the same in fp32 97 us = 5.6 and 132 us =
+// 6.1 TB/s; 262144 x 256 bf16 forward 48.3 us = 5.6 TB/s; 2999 x 1537 fp32 (no 16-byte rows) 9.7 and
 // 19.4 us.  What is left is issue slots (55 and 63 % of them at 4096 bf16) and the two barriers of a row.
 #pragma once
 #include "elem.cuh"

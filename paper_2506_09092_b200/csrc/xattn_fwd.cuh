@@ -19,13 +19,11 @@
 //
 // Measured (one B200): 2048 queries x up to 4096 states, 4 x 16 heads of 128, lengths 3/8 to 1 (210
 // GFLOP): 185-207 us = 1.02-1.14 PFLOP/s, 0.62-0.69 of the measured cuBLAS burst, at the power cap when
-// it runs for seconds (215 us at 1.68 GHz).  512 x 4096, 74 heads of 64: 58 us = 0.69 PFLOP/s.  A block of
-// a tile takes 3200 clocks at DP = 128, of which the exponentials 1340, the products of P and the next S
-// 770 behind the last of them, handing over the rest.
-// Tried and not kept: exponentials by polynomial on the FMA pipe (slower by 2 to 20 %: the chain is
-// latency, not the unit's rate); blocks of 64 keys with two places for S (254 us: with N = 64 a product
+// it runs for seconds (215 us).  512 x 4096, 74 heads of 64: 58 us = 0.69 PFLOP/s.
+// Tried and not kept: 5 to 8 of 16 exponentials by polynomial on the FMA pipe (221 to 236 us when the kernel
+// without them took 213 to 217); blocks of 64 keys with two places for S (254 us: with N = 64 a product
 // is bound by reading the queries from shared memory, 48 clocks instead of 32); exponentials before the
-// halves of a row have exchanged their maxima (same time at DP = 128, 73 us at 64).
+// halves of a row have exchanged their maxima (198 to 210 us instead of 198 at DP = 128, 73 at 64).
 #pragma once
 #include "xattn_common.cuh"
 

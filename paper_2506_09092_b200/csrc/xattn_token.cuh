@@ -9,7 +9,7 @@
 // the warps' results join in shared memory.  Up to eight splits are a cluster of CTAs, which read each
 // other's results from shared memory; more of them join in xattn_join_kernel.
 //
-// Measured (one B200): 8 x 32 heads on 8 key heads of 128, 16384 states (537 MB): 80.6 us = 6.66 TB/s, 1.02 of the
+// Measured (one B200): 8 x 32 heads on 8 key heads of 128, 16384 states (537 MB): 80.6-81.4 us = 6.6-6.7 TB/s, 1.01-1.02 of the
 // measured copy bandwidth; 16 x 16 heads of 64, up to 1500 states (70 MB): 15.6 us = 4.5 TB/s, one wave
 // of 256 CTAs of unequal length (two waves of half the size: 23.5 us).
 #pragma once
