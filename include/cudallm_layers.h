@@ -57,7 +57,7 @@ extern "C" {
  * rounded once.  A row that holds an infinity or a NaN gives NaN in that row only.
  * rows == 0 or n == 0: success, nothing written.
  * Errors: INVALID_DIM (negative, rows or n >= 2^31 - 1024, eps negative or not
- * finite), INVALID_LD, INVALID_DTYPE, INVALID_POINTER (x or y NULL), MISALIGNED
+ * finite), INVALID_LD (also for y == x with another pitch), INVALID_DTYPE, INVALID_POINTER (x or y NULL), MISALIGNED
  * (a pointer off its element size), UNSUPPORTED_DEVICE, CUDA.
  */
 int cudallm_layernorm_rows(const void *x, const void *gamma, const void *beta, void *y, float *mean, float *rstd,
@@ -169,7 +169,8 @@ typedef struct cudallm_xattn_shape {
  * Kernels: (q_heads / kv_heads) * q_rows <= 16 rows per key head (single tokens) take
  * a kernel that reads every K and V once and splits the keys over the GPU; longer
  * queries one that owns 256 query rows of a head per CTA, split over the keys where
- * there are too few of those.  Split calls join in a second launch.
+ * there are too few of those.  Up to eight splits of single tokens join inside the
+ * launch (a cluster of CTAs, no scratch); all other split calls in a second one.
  * batch, q_rows or q_heads == 0 or head_dim == 0: success, nothing written.
  * Errors: INVALID_POINTER (shape, q or o NULL; k or v NULL with kv_rows > 0),
  * INVALID_DTYPE, INVALID_DIM (negative or too large sizes, kv_heads not a divisor of

@@ -352,6 +352,7 @@ int cudallm_layernorm_rows(const void *x, const void *gamma, const void *beta, v
     if (rows == 0 || n == 0) return CUDALLM_OK;
     if ((st = check_ld(rows, n, ldx)) != CUDALLM_OK || (st = check_ld(rows, n, ldy)) != CUDALLM_OK) return st;
     if (!x || !y) return CUDALLM_ERR_INVALID_POINTER;
+    if (y == x && ldy != ldx && rows > 1) return CUDALLM_ERR_INVALID_LD;      // rows would be read after others lie over them
     const int es = elem_size(dtype), ps = elem_size(param_dtype);
     if (off(x, es) || off(y, es) || off(gamma, ps) || off(beta, ps) || off(mean, 4) || off(rstd, 4))
         return CUDALLM_ERR_MISALIGNED;
@@ -388,6 +389,7 @@ int cudallm_layernorm_rows_bwd(const void *dy, const void *x, const void *gamma,
         if ((st = check_ld(rows, n, lddy)) != CUDALLM_OK || (st = check_ld(rows, n, ldx)) != CUDALLM_OK) return st;
         if (dx && (st = check_ld(rows, n, lddx)) != CUDALLM_OK) return st;
         if (!dy || !x || !mean || !rstd) return CUDALLM_ERR_INVALID_POINTER;
+        if (rows > 1 && ((dx == x && lddx != ldx) || (dx == dy && lddx != lddy))) return CUDALLM_ERR_INVALID_LD;
     }
     if (off(dy, es) || off(x, es) || off(dx, es) || off(gamma, ps) || off(dgamma, ps) || off(dbeta, ps) || off(mean, 4)
         || off(rstd, 4))
