@@ -144,13 +144,14 @@ BwdPlan plan_bwd(const cudallm_xattn_shape &s)
 
 inline XaStrides strides(const int64_t (&s)[3]) { return XaStrides{(long long)s[0], (long long)s[1], (long long)s[2]}; }
 
-// Tensor map of an operand; an absent one (no rows) gets a map of `other` that no kernel uses.
+// Tensor map of an operand; an absent one (no rows; its strides are not checked then) gets a map of one row
+// of `other` that no kernel uses.
 int encode(CUtensorMap *tm, const void *base, const void *other, bool f16, const int64_t (&st)[3], int64_t batch, int64_t rows,
            int64_t heads, int64_t dim)
 {
     if (rows == 0) {
         base = other;
-        rows = 1;
+        batch = rows = heads = 1;
     }
     const uint64_t dims[4] = {(uint64_t)dim, (uint64_t)heads, (uint64_t)rows, (uint64_t)batch};
     const int64_t used[3] = {heads > 1 ? st[2] : 8, rows > 1 ? st[1] : 8, batch > 1 ? st[0] : 8};
