@@ -11,7 +11,7 @@
 //
 // Measured (one B200): 8 x 32 heads on 8 key heads of 128, 16384 states (537 MB): 80.6-81.4 us = 6.6-6.7 TB/s, 1.01-1.02 of the
 // measured copy bandwidth; 16 x 16 heads of 64, up to 1500 states (70 MB): 15.6 us = 4.5 TB/s, one wave
-// of 256 CTAs of unequal length (two waves of half the size: 23.5 us).
+// of 256 CTAs of unequal length (two waves of half the size: 23.5 us when one took 18.2).
 #pragma once
 #include "xattn_common.cuh"
 
