@@ -9,9 +9,11 @@
 // the warps' results join in shared memory.  Up to eight splits are a cluster of CTAs, which read each
 // other's results from shared memory; more of them join in xattn_join_kernel.
 //
-// Measured (one B200): 8 x 32 heads on 8 key heads of 128, 16384 states (537 MB): 80.6-81.4 us = 6.6-6.7 TB/s, 1.01-1.02 of the
-// measured copy bandwidth; 16 x 16 heads of 64, up to 1500 states (70 MB): 15.6 us = 4.5 TB/s, one wave
-// of 256 CTAs of unequal length (two waves of half the size: 23.5 us when one took 18.2).
+// Measured (one B200): 8 x 32 heads on 8 key heads of 128, 16384 states (537 MB): 79.8 us = 6.7 TB/s, 1.03 of the
+// measured copy bandwidth; 16 x 16 heads of 64, up to 1500 states (70 MB): 14.9 us = 4.7 TB/s, one wave
+// of 256 CTAs of unequal length (two waves of half the size: 19.4 us; smaller stages, so that all
+// 512 fit at once: 16.0).  Compiled for two CTAs an SM, which is what the shared memory holds: without
+// that hint 80.9 and 15.6 us.
 #pragma once
 #include "xattn_common.cuh"
 
@@ -106,7 +108,7 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N> __device__ __forceinline__ void cp_async_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <int DP, typename T>
-__global__ void __launch_bounds__(kXaTokThreads)
+__global__ void __launch_bounds__(kXaTokThreads, 2)
 xattn_token_kernel(const XaTokParams p)
 {
     using L = XaTokSmem<DP>;
