@@ -113,8 +113,8 @@ typedef struct cudallm_tensor {
 int cudallm_grad_norm(const cudallm_tensor *tensors, int64_t count, float *norm, void *scratch, size_t scratch_bytes,
                       void *stream);
 /*
- * out = g * c for every tensor, with c = min(1, max_norm / (norm[0] + eps)), the
- * product rounded once.  `norm` is on the device, from cudallm_grad_norm or, for
+ * out = g * c for every tensor, with c = min(1, max_norm / (norm[0] + eps)) (1 where
+ * max_norm >= norm[0] + eps, both zero or both infinite too), the product rounded once.  `norm` is on the device, from cudallm_grad_norm or, for
  * gradients spread over several devices, combined by the caller.  A NaN norm makes
  * all gradients NaN, an infinite one makes the finite ones zero.  Tensors that are
  * scaled in place stay untouched (no bit changes) where c is 1.

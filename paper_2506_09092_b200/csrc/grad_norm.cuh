@@ -211,8 +211,8 @@ grad_scale_kernel(const __grid_constant__ GradList<CAP> l, const double *partial
     } else {
         v = *norm;
     }
-    float coef = max_norm / (v + eps);
-    if (coef > 1.f) coef = 1.f;                       // (a NaN stays)
+    // (not min(1, quotient): 0 / 0 of zero gradients and inf / inf without a limit are 1; a NaN norm stays one)
+    const float coef = max_norm >= v + eps ? 1.f : max_norm / (v + eps);
     const unsigned total = l.first[l.count];
     for (unsigned b = blockIdx.x; b < total; b += gridDim.x) {
         const unsigned c = total - 1 - b;

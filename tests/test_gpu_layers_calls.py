@@ -133,3 +133,91 @@ def test_strides_of_operands_without_rows_do_not_matter(q_rows, bad):
     B.xattn_bwd(shape, None, k, v, None, None, None, None, None, dk, dv, None, 0, torch.cuda.current_stream())
     torch.cuda.synchronize()
     assert not dk.any() and not dv.any()
+
+
+@pytest.mark.parametrize("max_norm,eps,value", [(0.0, 0.0, 0.0), (float("inf"), 1e-6, float("inf")),
+                                                (0.0, 0.0, 2.0), (float("inf"), 0.0, float("nan"))])
+def test_clip_limits_at_both_ends(max_norm, eps, value):
+    """No limit leaves gradients alone whatever their norm, a limit of zero leaves zeros at zero."""
+    g = torch.tensor([0.0, 1.0 if value else 0.0, value], device="cuda")
+    out = torch.full_like(g, 7)
+    table, norm = B.tensor_table([g], [out]), torch.empty(1, device="cuda")
+    n = B.grad_norm_scratch_bytes(table)
+    scr = torch.empty(n, dtype=torch.uint8, device="cuda")
+    B.grad_clip_norm(table, max_norm, eps, norm, scr, n, torch.cuda.current_stream())
+    if value != value:
+        assert bool(out.isnan().all())
+    else:
+        want = torch.zeros_like(g) if max_norm == 0 else g
+        assert torch.equal(out, want)
+
+
+STRIDE = 1 << 23            # 300 rows of it: the last lies 2.5e9 elements into its buffer
+
+
+def far_rows(buf, rows, cols, at):
+    return torch.as_strided(buf, (rows, cols), (STRIDE, 1), at)
+
+
+def test_attention_gradients_with_more_than_32_bits_of_offset():
+    rows, dim = 300, 64
+    ops = torch.empty(rows * STRIDE, dtype=torch.bfloat16, device="cuda")
+    res = torch.empty_like(ops)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+
+    def far(buf, at):
+        return far_rows(buf, rows, dim, at).view(1, rows, 1, dim)
+    q, k, v, do, o = (far(ops, 4096 * i) for i in range(5))
+    for t in (q, k, v, do):
+        t.copy_(torch.randn(1, rows, 1, dim, generator=gen, device="cuda"))
+    dq, dk, dv = (far(res, 4096 * i) for i in range(3))
+
+    def run(q, k, v, do, o, dq, dk, dv):
+        lse = torch.empty(1, 1, rows, device="cuda")
+        shape = B.XattnShape.of(q, k, v, o)
+        nf, nb = B.xattn_fwd_scratch_bytes(shape), B.xattn_bwd_scratch_bytes(shape)
+        scr = torch.empty(max(nf, nb), dtype=torch.uint8, device="cuda")
+        B.xattn_fwd(shape, q, k, v, None, o, lse, scr, nf, torch.cuda.current_stream())
+        B.xattn_bwd(shape, q, k, v, None, o, lse, do, dq, dk, dv, scr, nb, torch.cuda.current_stream())
+        return o, dq, dk, dv
+    near = [t.contiguous() for t in (q, k, v, do)] + [torch.empty(1, rows, 1, dim, dtype=torch.bfloat16, device="cuda")
+                                                       for _ in range(4)]
+    for a, b in zip(run(q, k, v, do, o, dq, dk, dv), run(*near)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [200, 4096, 4097, 20000])
+def test_layernorm_rows_with_more_than_32_bits_of_offset(n):
+    rows = 300
+    buf = torch.empty(rows * STRIDE, dtype=torch.float16, device="cuda")
+    x, dy, y, dx = (far_rows(buf, rows, n, 65536 * i) for i in range(4))
+    for t in (x, dy):
+        t.copy_(torch.randn(rows, n, device="cuda"))
+
+    def run(x, dy, y, dx):
+        ld = x.stride(0)
+        mean, rstd, dg, db = (torch.empty(m, device="cuda") for m in (rows, rows, n, n))
+        size = B.layernorm_rows_bwd_scratch_bytes(rows, n)
+        scr, s = torch.empty(size, dtype=torch.uint8, device="cuda"), torch.cuda.current_stream()
+        B.layernorm_rows(x, None, None, y, mean, rstd, rows, n, ld, ld, B.F16, B.F32, stream=s)
+        B.layernorm_rows_bwd(dy, x, None, mean, rstd, dx, dg, db, rows, n, ld, ld, ld, B.F16, B.F32, scr, size, stream=s)
+        return y, mean, rstd, dx, dg, db
+    near = [x.contiguous(), dy.contiguous(), torch.empty(rows, n, dtype=torch.float16, device="cuda"),
+            torch.empty(rows, n, dtype=torch.float16, device="cuda")]
+    for a, b in zip(run(x, dy, y, dx), run(*near)):
+        assert torch.equal(a, b)
+
+
+def test_gradient_of_more_than_32_bits_of_elements():
+    n = (1 << 32) + 77
+    g = torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    table, norm = B.tensor_table([g]), torch.empty(1, device="cuda")
+    size = B.grad_norm_scratch_bytes(table)
+    scr = torch.empty(size, dtype=torch.uint8, device="cuda")
+    want = 0.5 * n ** 0.5
+    # the norm is exact but for its last rounding: every partial sum is a multiple of 1/4 below 2^53
+    B.grad_clip_norm(table, want / 4, 0.0, norm, scr, size, torch.cuda.current_stream())
+    assert abs(norm.item() - want) <= want * 2.0 ** -23
+    # c is off from 1/4 by at most a few 2^-24, far below half a step of bf16
+    lo, hi = torch.aminmax(g)
+    assert lo.item() == hi.item() == 0.125
