@@ -5,9 +5,9 @@
 // cut into chunks of p.chunk elements; a CTA visits chunks b, b + grid, ... and finds a
 // chunk's tensor by bisection.  Bound: HBM; the second kernel visits the chunks in reverse, so
 // that it starts with what the first one left in L2.
-// Measured (one B200): 403 M bf16 values in 291 tensors, scaled into other buffers: 414 us, the norm alone 130
-// us = 6.2 TB/s, the scaling 280 us = 5.8 TB/s; 6.8 M in 27 tensors: 10 us.  Eviction priorities for
-// the chunks that the second pass meets first: 407 to 410 us whatever was kept, so none are given.
+// Measured (one B200): 403 M bf16 values in 291 tensors, scaled into other buffers: 396 us; the norm alone 130-134
+// us = 6.0-6.2 TB/s, the scaling alone 278 us = 5.8 TB/s; 6.8 M in 27 tensors: 10 us.  Eviction priorities for the chunks
+// that the second pass meets first: 407 to 410 instead of then 414 us whatever was kept, so none are given.
 #pragma once
 #include "elem.cuh"
 
@@ -150,7 +150,8 @@ grad_norm_join_kernel(const double *partials, int count, float *norm)
     if (threadIdx.x == 0) *norm = v;
 }
 
-template <typename T>
+// U pieces in flight per thread.
+template <int U, typename T>
 __device__ __forceinline__ void chunk_scale(const T *src, T *dst, int len, float coef)
 {
     constexpr int kV = ElemVec<T>::kN;
@@ -163,12 +164,12 @@ __device__ __forceinline__ void chunk_scale(const T *src, T *dst, int len, float
     int i = threadIdx.x;
     const T *sb = src + head;
     T *db = dst + head;
-    for (; i + 3 * kGradThreads < nvec; i += 4 * kGradThreads) {
-        Piece<T, kV> v[4];
+    for (; i + (U - 1) * kGradThreads < nvec; i += U * kGradThreads) {
+        Piece<T, kV> v[U];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) v[u].load(sb + (i + u * kGradThreads) * kV);
+        for (int u = 0; u < U; ++u) v[u].load(sb + (i + u * kGradThreads) * kV);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
+        for (int u = 0; u < U; ++u) {
             float f[kV];
             v[u].unpack(f);
 #pragma unroll
@@ -196,7 +197,7 @@ __device__ __forceinline__ void chunk_scale(const T *src, T *dst, int len, float
 
 // partials != NULL: the norm is joined here, by every CTA for itself (and written by the first
 // one); else it is read from `norm`.
-template <int CAP>
+template <int CAP, int U>
 __global__ void __launch_bounds__(kGradThreads)
 grad_scale_kernel(const __grid_constant__ GradList<CAP> l, const double *partials, int nparts, float *norm,
                   float max_norm, float eps)
@@ -220,11 +221,11 @@ grad_scale_kernel(const __grid_constant__ GradList<CAP> l, const double *partial
         void *src = l.data[g.tensor], *dst = l.out[g.tensor];
         if (coef == 1.f && src == dst) continue;
         if (l.dtype[g.tensor] == 0)
-            chunk_scale(static_cast<const float *>(src) + g.begin, static_cast<float *>(dst) + g.begin, g.len, coef);
+            chunk_scale<U>(static_cast<const float *>(src) + g.begin, static_cast<float *>(dst) + g.begin, g.len, coef);
         else if (l.dtype[g.tensor] == 1)
-            chunk_scale(static_cast<const __nv_bfloat16 *>(src) + g.begin, static_cast<__nv_bfloat16 *>(dst) + g.begin, g.len, coef);
+            chunk_scale<U>(static_cast<const __nv_bfloat16 *>(src) + g.begin, static_cast<__nv_bfloat16 *>(dst) + g.begin, g.len, coef);
         else
-            chunk_scale(static_cast<const __half *>(src) + g.begin, static_cast<__half *>(dst) + g.begin, g.len, coef);
+            chunk_scale<U>(static_cast<const __half *>(src) + g.begin, static_cast<__half *>(dst) + g.begin, g.len, coef);
     }
 }
 

@@ -221,3 +221,33 @@ def test_gradient_of_more_than_32_bits_of_elements():
     # c is off from 1/4 by at most a few 2^-24, far below half a step of bf16
     lo, hi = torch.aminmax(g)
     assert lo.item() == hi.item() == 0.125
+
+
+@pytest.mark.parametrize("count", [3, 70])
+@pytest.mark.parametrize("lead", [0, 1])
+def test_clip_of_many_elements_equals_the_formula(count, lead):
+    """More than 17 million elements: the same fp32 quotient, product and rounding as elementwise code."""
+    types = (torch.float32, torch.bfloat16, torch.float16)
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    size = 24_000_000 // count
+    bufs = [torch.randn(size + 13 * i + 8, generator=gen, device="cuda").to(types[i % 3]) for i in range(count)]
+    grads = [b[lead:lead + size + 13 * i] for i, b in enumerate(bufs)]
+    norm = torch.empty(1, device="cuda")
+    for shift in (0, 1, None):                   # beside, off by one element, in place
+        if shift is None:
+            keep = [b.clone() for b in bufs]
+            src = out = [b[lead:lead + g.numel()] for b, g in zip(keep, grads)]
+        else:
+            keep = [torch.full((b.numel() + 8,), 7.0, dtype=b.dtype, device="cuda") for b in bufs]
+            src, out = grads, [b[lead + shift:lead + shift + g.numel()] for b, g in zip(keep, grads)]
+        table = B.tensor_table(src, out)
+        n = B.grad_norm_scratch_bytes(table)
+        scr = torch.empty(n, dtype=torch.uint8, device="cuda")
+        B.grad_clip_norm(table, 3.0, 1e-6, norm, scr, n, torch.cuda.current_stream())
+        # (a number divided by a tensor is its reciprocal times the number: rounded twice)
+        coef = torch.full_like(norm, 3.0) / (norm + 1e-6)
+        for g, o, b in zip(grads, out, keep):
+            assert torch.equal(o, (g.float() * coef).to(g.dtype))
+            if shift is not None:
+                first = lead + shift
+                assert bool((b[:first] == 7).all()) and bool((b[first + g.numel():] == 7).all())
