@@ -432,8 +432,10 @@ xattn_join_kernel(const XaJoinParams p)
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     const int col = lane * 4;
     for (int s = 0; s < p.splits; ++s) {
+        // (a weight that has vanished still multiplies: 0 x inf must make the row NaN, as it does in one part)
         const float ws = __shfl_sync(0xffffffffu, w, s) * inv;
-        if (ws == 0.f || col >= p.head_dim) continue;
+        const bool keys = __shfl_sync(0xffffffffu, part, s) != -INFINITY;
+        if (!keys || col >= p.head_dim) continue;
         const float4 v = *reinterpret_cast<const float4 *>(p.o_part + (s * p.rows_all + row) * p.head_dim + col);
         acc.x = fmaf(ws, v.x, acc.x);
         acc.y = fmaf(ws, v.y, acc.y);
