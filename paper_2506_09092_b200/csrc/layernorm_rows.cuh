@@ -780,9 +780,9 @@ layernorm_long_columns_kernel(const LnRowsParams p)
         dg += g;
         db += b;
     }
-    float *out = p.partials + (long long)blockIdx.y * 2 * p.n;
-    out[c] = dg;
-    out[p.n + c] = db;
+    float *out = p.partials + (long long)blockIdx.y * 2 * p.n + c;
+    out[0] = dg;
+    out[p.n] = db;                                                 // (n + c may pass 2^31)
 }
 
 }  // namespace cudallm

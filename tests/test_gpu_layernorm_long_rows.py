@@ -37,3 +37,22 @@ def test_roundings_that_all_point_one_way(rows, n, value):
         part = slice(c, min(c + 8192, n))
         want = ((x[:, part].double() + 0.5) * 0.75 * dy[0, 0].double()).sum(0)
         assert float(((dg[part].double() - want).abs() / want).max()) <= bound
+
+
+@pytest.mark.parametrize("rows", [1, 2])
+def test_columns_whose_partial_rows_lie_beyond_32_bits(rows):
+    """More than 2^30 columns: the second partial row's elements have indexes beyond 2^31.  Values whose
+    products and sums are exact."""
+    n = (1 << 30) + 1000
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    x, dy = (torch.empty(rows, n, dtype=torch.bfloat16, device="cuda").random_(-3, 4, generator=gen) for _ in range(2))
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.full((rows,), 0.5, device="cuda")
+    dg, db = (torch.full((n,), 77.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    size = B.layernorm_rows_bwd_scratch_bytes(rows, n)
+    scratch = torch.empty(size, dtype=torch.uint8, device="cuda")
+    B.layernorm_rows_bwd(dy, x, None, mean, rstd, None, dg, db, rows, n, n, n, n, B.BF16, B.BF16, scratch, size,
+                         torch.cuda.current_stream())
+    for c in range(0, n, 1 << 27):
+        part = slice(c, min(c + (1 << 27), n))
+        assert torch.equal(db[part], dy[:, part].sum(0))
+        assert torch.equal(dg[part], (dy[:, part] * x[:, part] * 0.5).sum(0))
