@@ -73,6 +73,24 @@ class XattnShape(ctypes.Structure):
             setattr(s, field, (_i64 * 3)(*t.stride()[:3]))
         return s
 
+    def layouts(self):
+        """What tensors of q, k, v, o have to be, as the fields say: (strides, sizes, type, extent in elements) of each;
+        then the number and type of kv_lens and of lse.  Worked out anew whenever a field has changed."""
+        raw = bytes(self)
+        kept = getattr(self, "_kept", None)
+        if kept is None or kept[0] != raw:
+            import torch
+            dtype = {BF16: torch.bfloat16, F16: torch.float16}.get(self.dtype)
+            out = []
+            for rows, heads, st in ((self.q_rows, self.q_heads, self.q_stride), (self.kv_rows, self.kv_heads, self.k_stride),
+                                    (self.kv_rows, self.kv_heads, self.v_stride), (self.q_rows, self.q_heads, self.o_stride)):
+                size, strides = (self.batch, rows, heads, self.head_dim), (*st, 1)
+                extent = 0 if 0 in size else 1 + sum((n - 1) * d for n, d in zip(size, strides))
+                out.append((strides, torch.Size(size) if min(size) >= 0 else size, dtype, extent))
+            out += [(self.batch, torch.int32), (self.batch * self.q_heads * self.q_rows, torch.float32)]
+            kept = self._kept = (raw, out)
+        return kept[1]
+
 
 # name -> (restype, argtypes); mirrors include/cudallm_gemm.h, cudallm_tasks.h and cudallm_layers.h
 SIGNATURES = {
@@ -182,6 +200,35 @@ def _d(*xs):
                 raise ValueError(f"the tensor is on device {dev}, the current device is {cur}")
         out.append(x.data_ptr())
     return out
+
+
+def _laid_out(operands, kv_lens, at_lens, lse, at_lse):
+    """Refuses tensors that do not hold the attention operands as an XattnShape says.  `operands`: names, tensors
+    and their entries of ``layouts``; addresses are taken as they are."""
+    for name, t, at in operands:
+        if t is not None and t.__class__ is not int and not (
+                t.stride() == at[0] and t.shape == at[1] and t.dtype is at[2]):
+            _check_layout(name, t, *at)
+    for name, t, (n, dtype) in (("kv_lens", kv_lens, at_lens), ("lse", lse, at_lse)):
+        if t is not None and t.__class__ is not int:
+            if t.dtype is not dtype:
+                raise TypeError(f"{name} has to be {dtype}, not {t.dtype}")
+            if t.numel() < n or not t.is_contiguous():
+                raise ValueError(f"{name}: {n} contiguous elements are needed")
+
+
+def _check_layout(name, t, strides, size, dtype, extent):
+    """Another type; a (batch, rows, heads, head_dim) tensor of other strides (those of sizes of one do not count);
+    one of other sizes (a flat buffer, say) that ends before the operand does."""
+    if isinstance(t, int) or dtype is None or extent == 0:         # (a type that the C call refuses; nothing there)
+        return
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has to be {dtype}, as the shape says, not {t.dtype}")
+    if t.shape == size:
+        if any(n > 1 and a != b for n, a, b in zip(size, t.stride(), strides)):
+            raise ValueError(f"{name} has strides {t.stride()}, the shape says {strides}")
+    elif (1 + sum((n - 1) * d for n, d in zip(t.shape, t.stride())) if t.numel() else 0) < extent:
+        raise ValueError(f"{name}: {tuple(t.shape)} ends before {tuple(size)} of strides {strides} does")
 
 
 def _s(stream):
@@ -341,7 +388,11 @@ def xattn_fwd_scratch_bytes(shape) -> int:
 
 def xattn_fwd(shape, q, k, v, kv_lens, o, lse, scratch, scratch_bytes, stream=None, check=True):
     """Cross attention: o = softmax(scale q k^T) v over the first kv_lens[b] states of each batch item
-    (``shape``: an XattnShape); kv_lens, lse and scratch may be None."""
+    (``shape``: an XattnShape); kv_lens, lse and scratch may be None.  Tensors must be laid out as the shape
+    says, kv_lens int32 and lse contiguous fp32; addresses are not looked at."""
+    if isinstance(shape, XattnShape):
+        at_q, at_k, at_v, at_o, at_lens, at_lse = shape.layouts()
+        _laid_out((("q", q, at_q), ("k", k, at_k), ("v", v, at_v), ("o", o, at_o)), kv_lens, at_lens, lse, at_lse)
     st = lib().cudallm_xattn_fwd(shape, *_d(q, k, v, kv_lens, o, lse, scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_xattn_fwd", check)
 
@@ -352,7 +403,12 @@ def xattn_bwd_scratch_bytes(shape) -> int:
 
 def xattn_bwd(shape, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch, scratch_bytes, stream=None, check=True):
     """Gradients of ``xattn_fwd`` (d_o laid out like o, dq like q, dk like k, dv like v); dk and dv may
-    both be None."""
+    both be None.  Tensors are checked as there: ``torch.empty_like(k)`` of a k that is a part of a larger tensor
+    has other strides and is refused."""
+    if isinstance(shape, XattnShape):
+        at_q, at_k, at_v, at_o, at_lens, at_lse = shape.layouts()
+        _laid_out((("q", q, at_q), ("k", k, at_k), ("v", v, at_v), ("o", o, at_o), ("d_o", d_o, at_o), ("dq", dq, at_q),
+                   ("dk", dk, at_k), ("dv", dv, at_v)), kv_lens, at_lens, lse, at_lse)
     st = lib().cudallm_xattn_bwd(shape, *_d(q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_xattn_bwd", check)
 
