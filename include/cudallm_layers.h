@@ -88,7 +88,9 @@ size_t cudallm_layernorm_rows_bwd_scratch_bytes(int64_t rows, int64_t n);
 
 /* One gradient of a model: n contiguous elements of `dtype` at `data` (device).
  * `out` is where the scaled gradient goes: `data` itself (in place) or a buffer of
- * the same size and type that overlaps no other one of the list. */
+ * the same size and type that overlaps no `data` of the list.  No two `out` overlap,
+ * and one in place overlaps no other entry's `data` (one call would read it while
+ * it is scaled). */
 typedef struct cudallm_tensor {
     void *data;
     void *out;

@@ -329,33 +329,47 @@ class TensorTable:
         self._keep = (tensors, outs)
         spans, inputs = [], []
         for e, t, o in zip(self.array, tensors, outs):
-            if t.dtype != o.dtype or t.numel() != o.numel():
+            code = codes.get(str(t.dtype))
+            if o is not t and (t.dtype != o.dtype or t.numel() != o.numel()):
                 raise ValueError("an output has the size and type of its tensor")
-            if str(t.dtype) not in codes:
+            if code is None:
                 raise TypeError(f"fp32, bf16 or fp16 gradients, not {t.dtype}")
-            if not (t.is_contiguous() and o.is_contiguous()):
+            if not (t.is_contiguous() and (o is t or o.is_contiguous())):
                 raise ValueError("contiguous tensors are needed")
-            (e.data, e.out), e.n, e.dtype = _d(t, o), t.numel(), codes[str(t.dtype)]
-            if e.n:
-                nbytes = e.n * t.element_size()
-                spans.append((e.out, e.out + nbytes, e.data != e.out))
-                inputs.append((e.data, e.data + nbytes, False))
+            data, out = _d(t, o)
+            n = t.numel()
+            e.data, e.out, e.n, e.dtype = data, out, n, code
+            if n:
+                nbytes = n * t.element_size()
+                spans.append((out, out + nbytes, data != out))
+                inputs.append((data, data + nbytes, data != out))
         spans.sort()
         for (_, end, _a), (begin, _, _b) in zip(spans, spans[1:]):
             if begin < end:
                 raise ValueError("two outputs overlap (a gradient that is scaled in place may be listed once)")
-        # an output beside its tensor must not lie over any other input either
-        merged = sorted([(b, e, 1) for b, e, apart in spans if apart] + [(b, e, 0) for b, e, _ in inputs])
-        end = [0, 0]
-        for b, e, kind in merged:
-            if b < end[1 - kind]:
-                raise ValueError("an output overlaps a gradient of the list")
-            end[kind] = max(end[kind], e)
+        # An output beside its tensor must not lie over any input, one in place not over the input of an
+        # entry that is written elsewhere (inputs that are scaled in place are outputs, compared above).
+        apart = [s for s in spans if s[2]]
+        if apart and (_meet(apart, inputs) or _meet([s for s in spans if not s[2]], [s for s in inputs if s[2]])):
+            raise ValueError("an output overlaps a gradient of the list")
+
+
+def _meet(some, others):
+    """Whether one of `some` address ranges (begin, end, ...) overlaps one of `others`."""
+    if not some or not others:
+        return False
+    end = [0, 0]
+    for begin, stop, kind in sorted([(s[0], s[1], 0) for s in some] + [(s[0], s[1], 1) for s in others]):
+        if begin < end[1 - kind]:
+            return True
+        if stop > end[kind]:
+            end[kind] = stop
+    return False
 
 
 def tensor_table(tensors, outs=None) -> TensorTable:
     """Table of contiguous CUDA tensors for the grad_* calls; ``outs`` where the scaled ones go
-    (None: in place)."""
+    (None: in place).  Outputs that overlap each other, or what another entry reads, are refused."""
     return TensorTable(tensors, outs)
 
 
