@@ -68,14 +68,15 @@ static_assert(XaBwdSmem<64>::kBytes > 114 * 1024, "one CTA per SM (each takes al
 // Barriers, 8 bytes each from XaBwdSmem::kBars.
 enum : int { kBwStat = 0, kBwS = 1 /* 2 */, kBwDp = 3, kBwP = 4, kBwDs = 5, kBwDone = 6, kBwLFull = 7 /* 3 */,
              kBwLEmpty = 10 /* 3 */, kBwSFull = 13 /* 2 */, kBwSEmpty = 15 /* 2 */, kBwRowsFull = 17 /* 2 */,
-             kBwRowsEmpty = 19 /* 2 */ };
+             kBwRowsEmpty = 19 /* 2 */, kBwDrain = 21 };
 
 // The TMA warp of both kernels: the stationary tiles, then `n` pairs of tiles.  coords(i, h, row) gives
-// the head and first row of pair i.  Returns false if a wait ran out.
+// the head and first row of pair i.  Returns false if a wait ran out; `nl` and `ns`: tiles asked for in each ring.
 template <int DP, typename Coords>
 __device__ __forceinline__ bool xa_bwd_load(uint32_t sbase, const CUtensorMap *stat_a, const CUtensorMap *stat_b, int stat_h,
                                             int stat_row, const CUtensorMap *ring_l, const CUtensorMap *ring_s, int b, int n,
-                                            Coords coords, volatile int *abort_flag, unsigned long long limit)
+                                            Coords coords, volatile int *abort_flag, unsigned long long limit, int &nl,
+                                            int &ns)
 {
     using L = XaBwdSmem<DP>;
     const uint32_t bars = sbase + L::kBars;
@@ -83,7 +84,6 @@ __device__ __forceinline__ bool xa_bwd_load(uint32_t sbase, const CUtensorMap *s
     xa_load_tile<DP>(stat_a, sbase, bars + 8 * kBwStat, stat_h, stat_row, b);
     xa_load_tile<DP>(stat_b, sbase + L::kTile, bars + 8 * kBwStat, stat_h, stat_row, b);
     bool ok = true;
-    int nl = 0, ns = 0;
     for (int i = 0; i < n && ok; ++i) {
         int h, row;
         coords(i, h, row);
@@ -99,19 +99,6 @@ __device__ __forceinline__ bool xa_bwd_load(uint32_t sbase, const CUtensorMap *s
         xa_load_tile<DP>(ring_s, sbase + L::kRingS + ss * L::kTile, bars + 8 * (kBwSFull + ss), h, row, b);
         ++ns;
     }
-    if (!ok) {
-        // the copies in flight must land before the CTA ends
-        volatile int never = 0;
-        mbar_wait(bars + 8 * kBwStat, 0, &never, limit);
-        for (int s = 0; s < L::kLong; ++s) {
-            const int uses = (nl - s + L::kLong - 1) / L::kLong;
-            if (uses > 0) mbar_wait(bars + 8 * (kBwLFull + s), (uses - 1) & 1, &never, limit);
-        }
-        for (int s = 0; s < L::kShort; ++s) {
-            const int uses = (ns - s + L::kShort - 1) / L::kShort;
-            if (uses > 0) mbar_wait(bars + 8 * (kBwSFull + s), (uses - 1) & 1, &never, limit);
-        }
-    }
     return ok;
 }
 
@@ -125,25 +112,24 @@ __device__ __forceinline__ void xa_bwd_init(uint32_t bars, int lane, volatile in
     fence_mbar_init();
 }
 
-// End of both kernels, by all threads: after a failed wait the products in flight are waited for,
-// then tensor memory is released by warp 17.
-__device__ __forceinline__ void xa_bwd_finish(uint32_t bars, uint32_t tmem, volatile int *abort_flag, unsigned long long limit)
+// End of both kernels, by all threads.  After a failed wait the copies (lane 0 of warp 16 asked for nl and ns tiles)
+// and products in flight are waited for; then tensor memory is released by warp 17.
+template <int DP>
+__device__ __forceinline__ void xa_bwd_finish(uint32_t bars, uint32_t tmem, volatile int *abort_flag, int nl, int ns)
 {
+    using L = XaBwdSmem<DP>;
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag && nl > 0) {
+        volatile int never = 0;
+        mbar_wait(bars + 8 * kBwStat, 0, &never);
+        xa_ring_landed<L::kLong>(bars + 8 * kBwLFull, nl, &never);
+        xa_ring_landed<L::kShort>(bars + 8 * kBwSFull, ns, &never);
+    }
     if (threadIdx.x >> 5 == 17) {
         tc_fence_after();
-        if (*abort_flag) {
-            if ((threadIdx.x & 31) == 0) {
-                volatile int never = 0;
-                mbar_init(bars + 8 * kBwDone, 1);
-                fence_mbar_init();
-                umma_commit(bars + 8 * kBwDone);
-                mbar_wait(bars + 8 * kBwDone, 0, &never, limit);
-            }
-            __syncwarp();
-        }
+        if (*abort_flag) xa_products_done(bars + 8 * kBwDrain);
         tmem_dealloc(tmem, 512);
     }
 }
@@ -189,11 +175,12 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     const int blk0 = blockIdx.y * p.dq_blocks;                       // (the first of this part's blocks)
     const int nblk = min(p.dq_blocks, (keys + kXaRows - 1) / kXaRows - blk0);
     const unsigned long long limit = p.wait_limit_ns;
+    int nl = 0, ns = 0;
 
     if (warp == 16) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
             const bool ok = xa_bwd_load<DP>(sbase, &tm_q, &tm_do, h, row0, &tm_k, &tm_v, b, nblk,
-                                            [&](int i, int &hh, int &row) { hh = kvh; row = (blk0 + i) * kXaRows; }, abort_flag, limit);
+                                            [&](int i, int &hh, int &row) { hh = kvh; row = (blk0 + i) * kXaRows; }, abort_flag, limit, nl, ns);
             if (!ok) xa_report(p.status, kXaRoleDq, 1);
         }
     } else if (warp == 17) {
@@ -336,7 +323,7 @@ xattn_dq_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             xa_report(p.status, kXaRoleDq, 3);
         }
     }
-    xa_bwd_finish(bars, tmem, abort_flag, limit);
+    xa_bwd_finish<DP>(bars, tmem, abort_flag, nl, ns);
 }
 
 // ------------------------------------------------------------- dK, dV --
@@ -375,6 +362,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const int blk0 = blockIdx.y * p.dkv_blocks;
     const int nblk = key0 < keys ? min(p.dkv_blocks, p.group * p.q_tiles - blk0) : 0;
     const unsigned long long limit = p.wait_limit_ns;
+    int nl = 0, ns = 0;
 
     if (warp == 16) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
@@ -382,7 +370,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
                                             [&](int i, int &hh, int &row) {
                                                 hh = kvh * p.group + (blk0 + i) / p.q_tiles;
                                                 row = ((blk0 + i) % p.q_tiles) * kXaRows;
-                                            }, abort_flag, limit);
+                                            }, abort_flag, limit, nl, ns);
             if (!ok) xa_report(p.status, kXaRoleDkv, 1);
         }
     } else if (warp == 17) {
@@ -539,7 +527,7 @@ xattn_dkv_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
             xa_report(p.status, kXaRoleDkv, 3);
         }
     }
-    xa_bwd_finish(bars, tmem, abort_flag, limit);
+    xa_bwd_finish<DP>(bars, tmem, abort_flag, nl, ns);
 }
 
 // Adds the parts of one or two gradients in order and rounds the sums, times f0 and f1.  A thread takes four

@@ -171,6 +171,28 @@ __device__ __forceinline__ bool named_bar_all(int id, int threads, bool ok)
     return all != 0;
 }
 
+// What is left to wait for when a kernel has given up: the last copy into each stage of a ring of STAGES (`loads` of
+// them were issued, in turn), and the products in flight.  With the library's own limit: the caller's may have
+// run out because it is short, and copies must not land in what is another CTA's shared memory by then.
+template <int STAGES>
+__device__ __forceinline__ void xa_ring_landed(uint32_t full, int loads, volatile int *never)
+{
+    for (int s = 0; s < STAGES; ++s) {
+        const int uses = (loads - s + STAGES - 1) / STAGES;
+        if (uses > 0) mbar_wait(full + 8 * s, (uses - 1) & 1, never);
+    }
+}
+// (by the warp that issued the products; the same lane is elected each time, and a commit covers what that lane has issued)
+__device__ __forceinline__ void xa_products_done(uint32_t drain)
+{
+    if (elect_one()) {
+        volatile int never = 0;
+        umma_commit(drain);
+        mbar_wait(drain, 0, &never);
+    }
+    __syncwarp();
+}
+
 // Valid keys of batch item b.
 __device__ __forceinline__ int xa_keys(const int *lens, int b, int kv_rows)
 {

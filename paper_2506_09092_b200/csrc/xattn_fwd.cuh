@@ -65,8 +65,8 @@ template <int DP> struct XaFwdSmem {
     static constexpr int kStages = DP == 128 ? 4 : 7;
     static constexpr int kRing = 2 * kTile;
     static constexpr int kBars = kRing + kStages * kTile;
-    // q_full, s_full[2], p_full[2], pv_done[2], s_read[2], p_half[2], turn[2], full[kStages], empty[kStages]
-    static constexpr int kNumBars = 13 + 2 * kStages;
+    // q_full, s_full[2], p_full[2], pv_done[2], s_read[2], p_half[2], turn[2], full[kStages], empty[kStages], drain
+    static constexpr int kNumBars = 14 + 2 * kStages;
     static constexpr int kMisc = kBars + kNumBars * 8;
     static constexpr int kXch = kMisc + 16 + 8 * (kNumBars & 1);   // floats: [tile][parity][half][row]
     // 4 KiB per softmax warp for the output's rows: where the queries were (two tiles of 32 KiB), or behind
@@ -89,7 +89,8 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const uint32_t sbase = smem_u32(smem);
     const uint32_t bars = sbase + L::kBars;
     const uint32_t q_full = bars, s_full = bars + 8, p_full = bars + 24, pv_done = bars + 40, s_read = bars + 56,
-                   p_half = bars + 72, turn = bars + 88, full = bars + 104, empty = full + 8 * L::kStages;
+                   p_half = bars + 72, turn = bars + 88, full = bars + 104, empty = full + 8 * L::kStages,
+                   drain = empty + 8 * L::kStages;
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::kMisc);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(smem + L::kMisc + 4);
 
@@ -124,33 +125,25 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
     const int key0 = blockIdx.y * p.tiles_per_split * kXaRows;
     const int nkeys = min(p.tiles_per_split * kXaRows, keys - key0);                      // <= 0: no keys here
     const int nblk = (nkeys + kXaRows - 1) / kXaRows;
+    int loads = 0;                                                                       // (lane 0 of warp 16: tiles asked for)
 
     if (warp == 16) {
         if (lane == 0 && nblk > 0 && !p.skip_loads) {
             mbar_expect_tx(q_full, tiles * L::kTile);
             for (int j = 0; j < tiles; ++j) xa_load_tile<DP>(&tm_q, sbase + j * L::kTile, q_full, h, row0 + j * kXaRows, b);
             bool ok = true;
-            int it = 0;
             for (int i = 0; i < nblk && ok; ++i) {
-                for (int w = 0; w < 2; ++w, ++it) {                       // K, then V
-                    const int s = it % L::kStages, use = it / L::kStages;
+                for (int w = 0; w < 2; ++w) {                             // K, then V
+                    const int s = loads % L::kStages, use = loads / L::kStages;
                     if (use > 0) ok = mbar_wait(empty + 8 * s, (use - 1) & 1, abort_flag, p.wait_limit_ns);
                     if (!ok) break;
                     mbar_expect_tx(full + 8 * s, L::kTile);
                     xa_load_tile<DP>(w ? &tm_v : &tm_k, sbase + L::kRing + s * L::kTile, full + 8 * s, kvh,
                                      key0 + i * kXaRows, b);
+                    ++loads;
                 }
             }
-            if (!ok) {
-                // another role gave up: the copies in flight must land before the CTA ends
-                xa_report(p.status, kXaRoleLoad, 1);
-                volatile int never = 0;
-                mbar_wait(q_full, 0, &never, p.wait_limit_ns);
-                for (int s = 0; s < L::kStages; ++s) {
-                    const int uses = (it - s + L::kStages - 1) / L::kStages;      // loads issued into stage s
-                    if (uses > 0) mbar_wait(full + 8 * s, (uses - 1) & 1, &never, p.wait_limit_ns);
-                }
-            }
+            if (!ok) xa_report(p.status, kXaRoleLoad, 1);
         }
     } else if (warp == 17) {
         if (nblk > 0) {
@@ -379,22 +372,18 @@ xattn_fwd_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant
         }
     }
     __syncwarp();
-    // all products have been waited for (o_done), or the kernel gave up after a failed wait;
-    // then the tensor core's queue is drained before tensor memory is released
+    // All copies and products have been waited for (pv_done), or a wait ran out.  Then those in flight are waited for
+    // here, whichever role gave up and when, before shared and tensor memory are another CTA's.
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag && warp == 16 && lane == 0 && loads > 0) {
+        volatile int never = 0;
+        mbar_wait(q_full, 0, &never);
+        xa_ring_landed<L::kStages>(full, loads, &never);
+    }
     if (warp == 17) {
         tc_fence_after();
-        if (*abort_flag) {
-            if (lane == 0) {
-                volatile int never = 0;
-                mbar_init(q_full, 1);
-                fence_mbar_init();
-                umma_commit(q_full);
-                mbar_wait(q_full, 0, &never, p.wait_limit_ns);
-            }
-            __syncwarp();
-        }
+        if (*abort_flag) xa_products_done(drain);
         tmem_dealloc(tmem, 512);
     }
 }
