@@ -37,22 +37,21 @@ int check_ld(int64_t rows, int64_t n, int64_t ld)
     return CUDALLM_OK;
 }
 
-// CTAs of `kernel` that one SM holds (asked once per kernel, device and size of shared memory).
+// CTAs of `kernel` that one SM holds, asked once per kernel and device, for the most shared memory that
+// the kernel is ever launched with: grids, and with them the order of the sums, do not depend on earlier calls.
 struct Residency {
     std::atomic<int> ctas[kRtMaxDevices];
-    std::atomic<int> smem[kRtMaxDevices];
 };
 template <typename Kernel>
-int resident(Kernel kernel, int threads, int smem, int dev, Residency &cache, int *out)
+int resident(Kernel kernel, int threads, int max_smem, int dev, Residency &cache, int *out)
 {
     int v = cache.ctas[dev].load(std::memory_order_relaxed);
-    if (v == 0 || cache.smem[dev].load(std::memory_order_relaxed) != smem) {
-        if (smem > 48 * 1024)
-            RT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-        RT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&v, kernel, threads, smem));
+    if (v == 0) {
+        if (max_smem > 48 * 1024)
+            RT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, max_smem));
+        RT_CUDA_TRY(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&v, kernel, threads, max_smem));
         if (v < 1) v = 1;
         cache.ctas[dev].store(v, std::memory_order_relaxed);
-        cache.smem[dev].store(smem, std::memory_order_relaxed);
     }
     *out = v;
     return CUDALLM_OK;
@@ -68,9 +67,9 @@ int launch_warp(const LnRowsParams &p, const LnLaunch &at)
 {
     static Residency occ = {};
     auto kernel = layernorm_warp_kernel<T, VEC, TPR, E / kUnit<VEC>, R>;
-    const int smem = 2 * p.n * (int)sizeof(float);
+    const int smem = 2 * p.n * (int)sizeof(float);                 // (n <= TPR * E)
     int per_sm = 0;
-    const int st = resident(kernel, kLnWarpThreads, smem, at.dev, occ, &per_sm);
+    const int st = resident(kernel, kLnWarpThreads, 2 * TPR * E * (int)sizeof(float), at.dev, occ, &per_sm);
     if (st != CUDALLM_OK) return st;
     const int64_t grid = std::min<int64_t>(cdiv(p.rows, R * (kLnWarpThreads / TPR)), (int64_t)at.sms * per_sm);
     return rt_launch(kernel, dim3((unsigned)grid), kLnWarpThreads, (size_t)smem, at.stream, p);
@@ -135,7 +134,7 @@ int launch_warp_bwd(const LnRowsParams &p, const LnLaunch &at, int *parts)
     constexpr int kRows = kLnWarpThreads / TPR;
     const int smem = kRows * p.n * (int)sizeof(float);
     int per_sm = 0;
-    const int st = resident(kernel, kLnWarpThreads, smem, at.dev, occ, &per_sm);
+    const int st = resident(kernel, kLnWarpThreads, kRows * TPR * E * (int)sizeof(float), at.dev, occ, &per_sm);
     if (st != CUDALLM_OK) return st;
     const int64_t grid = std::min<int64_t>({cdiv(p.rows, R * kRows), (int64_t)at.sms * per_sm, ln_max_parts(p.n)});
     *parts = (int)grid;
