@@ -105,15 +105,19 @@ int launch_ln_by_length(const LnRowsParams &p, const LnLaunch &at)
         if (p.n <= 1024) return launch_warp<T, VEC, 32, 32, 1>(p, at);
     }
     if (p.n <= 256) return launch_warp<T, VEC, 32, 8, 2>(p, at);
-    if (VEC > 1 && p.rows >= 4 * at.sms) {
-        if (p.n <= 2048) return launch_block<T, VEC, 64, 32, 1>(p, at);
-        if (p.n <= 4096) return launch_block<T, VEC, 128, 32, 1>(p, at);
-        if (p.n <= 8192) return launch_block<T, VEC, 256, 32, 1>(p, at);
-    }
+    if constexpr (VEC > 1)
+        if (p.rows >= 4 * at.sms) {
+            if (p.n <= 2048) return launch_block<T, VEC, 64, 32, 1>(p, at);
+            if (p.n <= 4096) return launch_block<T, VEC, 128, 32, 1>(p, at);
+            if (p.n <= 8192) return launch_block<T, VEC, 256, 32, 1>(p, at);
+        }
     if (p.n <= 1024) return launch_block<T, VEC, 128, 8, 1>(p, at);
-    if (VEC == 1 && p.n <= 2048) return launch_block<T, VEC, 128, 16, 1>(p, at);
-    if (VEC == 1 && p.n <= 4096) return launch_block<T, VEC, 256, 16, 1>(p, at);
-    if (p.n <= 4096) return launch_block<T, VEC, 512, 8, 1>(p, at);
+    if constexpr (VEC == 1) {
+        if (p.n <= 2048) return launch_block<T, VEC, 128, 16, 1>(p, at);
+        if (p.n <= 4096) return launch_block<T, VEC, 256, 16, 1>(p, at);
+    } else {
+        if (p.n <= 4096) return launch_block<T, VEC, 512, 8, 1>(p, at);
+    }
     if (p.n <= 16384) return launch_block<T, VEC, 512, 32, 1>(p, at);
     const int64_t grid = std::min<int64_t>(p.rows, (int64_t)at.sms * 2);
     return rt_launch(layernorm_long_kernel<T>, dim3((unsigned)grid), kLnLongThreads, 0, at.stream, p);
@@ -168,11 +172,12 @@ int launch_ln_bwd_by_length(const LnRowsParams &p, const LnLaunch &at, int *part
         if (p.n <= 512) return launch_warp_bwd<T, VEC, 32, 16, 2>(p, at, parts);
     }
     if (p.n <= 256) return launch_warp_bwd<T, VEC, 32, 8, 1>(p, at, parts);
-    if (VEC > 1 && p.rows >= 4 * at.sms) {
-        if (p.n <= 1024) return launch_block_bwd<T, VEC, 128, 8, 4>(p, at, parts);
-        if (p.n <= 2048) return launch_block_bwd<T, VEC, 256, 8, 2>(p, at, parts);
-        if (p.n <= 4096) return launch_block_bwd<T, VEC, 512, 8, 2>(p, at, parts);
-    }
+    if constexpr (VEC > 1)
+        if (p.rows >= 4 * at.sms) {
+            if (p.n <= 1024) return launch_block_bwd<T, VEC, 128, 8, 4>(p, at, parts);
+            if (p.n <= 2048) return launch_block_bwd<T, VEC, 256, 8, 2>(p, at, parts);
+            if (p.n <= 4096) return launch_block_bwd<T, VEC, 512, 8, 2>(p, at, parts);
+        }
     if (p.n <= 1024) return launch_block_bwd<T, VEC, 128, 8, 1>(p, at, parts);
     if (p.n <= 2048) return launch_block_bwd<T, VEC, 256, 8, 1>(p, at, parts);
     if (p.n <= 4096) return launch_block_bwd<T, VEC, 512, 8, 1>(p, at, parts);
