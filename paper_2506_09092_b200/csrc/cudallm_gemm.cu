@@ -1753,7 +1753,7 @@ int cudallm_device_status(void *stream_v, int *code, int *detail)
     Workspace &w = workspace_for(d, stream);
     int host[2] = {0, 0};
     if (d.probed && d.supported) {                     // the attention kernels' word is not in a workspace
-        const int st = rt_xattn_status(host);
+        const int st = rt_xattn_status(dev, host);
         if (st != CUDALLM_OK) return st;
         if (host[0] != 0) {
             if (code) *code = host[0];

@@ -27,9 +27,9 @@ int rt_encode_rows(CUtensorMap *tm, const void *base, bool f16, const uint64_t (
 unsigned long long rt_wait_limit_ns();
 bool rt_take_skip_loads();             // one-shot: the next attention launch loads nothing
 
-// Status word of the attention kernels on device `dev` (current): read, and cleared if it was set.
-// Defined in xattn.cu.
-int rt_xattn_status(int (&host)[2]);
+// Status word of the attention kernels on device `dev` (current): read, and cleared if it was set; left alone (`host`
+// too) where none of them has been launched.  Defined in xattn.cu.
+int rt_xattn_status(int dev, int (&host)[2]);
 
 #define RT_CUDA_TRY(expr)                                              \
     do {                                                               \

@@ -159,13 +159,14 @@ int encode(CUtensorMap *tm, const void *base, const void *other, bool f16, const
     return rt_encode_rows(tm, base, f16, dims, bytes, kXaRows);
 }
 
+std::atomic<int *> g_status_at[kRtMaxDevices] = {};      // g_xattn_status of each device that has launched a kernel which writes it
+
 int status_word(int dev, int **out)
 {
-    static std::atomic<int *> cache[kRtMaxDevices] = {};
-    int *p = cache[dev].load(std::memory_order_relaxed);
+    int *p = g_status_at[dev].load(std::memory_order_relaxed);
     if (!p) {
         RT_CUDA_TRY(cudaGetSymbolAddress(reinterpret_cast<void **>(&p), g_xattn_status));
-        cache[dev].store(p, std::memory_order_relaxed);
+        g_status_at[dev].store(p, std::memory_order_relaxed);
     }
     *out = p;
     return CUDALLM_OK;
@@ -306,13 +307,12 @@ int run_bwd(const cudallm_xattn_shape &s, const void *q, const void *k, const vo
 
 namespace cudallm {
 
-int rt_xattn_status(int (&host)[2])
+int rt_xattn_status(int dev, int (&host)[2])
 {
-    RT_CUDA_TRY(cudaMemcpyFromSymbol(host, g_xattn_status, sizeof host));
-    if (host[0] != 0) {
-        const int zero[2] = {0, 0};
-        RT_CUDA_TRY(cudaMemcpyToSymbol(g_xattn_status, zero, sizeof zero));
-    }
+    int *p = g_status_at[dev].load(std::memory_order_relaxed);
+    if (!p) return CUDALLM_OK;
+    RT_CUDA_TRY(cudaMemcpy(host, p, sizeof host, cudaMemcpyDeviceToHost));
+    if (host[0] != 0) RT_CUDA_TRY(cudaMemset(p, 0, sizeof host));
     return CUDALLM_OK;
 }
 

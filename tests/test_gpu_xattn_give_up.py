@@ -1,5 +1,7 @@
 """Waits that run out while copies and products are in flight: whichever role gives up first, a kernel waits for
 what it has asked for before it ends, so the next call finds shared and tensor memory to itself."""
+import subprocess
+import sys
 import time
 
 import pytest
@@ -46,3 +48,34 @@ def test_a_limit_far_too_short(q_rows, heads, dim):
     got = step()
     assert B.device_status(stream)[0] == B.OK
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+STATUS = r"""
+import torch
+from paper_2506_09092_b200 import binding as B
+stream = torch.cuda.current_stream()
+a, c = torch.ones(128, 128, device="cuda").bfloat16(), torch.empty(128, 128, device="cuda")
+assert B.device_status(stream) == (B.OK, 0)                     # nothing has run
+B.gemm_bf16(a, a, c, 128, 128, 128, 128, 128, 128, B.F32, stream)
+assert B.device_status(stream) == (B.OK, 0) and bool((c == 128).all())
+q = torch.randn(1, 40, 2, 64, device="cuda").bfloat16()
+o, lse, dq = torch.empty_like(q), torch.empty(1, 2, 40, device="cuda"), torch.empty_like(q)
+shape = B.XattnShape.of(q, q, q, o)
+n = B.xattn_bwd_scratch_bytes(shape)
+scratch = torch.empty(n, dtype=torch.uint8, device="cuda")
+B.debug_set(B.DEBUG_WAIT_LIMIT_NS, 1_000_000)
+B.debug_set(B.DEBUG_SKIP_NEXT_XATTN_LOADS, 1)
+B.xattn_fwd(shape, q, q, q, None, o, lse, None, 0, stream)
+assert B.device_status(stream)[0] == B.ERR_DEVICE_TIMEOUT       # the first attention call gave up
+assert B.device_status(stream) == (B.OK, 0)                     # reported once
+B.debug_set(B.DEBUG_WAIT_LIMIT_NS, 0)
+B.xattn_fwd(shape, q, q, q, None, o, lse, None, 0, stream)
+B.xattn_bwd(shape, q, q, q, None, o, lse, o, dq, None, None, scratch, n, stream)
+assert B.device_status(stream) == (B.OK, 0) and bool(o.isfinite().all())
+print("reported once")
+"""
+
+
+def test_status_before_and_after_the_first_attention_call():
+    run = subprocess.run([sys.executable, "-c", STATUS], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "reported once" in run.stdout, run.stderr[-2000:]
