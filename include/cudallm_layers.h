@@ -54,9 +54,11 @@ extern "C" {
  *   dtype       : CUDALLM_F32, _BF16 or _F16; param_dtype: dtype or CUDALLM_F32
  * Statistics and arithmetic are in fp32 (mean and variance from differences to a
  * first mean, so a mean far above the spread costs no accuracy of y); y is
- * rounded once.  A row that holds an infinity or a NaN gives NaN in that row only.
+ * rounded once.  A row that holds an infinity or a NaN gives NaN in that row only; so
+ * does a finite row whose sum leaves fp32's range, and one whose squared differences
+ * do (differences of 1e19 and more) has rstd = 0 and y = beta.
  * rows == 0 or n == 0: success, nothing written.
- * Errors: INVALID_DIM (negative, rows or n >= 2^31 - 1024, eps negative or not
+ * Errors: INVALID_DIM (negative, rows or n > 2^31 - 1024, eps negative or not
  * finite), INVALID_LD (also for y == x with another pitch), INVALID_DTYPE, INVALID_POINTER (x or y NULL), MISALIGNED
  * (a pointer off its element size), UNSUPPORTED_DEVICE, CUDA.
  */
@@ -166,8 +168,9 @@ typedef struct cudallm_xattn_shape {
  * lse = -inf.  A query, key or value that is not finite makes the rows that see it
  * not finite, and no others.
  * Products are taken on the tensor cores with fp32 accumulation; maxima and sums in
- * fp32; the probabilities are rounded to dtype for the second product (relative to a
- * maximum: at most 2^-8 (bf16) or 2^-11 (fp16) of themselves each), O once.
+ * fp32; the probabilities, relative to a maximum, are rounded to dtype for the second
+ * product: by at most 2^-8 (bf16) or 2^-11 (fp16) of themselves each, and in fp16 by
+ * up to 2^-25 (of the maximum) where they are below 2^-14.  O is rounded once.
  * Kernels: (q_heads / kv_heads) * q_rows <= 16 rows per key head (single tokens) take
  * a kernel that reads every K and V once and splits the keys over the GPU; longer
  * queries one that owns 256 query rows of a head per CTA, split over the keys where

@@ -8,6 +8,7 @@
 // Measured (one B200): 403 M bf16 values in 291 tensors, scaled into other buffers: 396 us; the norm alone 130-134
 // us = 6.0-6.2 TB/s, the scaling alone 278 us = 5.8 TB/s; 6.8 M in 27 tensors: 10 us.  Eviction priorities for the chunks
 // that the second pass meets first: 407 to 410 instead of then 414 us whatever was kept, so none are given.
+// In place: 408 and 10.9 us.  A group of zeros goes the way of doubles: the norm of 403 M zeros takes 143 us.
 #pragma once
 #include "elem.cuh"
 

@@ -18,7 +18,9 @@
 // Measured (one B200; bytes read and written once): 16384 x 4096 bf16 forward 48.4 us = 5.5 TB/s (0.85 of the
 // measured copy bandwidth), backward 82.2 us = 4.9 TB/s; the same in fp32 97 us = 5.6 and 132 us =
 // 6.1 TB/s; 262144 x 256 bf16 forward 48.3 us = 5.6 TB/s; 2999 x 1537 fp32 (no 16-byte rows) 9.7 and
-// 19.4 us.  What is left is issue slots (55 and 63 % of them at 4096 bf16) and the two barriers of a row.
+// 19.4 us.  What is left is issue slots (55 and 63 % of them at 4096 bf16) and the two barriers of a row.  Longer rows are
+// slower: 4096 x 12288 bf16 backward 130 us = 2.3 TB/s (64 registers a thread, some spilled), with 12289 columns 262 forward and
+// 416 us backward; 2048 x 32768 fp32, read again for every pass, 160 us = 3.4 and 428 us = 1.9 TB/s.
 #pragma once
 #include "elem.cuh"
 

@@ -91,8 +91,11 @@ int launch_block(const LnRowsParams &p, const LnLaunch &at)
 // Lanes or threads per row, values per thread and rows at a time by the row's length.  Where there are rows
 // for every SM's warps, 32 values a thread: the shuffles and addresses of a row are then shared by
 // enough of them (16384 x 4096 bf16: 48.3 us; with 16 values 56, with 8 60; 262144 x 256 on 8 lanes 48.3 us,
-// on 32 lanes 61).  With few rows a row's latency counts and it is spread over more threads.  Rows
-// that are not whole 16-byte pieces carry the next row in registers and take 16 values.
+// on 32 lanes 61).  With few rows a row's latency counts and it is spread over more threads.  The numbers of rows
+// at which that turns, bf16, the form for few rows | for many: 256 columns 4700 rows 2.9 | 3.3 us, 9472 rows 4.1 | 3.5;
+// 4096 columns 580 rows 5.8 | 6.8 us, 2368 rows 12.7 | 12.1; 8192 columns 580 rows 8.5 | 8.4, 1184 rows 14.0 | 12.3 (rows of 512
+// and 1024 turn earlier: 512 columns 4700 rows 6.4 | 4.4).  Rows that are not whole 16-byte pieces carry the next row in
+// registers and take 16 values.
 template <typename T, int VEC>
 int launch_ln_by_length(const LnRowsParams &p, const LnLaunch &at)
 {
@@ -160,7 +163,9 @@ int launch_block_bwd(const LnRowsParams &p, const LnLaunch &at, int *parts)
 }
 
 // The same for the gradient, whose column sums take registers too: 8 values a thread and two or four rows at
-// a time (16384 x 4096 bf16: 82.5 us; 16 values 85.8, one row at a time 97 to 112).
+// a time (16384 x 4096 bf16: 82.5 us; 16 values 85.8, one row at a time 97 to 112).  Few | many: 256 columns 4700 rows 7.1 | 8.0 us,
+// 18944 rows 13.9 | 12.5; 512 columns 4700 rows 11.7 | 9.2; 1024 columns 580 rows 12.0 | 12.5, 1184 rows 13.4 | 12.8; 4096 columns
+// 580 rows 14.8 | 14.4, 2368 rows 24.8 | 22.6.
 template <typename T, int VEC>
 int launch_ln_bwd_by_length(const LnRowsParams &p, const LnLaunch &at, int *parts)
 {

@@ -5,8 +5,8 @@
 // and equal inputs give equal bits: one owns 128 query rows of a head and walks the keys (S, dP,
 // dQ: three products per block, and delta on the way), one owns 128 keys of a key head and walks
 // the queries of all heads that share it (S^T, dP^T, dV, dK: four).  Seven products where five
-// would do with dQ added up through memory; the two extra ones cost less than writing and reading
-// dS or ordered fp32 additions into dQ.
+// would do with dQ added up through memory in a fixed order, which has not been tried (1.6 GB of additions
+// at the size below).
 //
 // Both run the same roles: 512 threads on the 128 x 128 blocks (a thread is a row and a quarter of the
 // columns), a TMA warp, a warp that issues the products, and (keys) a warp that brings the
@@ -18,9 +18,10 @@
 // P and dS are rounded to the operands' type: that is what the tensor core multiplies.
 //
 // Measured (one B200): 2048 x up to 4096, 4 x 16 heads of 128 (526 GFLOP in five products): 630-650 us
-// = 0.81-0.83 PFLOP/s, that is 1.13-1.17 PFLOP/s of the seven that are executed, 0.82-0.85 of the
-// sustained cuBLAS rate: the call runs at the power cap, and neither shorter chains (a quarter to a half of the
-// exponentials by polynomial) nor more warps changed its time by more than 2 %.  A block takes about 2400
+// = 0.81-0.83 PFLOP/s in short bursts, that is 1.13-1.17 PFLOP/s of the seven that are executed, 0.70 of cuBLAS's burst
+// rate; over seconds, at the power cap, 723-740 us = 0.72-0.74 of cuBLAS's sustained rate.  Neither shorter chains (a quarter to a
+// half of the exponentials by polynomial) nor more warps changed it by more than 2 %.  The same with heads of 64, all
+// 4096 states: 631 us = 0.54 PFLOP/s, bound by the exponentials.  A block takes about 2400
 // clocks (dQ) and 3000 (dK, dV).
 #pragma once
 #include "xattn_common.cuh"

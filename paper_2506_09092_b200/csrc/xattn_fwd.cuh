@@ -13,13 +13,13 @@
 //
 // Bound: at DP = 128 the chain softmax -> P V -> next S of a tile, which only the other tile's
 // chain covers: tensor memory (S 2 x 128 columns, O 2 x 128) has no room for a second S, and P lies
-// over S.  At DP = 64 P has columns of its own, the next S starts as soon as this one is in
+// over S (with P in shared memory the next S could start earlier: not tried).  At DP = 64 P has columns of its own, the next S starts as soon as this one is in
 // registers, and the special-function unit (16 exponentials per clock) is the bound; the tiles take
 // turns at it, since together they would also leave it together (66 instead of 58 us below).
 //
 // Measured (one B200): 2048 queries x up to 4096 states, 4 x 16 heads of 128, lengths 3/8 to 1 (210
 // GFLOP): 185-207 us = 1.02-1.14 PFLOP/s, 0.62-0.69 of the measured cuBLAS burst, at the power cap when
-// it runs for seconds (215 us).  512 x 4096, 74 heads of 64: 58 us = 0.69 PFLOP/s.
+// it runs for seconds (217 us).  512 x 4096, 74 heads of 64: 58 us = 0.69 PFLOP/s.
 // Tried and not kept: 5 to 8 of 16 exponentials by polynomial on the FMA pipe (221 to 236 us when the kernel
 // without them took 213 to 217); blocks of 64 keys with two places for S (254 us: with N = 64 a product
 // is bound by reading the queries from shared memory, 48 clocks instead of 32); exponentials before the

@@ -31,7 +31,7 @@ struct XaTokParams {
     const int *lens;
     XaStrides sq, sk, sv, so;
     int q_rows, kv_rows, q_heads, kv_heads, group, batch, head_dim;
-    int splits, keys_per_split;                // keys_per_split: a multiple of 16
+    int splits, keys_per_split;                // keys_per_split: a multiple of 32
     int cluster;                               // the splits of a key head are one cluster
     float scale, scale_log2;
 };
