@@ -92,7 +92,78 @@ class XattnShape(ctypes.Structure):
         return kept[1]
 
 
-# name -> (restype, argtypes); mirrors include/cudallm_gemm.h, cudallm_tasks.h and cudallm_layers.h
+class PagedShape(ctypes.Structure):
+    """``cudallm_paged_shape`` of include/cudallm_cache.h: sizes, strides and scale of a layer with a paged cache."""
+    _fields_ = [(n, _i64) for n in ("batch", "q_rows", "q_heads", "kv_heads", "head_dim", "pages", "page_rows", "slots",
+                                    "table_cols", "table_stride")] + [
+        (n, _i64 * 3) for n in ("q_stride", "o_stride", "kn_stride", "vn_stride", "k_stride", "v_stride")] + [
+        ("dtype", ctypes.c_int32), ("scale", _f32)]
+
+    @classmethod
+    def of(cls, q, k, v, o, table, k_new=None, v_new=None, scale=None):
+        """From q and o (batch, tokens, q_heads, head_dim), the pools k and v (pages, page_rows, kv_heads, head_dim), the
+        table (slots, columns) and, for ``cache_append``, k_new and v_new (batch, tokens, kv_heads, head_dim): any strides
+        with a contiguous last dimension.  scale defaults to 1 / sqrt(head_dim)."""
+        new = [t for t in (k_new, v_new) if t is not None]
+        if not (q.dim() == k.dim() == 4 and q.shape == o.shape and k.shape == v.shape and q.shape[3] == k.shape[3]
+                and table.dim() == 2 and all(t.shape == (*q.shape[:2], *k.shape[2:]) for t in new)):
+            raise ValueError("q and o (batch, tokens, q_heads, head_dim), k and v (pages, page_rows, kv_heads, head_dim), "
+                             "table (slots, columns), k_new and v_new (batch, tokens, kv_heads, head_dim)")
+        if any(t.dtype != q.dtype for t in (k, v, o, *new)):
+            raise TypeError("operands of one type are needed")
+        code = {"torch.bfloat16": BF16, "torch.float16": F16}.get(str(q.dtype))
+        if code is None:
+            raise TypeError(f"bf16 or fp16 operands, not {q.dtype}")
+        if any(t.shape[-1] > 1 and t.stride(-1) != 1 for t in (q, k, v, o, table, *new)):
+            raise ValueError("the last dimension must be contiguous")
+        s = cls(batch=q.shape[0], q_rows=q.shape[1], q_heads=q.shape[2], kv_heads=k.shape[2], head_dim=q.shape[3],
+                pages=k.shape[0], page_rows=k.shape[1], slots=table.shape[0], table_cols=table.shape[1],
+                table_stride=table.stride(0), dtype=code,
+                scale=(q.shape[3] ** -0.5 if q.shape[3] else 1.0) if scale is None else scale)
+        for field, t in (("q_stride", q), ("o_stride", o), ("k_stride", k), ("v_stride", v), ("kn_stride", k_new),
+                         ("vn_stride", v_new)):
+            if t is not None:
+                setattr(s, field, (_i64 * 3)(*t.stride()[:3]))
+        return s
+
+    def layouts(self):
+        """What tensors of q, o, k_new, v_new, k, v and the table have to be, as the fields say: (strides, sizes, type, extent in
+        elements) of each, by name; then the least number of elements of lens, slot_of, new_lens and lse.  Worked out anew whenever
+        a field has changed."""
+        raw = bytes(self)
+        kept = getattr(self, "_kept", None)
+        if kept is None or kept[0] != raw:
+            import torch
+            dtype = {BF16: torch.bfloat16, F16: torch.float16}.get(self.dtype)
+            items, pool = (self.batch, self.q_rows), (self.pages, self.page_rows, self.kv_heads, self.head_dim)
+            out = {}
+            for name, size, st, t in (
+                    ("q", (*items, self.q_heads, self.head_dim), self.q_stride, dtype),
+                    ("o", (*items, self.q_heads, self.head_dim), self.o_stride, dtype),
+                    ("k_new", (*items, self.kv_heads, self.head_dim), self.kn_stride, dtype),
+                    ("v_new", (*items, self.kv_heads, self.head_dim), self.vn_stride, dtype),
+                    ("k", pool, self.k_stride, dtype), ("v", pool, self.v_stride, dtype),
+                    ("table", (self.slots, self.table_cols), (self.table_stride,), torch.int32)):
+                strides = (*st, 1)
+                extent = 0 if 0 in size else 1 + sum((n - 1) * d for n, d in zip(size, strides))
+                out[name] = (strides, torch.Size(size) if min(size) >= 0 else size, t, extent)
+            out["counts"] = (self.slots, self.batch, self.batch, self.batch * self.q_heads * self.q_rows)
+            kept = self._kept = (raw, out)
+        return kept[1]
+
+
+class CPagePool(ctypes.Structure):
+    """``cudallm_page_pool`` of include/cudallm_cache.h."""
+    _fields_ = [("data", _vp), ("stride", _i64), ("bytes", _i64)]
+
+
+class CPageBook(ctypes.Structure):
+    """``cudallm_page_book`` of include/cudallm_cache.h."""
+    _fields_ = [(n, _vp) for n in ("refs", "lens", "table", "turn")] + [
+        (n, _i64) for n in ("pages", "page_rows", "slots", "table_cols", "table_stride")]
+
+
+# name -> (restype, argtypes); mirrors include/cudallm_gemm.h, cudallm_tasks.h, cudallm_layers.h and cudallm_cache.h
 SIGNATURES = {
     "cudallm_gemm_bf16": (_int, [_vp, _vp, _vp] + [_i64] * 6 + [_int, _vp]),
     "cudallm_gemm_f32": (_int, [_vp, _vp, _vp] + [_i64] * 6 + [_int, _vp]),
@@ -138,6 +209,18 @@ SIGNATURES = {
     "cudallm_xattn_fwd_scratch_bytes": (_sz, [ctypes.POINTER(XattnShape)]),
     "cudallm_xattn_bwd": (_int, [ctypes.POINTER(XattnShape)] + [_vp] * 11 + [_sz, _vp]),
     "cudallm_xattn_bwd_scratch_bytes": (_sz, [ctypes.POINTER(XattnShape)]),
+    "cudallm_cache_append": (_int, [ctypes.POINTER(PagedShape)] + [_vp] * 9),
+    "cudallm_paged_attn": (_int, [ctypes.POINTER(PagedShape)] + [_vp] * 10 + [_sz, _vp]),
+    "cudallm_paged_attn_scratch_bytes": (_sz, [ctypes.POINTER(PagedShape)]),
+    "cudallm_pages_copy": (_int, [ctypes.POINTER(CPagePool), _i64, _i64, _vp, _vp, _i64, _vp]),
+    "cudallm_pages_fork": (_int, [ctypes.POINTER(CPageBook), _vp, _vp, _i64, _vp, _sz, _vp]),
+    "cudallm_pages_fork_scratch_bytes": (_sz, [ctypes.POINTER(CPageBook), _i64]),
+    "cudallm_pages_resize": (_int, [ctypes.POINTER(CPageBook), ctypes.POINTER(CPagePool), _i64, _vp, _vp, _i64, _vp, _vp, _sz,
+                                    _vp]),
+    "cudallm_pages_resize_scratch_bytes": (_sz, [ctypes.POINTER(CPageBook), _i64]),
+    "cudallm_pages_compact": (_int, [ctypes.POINTER(CPageBook), ctypes.POINTER(CPagePool), _i64, _vp, _vp, _sz, _vp]),
+    "cudallm_pages_compact_scratch_bytes": (_sz, [ctypes.POINTER(CPageBook)]),
+    "cudallm_draft_verify": (_int, [_vp] * 7 + [_i64] * 5 + [_int, _vp]),
 }
 
 
@@ -425,6 +508,188 @@ def xattn_bwd(shape, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch, scratch
                    ("dk", dk, at_k), ("dv", dv, at_v)), kv_lens, at_lens, lse, at_lse)
     st = lib().cudallm_xattn_bwd(shape, *_d(q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_xattn_bwd", check)
+
+
+def _paged_operands(shape, lens, slot_of, new_lens, lse=None, **tensors):
+    """Refuses tensors that do not hold the operands as a PagedShape says; addresses are taken as they are."""
+    if not isinstance(shape, PagedShape):
+        return
+    at = shape.layouts()
+    for name, t in tensors.items():
+        if t is not None and t.__class__ is not int:
+            want = at[name]
+            if not (t.stride() == want[0] and t.shape == want[1] and t.dtype is want[2]):
+                _check_layout(name, t, *want)
+    for (name, t, dtype), n in zip((("lens", lens, "torch.int32"), ("slot_of", slot_of, "torch.int32"),
+                                    ("new_lens", new_lens, "torch.int32"), ("lse", lse, "torch.float32")), at["counts"]):
+        _check_vector(name, t, dtype, n)
+
+
+def _check_vector(name, t, dtype, n):
+    if t is not None and t.__class__ is not int:
+        if str(t.dtype) != dtype:
+            raise TypeError(f"{name} has to be {dtype}, not {t.dtype}")
+        if t.numel() < n or not t.is_contiguous():
+            raise ValueError(f"{name}: {n} contiguous elements are needed")
+
+
+def cache_append(shape, k_new, v_new, k, v, table, lens, slot_of=None, new_lens=None, stream=None, check=True):
+    """Keys and values of the new tokens into the pages (``shape``: a PagedShape); slot_of and new_lens may be None.
+    Tensors must be laid out as the shape says; addresses are not looked at."""
+    _paged_operands(shape, lens, slot_of, new_lens, k_new=k_new, v_new=v_new, k=k, v=v, table=table)
+    st = lib().cudallm_cache_append(shape, *_d(k_new, v_new, k, v, table, lens, slot_of, new_lens), _s(stream))
+    return _check(st, "cudallm_cache_append", check)
+
+
+def paged_attn_scratch_bytes(shape) -> int:
+    return int(lib().cudallm_paged_attn_scratch_bytes(shape))
+
+
+def paged_attn(shape, q, k, v, table, lens, slot_of, new_lens, o, lse, scratch, scratch_bytes, stream=None, check=True):
+    """Attention of the new tokens over their sequence's pages; slot_of, new_lens, lse and scratch may be None.
+    Tensors are checked as in ``cache_append``."""
+    _paged_operands(shape, lens, slot_of, new_lens, lse, q=q, k=k, v=v, table=table, o=o)
+    st = lib().cudallm_paged_attn(shape, *_d(q, k, v, table, lens, slot_of, new_lens, o, lse, scratch), scratch_bytes,
+                                  _s(stream))
+    return _check(st, "cudallm_paged_attn", check)
+
+
+class PagePools:
+    """The tensors that hold a cache's pages (every layer's keys and values), as the C calls take them: a host array of
+    ``cudallm_page_pool``.  Built once; holds references to the tensors."""
+
+    def __init__(self, tensors):
+        tensors = list(tensors)
+        self.count = len(tensors)
+        self.array = (CPagePool * max(self.count, 1))()
+        self.pages = tensors[0].shape[0] if tensors else 0
+        self._keep = tensors
+        spans = []
+        for e, t in zip(self.array, tensors):
+            if t.dim() < 2 or t.shape[0] != self.pages:
+                raise ValueError("tensors (pages, ...) of as many pages each are needed")
+            if t.numel() and not t[0].is_contiguous():
+                raise ValueError("the values of a page must be contiguous")
+            e.data, = _d(t)
+            e.bytes = t[0].numel() * t.element_size() if self.pages else 0
+            e.stride = t.stride(0) * t.element_size()
+            if t.numel():
+                spans.append((e.data, e.data + (self.pages - 1) * e.stride + e.bytes, e.stride, e.bytes))
+        spans.sort()
+        for a, b in zip(spans, spans[1:]):
+            if b[0] < a[1] and not (a[2] == b[2] and (b[0] - a[0]) % a[2] >= a[3] and (b[0] - a[0]) % a[2] + b[3] <= a[2]):
+                raise ValueError("two pools overlap")
+
+
+def page_pools(tensors) -> PagePools:
+    """Table of CUDA tensors (pages, ...) for the pages_* calls; each page's values contiguous."""
+    return PagePools(tensors)
+
+
+class PageBook:
+    """Which sequence holds which pages: one int32 tensor ``data`` (on the current device) and its parts ``refs`` (pages),
+    ``lens`` (slots) and ``table`` (slots, table_cols), which go into the attention calls as they are.  All zeros: every page
+    free, every slot empty.  A copy of ``data`` put back undoes what was done in between."""
+
+    def __init__(self, pages, page_rows, slots, table_cols, device="cuda"):
+        import torch
+        up = lambda n: (n + 3) // 4 * 4
+        at = [0, 4]
+        for n in (pages, slots, slots * table_cols):
+            at.append(at[-1] + up(n))
+        self.data = torch.zeros(at[-1], dtype=torch.int32, device=device)
+        self.page_rows = page_rows
+        self.refs, self.lens = self.data[at[1]:at[1] + pages], self.data[at[2]:at[2] + slots]
+        self.table = self.data[at[3]:at[3] + slots * table_cols].view(slots, table_cols)
+        self.c = CPageBook(pages=pages, page_rows=page_rows, slots=slots, table_cols=table_cols, table_stride=table_cols)
+        base = self.data.data_ptr()
+        self.c.turn, self.c.refs, self.c.lens, self.c.table = (base + 4 * i for i in at[:4])
+
+    def _here(self):
+        _d(self.data)
+        return self.c
+
+
+def _pool_array(pools):
+    return (None, 0) if pools is None else (pools.array, pools.count)
+
+
+def _pools_of(book, pools):
+    if pools is not None and pools.count and pools.pages != book.c.pages:
+        raise ValueError(f"pools of {pools.pages} pages, a book of {book.c.pages}")
+    return _pool_array(pools)
+
+
+def pages_copy(pools, src, dst, n, stream=None, check=True):
+    """Page src[i] to page dst[i] in every pool, i < n (int32 on the device)."""
+    _check_vector("src", src, "torch.int32", n)
+    _check_vector("dst", dst, "torch.int32", n)
+    st = lib().cudallm_pages_copy(pools.array, pools.count, pools.pages, *_d(src, dst), n, _s(stream))
+    return _check(st, "cudallm_pages_copy", check)
+
+
+def pages_fork_scratch_bytes(book, n) -> int:
+    return int(lib().cudallm_pages_fork_scratch_bytes(book.c, n))
+
+
+def pages_fork(book, src, dst, n, scratch, scratch_bytes, stream=None, check=True):
+    """The sequence in slot dst[i] becomes what the one in src[i] was, sharing its pages, i < n (int32 on the device)."""
+    _check_vector("src", src, "torch.int32", n)
+    _check_vector("dst", dst, "torch.int32", n)
+    st = lib().cudallm_pages_fork(book._here(), *_d(src, dst), n, *_d(scratch), scratch_bytes, _s(stream))
+    return _check(st, "cudallm_pages_fork", check)
+
+
+def pages_resize_scratch_bytes(book, n) -> int:
+    return int(lib().cudallm_pages_resize_scratch_bytes(book.c, n))
+
+
+def pages_resize(book, pools, slot_of, new_lens, n, result, scratch, scratch_bytes, stream=None, check=True):
+    """The sequence in slot slot_of[i] gets the length new_lens[i], i < n (int32 on the device); pages are taken or given back,
+    shared last pages copied in ``pools`` (may be None: a book without data).  slot_of may be None: slots 0..n-1.
+    result[0] (int32 on the device, or None): 0, or why nothing was done."""
+    _check_vector("slot_of", slot_of, "torch.int32", n)
+    _check_vector("new_lens", new_lens, "torch.int32", n)
+    _check_vector("result", result, "torch.int32", 1)
+    array, count = _pools_of(book, pools)
+    st = lib().cudallm_pages_resize(book._here(), array, count, *_d(slot_of, new_lens), n, *_d(result, scratch), scratch_bytes,
+                                    _s(stream))
+    return _check(st, "cudallm_pages_resize", check)
+
+
+def pages_compact_scratch_bytes(book) -> int:
+    return int(lib().cudallm_pages_compact_scratch_bytes(book.c))
+
+
+def pages_compact(book, pools, used, scratch, scratch_bytes, stream=None, check=True):
+    """The pages in use move down to the lowest numbers, in ``pools`` (may be None) and the book; used[0] (int32 on the device,
+    or None): how many there are."""
+    _check_vector("used", used, "torch.int32", 1)
+    array, count = _pools_of(book, pools)
+    st = lib().cudallm_pages_compact(book._here(), array, count, *_d(used, scratch), scratch_bytes, _s(stream))
+    return _check(st, "cudallm_pages_compact", check)
+
+
+def draft_verify(p, q, drafts, draft_lens, u, tokens, accepted, batch, n, vocab, ldp, ldq, dtype, stream=None, check=True):
+    """Drafted tokens against the target's probabilities p (batch * (n + 1) rows) and the draft's q (batch * n rows, or
+    None: the drafts were certain), by the random numbers u: tokens (batch, n + 1) and accepted (batch) are written."""
+    rows = batch * (n + 1)
+    for name, t, want, count in (("drafts", drafts, "torch.int32", batch * n), ("draft_lens", draft_lens, "torch.int32", batch),
+                                 ("u", u, "torch.float32", rows), ("tokens", tokens, "torch.int32", rows),
+                                 ("accepted", accepted, "torch.int32", batch)):
+        _check_vector(name, t, want, count)
+    want = {F32: "torch.float32", BF16: "torch.bfloat16", F16: "torch.float16"}.get(dtype)
+    for name, t, r, ld in (("p", p, rows, ldp), ("q", q, batch * n, ldq)):
+        if t is not None and t.__class__ is not int and want is not None:
+            if str(t.dtype) != want:
+                raise TypeError(f"{name} has to be {want}, not {t.dtype}")
+            if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+                raise ValueError(f"{name}: the last dimension must be contiguous")
+            if r > 0 and (1 + sum((s - 1) * d for s, d in zip(t.shape, t.stride())) if t.numel() else 0) < (r - 1) * ld + vocab:
+                raise ValueError(f"{name}: {tuple(t.shape)} ends before {r} rows of pitch {ld} do")
+    st = lib().cudallm_draft_verify(*_d(p, q, drafts, draft_lens, u, tokens, accepted), batch, n, vocab, ldp, ldq, dtype,
+                                    _s(stream))
+    return _check(st, "cudallm_draft_verify", check)
 
 
 def gemm_bf16_batched(A, B, C, M, N, K, lda, ldb, ldc, strideA, strideB, strideC, batch,

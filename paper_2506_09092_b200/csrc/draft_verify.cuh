@@ -1,0 +1,215 @@
+// Drafted tokens against the target's probabilities.
+//
+// Bound: latency where the vocabulary is small (numbers of the drafts -> their probabilities -> the row to draw from, three
+// dependent loads), HBM where it is large (one row of p and one of q per sequence are read once).  A
+// cluster of CTAs works on a sequence: each decides which drafts hold by itself, sums up its part of the
+// row that the next token is drawn from, chunk by chunk, and learns the others' sums from their shared
+// memory.  The CTA whose part holds the drawn point reads one chunk again (from L2), element by element.
+//
+// Everything is in 64 bits: products of two fp32 values and differences of two are exact there, and a sum
+// is off by 2^-53 of itself per addition, so that the point drawn is the one that any order of summation
+// would give but for one in some 10^10.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "elem.cuh"
+#include "mma_sync.cuh"
+#include "ptx.cuh"
+
+namespace cudallm {
+
+constexpr int kVerifyThreads = 256;
+constexpr int kVerifyWarps = kVerifyThreads / 32;
+constexpr int kVerifyChunk = 512;              // elements that a warp sums up at a time (or a multiple, for huge rows)
+constexpr int kVerifyChunks = 1024;            // of a CTA at most
+constexpr int kVerifyCluster = 8;
+
+struct VerifyParams {
+    const void *p, *q;
+    const int *drafts, *draft_lens;
+    const float *u;
+    int *tokens, *accepted;
+    long long ldp, ldq;
+    int n, vocab, cluster;
+    int chunk, chunks;                         // elements of a chunk (a multiple of 512), chunks of a CTA
+};
+
+template <typename T> __device__ __forceinline__ double elem_to_double(T v) { return (double)elem_to_float(v); }
+__device__ __forceinline__ double cluster_ld_f64(uint32_t addr)
+{
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kVerifyThreads)
+draft_verify_kernel(const VerifyParams p)
+{
+    __shared__ double sums[kVerifyChunks], cta_sum;
+    __shared__ int s_accepted;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = blockIdx.x % p.cluster, b = blockIdx.x / p.cluster;
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    const T *pp = static_cast<const T *>(p.p) + (long long)b * (p.n + 1) * p.ldp;
+    const T *qq = p.q ? static_cast<const T *>(p.q) + (long long)b * p.n * p.ldq : nullptr;
+    const int *drafts = p.drafts + (long long)b * p.n;
+    const float *u = p.u + (long long)b * (p.n + 1);
+    const int m = p.draft_lens ? min(max(p.draft_lens[b], 0), p.n) : p.n;
+    if (warp == 0) {
+        int a = m;
+        for (int t0 = 0; t0 < m; t0 += 32) {
+            const int t = t0 + lane;
+            bool good = true;
+            if (t < m) {
+                const int x = drafts[t];
+                good = false;
+                if ((unsigned)x < (unsigned)p.vocab) {
+                    const double qx = qq ? elem_to_double(qq[t * p.ldq + x]) : 1.0;
+                    good = (double)u[t] * qx < elem_to_double(pp[t * p.ldp + x]);
+                }
+            }
+            const uint32_t bad = __ballot_sync(0xffffffffu, !good);
+            if (bad) {
+                a = t0 + __ffs(bad) - 1;
+                break;
+            }
+        }
+        if (lane == 0) s_accepted = a;
+    }
+    __syncthreads();
+    const int a = s_accepted;
+    // what is drawn from: max(p_a - q_a, 0) while drafts are left, q_a being a row or 1 at `certain`; else p_a
+    const T *prow = pp + a * p.ldp, *qrow = a < m && qq ? qq + a * p.ldq : nullptr;
+    int certain = a < m && !qq ? drafts[a] : -1;
+    auto mass = [&](T pv, T qv, long long v) {
+        const double r = elem_to_double(pv) - (v == certain ? 1.0 : elem_to_double(qv));
+        return r > 0.0 && r < (double)INFINITY ? r : 0.0;
+    };
+    // 16 x 32 elements from `from` on, element i * 32 + lane in register i
+    const T zero = elem_from_float<T>(0.f);
+    auto load = [&](long long from, T (&pv)[16], T (&qv)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const long long v = from + i * 32 + lane;
+            pv[i] = v < p.vocab ? prow[v] : zero;
+            qv[i] = qrow && v < p.vocab ? qrow[v] : zero;
+        }
+    };
+
+    const double draw = (double)u[p.n];
+    double point, before;                                          // where in the sum of all; the sum of the CTAs before this one
+    int owner;                                                     // the CTA that holds the point
+    for (int pass = 0;; ++pass) {
+        for (int c = warp; c < p.chunks; c += kVerifyWarps) {
+            double s = 0.0;
+            for (int part = 0; part < p.chunk; part += kVerifyChunk) {
+                const long long from = ((long long)rank * p.chunks + c) * p.chunk + part;
+                T pv[16], qv[16];
+                load(from, pv, qv);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s += mass(pv[i], qv[i], from + i * 32 + lane);
+            }
+#pragma unroll
+            for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+            if (lane == 0) sums[c] = s;
+        }
+        __syncthreads();
+        if (warp == 0) {                                           // chunks' sums become sums up to and with each
+            double upto = 0.0;
+            for (int c0 = 0; c0 < p.chunks; c0 += 32) {
+                double s = c0 + lane < p.chunks ? sums[c0 + lane] : 0.0;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const double x = __shfl_up_sync(0xffffffffu, s, d);
+                    if (lane >= d) s += x;
+                }
+                s += upto;
+                if (c0 + lane < p.chunks) sums[c0 + lane] = s;
+                upto = __shfl_sync(0xffffffffu, s, 31);
+            }
+            if (lane == 0) cta_sum = upto;
+        }
+        __syncthreads();
+        double cta[kVerifyCluster], all = 0.0;
+        if (p.cluster > 1) cluster_sync_all();
+#pragma unroll
+        for (int c = 0; c < kVerifyCluster; ++c) {
+            cta[c] = c >= p.cluster ? 0.0 : p.cluster > 1 ? cluster_ld_f64(cluster_map(smem_u32(&cta_sum), c)) : cta_sum;
+            all += cta[c];
+        }
+        point = draw * all;
+        owner = -1;
+        before = 0.0;
+        double upto = 0.0;
+        int last = -1;
+#pragma unroll
+        for (int c = 0; c < kVerifyCluster; ++c) {
+            if (c == rank) before = upto;
+            if (cta[c] > 0.0) {
+                last = c;
+                if (owner < 0 && upto + cta[c] > point) owner = c;
+            }
+            upto += cta[c];
+        }
+        if (owner < 0) owner = last;                               // a point behind the end: the last element with mass
+        if (p.cluster > 1) cluster_sync_all();                     // the sums have been read
+        if (owner >= 0 || pass == 1 || a == m) break;
+        qrow = nullptr;                                            // nothing is left of p_a - q_a: p_a itself
+        certain = -1;
+    }
+
+    int *out = p.tokens + (long long)b * (p.n + 1);
+    if (rank == 0) {
+        for (int t = tid; t <= p.n; t += kVerifyThreads)
+            if (t != a || owner < 0) out[t] = t < a ? drafts[t] : -1;
+        if (tid == 0) p.accepted[b] = a;
+    }
+    if (rank != owner) return;
+    // the chunk that holds the point, or the last one with mass
+    __shared__ int s_hit, s_last;
+    if (tid == 0) {
+        s_hit = p.chunks;
+        s_last = 0;
+    }
+    __syncthreads();
+    for (int c = tid; c < p.chunks; c += kVerifyThreads) {
+        const double below = c ? sums[c - 1] : 0.0;
+        if (sums[c] > below) {
+            atomicMax(&s_last, c);
+            if (before + sums[c] > point) atomicMin(&s_hit, c);
+        }
+    }
+    __syncthreads();
+    if (warp != 0) return;
+    const int c = s_hit < p.chunks ? s_hit : s_last;
+    double upto = before + (c ? sums[c - 1] : 0.0);
+    long long token = -1;
+    for (int part = 0; part < p.chunk; part += kVerifyChunk) {
+        const long long from = ((long long)rank * p.chunks + c) * p.chunk + part;
+        T pv[16], qv[16];
+        load(from, pv, qv);
+        bool found = false;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const double r = mass(pv[i], qv[i], from + i * 32 + lane);
+            double s = r;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const double x = __shfl_up_sync(0xffffffffu, s, d);
+                if (lane >= d) s += x;
+            }
+            const uint32_t there = __ballot_sync(0xffffffffu, r > 0.0), over = __ballot_sync(0xffffffffu, r > 0.0 && upto + s > point);
+            if (!found && there) token = from + i * 32 + (over ? __ffs(over) - 1 : 31 - __clz(there));
+            found |= over != 0;
+            upto += __shfl_sync(0xffffffffu, s, 31);
+        }
+        if (found) break;
+    }
+    if (lane == 0) out[a] = (int)token;
+}
+
+}  // namespace cudallm

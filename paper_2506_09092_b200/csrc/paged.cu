@@ -1,0 +1,220 @@
+// Paged cache entry points of include/cudallm_cache.h: appending keys and values, attention of the newest
+// tokens.  Validation, the choice of the split, launches.
+#include "../../include/cudallm_cache.h"
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "runtime.h"
+#include "paged_attn.cuh"
+
+using namespace cudallm;
+
+namespace {
+
+constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
+constexpr int64_t kMaxElems = int64_t(1) << 46;          // of an operand, strides included
+constexpr int64_t kPlanSms = 148;                        // the split is planned for this many SMs
+
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline bool off(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
+
+// Strides of a three-level operand: multiples of 8, no two elements in one place.
+int check_strides(const int64_t (&st)[3], int64_t e0, int64_t e1, int64_t e2, int64_t dim)
+{
+    const int64_t ext[3] = {e0, e1, e2};
+    int order[3], n = 0;
+    for (int i = 0; i < 3; ++i)
+        if (ext[i] > 1) order[n++] = i;
+    for (int i = 0; i < n; ++i)
+        if (st[order[i]] <= 0) return CUDALLM_ERR_INVALID_LD;
+    std::sort(order, order + n, [&](int a, int b) { return st[a] < st[b]; });
+    long double cover = (long double)dim;
+    for (int i = 0; i < n; ++i) {
+        const int64_t s = st[order[i]];
+        if ((long double)s < cover) return CUDALLM_ERR_INVALID_LD;
+        cover += (long double)s * (long double)(ext[order[i]] - 1);
+        if (cover > (long double)kMaxElems) return CUDALLM_ERR_INVALID_DIM;
+    }
+    for (int i = 0; i < n; ++i)
+        if (st[order[i]] % 8) return CUDALLM_ERR_UNSUPPORTED_SHAPE;
+    return CUDALLM_OK;
+}
+
+bool no_states(const cudallm_paged_shape &s) { return s.pages == 0 || s.table_cols == 0; }
+// Nothing to write: no items, tokens or values, or no item that is there.
+bool append_empty(const cudallm_paged_shape &s)
+{
+    return s.batch == 0 || s.q_rows == 0 || s.kv_heads == 0 || s.head_dim == 0 || s.slots == 0 || no_states(s);
+}
+bool attn_empty(const cudallm_paged_shape &s)
+{
+    return s.batch == 0 || s.q_rows == 0 || s.q_heads == 0 || s.head_dim == 0 || s.slots == 0;
+}
+
+int check_shape(const cudallm_paged_shape *sp)
+{
+    if (!sp) return CUDALLM_ERR_INVALID_POINTER;
+    const cudallm_paged_shape &s = *sp;
+    if (s.dtype != CUDALLM_BF16 && s.dtype != CUDALLM_F16) return CUDALLM_ERR_INVALID_DTYPE;
+    for (int64_t v : {s.batch, s.q_rows, s.q_heads, s.kv_heads, s.head_dim, s.pages, s.slots, s.table_cols})
+        if (v < 0 || v > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
+    if (s.page_rows < 1 || s.page_rows > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
+    if (!(s.scale >= 0.f) || !(s.scale <= 3.0e38f)) return CUDALLM_ERR_INVALID_DIM;
+    if (s.q_heads > 0 && (s.kv_heads == 0 || s.q_heads % s.kv_heads)) return CUDALLM_ERR_INVALID_DIM;
+    if (s.table_cols > kMaxDim / s.page_rows) return CUDALLM_ERR_INVALID_DIM;
+    if (s.slots > 1 && s.table_stride < s.table_cols) return CUDALLM_ERR_INVALID_LD;
+    if (s.slots > 1 && (long double)s.table_stride * s.slots > (long double)kMaxElems) return CUDALLM_ERR_INVALID_DIM;
+    if (s.head_dim % 8 || s.head_dim > 128) return CUDALLM_ERR_UNSUPPORTED_SHAPE;
+    // items x key heads x row tiles, and rows of an item and key head, are counted in 31 bits
+    if ((long double)s.batch * std::max(s.q_heads, s.kv_heads) * s.q_rows > (long double)(kMaxDim / 8)) return CUDALLM_ERR_INVALID_DIM;
+    if (no_states(s) || s.kv_heads == 0 || s.head_dim == 0) return CUDALLM_OK;
+    int st = check_strides(s.k_stride, s.pages, s.page_rows, s.kv_heads, s.head_dim);
+    if (st == CUDALLM_OK) st = check_strides(s.v_stride, s.pages, s.page_rows, s.kv_heads, s.head_dim);
+    return st;
+}
+
+// How an attention call runs.
+struct Plan {
+    bool wide;                  // head dims above 64
+    int mt, row_tiles;          // row tiles of 16 mt rows
+    int cluster;                // CTAs a cluster; 0: equal shares
+    int ctas;
+    size_t part_bytes, scratch;
+};
+Plan plan_attn(const cudallm_paged_shape &s)
+{
+    Plan f{};
+    const int64_t rows = (s.q_heads / s.kv_heads) * s.q_rows;
+    f.wide = s.head_dim > 64;
+    f.mt = rows <= 16 ? 1 : 2;
+    f.row_tiles = (int)cdiv(rows, 16 * f.mt);
+    const int64_t items = s.batch * s.kv_heads * f.row_tiles, full = 2 * kPlanSms;
+    const int64_t blocks = std::max<int64_t>(1, cdiv(no_states(s) ? 0 : s.table_cols * s.page_rows, f.wide ? 64 : 128));
+    const int64_t fits = std::min<int64_t>({int64_t(kPaCluster), full / std::max<int64_t>(items, 1), blocks});
+    if (items <= kPlanSms && (items * kPaCluster >= kPlanSms || blocks <= 4 * kPaCluster)) {
+        f.cluster = (int)std::max<int64_t>(1, fits);
+        f.ctas = (int)(items * f.cluster);
+    } else {
+        f.ctas = (int)std::min<int64_t>(full, items * blocks);
+        const size_t slot = (size_t)16 * f.mt * ((f.wide ? 128 : 64) + 1) * sizeof(float);
+        f.part_bytes = 2 * (size_t)f.ctas * slot;
+        f.scratch = f.part_bytes + (size_t)f.ctas * kPaDesc * sizeof(int);
+    }
+    return f;
+}
+
+// Factor of the exponentials' arguments.  Masked scores are -inf, and -inf x 0 is no number, so a
+// scale of 0 enters as 1e-30: every finite score then gives exp2(0) = 1 all the same.
+inline float scale_log2(float scale) { return std::max(scale, 1e-30f) * 1.4426950408889634f; }
+
+inline XaStrides strides(const int64_t (&s)[3]) { return XaStrides{(long long)s[0], (long long)s[1], (long long)s[2]}; }
+inline PagedStrides page_strides(const int64_t (&s)[3]) { return PagedStrides{(long long)s[0], (long long)s[1], (long long)s[2]}; }
+inline XaStrides pieces(const int64_t (&s)[3]) { return XaStrides{s[0] / 8, s[1] / 8, s[2] / 8}; }
+inline PagedStrides page_pieces(const int64_t (&s)[3]) { return PagedStrides{s[0] / 8, s[1] / 8, s[2] / 8}; }
+
+template <int DP, int MT, typename T>
+int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
+{
+    using L = PagedSmem<DP, MT>;
+    static std::atomic<bool> done[kRtMaxDevices] = {};
+    if (!done[dev].load(std::memory_order_relaxed)) {
+        RT_CUDA_TRY(cudaFuncSetAttribute(paged_attn_kernel<DP, MT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
+        done[dev].store(true, std::memory_order_relaxed);
+    }
+    const int st = rt_launch_cluster(paged_attn_kernel<DP, MT, T>, dim3((unsigned)f.ctas), f.cluster ? (unsigned)f.cluster : 1u,
+                                     kPaThreads, (size_t)L::kBytes, stream, p);
+    if (st != CUDALLM_OK || f.cluster || f.ctas == 1) return st;
+    const int64_t rows = std::min<int64_t>(L::kRows, (int64_t)p.group * s.q_rows);
+    return rt_launch(paged_join_kernel<DP, MT, T>, dim3((unsigned)f.ctas, (unsigned)cdiv(rows, 128 / (DP / 8))), 128, 0, stream, p);
+}
+template <typename T>
+int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
+{
+    if (f.wide) return f.mt == 1 ? run<128, 1, T>(s, f, p, dev, stream) : run<128, 2, T>(s, f, p, dev, stream);
+    return f.mt == 1 ? run<64, 1, T>(s, f, p, dev, stream) : run<64, 2, T>(s, f, p, dev, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t cudallm_paged_attn_scratch_bytes(const cudallm_paged_shape *shape)
+{
+    if (check_shape(shape) != CUDALLM_OK || attn_empty(*shape)) return 0;
+    return plan_attn(*shape).scratch;
+}
+
+int cudallm_paged_attn(const cudallm_paged_shape *shape, const void *q, const void *k, const void *v, const int32_t *table,
+                       const int32_t *lens, const int32_t *slot_of, const int32_t *new_lens, void *o, float *lse,
+                       void *scratch, size_t scratch_bytes, void *stream)
+{
+    int st = check_shape(shape);
+    if (st != CUDALLM_OK) return st;
+    const cudallm_paged_shape &s = *shape;
+    if (attn_empty(s)) return CUDALLM_OK;
+    st = check_strides(s.q_stride, s.batch, s.q_rows, s.q_heads, s.head_dim);
+    if (st == CUDALLM_OK) st = check_strides(s.o_stride, s.batch, s.q_rows, s.q_heads, s.head_dim);
+    if (st != CUDALLM_OK) return st;
+    const bool states = !no_states(s);
+    if (!q || !o || !lens || (states && (!k || !v || !table))) return CUDALLM_ERR_INVALID_POINTER;
+    if (off(table, 4) || off(lens, 4) || off(slot_of, 4) || off(new_lens, 4) || off(lse, 4)) return CUDALLM_ERR_MISALIGNED;
+    if (off(q, 16) || off(o, 16) || (states && (off(k, 16) || off(v, 16)))) return CUDALLM_ERR_UNSUPPORTED_SHAPE;
+    const Plan f = plan_attn(s);
+    if (f.scratch && (!scratch || off(scratch, 16) || scratch_bytes < f.scratch)) return CUDALLM_ERR_WORKSPACE;
+    int dev = 0, sms = 0;
+    if ((st = rt_current_device(&dev, &sms)) != CUDALLM_OK) return st;
+    PagedParams p{};
+    p.q = q; p.k = k; p.v = v; p.o = o; p.lse = lse;
+    if (f.scratch) {
+        p.part = static_cast<float *>(scratch);
+        p.desc = reinterpret_cast<int *>(static_cast<char *>(scratch) + f.part_bytes);
+    }
+    p.table = table; p.lens = lens; p.slot_of = slot_of; p.new_lens = new_lens;
+    p.sq = strides(s.q_stride); p.so = strides(s.o_stride);
+    p.sk = page_strides(s.k_stride); p.sv = page_strides(s.v_stride);
+    p.table_stride = s.table_stride;
+    p.batch = (int)s.batch; p.q_rows = (int)s.q_rows; p.q_heads = (int)s.q_heads; p.kv_heads = (int)s.kv_heads;
+    p.group = (int)(s.q_heads / s.kv_heads); p.head_dim = (int)s.head_dim;
+    p.pages = (int)s.pages; p.page_rows = (int)s.page_rows; p.slots = (int)s.slots;
+    p.cap = states ? (int)(s.table_cols * s.page_rows) : 0;
+    p.row_tiles = f.row_tiles;
+    p.cluster = f.cluster;
+    p.scale = s.scale; p.scale_log2 = scale_log2(s.scale);
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    return s.dtype == CUDALLM_BF16 ? run<__nv_bfloat16>(s, f, p, dev, cs) : run<__half>(s, f, p, dev, cs);
+}
+
+int cudallm_cache_append(const cudallm_paged_shape *shape, const void *k_new, const void *v_new, void *k, void *v,
+                         const int32_t *table, const int32_t *lens, const int32_t *slot_of, const int32_t *new_lens,
+                         void *stream)
+{
+    int st = check_shape(shape);
+    if (st != CUDALLM_OK) return st;
+    const cudallm_paged_shape &s = *shape;
+    if (append_empty(s)) return CUDALLM_OK;
+    st = check_strides(s.kn_stride, s.batch, s.q_rows, s.kv_heads, s.head_dim);
+    if (st == CUDALLM_OK) st = check_strides(s.vn_stride, s.batch, s.q_rows, s.kv_heads, s.head_dim);
+    if (st != CUDALLM_OK) return st;
+    if (!k_new || !v_new || !k || !v || !table || !lens) return CUDALLM_ERR_INVALID_POINTER;
+    if (off(table, 4) || off(lens, 4) || off(slot_of, 4) || off(new_lens, 4)) return CUDALLM_ERR_MISALIGNED;
+    if (off(k_new, 16) || off(v_new, 16) || off(k, 16) || off(v, 16)) return CUDALLM_ERR_UNSUPPORTED_SHAPE;
+    int dev = 0, sms = 0;
+    if ((st = rt_current_device(&dev, &sms)) != CUDALLM_OK) return st;
+    AppendParams p{};
+    p.k_new = static_cast<const uint4 *>(k_new); p.v_new = static_cast<const uint4 *>(v_new);
+    p.k = static_cast<uint4 *>(k); p.v = static_cast<uint4 *>(v);
+    p.table = table; p.lens = lens; p.slot_of = slot_of; p.new_lens = new_lens;
+    p.skn = pieces(s.kn_stride); p.svn = pieces(s.vn_stride);
+    p.sk = page_pieces(s.k_stride); p.sv = page_pieces(s.v_stride);
+    p.table_stride = s.table_stride;
+    p.chunks = (int)(s.head_dim / 8);
+    p.total = s.batch * s.q_rows * s.kv_heads * p.chunks;
+    p.q_rows = (int)s.q_rows; p.kv_heads = (int)s.kv_heads; p.pages = (int)s.pages; p.page_rows = (int)s.page_rows;
+    p.slots = (int)s.slots; p.cap = (int)(s.table_cols * s.page_rows);
+    const int64_t ctas = std::min<int64_t>(cdiv(p.total, 256), 64 * kPlanSms);
+    return rt_launch(cache_append_kernel, dim3((unsigned)ctas), 256, 0, static_cast<cudaStream_t>(stream), p);
+}
+
+}  // extern "C"

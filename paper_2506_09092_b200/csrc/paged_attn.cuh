@@ -1,0 +1,736 @@
+// Attention of the newest tokens of each sequence over its pages, and writing their keys and values there.
+//
+// Bound: HBM (K and V of every sequence are read once; 16 or 32 rows of arithmetic per key are far below
+// any pipe's rate), so what matters is bytes in flight and an even split.  A CTA has four warps; each walks
+// its own tiles of 32 keys (16 at head dims above 64) through its own ring of cp.async stages, no barrier
+// between warps.  A lane looks up the page of "its" row of the next tile one tile ahead, and the rows'
+// offsets go round by shuffle, so pages may have any number of rows.  The rows that share a key head
+// (query heads x new tokens) are the M of mma.sync.m16n8k16, one or two tiles of 16: a tcgen05 tile would be 128
+// rows, most of them empty, and 16 rows need a tenth of mma.sync's rate at the full speed of HBM.
+//
+// Only the device knows the lengths, so the split is made there, in one of two ways:
+//  * a cluster of CTAs per (item, key head, row tile), each with an equal share of its keys; they join
+//    through each other's shared memory.  One launch, but as long as the longest sequence takes.
+//  * equal shares: all blocks of keys of all items in one line, cut into as many equal pieces as CTAs fit.
+//    A CTA's piece may begin and end inside an item; such parts go to scratch (two slots a CTA) and
+//    paged_join_kernel adds them up in order.
+#pragma once
+#include "mma_sync.cuh"
+#include "xattn_common.cuh"
+
+namespace cudallm {
+
+constexpr int kPaWarps = 4;
+constexpr int kPaThreads = 32 * kPaWarps;
+constexpr int kPaCluster = 8;
+
+struct PagedStrides { long long page, row, head; };
+
+struct PagedParams {
+    const void *q, *k, *v;
+    void *o;
+    float *lse;
+    float *part;                               // equal shares: parts' results, two slots a CTA ...
+    int *desc;                                 // ... and kPaDesc words a CTA
+    const int *table, *lens, *slot_of, *new_lens;
+    XaStrides sq, so;
+    PagedStrides sk, sv;
+    long long table_stride;
+    int batch, q_rows, q_heads, kv_heads, group, head_dim;
+    int pages, page_rows, slots, cap;          // cap: states that a row of the table holds
+    int row_tiles;                             // tiles of 16 or 32 rows of an item and key head at most
+    int cluster;                               // CTAs per item, key head and row tile; 0: equal shares
+    float scale, scale_log2;
+};
+constexpr int kPaDesc = 4;                     // parts (0: none begins here), item, key head, row tile
+
+template <int DP, int MT> struct PagedSmem {
+    static constexpr int kRows = 16 * MT;
+    static constexpr int kKeys = DP == 128 ? 16 : 32;              // of a stage
+    static constexpr int kBlock = kKeys * kPaWarps;                // of a round of the four warps: unit of the split
+    static constexpr int kStages = 3;                              // 96 KiB a CTA: two on an SM
+    static constexpr int kTile = kKeys * DP * 2;                   // one of K, V
+    static constexpr int kWarp = kStages * 2 * kTile;
+    static constexpr int kRing = kPaWarps * kWarp;
+    static constexpr int kPitch = DP + 4;                          // floats per row of the joining block
+    static constexpr int kJoinWarp = (kRows * kPitch + 2 * kRows) * 4;
+    // a CTA's result for its cluster: [row][DP] fp32, then the rows' lse
+    static constexpr int kShare = (kPaWarps * kJoinWarp + 127) / 128 * 128;
+    static_assert(kShare + kRows * (DP + 1) * 4 <= kRing, "behind the warps' results");
+    static constexpr int kQ = MT > 1 ? kRows * DP * 2 : 0;         // two row tiles' queries stay in shared memory
+    static constexpr int kBytes = kRing + kQ;
+    static constexpr int kSlot = kRows * (DP + 1);                 // floats of a part's result
+};
+
+// An item: its row of the table, its states, its new tokens (0: none, or the item is not there).
+struct PagedItem { const int *row; int len, news; };
+__device__ __forceinline__ PagedItem paged_item(const int *table, long long stride, const int *lens, const int *slot_of,
+                                                const int *new_lens, int b, int slots, int cap, int q_rows)
+{
+    const int slot = slot_of ? slot_of[b] : b;
+    if ((unsigned)slot >= (unsigned)slots) return PagedItem{table, 0, 0};
+    const int len = min(max(lens[slot], 0), cap);
+    const int news = new_lens ? min(max(new_lens[b], 0), q_rows) : q_rows;
+    return PagedItem{table + slot * stride, len, news};
+}
+__device__ __forceinline__ PagedItem paged_item(const PagedParams &p, int b)
+{
+    return paged_item(p.table, p.table_stride, p.lens, p.slot_of, p.new_lens, b, p.slots, p.cap, p.q_rows);
+}
+// States that token t sees; states that a row tile's last token sees; its blocks of keys (at least one, so that
+// somebody writes the result; none without rows).
+__device__ __forceinline__ int paged_seen(const PagedItem &it, int t) { return max(it.len - it.news + t + 1, 0); }
+__device__ __forceinline__ int paged_tile_seen(const PagedItem &it, int group, int rows, int rt)
+{
+    return paged_seen(it, (min(it.news * group, (rt + 1) * rows) - 1) / group);
+}
+__device__ __forceinline__ int paged_blocks(const PagedItem &it, int group, int rows, int rt, int block)
+{
+    if (rt * rows >= it.news * group) return 0;
+    return max(1, (paged_tile_seen(it, group, rows, rt) + block - 1) / block);
+}
+
+// (as an instruction: a choice among registers must not become an address into a copy of them in local memory)
+__device__ __forceinline__ float select(bool first, float a, float b)
+{
+    float r;
+    asm("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %3, 0;\n\tselp.f32 %0, %1, %2, p;\n\t}" : "=f"(r) : "f"(a), "f"(b), "r"((int)first));
+    return r;
+}
+
+// The lowest n bits.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1; }
+
+template <typename T> __device__ __forceinline__ bool any_not_finite(uint4 v);
+template <> __device__ __forceinline__ bool any_not_finite<__nv_bfloat16>(uint4 v)
+{
+    bool bad = false;
+    for (uint32_t w : {v.x, v.y, v.z, v.w}) bad |= (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+    return bad;
+}
+template <> __device__ __forceinline__ bool any_not_finite<__half>(uint4 v)
+{
+    bool bad = false;
+    for (uint32_t w : {v.x, v.y, v.z, v.w}) bad |= (w & 0x7C00u) == 0x7C00u || (w & 0x7C000000u) == 0x7C000000u;
+    return bad;
+}
+__device__ __forceinline__ uint4 ld_shared_v4(uint32_t addr)
+{
+    uint4 w;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "r"(addr) : "memory");
+    return w;
+}
+__device__ __forceinline__ uint32_t ld_shared_u32(uint32_t addr)
+{
+    uint32_t w;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(addr) : "memory");
+    return w;
+}
+template <typename T> __device__ __forceinline__ float2 unpack2(uint32_t w);
+template <> __device__ __forceinline__ float2 unpack2<__nv_bfloat16>(uint32_t w)
+{
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <> __device__ __forceinline__ float2 unpack2<__half>(uint32_t w)
+{
+    return __half22float2(*reinterpret_cast<const __half2 *>(&w));
+}
+
+// Eight columns of a row of the result, rounded once.
+template <typename T>
+__device__ __forceinline__ void paged_store(const PagedParams &p, int b, int t, int h, int c, const float (&v)[8])
+{
+    if (c * 8 < p.head_dim)
+        *reinterpret_cast<uint4 *>(static_cast<T *>(p.o) + b * p.so.b + t * p.so.r + h * p.so.h + c * 8) =
+            make_uint4(XaElem<T>::pack(v[0], v[1]), XaElem<T>::pack(v[2], v[3]), XaElem<T>::pack(v[4], v[5]),
+                       XaElem<T>::pack(v[6], v[7]));
+}
+__device__ __forceinline__ void paged_store_lse(const PagedParams &p, int b, int t, int h, float lse)
+{
+    if (p.lse) p.lse[((long long)b * p.q_heads + h) * p.q_rows + t] = lse;
+}
+
+// Blocks blk0 .. blk1 - 1 of an item's keys for one key head and row tile.  Leaves each warp's sums, not yet
+// normalised, in its joining block: rows x DP, then the rows' maxima (of the scores), then the sums of
+// exponentials.  A row that has seen no state has maximum -inf and sum 0.
+template <int DP, int MT, typename T>
+__device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, const PagedItem &it, int b, int kvh, int rt,
+                                           int blk0, int blk1)
+{
+    using L = PagedSmem<DP, MT>;
+    constexpr int kChunks = DP / 8;                                // 16-byte pieces of a row
+    constexpr int kKeys = L::kKeys, kRowStep = 32 / kChunks;       // rows that a copy instruction covers
+    constexpr uint32_t kAll = kKeys == 32 ? 0xffffffffu : (1u << kKeys) - 1;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);     // row r: token r / group, query head r % group
+    const int seen_lo = paged_seen(it, rt * L::kRows / p.group);
+    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(it, p.group, L::kRows, rt), blk1 * L::kBlock);
+    const int ntiles = key_end > key0 ? (key_end - key0 + kKeys - 1) / kKeys : 0;
+    const int mine = ntiles > warp ? (ntiles - warp + kPaWarps - 1) / kPaWarps : 0;         // tiles warp, warp + 4, ...
+    const int first = key0 + warp * kKeys;                         // this warp's tile t begins at key first + t * kBlock
+
+    const T *kbase = static_cast<const T *>(p.k) + kvh * p.sk.head;
+    const T *vbase = static_cast<const T *>(p.v) + kvh * p.sv.head;
+    const uint32_t ring = smem_u32(smem) + warp * L::kWarp;
+    const bool same = p.sk.page == p.sv.page && p.sk.row == p.sv.row;
+
+    // this lane's row of the next tile: its page, and where in the page
+    int page = -1, in_page = 0;
+    auto look_up = [&](int t) {
+        page = -1;
+        const int pos = first + t * L::kBlock + (lane & (kKeys - 1));
+        if (t < mine && pos < key_end) {
+            const int col = (unsigned)pos / (unsigned)p.page_rows;
+            in_page = pos - col * p.page_rows;
+            page = it.row[col];
+        }
+    };
+    // one stage of K and of V; the pieces of a row go to neighbouring lanes, piece c of row r to position
+    // c ^ (r & 7) (conflict-free ldmatrix).  Returns which rows are there; the others become zeros.
+    const int lc = lane % kChunks, lr = lane / kChunks;
+    const bool lc_live = lc * 8 < p.head_dim;
+    auto load = [&](int t) -> uint32_t {
+        uint32_t mask = 0;
+        if (t < mine) {
+            const bool ok = (unsigned)page < (unsigned)p.pages;
+            mask = __ballot_sync(0xffffffffu, ok) & kAll;
+            const long long off_k = ok ? page * p.sk.page + in_page * p.sk.row : 0;
+            const long long off_v = ok && !same ? page * p.sv.page + in_page * p.sv.row : 0;
+            look_up(t + 1);
+            const uint32_t st = ring + (t % L::kStages) * 2 * L::kTile;
+#pragma unroll
+            for (int n = 0; n < kKeys / kRowStep; ++n) {
+                const int r = lr + n * kRowStep;
+                const uint32_t bytes = lc_live && (mask >> r & 1) ? 16 : 0;
+                const uint32_t dst = st + r * DP * 2 + ((lc ^ (r & 7)) << 4);
+                const long long ok_ = __shfl_sync(0xffffffffu, off_k, r);
+                const long long ov_ = same ? ok_ : __shfl_sync(0xffffffffu, off_v, r);
+                const int col = lc_live ? lc * 8 : 0;
+                cp_async_16_cg(dst, kbase + ok_ + col, bytes);
+                cp_async_16_cg(dst + L::kTile, vbase + ov_ + col, bytes);
+            }
+        }
+        cp_async_commit();
+        return mask;
+    };
+    look_up(0);
+    uint32_t there[L::kStages - 1];                                // of tiles t, t + 1
+#pragma unroll
+    for (int t = 0; t < L::kStages - 1; ++t) there[t] = load(t);
+
+    // Q as the A operand: rows g and g + 8 of 16, columns 2 q, 2 q + 1 and + 8 of every 16
+    const int g = lane >> 2, q4 = lane & 3;
+    uint32_t qa[MT == 1 ? DP / 16 : 1][4];
+    const uint32_t qs = smem_u32(smem) + L::kRing;
+    auto q_row = [&](int r) -> const T * {
+        const int row = rt * L::kRows + r, t = row / p.group, h = row - t * p.group;
+        return static_cast<const T *>(p.q) + b * p.sq.b + t * p.sq.r + (long long)(kvh * p.group + h) * p.sq.h;
+    };
+    if constexpr (MT == 1) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int r = g + 8 * half;
+            const T *src = r < rows ? q_row(r) : nullptr;
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+                for (int hi = 0; hi < 2; ++hi) {
+                    const int d = k * 16 + hi * 8 + q4 * 2;
+                    qa[k][half + 2 * hi] = (src && d < p.head_dim) ? *reinterpret_cast<const uint32_t *>(src + d) : 0u;
+                }
+        }
+    } else {
+        for (int i = tid; i < L::kRows * kChunks; i += kPaThreads) {
+            const int r = i / kChunks, c = i % kChunks;
+            uint4 w = make_uint4(0, 0, 0, 0);
+            if (r < rows && c * 8 < p.head_dim) w = *reinterpret_cast<const uint4 *>(q_row(r) + c * 8);
+            st_shared_v4_b32(qs + r * DP * 2 + ((c ^ (r & 7)) << 4), w.x, w.y, w.z, w.w);
+        }
+        __syncthreads();
+    }
+
+    int seen[MT][2];                                               // keys that a row sees lie below this
+    float m[MT][2], l[MT][2];
+    bool any[MT][2];
+    float o[MT][DP / 8][4];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int r = i * 16 + g + 8 * half;
+            seen[i][half] = r < rows ? paged_seen(it, (rt * L::kRows + r) / p.group) : 0x7fffffff;
+            m[i][half] = -INFINITY;
+            l[i][half] = 0.f;
+            any[i][half] = false;
+        }
+#pragma unroll
+        for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
+    }
+
+    for (int t = 0; t < mine; ++t) {
+        cp_async_wait_group<L::kStages - 2>();
+        __syncwarp();                                              // every lane's copies of stage t have landed
+        const uint32_t mask = there[0];
+#pragma unroll
+        for (int i = 0; i + 1 < L::kStages - 1; ++i) there[i] = there[i + 1];
+        there[L::kStages - 2] = load(t + L::kStages - 1);          // (its stage was read in round t - 1)
+        const uint32_t sk = ring + (t % L::kStages) * 2 * L::kTile, sv = sk + L::kTile;
+        constexpr int kN = kKeys / 8;                              // tiles of eight keys
+        float s[MT][kN][4] = {};
+        {
+            const int idx = lane >> 3, kr = (idx >> 1) * 8 + (lane & 7);
+#pragma unroll
+            for (int k = 0; k < DP / 16; ++k) {
+                uint32_t a[MT][4];
+                if constexpr (MT == 1) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a[0][e] = qa[k][e];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        const int r = i * 16 + (lane & 15), c = 2 * k + (lane >> 4);
+                        ldmatrix_x4(a[i], qs + r * DP * 2 + ((c ^ (r & 7)) << 4));
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < kN; n += 2) {
+                    uint32_t bf[4];
+                    ldmatrix_x4(bf, sk + (n * 8 + kr) * DP * 2 + (((2 * k + (idx & 1)) ^ (kr & 7)) << 4));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        mma_16x8x16<T>(s[i][n], a[i], bf[0], bf[1]);
+                        mma_16x8x16<T>(s[i][n + 1], a[i], bf[2], bf[3]);
+                    }
+                }
+            }
+        }
+        const int pos0 = first + t * L::kBlock;
+        const bool full = mask == kAll && pos0 + kKeys <= seen_lo;     // every row sees every key
+        if (!full) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int key = n * 8 + q4 * 2 + (e & 1);
+                        if (!(mask >> key & 1) || pos0 + key >= seen[i][e >> 1]) s[i][n][e] = -INFINITY;
+                    }
+        }
+        bool more = false;
+        float bm[MT][2];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float v = fmaxf(s[i][0][2 * half], s[i][0][2 * half + 1]);
+#pragma unroll
+                for (int n = 1; n < kN; ++n) v = fmaxf(v, fmaxf(s[i][n][2 * half], s[i][n][2 * half + 1]));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+                v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+                bm[i][half] = v;
+                more |= v > m[i][half];
+                any[i][half] |= full || (mask & low_bits(seen[i][half] - pos0)) != 0;
+            }
+        if (__any_sync(0xffffffffu, more)) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                float alpha[2];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const float nm = fmaxf(m[i][half], bm[i][half]);
+                    alpha[half] = nm == m[i][half] ? 1.f : xa_exp2((m[i][half] - nm) * p.scale_log2);
+                    m[i][half] = nm;
+                    l[i][half] *= alpha[half];
+                }
+#pragma unroll
+                for (int n = 0; n < DP / 8; ++n) {
+                    o[i][n][0] *= alpha[0];
+                    o[i][n][1] *= alpha[0];
+                    o[i][n][2] *= alpha[1];
+                    o[i][n][3] *= alpha[1];
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            // (a row that has seen nothing yet: all its scores are -inf, and so are their differences to 0)
+            const float neg[2] = {m[i][0] == -INFINITY ? 0.f : -m[i][0] * p.scale_log2,
+                                  m[i][1] == -INFINITY ? 0.f : -m[i][1] * p.scale_log2};
+#pragma unroll
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[i][n][e] = xa_exp2(fmaf(s[i][n][e], p.scale_log2, neg[e >> 1]));
+                    l[i][e >> 1] += s[i][n][e];
+                }
+        }
+        // Keys that some of the rows do not see: 0 x a value that is not finite would reach those rows through
+        // the product, so such a value's rows are added by hand and it becomes zero.
+        uint32_t partly = full ? 0u : mask & ~low_bits(seen_lo - pos0);
+        while (partly) {
+            const int j = __ffs(partly) - 1;
+            partly &= partly - 1;
+            const uint32_t row = sv + j * DP * 2;
+            const bool bad = lane < kChunks && any_not_finite<T>(ld_shared_v4(row + ((lane ^ (j & 7)) << 4)));
+            if (!__any_sync(0xffffffffu, bad)) continue;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    float w = 0.f;
+#pragma unroll
+                    for (int n = 0; n < kN; ++n)
+                        w = select(n == j >> 3, select(j & 1, s[i][n][2 * half + 1], s[i][n][2 * half]), w);
+                    w = __shfl_sync(0xffffffffu, w, (lane & ~3) | ((j & 7) >> 1));
+                    if (pos0 + j < seen[i][half]) {
+#pragma unroll
+                        for (int n = 0; n < DP / 8; ++n) {
+                            const float2 f = unpack2<T>(ld_shared_u32(row + ((n ^ (j & 7)) << 4) + q4 * 4));
+                            o[i][n][2 * half] = fmaf(w, f.x, o[i][n][2 * half]);
+                            o[i][n][2 * half + 1] = fmaf(w, f.y, o[i][n][2 * half + 1]);
+                        }
+                    }
+                }
+            __syncwarp();
+            if (lane < kChunks) st_shared_v4_b32(row + (lane << 4), 0, 0, 0, 0);
+            __syncwarp();
+        }
+        {
+            const int idx = lane >> 3, kr = (idx & 1) * 8 + (lane & 7);
+#pragma unroll
+            for (int h = 0; h < kN; h += 2) {
+                uint32_t pa[MT][4];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    pa[i][0] = XaElem<T>::pack(s[i][h][0], s[i][h][1]);
+                    pa[i][1] = XaElem<T>::pack(s[i][h][2], s[i][h][3]);
+                    pa[i][2] = XaElem<T>::pack(s[i][h + 1][0], s[i][h + 1][1]);
+                    pa[i][3] = XaElem<T>::pack(s[i][h + 1][2], s[i][h + 1][3]);
+                }
+#pragma unroll
+                for (int n = 0; n < DP / 16; ++n) {
+                    uint32_t bf[4];
+                    ldmatrix_x4_trans(bf, sv + (h * 8 + kr) * DP * 2 + (((2 * n + (idx >> 1)) ^ (kr & 7)) << 4));
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        mma_16x8x16<T>(o[i][2 * n], pa[i], bf[0], bf[1]);
+                        mma_16x8x16<T>(o[i][2 * n + 1], pa[i], bf[2], bf[3]);
+                    }
+                }
+            }
+        }
+        __syncwarp();                                              // stage t has been read by every lane
+    }
+    cp_async_wait_group<0>();
+    __syncthreads();                                               // the rings are free
+    float *jo = reinterpret_cast<float *>(smem) + warp * (L::kJoinWarp / 4);
+    float *jm = jo + L::kRows * L::kPitch, *jl = jm + L::kRows;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+        for (int n = 0; n < DP / 8; ++n) {
+            *reinterpret_cast<float2 *>(jo + (i * 16 + g) * L::kPitch + n * 8 + q4 * 2) = make_float2(o[i][n][0], o[i][n][1]);
+            *reinterpret_cast<float2 *>(jo + (i * 16 + g + 8) * L::kPitch + n * 8 + q4 * 2) = make_float2(o[i][n][2], o[i][n][3]);
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            l[i][half] += __shfl_xor_sync(0xffffffffu, l[i][half], 1);
+            l[i][half] += __shfl_xor_sync(0xffffffffu, l[i][half], 2);
+            // scores of -inf alone are not the same as no scores
+            if (any[i][half] && m[i][half] == -INFINITY) l[i][half] = __int_as_float(0x7fc00000);
+            if (q4 == 0) {
+                jm[i * 16 + g + 8 * half] = m[i][half];
+                jl[i * 16 + g + 8 * half] = l[i][half];
+            }
+        }
+    }
+    __syncthreads();
+}
+
+// Eight columns (c) of row r: the four warps' sums, weighted to the common maximum, normalised; returns lse
+// (-inf: no states, and zeros).
+template <int DP, int MT>
+__device__ __forceinline__ float paged_join_warps(const PagedParams &p, const uint8_t *smem, int r, int c, float (&acc)[8])
+{
+    using L = PagedSmem<DP, MT>;
+    const float *base = reinterpret_cast<const float *>(smem);
+    constexpr int kStep = L::kJoinWarp / 4;
+    float wm[kPaWarps], wl[kPaWarps], mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPaWarps; ++w) {
+        wm[w] = base[w * kStep + L::kRows * L::kPitch + r];
+        wl[w] = base[w * kStep + L::kRows * L::kPitch + L::kRows + r];
+        mx = fmaxf(mx, wm[w]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPaWarps; ++w) {
+        if (wl[w] == 0.f) continue;                                // a warp without keys
+        const float a = xa_exp2((wm[w] - mx) * p.scale_log2);
+        sum = fmaf(a, wl[w], sum);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = fmaf(a, base[w * kStep + r * L::kPitch + c * 8 + e], acc[e]);
+    }
+    if (sum == 0.f) return -INFINITY;
+    const float inv = 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= inv;
+    return fmaf(mx, p.scale, logf(sum));
+}
+
+template <int DP, int MT, typename T>
+__global__ void __launch_bounds__(kPaThreads, 2)
+paged_attn_kernel(const PagedParams p)
+{
+    using L = PagedSmem<DP, MT>;
+    constexpr int kChunks = DP / 8;
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    PagedItem it;
+    int b = 0, kvh = 0, rt = 0, blk0 = 0, blk1 = 0, blocks = 0;
+    long long pos = 0, end = 0, rem = 0, per = 0;
+    auto item_blocks = [&](const PagedItem &x) {
+        long long n = 0;
+        for (int r = 0; r < p.row_tiles; ++r) n += paged_blocks(x, p.group, L::kRows, r, L::kBlock);
+        return n * p.kv_heads;
+    };
+    const int cta = blockIdx.x, rank = p.cluster ? cta % p.cluster : 0;
+    if (p.cluster) {
+        int x = cta / p.cluster;
+        rt = x % p.row_tiles;
+        x /= p.row_tiles;
+        kvh = x % p.kv_heads;
+        b = x / p.kv_heads;
+        it = paged_item(p, b);
+        blocks = paged_blocks(it, p.group, L::kRows, rt, L::kBlock);
+        if (blocks == 0) return;                                   // (the whole cluster)
+        blk0 = (int)((long long)blocks * rank / p.cluster);
+        blk1 = (int)((long long)blocks * (rank + 1) / p.cluster);
+    } else {
+        // Equal shares.  Items in order, in each the key heads, in each the row tiles, in each the blocks of keys: how
+        // many blocks there are in all, and which item this CTA's first one lies in (thread t counts `each` items).
+        __shared__ long long warp_sum[kPaWarps], s_rem;
+        __shared__ int s_item;
+        const int each = (p.batch + kPaThreads - 1) / kPaThreads;
+        long long sum = 0;
+        for (int i = 0; i < each; ++i)
+            if (tid * each + i < p.batch) sum += item_blocks(paged_item(p, tid * each + i));
+        long long upto = sum;                                      // blocks of all threads up to this one
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const long long v = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += v;
+        }
+        if (lane == 31) warp_sum[warp] = upto;
+        __syncthreads();
+        long long total = 0;
+#pragma unroll
+        for (int w = 0; w < kPaWarps; ++w) {
+            if (w < warp) upto += warp_sum[w];
+            total += warp_sum[w];
+        }
+        per = max((total + gridDim.x - 1) / gridDim.x, 1LL);
+        pos = cta * per;
+        end = min(total, pos + per);
+        if (tid == 0) p.desc[cta * kPaDesc] = 0;
+        if (pos >= end) return;
+        if (pos >= upto - sum && pos < upto) {
+            long long left = pos - (upto - sum);
+            int x = tid * each;
+            for (;; ++x) {
+                const long long n = item_blocks(paged_item(p, x));
+                if (left < n) break;
+                left -= n;
+            }
+            s_item = x;
+            s_rem = left;
+        }
+        __syncthreads();
+        b = s_item;
+        rem = s_rem;
+    }
+
+    for (;;) {
+        if (!p.cluster) {
+            long long all;
+            for (;; ++b) {
+                it = paged_item(p, b);
+                all = item_blocks(it);
+                if (rem < all) break;
+                rem -= all;
+            }
+            const long long head = all / p.kv_heads;
+            kvh = (int)(rem / head);
+            blk0 = (int)(rem - kvh * head);
+            for (rt = 0; blk0 >= (blocks = paged_blocks(it, p.group, L::kRows, rt, L::kBlock)); ++rt) blk0 -= blocks;
+            blk1 = (int)min((long long)blocks, blk0 + (end - pos));
+        }
+        paged_walk<DP, MT, T>(p, smem, it, b, kvh, rt, blk0, blk1);
+        // whole results leave at once, parts go to the cluster's or the call's scratch
+        const bool whole = blk0 == 0 && blk1 == blocks && p.cluster <= 1;
+        const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
+        float *slot = p.cluster ? reinterpret_cast<float *>(smem + L::kShare) : p.part + (2LL * cta + (blk0 == 0)) * L::kSlot;
+        for (int i = tid; i < rows * kChunks; i += kPaThreads) {
+            const int r = i / kChunks, c = i % kChunks;
+            float acc[8];
+            const float lse = paged_join_warps<DP, MT>(p, smem, r, c, acc);
+            if (whole) {
+                const int row = rt * L::kRows + r, t = row / p.group, h = kvh * p.group + row - t * p.group;
+                paged_store<T>(p, b, t, h, c, acc);
+                if (c == 0) paged_store_lse(p, b, t, h, lse);
+            } else {
+                float4 *dst = reinterpret_cast<float4 *>(slot + r * DP + c * 8);
+                dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+                dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+                if (c == 0) slot[L::kRows * DP + r] = lse;
+            }
+        }
+        if (p.cluster) break;
+        if (tid == 0 && blk0 == 0 && !whole) {                     // the first of the parts: how many CTAs share it
+            int *d = p.desc + cta * kPaDesc;
+            d[0] = (int)((pos + blocks - 1) / per) - cta + 1;
+            d[1] = b;
+            d[2] = kvh;
+            d[3] = rt;
+        }
+        pos += blk1 - blk0;
+        rem += blk1 - blk0;
+        if (pos >= end) return;
+        __syncthreads();                                           // the joining blocks have been read
+    }
+    if (p.cluster == 1) return;
+
+    // the cluster's CTAs each write a share of the rows' pieces, from all of their results
+    cluster_sync_all();
+    const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
+    const uint32_t at = smem_u32(smem) + L::kShare;
+    for (int i = rank * kPaThreads + tid; i < rows * kChunks; i += p.cluster * kPaThreads) {
+        const int r = i / kChunks, c = i % kChunks;
+        float part[kPaCluster], mx = -INFINITY, sum = 0.f, acc[8] = {};
+#pragma unroll
+        for (int s = 0; s < kPaCluster; ++s) {
+            part[s] = s < p.cluster ? cluster_ld(cluster_map(at + (L::kRows * DP + r) * 4, s)) : -INFINITY;
+            mx = fmaxf(mx, part[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < kPaCluster; ++s) {
+            if (part[s] == -INFINITY) continue;                    // no keys there (a NaN goes on)
+            const float w = expf(part[s] - mx);
+            sum += w;
+            const uint32_t src = cluster_map(at + (r * DP + c * 8) * 4, s);
+            const float4 a = cluster_ld4(src), b4 = cluster_ld4(src + 16);
+            acc[0] = fmaf(w, a.x, acc[0]); acc[1] = fmaf(w, a.y, acc[1]); acc[2] = fmaf(w, a.z, acc[2]); acc[3] = fmaf(w, a.w, acc[3]);
+            acc[4] = fmaf(w, b4.x, acc[4]); acc[5] = fmaf(w, b4.y, acc[5]); acc[6] = fmaf(w, b4.z, acc[6]); acc[7] = fmaf(w, b4.w, acc[7]);
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] *= inv;
+        const int row = rt * L::kRows + r, t = row / p.group, h = kvh * p.group + row - t * p.group;
+        paged_store<T>(p, b, t, h, c, acc);
+        if (c == 0) paged_store_lse(p, b, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
+    }
+    cluster_sync_all();                                            // nobody's shared memory goes while it is read
+}
+
+// The parts of an item's key head and row tile that several CTAs worked on, added up in order: the first lies in slot 1 of
+// the CTA that it began in, the others in slot 0 of those after it.  blockIdx.x: that CTA; blockIdx.y: four rows.
+template <int DP, int MT, typename T>
+__global__ void __launch_bounds__(128)
+paged_join_kernel(const PagedParams p)
+{
+    using L = PagedSmem<DP, MT>;
+    constexpr int kChunks = DP / 8;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int cta = blockIdx.x;
+    const int4 d = *reinterpret_cast<const int4 *>(p.desc + cta * kPaDesc);
+    if (d.x == 0) return;
+    const int news = paged_item(p, d.y).news;
+    const int r = blockIdx.y * (128 / kChunks) + threadIdx.x / kChunks, c = threadIdx.x % kChunks;
+    const int row = d.w * L::kRows + r;
+    if (r >= L::kRows || row >= news * p.group) return;
+    const float *first = p.part + (2LL * cta + 1) * L::kSlot, *next = p.part + 2LL * (cta + 1) * L::kSlot;
+    float mx = -INFINITY, sum = 0.f, acc[8] = {};
+    for (int s0 = 0; s0 < d.x; s0 += 8) {
+        float lse[8], top = mx;
+        float4 v[8][2];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const float *src = s0 + s == 0 ? first : next + 2LL * (s0 + s - 1) * L::kSlot;
+            const bool live = s0 + s < d.x;
+            lse[s] = live ? src[L::kRows * DP + r] : -INFINITY;
+            if (live) {
+                v[s][0] = *reinterpret_cast<const float4 *>(src + r * DP + c * 8);
+                v[s][1] = *reinterpret_cast<const float4 *>(src + r * DP + c * 8 + 4);
+            }
+            top = fmaxf(top, lse[s]);
+        }
+        if (top > mx) {
+            const float f = expf(mx - top);                        // (0 at the first; a NaN stays one)
+            sum *= f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] *= f;
+            mx = top;
+        }
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            if (lse[s] == -INFINITY) continue;                     // no states there (a NaN goes on)
+            const float w = expf(lse[s] - mx);
+            sum += w;
+            acc[0] = fmaf(w, v[s][0].x, acc[0]); acc[1] = fmaf(w, v[s][0].y, acc[1]);
+            acc[2] = fmaf(w, v[s][0].z, acc[2]); acc[3] = fmaf(w, v[s][0].w, acc[3]);
+            acc[4] = fmaf(w, v[s][1].x, acc[4]); acc[5] = fmaf(w, v[s][1].y, acc[5]);
+            acc[6] = fmaf(w, v[s][1].z, acc[6]); acc[7] = fmaf(w, v[s][1].w, acc[7]);
+        }
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= inv;
+    const int t = row / p.group, h = d.z * p.group + row - t * p.group;
+    paged_store<T>(p, d.y, t, h, c, acc);
+    if (c == 0) paged_store_lse(p, d.y, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
+}
+
+// ------------------------------------------------------------------ append --
+struct AppendParams {
+    const uint4 *k_new, *v_new;                // in pieces of 16 bytes, as are the strides
+    uint4 *k, *v;
+    const int *table, *lens, *slot_of, *new_lens;
+    XaStrides skn, svn;
+    PagedStrides sk, sv;
+    long long table_stride, total;             // pieces of the new keys
+    int q_rows, kv_heads, chunks, pages, page_rows, slots, cap;
+};
+
+// A thread moves one 16-byte piece of a key and of a value.
+__global__ void __launch_bounds__(256)
+cache_append_kernel(const AppendParams p)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < p.total; i += gridDim.x * 256LL) {
+        const unsigned c = (unsigned)(i % p.chunks);
+        const long long rest = i / p.chunks, token = rest / p.kv_heads;
+        const unsigned h = (unsigned)(rest - token * p.kv_heads);
+        const int b = (int)(token / p.q_rows), t = (int)(token - (long long)b * p.q_rows);
+        const uint4 key = p.k_new[b * p.skn.b + t * p.skn.r + h * p.skn.h + c];
+        const uint4 value = p.v_new[b * p.svn.b + t * p.svn.r + h * p.svn.h + c];
+        const PagedItem it = paged_item(p.table, p.table_stride, p.lens, p.slot_of, p.new_lens, b, p.slots, p.cap, p.q_rows);
+        const int pos = it.len - it.news + t;
+        if (t >= it.news || pos < 0) continue;
+        const int col = (unsigned)pos / (unsigned)p.page_rows;
+        const int page = it.row[col], in_page = pos - col * p.page_rows;
+        if ((unsigned)page >= (unsigned)p.pages) continue;
+        p.k[page * p.sk.page + in_page * p.sk.row + h * p.sk.head + c] = key;
+        p.v[page * p.sv.page + in_page * p.sv.row + h * p.sv.head + c] = value;
+    }
+}
+
+}  // namespace cudallm
