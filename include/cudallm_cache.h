@@ -142,15 +142,14 @@ int cudallm_pages_copy(const cudallm_page_pool *pools, int64_t count, int64_t pa
  *   lens  : int32, `slots` elements: states of the sequence in each slot, 0 for none
  *   table : int32, slots rows of table_cols page numbers, pitch table_stride; a sequence
  *           holds the first ceil(lens / page_rows) entries of its row, the others mean nothing
- *   turn  : int32, one word that the calls use among themselves: 0 at the start, 0 after every call
- * A new book is all zeros.  The book is the caller's: it can be copied and put back as a whole (all four
+ * A new book is all zeros.  The book is the caller's: it can be copied and put back as a whole (all three
  * arrays), and lens and table go into the calls above as they are.  Calls that change
  * one book must not overlap.  A book that contradicts itself gives wrong page
  * numbers, never an access outside the arrays; page numbers outside 0..pages-1 are passed over,
  * lengths outside 0..table_cols * page_rows taken as the nearer end.
  */
 typedef struct cudallm_page_book {
-    int32_t *refs, *lens, *table, *turn;
+    int32_t *refs, *lens, *table;
     int64_t pages, page_rows, slots, table_cols, table_stride;
 } cudallm_page_book;
 
@@ -161,7 +160,7 @@ typedef struct cudallm_page_book {
  * given back.  Entries with a slot outside 0..slots-1 are passed over; of several with the same
  * dst the first counts; dst == src changes nothing.
  *   src, dst : int32, n elements on the device
- * Errors: INVALID_POINTER, INVALID_DIM (also pages > 2^20, n > 65536, table_cols * page_rows > 2^31 - 1024),
+ * Errors: INVALID_POINTER, INVALID_DIM (also pages > 2^20, n > 16384, table_cols * page_rows > 2^31 - 1024),
  * INVALID_LD (table_stride < table_cols), MISALIGNED, WORKSPACE, UNSUPPORTED_DEVICE, CUDA.
  */
 int cudallm_pages_fork(const cudallm_page_book *book, const int32_t *src, const int32_t *dst, int64_t n,

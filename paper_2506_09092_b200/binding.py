@@ -128,7 +128,7 @@ class PagedShape(ctypes.Structure):
 
     def layouts(self):
         """What tensors of q, o, k_new, v_new, k, v and the table have to be, as the fields say: (strides, sizes, type, extent in
-        elements) of each, by name; then the least number of elements of lens, slot_of, new_lens and lse.  Worked out anew whenever
+        elements) of each, by name; then the least number of elements of lens, of slot_of and new_lens, and of lse.  Worked out anew whenever
         a field has changed."""
         raw = bytes(self)
         kept = getattr(self, "_kept", None)
@@ -147,7 +147,7 @@ class PagedShape(ctypes.Structure):
                 strides = (*st, 1)
                 extent = 0 if 0 in size else 1 + sum((n - 1) * d for n, d in zip(size, strides))
                 out[name] = (strides, torch.Size(size) if min(size) >= 0 else size, t, extent)
-            out["counts"] = (self.slots, self.batch, self.batch, self.batch * self.q_heads * self.q_rows)
+            out["counts"] = (self.slots, self.batch, self.batch * self.q_heads * self.q_rows)
             kept = self._kept = (raw, out)
         return kept[1]
 
@@ -159,7 +159,7 @@ class CPagePool(ctypes.Structure):
 
 class CPageBook(ctypes.Structure):
     """``cudallm_page_book`` of include/cudallm_cache.h."""
-    _fields_ = [(n, _vp) for n in ("refs", "lens", "table", "turn")] + [
+    _fields_ = [(n, _vp) for n in ("refs", "lens", "table")] + [
         (n, _i64) for n in ("pages", "page_rows", "slots", "table_cols", "table_stride")]
 
 
@@ -510,33 +510,42 @@ def xattn_bwd(shape, q, k, v, kv_lens, o, lse, d_o, dq, dk, dv, scratch, scratch
     return _check(st, "cudallm_xattn_bwd", check)
 
 
-def _paged_operands(shape, lens, slot_of, new_lens, lse=None, **tensors):
-    """Refuses tensors that do not hold the operands as a PagedShape says; addresses are taken as they are."""
-    if not isinstance(shape, PagedShape):
-        return
-    at = shape.layouts()
-    for name, t in tensors.items():
+_INT32 = _FLOAT32 = None
+
+
+def _vectors(*checked):
+    """Refuses vectors of another type than int32 (or, for u and lse, fp32), or shorter than their number of elements, or
+    with gaps.  Names, tensors and numbers; addresses and None are taken as they are."""
+    global _INT32, _FLOAT32
+    if _INT32 is None:
+        import torch
+        _INT32, _FLOAT32 = torch.int32, torch.float32
+    for name, t, n in checked:
+        if t is not None and t.__class__ is not int:
+            want = _FLOAT32 if name == "lse" or name == "u" else _INT32
+            if t.dtype is not want:
+                raise TypeError(f"{name} has to be {want}, not {t.dtype}")
+            if t.numel() < n or not t.is_contiguous():
+                raise ValueError(f"{name}: {n} contiguous elements are needed")
+
+
+def _tensors(at, *checked):
+    """Refuses tensors that do not hold the operands as a PagedShape says (``at``: its layouts)."""
+    for name, t in checked:
         if t is not None and t.__class__ is not int:
             want = at[name]
             if not (t.stride() == want[0] and t.shape == want[1] and t.dtype is want[2]):
                 _check_layout(name, t, *want)
-    for (name, t, dtype), n in zip((("lens", lens, "torch.int32"), ("slot_of", slot_of, "torch.int32"),
-                                    ("new_lens", new_lens, "torch.int32"), ("lse", lse, "torch.float32")), at["counts"]):
-        _check_vector(name, t, dtype, n)
-
-
-def _check_vector(name, t, dtype, n):
-    if t is not None and t.__class__ is not int:
-        if str(t.dtype) != dtype:
-            raise TypeError(f"{name} has to be {dtype}, not {t.dtype}")
-        if t.numel() < n or not t.is_contiguous():
-            raise ValueError(f"{name}: {n} contiguous elements are needed")
 
 
 def cache_append(shape, k_new, v_new, k, v, table, lens, slot_of=None, new_lens=None, stream=None, check=True):
     """Keys and values of the new tokens into the pages (``shape``: a PagedShape); slot_of and new_lens may be None.
     Tensors must be laid out as the shape says; addresses are not looked at."""
-    _paged_operands(shape, lens, slot_of, new_lens, k_new=k_new, v_new=v_new, k=k, v=v, table=table)
+    if isinstance(shape, PagedShape):
+        at = shape.layouts()
+        _tensors(at, ("k_new", k_new), ("v_new", v_new), ("k", k), ("v", v), ("table", table))
+        n = at["counts"]
+        _vectors(("lens", lens, n[0]), ("slot_of", slot_of, n[1]), ("new_lens", new_lens, n[1]))
     st = lib().cudallm_cache_append(shape, *_d(k_new, v_new, k, v, table, lens, slot_of, new_lens), _s(stream))
     return _check(st, "cudallm_cache_append", check)
 
@@ -548,7 +557,11 @@ def paged_attn_scratch_bytes(shape) -> int:
 def paged_attn(shape, q, k, v, table, lens, slot_of, new_lens, o, lse, scratch, scratch_bytes, stream=None, check=True):
     """Attention of the new tokens over their sequence's pages; slot_of, new_lens, lse and scratch may be None.
     Tensors are checked as in ``cache_append``."""
-    _paged_operands(shape, lens, slot_of, new_lens, lse, q=q, k=k, v=v, table=table, o=o)
+    if isinstance(shape, PagedShape):
+        at = shape.layouts()
+        _tensors(at, ("q", q), ("k", k), ("v", v), ("table", table), ("o", o))
+        n = at["counts"]
+        _vectors(("lens", lens, n[0]), ("slot_of", slot_of, n[1]), ("new_lens", new_lens, n[1]), ("lse", lse, n[2]))
     st = lib().cudallm_paged_attn(shape, *_d(q, k, v, table, lens, slot_of, new_lens, o, lse, scratch), scratch_bytes,
                                   _s(stream))
     return _check(st, "cudallm_paged_attn", check)
@@ -594,16 +607,16 @@ class PageBook:
     def __init__(self, pages, page_rows, slots, table_cols, device="cuda"):
         import torch
         up = lambda n: (n + 3) // 4 * 4
-        at = [0, 4]
+        at = [0]
         for n in (pages, slots, slots * table_cols):
             at.append(at[-1] + up(n))
         self.data = torch.zeros(at[-1], dtype=torch.int32, device=device)
         self.page_rows = page_rows
-        self.refs, self.lens = self.data[at[1]:at[1] + pages], self.data[at[2]:at[2] + slots]
-        self.table = self.data[at[3]:at[3] + slots * table_cols].view(slots, table_cols)
+        self.refs, self.lens = self.data[:pages], self.data[at[1]:at[1] + slots]
+        self.table = self.data[at[2]:at[2] + slots * table_cols].view(slots, table_cols)
         self.c = CPageBook(pages=pages, page_rows=page_rows, slots=slots, table_cols=table_cols, table_stride=table_cols)
         base = self.data.data_ptr()
-        self.c.turn, self.c.refs, self.c.lens, self.c.table = (base + 4 * i for i in at[:4])
+        self.c.refs, self.c.lens, self.c.table = (base + 4 * i for i in at[:3])
 
     def _here(self):
         _d(self.data)
@@ -622,8 +635,7 @@ def _pools_of(book, pools):
 
 def pages_copy(pools, src, dst, n, stream=None, check=True):
     """Page src[i] to page dst[i] in every pool, i < n (int32 on the device)."""
-    _check_vector("src", src, "torch.int32", n)
-    _check_vector("dst", dst, "torch.int32", n)
+    _vectors(("src", src, n), ("dst", dst, n))
     st = lib().cudallm_pages_copy(pools.array, pools.count, pools.pages, *_d(src, dst), n, _s(stream))
     return _check(st, "cudallm_pages_copy", check)
 
@@ -634,8 +646,7 @@ def pages_fork_scratch_bytes(book, n) -> int:
 
 def pages_fork(book, src, dst, n, scratch, scratch_bytes, stream=None, check=True):
     """The sequence in slot dst[i] becomes what the one in src[i] was, sharing its pages, i < n (int32 on the device)."""
-    _check_vector("src", src, "torch.int32", n)
-    _check_vector("dst", dst, "torch.int32", n)
+    _vectors(("src", src, n), ("dst", dst, n))
     st = lib().cudallm_pages_fork(book._here(), *_d(src, dst), n, *_d(scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_pages_fork", check)
 
@@ -648,9 +659,7 @@ def pages_resize(book, pools, slot_of, new_lens, n, result, scratch, scratch_byt
     """The sequence in slot slot_of[i] gets the length new_lens[i], i < n (int32 on the device); pages are taken or given back,
     shared last pages copied in ``pools`` (may be None: a book without data).  slot_of may be None: slots 0..n-1.
     result[0] (int32 on the device, or None): 0, or why nothing was done."""
-    _check_vector("slot_of", slot_of, "torch.int32", n)
-    _check_vector("new_lens", new_lens, "torch.int32", n)
-    _check_vector("result", result, "torch.int32", 1)
+    _vectors(("slot_of", slot_of, n), ("new_lens", new_lens, n), ("result", result, 1))
     array, count = _pools_of(book, pools)
     st = lib().cudallm_pages_resize(book._here(), array, count, *_d(slot_of, new_lens), n, *_d(result, scratch), scratch_bytes,
                                     _s(stream))
@@ -664,28 +673,38 @@ def pages_compact_scratch_bytes(book) -> int:
 def pages_compact(book, pools, used, scratch, scratch_bytes, stream=None, check=True):
     """The pages in use move down to the lowest numbers, in ``pools`` (may be None) and the book; used[0] (int32 on the device,
     or None): how many there are."""
-    _check_vector("used", used, "torch.int32", 1)
+    _vectors(("used", used, 1))
     array, count = _pools_of(book, pools)
     st = lib().cudallm_pages_compact(book._here(), array, count, *_d(used, scratch), scratch_bytes, _s(stream))
     return _check(st, "cudallm_pages_compact", check)
+
+
+_PROBABILITIES = {}
+
+
+def _probabilities(t, dtype):
+    """Whether t has the type of the code (codes that the C call refuses are let through)."""
+    if not _PROBABILITIES:
+        import torch
+        _PROBABILITIES.update({F32: torch.float32, BF16: torch.bfloat16, F16: torch.float16})
+    return _PROBABILITIES.get(dtype, t.dtype) is t.dtype
 
 
 def draft_verify(p, q, drafts, draft_lens, u, tokens, accepted, batch, n, vocab, ldp, ldq, dtype, stream=None, check=True):
     """Drafted tokens against the target's probabilities p (batch * (n + 1) rows) and the draft's q (batch * n rows, or
     None: the drafts were certain), by the random numbers u: tokens (batch, n + 1) and accepted (batch) are written."""
     rows = batch * (n + 1)
-    for name, t, want, count in (("drafts", drafts, "torch.int32", batch * n), ("draft_lens", draft_lens, "torch.int32", batch),
-                                 ("u", u, "torch.float32", rows), ("tokens", tokens, "torch.int32", rows),
-                                 ("accepted", accepted, "torch.int32", batch)):
-        _check_vector(name, t, want, count)
-    want = {F32: "torch.float32", BF16: "torch.bfloat16", F16: "torch.float16"}.get(dtype)
+    _vectors(("drafts", drafts, batch * n), ("draft_lens", draft_lens, batch), ("u", u, rows), ("tokens", tokens, rows),
+             ("accepted", accepted, batch))
     for name, t, r, ld in (("p", p, rows, ldp), ("q", q, batch * n, ldq)):
-        if t is not None and t.__class__ is not int and want is not None:
-            if str(t.dtype) != want:
-                raise TypeError(f"{name} has to be {want}, not {t.dtype}")
+        if t is not None and t.__class__ is not int:
+            if (t.is_contiguous() and t.numel() >= r * ld or r <= 0) and _probabilities(t, dtype):
+                continue
+            if not _probabilities(t, dtype):
+                raise TypeError(f"{name} has to be of the type that dtype says, not {t.dtype}")
             if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
                 raise ValueError(f"{name}: the last dimension must be contiguous")
-            if r > 0 and (1 + sum((s - 1) * d for s, d in zip(t.shape, t.stride())) if t.numel() else 0) < (r - 1) * ld + vocab:
+            if (1 + sum((s - 1) * d for s, d in zip(t.shape, t.stride())) if t.numel() else 0) < (r - 1) * ld + vocab:
                 raise ValueError(f"{name}: {tuple(t.shape)} ends before {r} rows of pitch {ld} do")
     st = lib().cudallm_draft_verify(*_d(p, q, drafts, draft_lens, u, tokens, accepted), batch, n, vocab, ldp, ldq, dtype,
                                     _s(stream))

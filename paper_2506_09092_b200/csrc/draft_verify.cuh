@@ -44,10 +44,10 @@ __device__ __forceinline__ double cluster_ld_f64(uint32_t addr)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads)
+__global__ void __launch_bounds__(kVerifyThreads, 4)
 draft_verify_kernel(const VerifyParams p)
 {
-    __shared__ double sums[kVerifyChunks], cta_sum;
+    __shared__ double masses[kVerifyChunks], sums[kVerifyChunks], cta_sum;     // of each chunk; up to and with each; of all
     __shared__ int s_accepted;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = blockIdx.x % p.cluster, b = blockIdx.x / p.cluster;
@@ -85,19 +85,39 @@ draft_verify_kernel(const VerifyParams p)
     // what is drawn from: max(p_a - q_a, 0) while drafts are left, q_a being a row or 1 at `certain`; else p_a
     const T *prow = pp + a * p.ldp, *qrow = a < m && qq ? qq + a * p.ldq : nullptr;
     int certain = a < m && !qq ? drafts[a] : -1;
-    auto mass = [&](T pv, T qv, long long v) {
-        const double r = elem_to_double(pv) - (v == certain ? 1.0 : elem_to_double(qv));
-        return r > 0.0 && r < (double)INFINITY ? r : 0.0;
+    // (compared in 32 bits, where p > q says exactly that p - q > 0; only then subtracted)
+    auto mass = [&](T pv, T qv) {
+        const float x = elem_to_float(pv), y = elem_to_float(qv);
+        return x > y && x < INFINITY && y > -INFINITY ? (double)x - (double)y : 0.0;
     };
-    // 16 x 32 elements from `from` on, element i * 32 + lane in register i
-    const T zero = elem_from_float<T>(0.f);
-    auto load = [&](long long from, T (&pv)[16], T (&qv)[16]) {
+    const T zero = elem_from_float<T>(0.f), one = elem_from_float<T>(1.f);
+    // element v of the row, v anywhere
+    auto mass_at = [&](long long v) {
+        return v < p.vocab ? mass(prow[v], v == certain ? one : qrow ? qrow[v] : zero) : 0.0;
+    };
+    // this lane's sum over 512 elements from `from` on
+    auto sum_of = [&](long long from) {
+        double s[4] = {};
+        if (from + kVerifyChunk <= p.vocab && !(certain >= from && certain < from + kVerifyChunk)) {
+            T pv[16], qv[16];
+            const T *ps = prow + from + lane;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const long long v = from + i * 32 + lane;
-            pv[i] = v < p.vocab ? prow[v] : zero;
-            qv[i] = qrow && v < p.vocab ? qrow[v] : zero;
+            for (int i = 0; i < 16; ++i) pv[i] = ps[i * 32];
+            if (qrow) {
+                const T *qs = qrow + from + lane;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) qv[i] = qs[i * 32];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) qv[i] = zero;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i % 4] += mass(pv[i], qv[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i % 4] += mass_at(from + i * 32 + lane);
         }
+        return (s[0] + s[1]) + (s[2] + s[3]);
     };
 
     const double draw = (double)u[p.n];
@@ -106,22 +126,16 @@ draft_verify_kernel(const VerifyParams p)
     for (int pass = 0;; ++pass) {
         for (int c = warp; c < p.chunks; c += kVerifyWarps) {
             double s = 0.0;
-            for (int part = 0; part < p.chunk; part += kVerifyChunk) {
-                const long long from = ((long long)rank * p.chunks + c) * p.chunk + part;
-                T pv[16], qv[16];
-                load(from, pv, qv);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s += mass(pv[i], qv[i], from + i * 32 + lane);
-            }
+            for (int part = 0; part < p.chunk; part += kVerifyChunk) s += sum_of(((long long)rank * p.chunks + c) * p.chunk + part);
 #pragma unroll
             for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
-            if (lane == 0) sums[c] = s;
+            if (lane == 0) masses[c] = s;
         }
         __syncthreads();
-        if (warp == 0) {                                           // chunks' sums become sums up to and with each
+        if (warp == 0) {
             double upto = 0.0;
             for (int c0 = 0; c0 < p.chunks; c0 += 32) {
-                double s = c0 + lane < p.chunks ? sums[c0 + lane] : 0.0;
+                double s = c0 + lane < p.chunks ? masses[c0 + lane] : 0.0;
 #pragma unroll
                 for (int d = 1; d < 32; d *= 2) {
                     const double x = __shfl_up_sync(0xffffffffu, s, d);
@@ -168,46 +182,58 @@ draft_verify_kernel(const VerifyParams p)
             if (t != a || owner < 0) out[t] = t < a ? drafts[t] : -1;
         if (tid == 0) p.accepted[b] = a;
     }
-    if (rank != owner) return;
+    if (rank != owner || warp != 0) return;
     // the chunk that holds the point, or the last one with mass
-    __shared__ int s_hit, s_last;
-    if (tid == 0) {
-        s_hit = p.chunks;
-        s_last = 0;
+    int hit = -1, last = 0;
+    for (int c0 = 0; c0 < p.chunks && hit < 0; c0 += 32) {
+        const int c = c0 + lane;
+        const bool some = c < p.chunks && masses[c] > 0.0;
+        const uint32_t there = __ballot_sync(0xffffffffu, some), over = __ballot_sync(0xffffffffu, some && before + sums[c] > point);
+        if (there) last = c0 + 31 - __clz(there);
+        if (over) hit = c0 + __ffs(over) - 1;
     }
-    __syncthreads();
-    for (int c = tid; c < p.chunks; c += kVerifyThreads) {
-        const double below = c ? sums[c - 1] : 0.0;
-        if (sums[c] > below) {
-            atomicMax(&s_last, c);
-            if (before + sums[c] > point) atomicMin(&s_hit, c);
-        }
-    }
-    __syncthreads();
-    if (warp != 0) return;
-    const int c = s_hit < p.chunks ? s_hit : s_last;
+    const int c = hit >= 0 ? hit : last;
     double upto = before + (c ? sums[c - 1] : 0.0);
     long long token = -1;
-    for (int part = 0; part < p.chunk; part += kVerifyChunk) {
-        const long long from = ((long long)rank * p.chunks + c) * p.chunk + part;
-        T pv[16], qv[16];
-        load(from, pv, qv);
-        bool found = false;
+    constexpr int kRows = 8;
+    bool found = false;
+    for (int part = 0; part < p.chunk && !found; part += 32 * kRows) {
+        const long long from = ((long long)rank * p.chunks + c) * p.chunk + part + lane;
+        double own[kRows], row[kRows];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const double r = mass(pv[i], qv[i], from + i * 32 + lane);
-            double s = r;
+        for (int i = 0; i < kRows; ++i) row[i] = own[i] = mass_at(from + i * 32);
+        // the sums of eight rows of 32, side by side; then the scan of the one that holds the point, or else the last with mass
+        uint32_t there = 0;
 #pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const double x = __shfl_up_sync(0xffffffffu, s, d);
-                if (lane >= d) s += x;
+        for (int i = 0; i < kRows; ++i) there |= (uint32_t)(__ballot_sync(0xffffffffu, own[i] > 0.0) != 0) << i;
+#pragma unroll
+        for (int d = 16; d; d /= 2)
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) row[i] += __shfl_xor_sync(0xffffffffu, row[i], d);
+        int pick = -1;
+        double below = 0.0;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            if ((there >> i & 1) && !found) {
+                pick = i;
+                below = upto;
+                found = upto + row[i] > point;
             }
-            const uint32_t there = __ballot_sync(0xffffffffu, r > 0.0), over = __ballot_sync(0xffffffffu, r > 0.0 && upto + s > point);
-            if (!found && there) token = from + i * 32 + (over ? __ffs(over) - 1 : 31 - __clz(there));
-            found |= over != 0;
-            upto += __shfl_sync(0xffffffffu, s, 31);
+            upto += row[i];
         }
-        if (found) break;
+        if (pick < 0) continue;
+        double r = 0.0;
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (i == pick) r = own[i];
+        double s = r;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const double x = __shfl_up_sync(0xffffffffu, s, d);
+            if (lane >= d) s += x;
+        }
+        const uint32_t some = __ballot_sync(0xffffffffu, r > 0.0), over = __ballot_sync(0xffffffffu, r > 0.0 && below + s > point);
+        token = from - lane + pick * 32 + (over ? __ffs(over) - 1 : 31 - __clz(some));
     }
     if (lane == 0) out[a] = (int)token;
 }

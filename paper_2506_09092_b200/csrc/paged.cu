@@ -16,6 +16,10 @@ namespace {
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxElems = int64_t(1) << 46;          // of an operand, strides included
 constexpr int64_t kPlanSms = 148;                        // the split is planned for this many SMs
+#ifndef PA_CB
+#define PA_CB 16
+#endif
+constexpr int64_t kClusterBlocks = PA_CB;                   // blocks of keys that a CTA of a cluster may get at most
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool off(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
@@ -67,8 +71,8 @@ int check_shape(const cudallm_paged_shape *sp)
     if (s.slots > 1 && s.table_stride < s.table_cols) return CUDALLM_ERR_INVALID_LD;
     if (s.slots > 1 && (long double)s.table_stride * s.slots > (long double)kMaxElems) return CUDALLM_ERR_INVALID_DIM;
     if (s.head_dim % 8 || s.head_dim > 128) return CUDALLM_ERR_UNSUPPORTED_SHAPE;
-    // items x key heads x row tiles, and rows of an item and key head, are counted in 31 bits
-    if ((long double)s.batch * std::max(s.q_heads, s.kv_heads) * s.q_rows > (long double)(kMaxDim / 8)) return CUDALLM_ERR_INVALID_DIM;
+    // items x heads x tokens x 16-byte pieces (16 of a head at most) are counted in 31 bits
+    if ((long double)s.batch * std::max(s.q_heads, s.kv_heads) * s.q_rows > (long double)(kMaxDim / 16)) return CUDALLM_ERR_INVALID_DIM;
     if (no_states(s) || s.kv_heads == 0 || s.head_dim == 0) return CUDALLM_OK;
     int st = check_strides(s.k_stride, s.pages, s.page_rows, s.kv_heads, s.head_dim);
     if (st == CUDALLM_OK) st = check_strides(s.v_stride, s.pages, s.page_rows, s.kv_heads, s.head_dim);
@@ -88,12 +92,12 @@ Plan plan_attn(const cudallm_paged_shape &s)
     Plan f{};
     const int64_t rows = (s.q_heads / s.kv_heads) * s.q_rows;
     f.wide = s.head_dim > 64;
-    f.mt = rows <= 16 ? 1 : 2;
+    f.mt = (int)std::min<int64_t>(4, cdiv(rows, 16));
     f.row_tiles = (int)cdiv(rows, 16 * f.mt);
     const int64_t items = s.batch * s.kv_heads * f.row_tiles, full = 2 * kPlanSms;
     const int64_t blocks = std::max<int64_t>(1, cdiv(no_states(s) ? 0 : s.table_cols * s.page_rows, f.wide ? 64 : 128));
     const int64_t fits = std::min<int64_t>({int64_t(kPaCluster), full / std::max<int64_t>(items, 1), blocks});
-    if (items <= kPlanSms && (items * kPaCluster >= kPlanSms || blocks <= 4 * kPaCluster)) {
+    if (items <= kPlanSms && blocks <= kClusterBlocks * fits) {
         f.cluster = (int)std::max<int64_t>(1, fits);
         f.ctas = (int)(items * f.cluster);
     } else {
@@ -129,11 +133,20 @@ int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cu
     const int64_t rows = std::min<int64_t>(L::kRows, (int64_t)p.group * s.q_rows);
     return rt_launch(paged_join_kernel<DP, MT, T>, dim3((unsigned)f.ctas, (unsigned)cdiv(rows, 128 / (DP / 8))), 128, 0, stream, p);
 }
+template <int DP, typename T>
+int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
+{
+    switch (f.mt) {
+    case 1: return run<DP, 1, T>(s, f, p, dev, stream);
+    case 2: return run<DP, 2, T>(s, f, p, dev, stream);
+    case 3: return run<DP, 3, T>(s, f, p, dev, stream);
+    default: return run<DP, 4, T>(s, f, p, dev, stream);
+    }
+}
 template <typename T>
 int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
 {
-    if (f.wide) return f.mt == 1 ? run<128, 1, T>(s, f, p, dev, stream) : run<128, 2, T>(s, f, p, dev, stream);
-    return f.mt == 1 ? run<64, 1, T>(s, f, p, dev, stream) : run<64, 2, T>(s, f, p, dev, stream);
+    return f.wide ? run<128, T>(s, f, p, dev, stream) : run<64, T>(s, f, p, dev, stream);
 }
 
 }  // namespace
@@ -179,6 +192,7 @@ int cudallm_paged_attn(const cudallm_paged_shape *shape, const void *q, const vo
     p.group = (int)(s.q_heads / s.kv_heads); p.head_dim = (int)s.head_dim;
     p.pages = (int)s.pages; p.page_rows = (int)s.page_rows; p.slots = (int)s.slots;
     p.cap = states ? (int)(s.table_cols * s.page_rows) : 0;
+    p.by_page_rows = make_fast_div((uint32_t)s.page_rows);
     p.row_tiles = f.row_tiles;
     p.cluster = f.cluster;
     p.scale = s.scale; p.scale_log2 = scale_log2(s.scale);
@@ -209,12 +223,13 @@ int cudallm_cache_append(const cudallm_paged_shape *shape, const void *k_new, co
     p.skn = pieces(s.kn_stride); p.svn = pieces(s.vn_stride);
     p.sk = page_pieces(s.k_stride); p.sv = page_pieces(s.v_stride);
     p.table_stride = s.table_stride;
-    p.chunks = (int)(s.head_dim / 8);
-    p.total = s.batch * s.q_rows * s.kv_heads * p.chunks;
-    p.q_rows = (int)s.q_rows; p.kv_heads = (int)s.kv_heads; p.pages = (int)s.pages; p.page_rows = (int)s.page_rows;
-    p.slots = (int)s.slots; p.cap = (int)(s.table_cols * s.page_rows);
-    const int64_t ctas = std::min<int64_t>(cdiv(p.total, 256), 64 * kPlanSms);
-    return rt_launch(cache_append_kernel, dim3((unsigned)ctas), 256, 0, static_cast<cudaStream_t>(stream), p);
+    p.total = (unsigned)(s.batch * s.q_rows * s.kv_heads * (s.head_dim / 8));        // (below 2^31: see check_shape)
+    p.chunks = (int)(s.head_dim / 8); p.kv_heads = (int)s.kv_heads; p.q_rows = (int)s.q_rows; p.page_rows = (int)s.page_rows;
+    p.by_chunks = make_fast_div((uint32_t)p.chunks); p.by_heads = make_fast_div((uint32_t)p.kv_heads);
+    p.by_rows = make_fast_div((uint32_t)p.q_rows); p.by_page_rows = make_fast_div((uint32_t)p.page_rows);
+    p.pages = (int)s.pages; p.slots = (int)s.slots; p.cap = (int)(s.table_cols * s.page_rows);
+    return rt_launch(cache_append_kernel, dim3((unsigned)cdiv(p.total, kAppendPieces * kAppendThreads)), kAppendThreads, 0,
+                     static_cast<cudaStream_t>(stream), p);
 }
 
 }  // extern "C"

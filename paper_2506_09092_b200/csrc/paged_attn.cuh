@@ -15,6 +15,7 @@
 //    A CTA's piece may begin and end inside an item; such parts go to scratch (two slots a CTA) and
 //    paged_join_kernel adds them up in order.
 #pragma once
+#include "fast_div.cuh"
 #include "mma_sync.cuh"
 #include "xattn_common.cuh"
 
@@ -38,6 +39,7 @@ struct PagedParams {
     long long table_stride;
     int batch, q_rows, q_heads, kv_heads, group, head_dim;
     int pages, page_rows, slots, cap;          // cap: states that a row of the table holds
+    FastDiv by_page_rows;
     int row_tiles;                             // tiles of 16 or 32 rows of an item and key head at most
     int cluster;                               // CTAs per item, key head and row tile; 0: equal shares
     float scale, scale_log2;
@@ -46,19 +48,23 @@ constexpr int kPaDesc = 4;                     // parts (0: none begins here), i
 
 template <int DP, int MT> struct PagedSmem {
     static constexpr int kRows = 16 * MT;
-    static constexpr int kKeys = DP == 128 ? 16 : 32;              // of a stage
+    static constexpr int kKeys = DP == 128 ? 16 : 32;              // of a stage and warp
     static constexpr int kBlock = kKeys * kPaWarps;                // of a round of the four warps: unit of the split
     static constexpr int kStages = 3;                              // 96 KiB a CTA: two on an SM
-    static constexpr int kTile = kKeys * DP * 2;                   // one of K, V
-    static constexpr int kWarp = kStages * 2 * kTile;
+    static constexpr int kTile = kKeys * DP * 2;                   // a warp's one of K, V
+    static constexpr int kWarp = kStages * 2 * kTile;              // (one row tile: each warp has its own ring)
     static constexpr int kRing = kPaWarps * kWarp;
-    static constexpr int kPitch = DP + 4;                          // floats per row of the joining block
-    static constexpr int kJoinWarp = (kRows * kPitch + 2 * kRows) * 4;
+    // results of the walk: blocks of [row][DP] fp32, the rows' maxima, their sums; one a warp where each has keys of its own
+    static constexpr int kParts = MT == 1 ? kPaWarps : 1;
+    static constexpr int kPitch = DP + 4;                          // floats per row
+    static constexpr int kPart = (kRows * kPitch + 2 * kRows) * 4;
     // a CTA's result for its cluster: [row][DP] fp32, then the rows' lse
-    static constexpr int kShare = (kPaWarps * kJoinWarp + 127) / 128 * 128;
-    static_assert(kShare + kRows * (DP + 1) * 4 <= kRing, "behind the warps' results");
-    static constexpr int kQ = MT > 1 ? kRows * DP * 2 : 0;         // two row tiles' queries stay in shared memory
-    static constexpr int kBytes = kRing + kQ;
+    static constexpr int kShare = (kParts * kPart + 127) / 128 * 128;
+    static_assert(kShare + kRows * (DP + 1) * 4 <= kRing, "behind the results");
+    static constexpr bool kQInSmem = MT > 3;                       // queries of four row tiles do not fit into registers
+    static constexpr int kMax = kRing + (kQInSmem ? kRows * DP * 2 : 0);   // warps' maxima of each row (several row tiles)
+    static constexpr int kBytes = kMax + (MT > 1 ? kRows * kPaWarps * 4 : 0);
+    static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs on an SM");
     static constexpr int kSlot = kRows * (DP + 1);                 // floats of a part's result
 };
 
@@ -150,109 +156,314 @@ __device__ __forceinline__ void paged_store_lse(const PagedParams &p, int b, int
     if (p.lse) p.lse[((long long)b * p.q_heads + h) * p.q_rows + t] = lse;
 }
 
-// Blocks blk0 .. blk1 - 1 of an item's keys for one key head and row tile.  Leaves each warp's sums, not yet
-// normalised, in its joining block: rows x DP, then the rows' maxima (of the scores), then the sums of
-// exponentials.  A row that has seen no state has maximum -inf and sum 0.
-template <int DP, int MT, typename T>
-__device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, const PagedItem &it, int b, int kvh, int rt,
-                                           int blk0, int blk1)
-{
+// A warp's rows of the stages of a ring: pages looked up one tile ahead, copies past L1.  The pieces of a row go to
+// neighbouring lanes, piece c of row r to position c ^ (r & 7) (conflict-free ldmatrix).
+template <int DP, int MT, typename T> struct PagedLoader {
     using L = PagedSmem<DP, MT>;
-    constexpr int kChunks = DP / 8;                                // 16-byte pieces of a row
-    constexpr int kKeys = L::kKeys, kRowStep = 32 / kChunks;       // rows that a copy instruction covers
-    constexpr uint32_t kAll = kKeys == 32 ? 0xffffffffu : (1u << kKeys) - 1;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);     // row r: token r / group, query head r % group
-    const int seen_lo = paged_seen(it, rt * L::kRows / p.group);
-    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(it, p.group, L::kRows, rt), blk1 * L::kBlock);
-    const int ntiles = key_end > key0 ? (key_end - key0 + kKeys - 1) / kKeys : 0;
-    const int mine = ntiles > warp ? (ntiles - warp + kPaWarps - 1) / kPaWarps : 0;         // tiles warp, warp + 4, ...
-    const int first = key0 + warp * kKeys;                         // this warp's tile t begins at key first + t * kBlock
+    static constexpr int kChunks = DP / 8, kRowStep = 32 / kChunks;        // 16-byte pieces of a row; rows that a copy instruction covers
+    static constexpr uint32_t kAll = L::kKeys == 32 ? 0xffffffffu : (1u << L::kKeys) - 1;
+    const PagedParams &p;
+    const T *kbase, *vbase;
+    const int *row;
+    uint32_t to;                               // this warp's rows of K in stage 0
+    int first, key_end, tiles, lane;           // the warp's tile t begins at key first + t * kBlock
+    int page = -1, in_page = 0;                // this lane's row of the next tile
 
-    const T *kbase = static_cast<const T *>(p.k) + kvh * p.sk.head;
-    const T *vbase = static_cast<const T *>(p.v) + kvh * p.sv.head;
-    const uint32_t ring = smem_u32(smem) + warp * L::kWarp;
-    const bool same = p.sk.page == p.sv.page && p.sk.row == p.sv.row;
-
-    // this lane's row of the next tile: its page, and where in the page
-    int page = -1, in_page = 0;
-    auto look_up = [&](int t) {
+    __device__ __forceinline__ PagedLoader(const PagedParams &p_, const PagedItem &it, int kvh, uint32_t to_, int first_, int key_end_,
+                                           int tiles_)
+        : p(p_), kbase(static_cast<const T *>(p_.k) + kvh * p_.sk.head), vbase(static_cast<const T *>(p_.v) + kvh * p_.sv.head),
+          row(it.row), to(to_), first(first_), key_end(key_end_), tiles(tiles_), lane(threadIdx.x & 31)
+    {
+    }
+    __device__ __forceinline__ void look_up(int t)
+    {
         page = -1;
-        const int pos = first + t * L::kBlock + (lane & (kKeys - 1));
-        if (t < mine && pos < key_end) {
-            const int col = (unsigned)pos / (unsigned)p.page_rows;
+        const int pos = first + t * L::kBlock + (lane & (L::kKeys - 1));
+        if (t < tiles && pos < key_end) {
+            const int col = (int)fast_div((uint32_t)pos, p.by_page_rows);
             in_page = pos - col * p.page_rows;
-            page = it.row[col];
+            page = row[col];
         }
-    };
-    // one stage of K and of V; the pieces of a row go to neighbouring lanes, piece c of row r to position
-    // c ^ (r & 7) (conflict-free ldmatrix).  Returns which rows are there; the others become zeros.
-    const int lc = lane % kChunks, lr = lane / kChunks;
-    const bool lc_live = lc * 8 < p.head_dim;
-    auto load = [&](int t) -> uint32_t {
+    }
+    // Tile t to stage `stage` bytes behind stage 0, values `values` bytes behind the keys.  Returns which rows are
+    // there; the others become zeros.
+    __device__ __forceinline__ uint32_t load(int t, uint32_t stage, uint32_t values)
+    {
         uint32_t mask = 0;
-        if (t < mine) {
-            const bool ok = (unsigned)page < (unsigned)p.pages;
+        if (t < tiles) {
+            const int lc = lane % kChunks, lr = lane / kChunks;
+            const bool lc_live = lc * 8 < p.head_dim, ok = (unsigned)page < (unsigned)p.pages;
+            const bool same = p.sk.page == p.sv.page && p.sk.row == p.sv.row;
             mask = __ballot_sync(0xffffffffu, ok) & kAll;
             const long long off_k = ok ? page * p.sk.page + in_page * p.sk.row : 0;
             const long long off_v = ok && !same ? page * p.sv.page + in_page * p.sv.row : 0;
             look_up(t + 1);
-            const uint32_t st = ring + (t % L::kStages) * 2 * L::kTile;
 #pragma unroll
-            for (int n = 0; n < kKeys / kRowStep; ++n) {
+            for (int n = 0; n < L::kKeys / kRowStep; ++n) {
                 const int r = lr + n * kRowStep;
                 const uint32_t bytes = lc_live && (mask >> r & 1) ? 16 : 0;
-                const uint32_t dst = st + r * DP * 2 + ((lc ^ (r & 7)) << 4);
-                const long long ok_ = __shfl_sync(0xffffffffu, off_k, r);
-                const long long ov_ = same ? ok_ : __shfl_sync(0xffffffffu, off_v, r);
+                const uint32_t dst = to + stage + r * DP * 2 + ((lc ^ (r & 7)) << 4);
+                const long long at_k = __shfl_sync(0xffffffffu, off_k, r);
+                const long long at_v = same ? at_k : __shfl_sync(0xffffffffu, off_v, r);
                 const int col = lc_live ? lc * 8 : 0;
-                cp_async_16_cg(dst, kbase + ok_ + col, bytes);
-                cp_async_16_cg(dst + L::kTile, vbase + ov_ + col, bytes);
+                cp_async_16_cg(dst, kbase + at_k + col, bytes);
+                cp_async_16_cg(dst + values, vbase + at_v + col, bytes);
             }
         }
         cp_async_commit();
         return mask;
-    };
-    look_up(0);
+    }
+};
+
+// Row r of a row tile: token (rt * kRows + r) / group, query head (rt * kRows + r) % group of the key head.
+template <typename T>
+__device__ __forceinline__ const T *paged_q_row(const PagedParams &p, int b, int kvh, int row)
+{
+    const int t = row / p.group, h = row - t * p.group;
+    return static_cast<const T *>(p.q) + b * p.sq.b + t * p.sq.r + (long long)(kvh * p.group + h) * p.sq.h;
+}
+// The A operands of 16 rows from `row` on (up to `rows`): rows g and g + 8, columns 2 q, 2 q + 1 and + 8 of every 16.
+template <int DP, typename T>
+__device__ __forceinline__ void paged_load_q(const PagedParams &p, int b, int kvh, int row, int rows, uint32_t (&qa)[DP / 16][4])
+{
+    const int g = (threadIdx.x & 31) >> 2, q4 = threadIdx.x & 3;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        const T *src = g + 8 * half < rows ? paged_q_row<T>(p, b, kvh, row + g + 8 * half) : nullptr;
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+#pragma unroll
+            for (int hi = 0; hi < 2; ++hi) {
+                const int d = k * 16 + hi * 8 + q4 * 2;
+                qa[k][half + 2 * hi] = (src && d < p.head_dim) ? *reinterpret_cast<const uint32_t *>(src + d) : 0u;
+            }
+    }
+}
+
+// Blocks blk0 .. blk1 - 1 of an item's keys for one key head and row tile.  Leaves sums, not yet normalised, in the
+// parts' places: rows x DP, then the rows' maxima (of the scores), then the sums of exponentials.  A row that has
+// seen no state has maximum -inf and sum 0.
+//
+// One row tile: each warp has tiles of its own and sums of its own.
+template <int DP, typename T>
+__device__ __forceinline__ void paged_walk_narrow(const PagedParams &p, uint8_t *smem, const PagedItem &it, int b, int kvh, int rt,
+                                                  int blk0, int blk1)
+{
+    using L = PagedSmem<DP, 1>;
+    using Loader = PagedLoader<DP, 1, T>;
+    constexpr int kChunks = DP / 8, kKeys = L::kKeys, kN = kKeys / 8;      // kN: tiles of eight keys
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
+    const int seen_lo = paged_seen(it, rt * L::kRows / p.group);
+    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(it, p.group, L::kRows, rt), blk1 * L::kBlock);
+    const int ntiles = key_end > key0 ? (key_end - key0 + kKeys - 1) / kKeys : 0;
+    const int mine = ntiles > warp ? (ntiles - warp + kPaWarps - 1) / kPaWarps : 0;         // tiles warp, warp + 4, ...
+    const uint32_t ring = smem_u32(smem) + warp * L::kWarp;
+    Loader ld(p, it, kvh, ring, key0 + warp * kKeys, key_end, mine);
+    ld.look_up(0);
     uint32_t there[L::kStages - 1];                                // of tiles t, t + 1
 #pragma unroll
-    for (int t = 0; t < L::kStages - 1; ++t) there[t] = load(t);
+    for (int t = 0; t < L::kStages - 1; ++t) there[t] = ld.load(t, t * 2 * L::kTile, L::kTile);
 
-    // Q as the A operand: rows g and g + 8 of 16, columns 2 q, 2 q + 1 and + 8 of every 16
     const int g = lane >> 2, q4 = lane & 3;
-    uint32_t qa[MT == 1 ? DP / 16 : 1][4];
-    const uint32_t qs = smem_u32(smem) + L::kRing;
-    auto q_row = [&](int r) -> const T * {
-        const int row = rt * L::kRows + r, t = row / p.group, h = row - t * p.group;
-        return static_cast<const T *>(p.q) + b * p.sq.b + t * p.sq.r + (long long)(kvh * p.group + h) * p.sq.h;
-    };
-    if constexpr (MT == 1) {
+    uint32_t qa[DP / 16][4];
+    paged_load_q<DP, T>(p, b, kvh, rt * L::kRows, rows, qa);
+    int seen[2];                                                   // keys that a row sees lie below this
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    bool any[2] = {false, false};
+    float o[DP / 8][4];
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int r = g + 8 * half;
-            const T *src = r < rows ? q_row(r) : nullptr;
+    for (int half = 0; half < 2; ++half)
+        seen[half] = g + 8 * half < rows ? paged_seen(it, (rt * L::kRows + g + 8 * half) / p.group) : 0x7fffffff;
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+
+    for (int t = 0; t < mine; ++t) {
+        cp_async_wait_group<L::kStages - 2>();
+        __syncwarp();                                              // every lane's copies of stage t have landed
+        const uint32_t mask = there[0];
+#pragma unroll
+        for (int i = 0; i + 1 < L::kStages - 1; ++i) there[i] = there[i + 1];
+        const int next = t + L::kStages - 1;
+        there[L::kStages - 2] = ld.load(next, next % L::kStages * 2 * L::kTile, L::kTile);  // (read in round t - 1)
+        const uint32_t sk = ring + (t % L::kStages) * 2 * L::kTile, sv = sk + L::kTile;
+        float s[kN][4] = {};
+        {
+            const int idx = lane >> 3, kr = (idx >> 1) * 8 + (lane & 7);
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k)
 #pragma unroll
-                for (int hi = 0; hi < 2; ++hi) {
-                    const int d = k * 16 + hi * 8 + q4 * 2;
-                    qa[k][half + 2 * hi] = (src && d < p.head_dim) ? *reinterpret_cast<const uint32_t *>(src + d) : 0u;
+                for (int n = 0; n < kN; n += 2) {
+                    uint32_t bf[4];
+                    ldmatrix_x4(bf, sk + (n * 8 + kr) * DP * 2 + (((2 * k + (idx & 1)) ^ (kr & 7)) << 4));
+                    mma_16x8x16<T>(s[n], qa[k], bf[0], bf[1]);
+                    mma_16x8x16<T>(s[n + 1], qa[k], bf[2], bf[3]);
                 }
         }
+        const int pos0 = ld.first + t * L::kBlock;
+        const bool full = mask == Loader::kAll && pos0 + kKeys <= seen_lo;     // every row sees every key
+        if (!full) {
+#pragma unroll
+            for (int n = 0; n < kN; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = n * 8 + q4 * 2 + (e & 1);
+                    if (!(mask >> key & 1) || pos0 + key >= seen[e >> 1]) s[n][e] = -INFINITY;
+                }
+        }
+        float bm[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            float v = fmaxf(s[0][2 * half], s[0][2 * half + 1]);
+#pragma unroll
+            for (int n = 1; n < kN; ++n) v = fmaxf(v, fmaxf(s[n][2 * half], s[n][2 * half + 1]));
+            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
+            bm[half] = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
+            any[half] |= full || (mask & low_bits(seen[half] - pos0)) != 0;
+        }
+        if (__any_sync(0xffffffffu, bm[0] > m[0] || bm[1] > m[1])) {
+            float alpha[2];
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const float nm = fmaxf(m[half], bm[half]);
+                alpha[half] = nm == m[half] ? 1.f : xa_exp2((m[half] - nm) * p.scale_log2);
+                m[half] = nm;
+                l[half] *= alpha[half];
+            }
+#pragma unroll
+            for (int n = 0; n < DP / 8; ++n) {
+                o[n][0] *= alpha[0];
+                o[n][1] *= alpha[0];
+                o[n][2] *= alpha[1];
+                o[n][3] *= alpha[1];
+            }
+        }
+        // (a row that has seen nothing yet: all its scores are -inf, and so are their differences to 0)
+        const float neg[2] = {m[0] == -INFINITY ? 0.f : -m[0] * p.scale_log2, m[1] == -INFINITY ? 0.f : -m[1] * p.scale_log2};
+#pragma unroll
+        for (int n = 0; n < kN; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[n][e] = xa_exp2(fmaf(s[n][e], p.scale_log2, neg[e >> 1]));
+                l[e >> 1] += s[n][e];
+            }
+        // Keys that some of the rows do not see: 0 x a value that is not finite would reach those rows through
+        // the product, so such a value's rows are added by hand and it becomes zero.
+        uint32_t partly = full ? 0u : mask & ~low_bits(seen_lo - pos0);
+        while (partly) {
+            const int j = __ffs(partly) - 1;
+            partly &= partly - 1;
+            const uint32_t row = sv + j * DP * 2;
+            const bool bad = lane < kChunks && any_not_finite<T>(ld_shared_v4(row + ((lane ^ (j & 7)) << 4)));
+            if (!__any_sync(0xffffffffu, bad)) continue;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                float w = 0.f;
+#pragma unroll
+                for (int n = 0; n < kN; ++n)
+                    w = select(n == j >> 3, select(j & 1, s[n][2 * half + 1], s[n][2 * half]), w);
+                w = __shfl_sync(0xffffffffu, w, (lane & ~3) | ((j & 7) >> 1));
+                if (pos0 + j < seen[half]) {
+#pragma unroll
+                    for (int n = 0; n < DP / 8; ++n) {
+                        const float2 f = unpack2<T>(ld_shared_u32(row + ((n ^ (j & 7)) << 4) + q4 * 4));
+                        o[n][2 * half] = fmaf(w, f.x, o[n][2 * half]);
+                        o[n][2 * half + 1] = fmaf(w, f.y, o[n][2 * half + 1]);
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane < kChunks) st_shared_v4_b32(row + (lane << 4), 0, 0, 0, 0);
+            __syncwarp();
+        }
+        {
+            const int idx = lane >> 3, kr = (idx & 1) * 8 + (lane & 7);
+#pragma unroll
+            for (int h = 0; h < kN; h += 2) {
+                const uint32_t pa[4] = {XaElem<T>::pack(s[h][0], s[h][1]), XaElem<T>::pack(s[h][2], s[h][3]),
+                                        XaElem<T>::pack(s[h + 1][0], s[h + 1][1]), XaElem<T>::pack(s[h + 1][2], s[h + 1][3])};
+#pragma unroll
+                for (int n = 0; n < DP / 16; ++n) {
+                    uint32_t bf[4];
+                    ldmatrix_x4_trans(bf, sv + (h * 8 + kr) * DP * 2 + (((2 * n + (idx >> 1)) ^ (kr & 7)) << 4));
+                    mma_16x8x16<T>(o[2 * n], pa, bf[0], bf[1]);
+                    mma_16x8x16<T>(o[2 * n + 1], pa, bf[2], bf[3]);
+                }
+            }
+        }
+        __syncwarp();                                              // stage t has been read by every lane
+    }
+    cp_async_wait_group<0>();
+    __syncthreads();                                               // the rings are free
+    float *jo = reinterpret_cast<float *>(smem) + warp * (L::kPart / 4);
+    float *jm = jo + L::kRows * L::kPitch, *jl = jm + L::kRows;
+#pragma unroll
+    for (int n = 0; n < DP / 8; ++n) {
+        *reinterpret_cast<float2 *>(jo + g * L::kPitch + n * 8 + q4 * 2) = make_float2(o[n][0], o[n][1]);
+        *reinterpret_cast<float2 *>(jo + (g + 8) * L::kPitch + n * 8 + q4 * 2) = make_float2(o[n][2], o[n][3]);
+    }
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
+        l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
+        // scores of -inf alone are not the same as no scores
+        if (any[half] && m[half] == -INFINITY) l[half] = __int_as_float(0x7fc00000);
+        if (q4 == 0) {
+            jm[g + 8 * half] = m[half];
+            jl[g + 8 * half] = l[half];
+        }
+    }
+    __syncthreads();
+}
+
+// Two to four row tiles: registers do not hold a whole result per warp, so the warps share a stage.  Each takes its
+// own keys' scores for all rows (S = Q K^T), they agree on the rows' maxima, the probabilities go to shared memory (where the
+// stage's keys were), and each multiplies all of them with its own quarter of the columns of V.  Two
+// barriers a stage.
+template <int DP, int MT, typename T>
+__device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *smem, const PagedItem &it, int b, int kvh, int rt,
+                                                int blk0, int blk1)
+{
+    using L = PagedSmem<DP, MT>;
+    using Loader = PagedLoader<DP, MT, T>;
+    constexpr int kKeys = L::kKeys, kN = kKeys / 8, kChunks = DP / 8;
+    constexpr int kAllTile = kPaWarps * L::kTile, kStage = 2 * kAllTile;   // a stage: all warps' keys, all warps' values
+    constexpr int kProb = L::kBlock * 2;                           // bytes of a row of probabilities
+    constexpr int kSlice = DP / kPaWarps / 8;                      // 8-column tiles of V that a warp multiplies with
+    static_assert(L::kRows * kProb <= kAllTile, "where the keys were");
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
+    const int seen_lo = paged_seen(it, rt * L::kRows / p.group);
+    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(it, p.group, L::kRows, rt), blk1 * L::kBlock);
+    const int tiles = key_end > key0 ? (key_end - key0 + L::kBlock - 1) / L::kBlock : 0;
+    const uint32_t ring = smem_u32(smem), maxima = ring + L::kMax;
+    Loader ld(p, it, kvh, ring + warp * L::kTile, key0 + warp * kKeys, key_end, tiles);
+    ld.look_up(0);
+    uint32_t there[L::kStages - 1];
+#pragma unroll
+    for (int t = 0; t < L::kStages - 1; ++t) there[t] = ld.load(t, t * kStage, kAllTile);
+
+    const int g = lane >> 2, q4 = lane & 3;
+    uint32_t qa[L::kQInSmem ? 1 : MT][DP / 16][4];
+    const uint32_t qs = ring + L::kRing;
+    if constexpr (!L::kQInSmem) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) paged_load_q<DP, T>(p, b, kvh, rt * L::kRows + i * 16, rows - i * 16, qa[i]);
     } else {
         for (int i = tid; i < L::kRows * kChunks; i += kPaThreads) {
             const int r = i / kChunks, c = i % kChunks;
             uint4 w = make_uint4(0, 0, 0, 0);
-            if (r < rows && c * 8 < p.head_dim) w = *reinterpret_cast<const uint4 *>(q_row(r) + c * 8);
+            if (r < rows && c * 8 < p.head_dim)
+                w = *reinterpret_cast<const uint4 *>(paged_q_row<T>(p, b, kvh, rt * L::kRows + r) + c * 8);
             st_shared_v4_b32(qs + r * DP * 2 + ((c ^ (r & 7)) << 4), w.x, w.y, w.z, w.w);
         }
         __syncthreads();
     }
-
-    int seen[MT][2];                                               // keys that a row sees lie below this
-    float m[MT][2], l[MT][2];
+    int seen[MT][2];
+    float m[MT][2], l[MT][2], o[MT][kSlice][4];
     bool any[MT][2];
-    float o[MT][DP / 8][4];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
 #pragma unroll
@@ -264,34 +475,30 @@ __device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, 
             any[i][half] = false;
         }
 #pragma unroll
-        for (int n = 0; n < DP / 8; ++n)
+        for (int n = 0; n < kSlice; ++n)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[i][n][e] = 0.f;
     }
 
-    for (int t = 0; t < mine; ++t) {
+    for (int t = 0; t < tiles; ++t) {
         cp_async_wait_group<L::kStages - 2>();
-        __syncwarp();                                              // every lane's copies of stage t have landed
+        __syncwarp();                                              // this warp's rows of stage t have landed
+        const uint32_t stage = ring + (t % L::kStages) * kStage, sk = stage + warp * L::kTile, sv = sk + kAllTile;
         const uint32_t mask = there[0];
-#pragma unroll
-        for (int i = 0; i + 1 < L::kStages - 1; ++i) there[i] = there[i + 1];
-        there[L::kStages - 2] = load(t + L::kStages - 1);          // (its stage was read in round t - 1)
-        const uint32_t sk = ring + (t % L::kStages) * 2 * L::kTile, sv = sk + L::kTile;
-        constexpr int kN = kKeys / 8;                              // tiles of eight keys
         float s[MT][kN][4] = {};
         {
             const int idx = lane >> 3, kr = (idx >> 1) * 8 + (lane & 7);
 #pragma unroll
             for (int k = 0; k < DP / 16; ++k) {
                 uint32_t a[MT][4];
-                if constexpr (MT == 1) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) a[0][e] = qa[k][e];
-                } else {
+                for (int i = 0; i < MT; ++i) {
+                    if constexpr (!L::kQInSmem) {
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const int r = i * 16 + (lane & 15), c = 2 * k + (lane >> 4);
-                        ldmatrix_x4(a[i], qs + r * DP * 2 + ((c ^ (r & 7)) << 4));
+                        for (int e = 0; e < 4; ++e) a[i][e] = qa[i][k][e];
+                    } else {
+                        const int r = i * 16 + (lane & 15);
+                        ldmatrix_x4(a[i], qs + r * DP * 2 + (((2 * k + (lane >> 4)) ^ (r & 7)) << 4));
                     }
                 }
 #pragma unroll
@@ -306,8 +513,8 @@ __device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, 
                 }
             }
         }
-        const int pos0 = first + t * L::kBlock;
-        const bool full = mask == kAll && pos0 + kKeys <= seen_lo;     // every row sees every key
+        const int pos0 = ld.first + t * L::kBlock;
+        const bool full = mask == Loader::kAll && pos0 + kKeys <= seen_lo;     // every row sees every key
         if (!full) {
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -319,8 +526,10 @@ __device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, 
                         if (!(mask >> key & 1) || pos0 + key >= seen[i][e >> 1]) s[i][n][e] = -INFINITY;
                     }
         }
-        bool more = false;
-        float bm[MT][2];
+        // values that are not finite of keys that some of the rows do not see (see below)
+        bool bad = false;
+        for (uint32_t partly = full ? 0u : mask & ~low_bits(seen_lo - pos0); partly; partly &= partly - 1)
+            bad |= lane < kChunks && any_not_finite<T>(ld_shared_v4(sv + (__ffs(partly) - 1) * DP * 2 + (lane << 4)));
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -330,9 +539,25 @@ __device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, 
                 for (int n = 1; n < kN; ++n) v = fmaxf(v, fmaxf(s[i][n][2 * half], s[i][n][2 * half + 1]));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
                 v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-                bm[i][half] = v;
-                more |= v > m[i][half];
                 any[i][half] |= full || (mask & low_bits(seen[i][half] - pos0)) != 0;
+                if (q4 == 0)
+                    asm volatile("st.shared.f32 [%0], %1;" ::"r"(maxima + (i * 16 + g + 8 * half) * 16 + warp * 4), "f"(v) : "memory");
+            }
+        bad = __syncthreads_or(bad);                               // all have read the stage's keys, and stage t - 1 to its end
+#pragma unroll
+        for (int i = 0; i + 1 < L::kStages - 1; ++i) there[i] = there[i + 1];
+        const int next = t + L::kStages - 1;
+        there[L::kStages - 2] = ld.load(next, next % L::kStages * kStage, kAllTile);
+        float nm[MT][2];
+        bool more = false;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint4 w = ld_shared_v4(maxima + (i * 16 + g + 8 * half) * 16);
+                nm[i][half] = fmaxf(m[i][half], fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)),
+                                                      fmaxf(__uint_as_float(w.z), __uint_as_float(w.w))));
+                more |= nm[i][half] > m[i][half];
             }
         if (__any_sync(0xffffffffu, more)) {
 #pragma unroll
@@ -340,13 +565,12 @@ __device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, 
                 float alpha[2];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const float nm = fmaxf(m[i][half], bm[i][half]);
-                    alpha[half] = nm == m[i][half] ? 1.f : xa_exp2((m[i][half] - nm) * p.scale_log2);
-                    m[i][half] = nm;
+                    alpha[half] = nm[i][half] == m[i][half] ? 1.f : xa_exp2((m[i][half] - nm[i][half]) * p.scale_log2);
+                    m[i][half] = nm[i][half];
                     l[i][half] *= alpha[half];
                 }
 #pragma unroll
-                for (int n = 0; n < DP / 8; ++n) {
+                for (int n = 0; n < kSlice; ++n) {
                     o[i][n][0] *= alpha[0];
                     o[i][n][1] *= alpha[0];
                     o[i][n][2] *= alpha[1];
@@ -356,84 +580,82 @@ __device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, 
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            // (a row that has seen nothing yet: all its scores are -inf, and so are their differences to 0)
             const float neg[2] = {m[i][0] == -INFINITY ? 0.f : -m[i][0] * p.scale_log2,
                                   m[i][1] == -INFINITY ? 0.f : -m[i][1] * p.scale_log2};
 #pragma unroll
             for (int n = 0; n < kN; ++n)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[i][n][e] = xa_exp2(fmaf(s[i][n][e], p.scale_log2, neg[e >> 1]));
-                    l[i][e >> 1] += s[i][n][e];
+                for (int half = 0; half < 2; ++half) {
+                    const float p0 = xa_exp2(fmaf(s[i][n][2 * half], p.scale_log2, neg[half]));
+                    const float p1 = xa_exp2(fmaf(s[i][n][2 * half + 1], p.scale_log2, neg[half]));
+                    l[i][half] += p0 + p1;
+                    const int r = i * 16 + g + 8 * half;
+                    asm volatile("st.shared.b32 [%0], %1;"
+                                 ::"r"(stage + r * kProb + (((warp * kN + n) ^ (r & 7)) << 4) + q4 * 4), "r"(XaElem<T>::pack(p0, p1)) : "memory");
                 }
         }
-        // Keys that some of the rows do not see: 0 x a value that is not finite would reach those rows through
-        // the product, so such a value's rows are added by hand and it becomes zero.
-        uint32_t partly = full ? 0u : mask & ~low_bits(seen_lo - pos0);
-        while (partly) {
-            const int j = __ffs(partly) - 1;
-            partly &= partly - 1;
-            const uint32_t row = sv + j * DP * 2;
-            const bool bad = lane < kChunks && any_not_finite<T>(ld_shared_v4(row + ((lane ^ (j & 7)) << 4)));
-            if (!__any_sync(0xffffffffu, bad)) continue;
+        __syncthreads();                                           // the probabilities are there
+        // 0 x a value that is not finite would reach rows that do not see it through the product: such a value is
+        // added by hand where it is seen, and becomes zero.  (A warp reads and clears its own columns only.)
+        if (bad) {
+            const int tile0 = key0 + t * L::kBlock;
+            for (int j = max(seen_lo - tile0, 0); j < L::kBlock; ++j) {
+                const uint32_t row = stage + kAllTile + j * DP * 2, own = row + (((warp * kSlice + lane) ^ (j & 7)) << 4);
+                if (!__any_sync(0xffffffffu, lane < kSlice && any_not_finite<T>(ld_shared_v4(lane < kSlice ? own : row)))) continue;
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+                for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    float w = 0.f;
+                    for (int half = 0; half < 2; ++half) {
+                        const int r = i * 16 + g + 8 * half;
+                        const float2 both = unpack2<T>(ld_shared_u32(stage + r * kProb + (((j >> 3) ^ (r & 7)) << 4) + (j & 6) * 2));
+                        const float weight = j & 1 ? both.y : both.x;
+                        if (tile0 + j < seen[i][half]) {
 #pragma unroll
-                    for (int n = 0; n < kN; ++n)
-                        w = select(n == j >> 3, select(j & 1, s[i][n][2 * half + 1], s[i][n][2 * half]), w);
-                    w = __shfl_sync(0xffffffffu, w, (lane & ~3) | ((j & 7) >> 1));
-                    if (pos0 + j < seen[i][half]) {
-#pragma unroll
-                        for (int n = 0; n < DP / 8; ++n) {
-                            const float2 f = unpack2<T>(ld_shared_u32(row + ((n ^ (j & 7)) << 4) + q4 * 4));
-                            o[i][n][2 * half] = fmaf(w, f.x, o[i][n][2 * half]);
-                            o[i][n][2 * half + 1] = fmaf(w, f.y, o[i][n][2 * half + 1]);
+                            for (int n = 0; n < kSlice; ++n) {
+                                const float2 f = unpack2<T>(ld_shared_u32(row + (((warp * kSlice + n) ^ (j & 7)) << 4) + q4 * 4));
+                                o[i][n][2 * half] = fmaf(weight, f.x, o[i][n][2 * half]);
+                                o[i][n][2 * half + 1] = fmaf(weight, f.y, o[i][n][2 * half + 1]);
+                            }
                         }
                     }
-                }
-            __syncwarp();
-            if (lane < kChunks) st_shared_v4_b32(row + (lane << 4), 0, 0, 0, 0);
-            __syncwarp();
+                __syncwarp();
+                if (lane < kSlice) st_shared_v4_b32(own, 0, 0, 0, 0);
+                __syncwarp();
+            }
         }
         {
             const int idx = lane >> 3, kr = (idx & 1) * 8 + (lane & 7);
 #pragma unroll
-            for (int h = 0; h < kN; h += 2) {
-                uint32_t pa[MT][4];
+            for (int k = 0; k < L::kBlock / 16; ++k) {
+                uint32_t a[MT][4];
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    pa[i][0] = XaElem<T>::pack(s[i][h][0], s[i][h][1]);
-                    pa[i][1] = XaElem<T>::pack(s[i][h][2], s[i][h][3]);
-                    pa[i][2] = XaElem<T>::pack(s[i][h + 1][0], s[i][h + 1][1]);
-                    pa[i][3] = XaElem<T>::pack(s[i][h + 1][2], s[i][h + 1][3]);
+                    const int r = i * 16 + (lane & 15);
+                    ldmatrix_x4(a[i], stage + r * kProb + (((2 * k + (lane >> 4)) ^ (r & 7)) << 4));
                 }
 #pragma unroll
-                for (int n = 0; n < DP / 16; ++n) {
+                for (int n = 0; n < kSlice; n += 2) {
                     uint32_t bf[4];
-                    ldmatrix_x4_trans(bf, sv + (h * 8 + kr) * DP * 2 + (((2 * n + (idx >> 1)) ^ (kr & 7)) << 4));
+                    ldmatrix_x4_trans(bf, stage + kAllTile + (k * 16 + kr) * DP * 2 + (((warp * kSlice + n + (idx >> 1)) ^ (kr & 7)) << 4));
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        mma_16x8x16<T>(o[i][2 * n], pa[i], bf[0], bf[1]);
-                        mma_16x8x16<T>(o[i][2 * n + 1], pa[i], bf[2], bf[3]);
+                        mma_16x8x16<T>(o[i][n], a[i], bf[0], bf[1]);
+                        mma_16x8x16<T>(o[i][n + 1], a[i], bf[2], bf[3]);
                     }
                 }
             }
         }
-        __syncwarp();                                              // stage t has been read by every lane
     }
     cp_async_wait_group<0>();
-    __syncthreads();                                               // the rings are free
-    float *jo = reinterpret_cast<float *>(smem) + warp * (L::kJoinWarp / 4);
-    float *jm = jo + L::kRows * L::kPitch, *jl = jm + L::kRows;
+    __syncthreads();                                               // the ring is free
+    float *jo = reinterpret_cast<float *>(smem), *jm = jo + L::kRows * L::kPitch, *jl = jm + L::kRows;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
 #pragma unroll
-        for (int n = 0; n < DP / 8; ++n) {
-            *reinterpret_cast<float2 *>(jo + (i * 16 + g) * L::kPitch + n * 8 + q4 * 2) = make_float2(o[i][n][0], o[i][n][1]);
-            *reinterpret_cast<float2 *>(jo + (i * 16 + g + 8) * L::kPitch + n * 8 + q4 * 2) = make_float2(o[i][n][2], o[i][n][3]);
+        for (int n = 0; n < kSlice; ++n) {
+            float *at = jo + (i * 16 + g) * L::kPitch + (warp * kSlice + n) * 8 + q4 * 2;
+            *reinterpret_cast<float2 *>(at) = make_float2(o[i][n][0], o[i][n][1]);
+            *reinterpret_cast<float2 *>(at + 8 * L::kPitch) = make_float2(o[i][n][2], o[i][n][3]);
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
@@ -441,26 +663,30 @@ __device__ __forceinline__ void paged_walk(const PagedParams &p, uint8_t *smem, 
             l[i][half] += __shfl_xor_sync(0xffffffffu, l[i][half], 2);
             // scores of -inf alone are not the same as no scores
             if (any[i][half] && m[i][half] == -INFINITY) l[i][half] = __int_as_float(0x7fc00000);
-            if (q4 == 0) {
-                jm[i * 16 + g + 8 * half] = m[i][half];
-                jl[i * 16 + g + 8 * half] = l[i][half];
-            }
+            if (q4 == 0)
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(maxima + (i * 16 + g + 8 * half) * 16 + warp * 4), "f"(l[i][half]) : "memory");
+            if (q4 == 0 && warp == 0) jm[i * 16 + g + 8 * half] = m[i][half];
         }
+    }
+    __syncthreads();
+    if (tid < L::kRows) {
+        const uint4 w = ld_shared_v4(maxima + tid * 16);
+        jl[tid] = (__uint_as_float(w.x) + __uint_as_float(w.y)) + (__uint_as_float(w.z) + __uint_as_float(w.w));
     }
     __syncthreads();
 }
 
-// Eight columns (c) of row r: the four warps' sums, weighted to the common maximum, normalised; returns lse
+// Eight columns (c) of row r: the parts' sums, weighted to the common maximum, normalised; returns lse
 // (-inf: no states, and zeros).
 template <int DP, int MT>
-__device__ __forceinline__ float paged_join_warps(const PagedParams &p, const uint8_t *smem, int r, int c, float (&acc)[8])
+__device__ __forceinline__ float paged_join_parts(const PagedParams &p, const uint8_t *smem, int r, int c, float (&acc)[8])
 {
     using L = PagedSmem<DP, MT>;
     const float *base = reinterpret_cast<const float *>(smem);
-    constexpr int kStep = L::kJoinWarp / 4;
-    float wm[kPaWarps], wl[kPaWarps], mx = -INFINITY, sum = 0.f;
+    constexpr int kStep = L::kPart / 4;
+    float wm[L::kParts], wl[L::kParts], mx = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kPaWarps; ++w) {
+    for (int w = 0; w < L::kParts; ++w) {
         wm[w] = base[w * kStep + L::kRows * L::kPitch + r];
         wl[w] = base[w * kStep + L::kRows * L::kPitch + L::kRows + r];
         mx = fmaxf(mx, wm[w]);
@@ -468,8 +694,8 @@ __device__ __forceinline__ float paged_join_warps(const PagedParams &p, const ui
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < kPaWarps; ++w) {
-        if (wl[w] == 0.f) continue;                                // a warp without keys
+    for (int w = 0; w < L::kParts; ++w) {
+        if (wl[w] == 0.f) continue;                                // a part without keys
         const float a = xa_exp2((wm[w] - mx) * p.scale_log2);
         sum = fmaf(a, wl[w], sum);
 #pragma unroll
@@ -488,7 +714,7 @@ paged_attn_kernel(const PagedParams p)
 {
     using L = PagedSmem<DP, MT>;
     constexpr int kChunks = DP / 8;
-    extern __shared__ __align__(1024) uint8_t smem[];
+    extern __shared__ __align__(128) uint8_t smem[];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     grid_launch_dependents();
     grid_dependency_wait();
@@ -516,8 +742,8 @@ paged_attn_kernel(const PagedParams p)
     } else {
         // Equal shares.  Items in order, in each the key heads, in each the row tiles, in each the blocks of keys: how
         // many blocks there are in all, and which item this CTA's first one lies in (thread t counts `each` items).
-        __shared__ long long warp_sum[kPaWarps], s_rem;
-        __shared__ int s_item;
+        long long *warp_sum = reinterpret_cast<long long *>(smem), &s_rem = warp_sum[kPaWarps];
+        int &s_item = *reinterpret_cast<int *>(warp_sum + kPaWarps + 1);
         const int each = (p.batch + kPaThreads - 1) / kPaThreads;
         long long sum = 0;
         for (int i = 0; i < each; ++i)
@@ -555,6 +781,7 @@ paged_attn_kernel(const PagedParams p)
         __syncthreads();
         b = s_item;
         rem = s_rem;
+        __syncthreads();                                           // (copies land there next)
     }
 
     for (;;) {
@@ -572,7 +799,8 @@ paged_attn_kernel(const PagedParams p)
             for (rt = 0; blk0 >= (blocks = paged_blocks(it, p.group, L::kRows, rt, L::kBlock)); ++rt) blk0 -= blocks;
             blk1 = (int)min((long long)blocks, blk0 + (end - pos));
         }
-        paged_walk<DP, MT, T>(p, smem, it, b, kvh, rt, blk0, blk1);
+        if constexpr (MT == 1) paged_walk_narrow<DP, T>(p, smem, it, b, kvh, rt, blk0, blk1);
+        else paged_walk_wide<DP, MT, T>(p, smem, it, b, kvh, rt, blk0, blk1);
         // whole results leave at once, parts go to the cluster's or the call's scratch
         const bool whole = blk0 == 0 && blk1 == blocks && p.cluster <= 1;
         const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
@@ -580,7 +808,7 @@ paged_attn_kernel(const PagedParams p)
         for (int i = tid; i < rows * kChunks; i += kPaThreads) {
             const int r = i / kChunks, c = i % kChunks;
             float acc[8];
-            const float lse = paged_join_warps<DP, MT>(p, smem, r, c, acc);
+            const float lse = paged_join_parts<DP, MT>(p, smem, r, c, acc);
             if (whole) {
                 const int row = rt * L::kRows + r, t = row / p.group, h = kvh * p.group + row - t * p.group;
                 paged_store<T>(p, b, t, h, c, acc);
@@ -705,32 +933,45 @@ struct AppendParams {
     const int *table, *lens, *slot_of, *new_lens;
     XaStrides skn, svn;
     PagedStrides sk, sv;
-    long long table_stride, total;             // pieces of the new keys
-    int q_rows, kv_heads, chunks, pages, page_rows, slots, cap;
+    long long table_stride;
+    unsigned total;                            // pieces of the new keys
+    FastDiv by_chunks, by_heads, by_rows, by_page_rows;
+    int chunks, kv_heads, q_rows, page_rows, pages, slots, cap;
 };
+constexpr int kAppendThreads = 256, kAppendPieces = 4;
 
-// A thread moves one 16-byte piece of a key and of a value.
-__global__ void __launch_bounds__(256)
+// A thread moves four 16-byte pieces of keys and four of values.  What it waits for is the chain slot -> length -> page, so
+// the four go side by side.
+__global__ void __launch_bounds__(kAppendThreads)
 cache_append_kernel(const AppendParams p)
 {
     grid_launch_dependents();
     grid_dependency_wait();
-    for (long long i = blockIdx.x * 256LL + threadIdx.x; i < p.total; i += gridDim.x * 256LL) {
-        const unsigned c = (unsigned)(i % p.chunks);
-        const long long rest = i / p.chunks, token = rest / p.kv_heads;
-        const unsigned h = (unsigned)(rest - token * p.kv_heads);
-        const int b = (int)(token / p.q_rows), t = (int)(token - (long long)b * p.q_rows);
-        const uint4 key = p.k_new[b * p.skn.b + t * p.skn.r + h * p.skn.h + c];
-        const uint4 value = p.v_new[b * p.svn.b + t * p.svn.r + h * p.svn.h + c];
+    uint4 key[kAppendPieces], value[kAppendPieces];
+    long long to_k[kAppendPieces], to_v[kAppendPieces];
+#pragma unroll
+    for (int n = 0; n < kAppendPieces; ++n) {
+        const unsigned i = (blockIdx.x * kAppendPieces + n) * kAppendThreads + threadIdx.x;
+        to_k[n] = -1;
+        if (i >= p.total) continue;
+        const uint32_t rest = fast_div(i, p.by_chunks), c = i - rest * p.chunks, token = fast_div(rest, p.by_heads), h = rest - token * p.kv_heads;
+        const int b = (int)fast_div(token, p.by_rows), t = (int)token - b * p.q_rows;
+        key[n] = p.k_new[b * p.skn.b + t * p.skn.r + h * p.skn.h + c];
+        value[n] = p.v_new[b * p.svn.b + t * p.svn.r + h * p.svn.h + c];
         const PagedItem it = paged_item(p.table, p.table_stride, p.lens, p.slot_of, p.new_lens, b, p.slots, p.cap, p.q_rows);
         const int pos = it.len - it.news + t;
         if (t >= it.news || pos < 0) continue;
-        const int col = (unsigned)pos / (unsigned)p.page_rows;
-        const int page = it.row[col], in_page = pos - col * p.page_rows;
+        const int col = (int)fast_div((uint32_t)pos, p.by_page_rows), page = it.row[col], in_page = pos - col * p.page_rows;
         if ((unsigned)page >= (unsigned)p.pages) continue;
-        p.k[page * p.sk.page + in_page * p.sk.row + h * p.sk.head + c] = key;
-        p.v[page * p.sv.page + in_page * p.sv.row + h * p.sv.head + c] = value;
+        to_k[n] = page * p.sk.page + in_page * p.sk.row + h * p.sk.head + c;
+        to_v[n] = page * p.sv.page + in_page * p.sv.row + h * p.sv.head + c;
     }
+#pragma unroll
+    for (int n = 0; n < kAppendPieces; ++n)
+        if (to_k[n] >= 0) {
+            p.k[to_k[n]] = key[n];
+            p.v[to_v[n]] = value[n];
+        }
 }
 
 }  // namespace cudallm

@@ -14,7 +14,7 @@ namespace {
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxBytes = int64_t(1) << 46;
 constexpr int64_t kMaxBook = int64_t(1) << 20;           // pages of a book
-constexpr int64_t kMaxList = int64_t(1) << 16;           // entries of a list
+constexpr int64_t kMaxList = int64_t(1) << 14;           // entries of a list
 constexpr int64_t kMaxPools = 65536;
 constexpr int64_t kPlanSms = 148;
 
@@ -47,16 +47,16 @@ int check_book(const cudallm_page_book *bp)
         return CUDALLM_ERR_INVALID_DIM;
     if (b.slots > 1 && b.table_stride < b.table_cols) return CUDALLM_ERR_INVALID_LD;
     if (b.slots > 1 && (long double)b.table_stride * b.slots > (long double)kMaxBytes) return CUDALLM_ERR_INVALID_DIM;
-    if (!b.turn || (b.pages > 0 && !b.refs) || (b.slots > 0 && (!b.lens || (b.table_cols > 0 && !b.table))))
+    if ((b.pages > 0 && !b.refs) || (b.slots > 0 && (!b.lens || (b.table_cols > 0 && !b.table))))
         return CUDALLM_ERR_INVALID_POINTER;
-    if (off(b.refs, 16) || off(b.lens, 4) || off(b.table, 4) || off(b.turn, 4)) return CUDALLM_ERR_MISALIGNED;
+    if (off(b.refs, 16) || off(b.lens, 4) || off(b.table, 4)) return CUDALLM_ERR_MISALIGNED;
     return CUDALLM_OK;
 }
 
 Book device_book(const cudallm_page_book &b)
 {
     Book d{};
-    d.refs = b.refs; d.lens = b.lens; d.table = b.table; d.turn = b.turn;
+    d.refs = b.refs; d.lens = b.lens; d.table = b.table;
     d.stride = b.table_stride;
     d.pages = (int)b.pages; d.rows = (int)b.page_rows; d.slots = (int)b.slots; d.cols = (int)b.table_cols;
     d.cap = (int)(b.table_cols * b.page_rows);
@@ -99,6 +99,9 @@ size_t fork_bytes(const cudallm_page_book &b, int64_t n) { return (size_t)(cdiv(
 
 bool list_size(int64_t n) { return n >= 0 && n <= kMaxList; }
 bool scratch_short(const void *scratch, size_t have, size_t need) { return !scratch || off(scratch, 16) || have < need; }
+
+// CTAs of a cluster for so many CTAs' worth of work: one, two, four or eight.
+int64_t cluster_for(int64_t ctas) { return ctas <= 1 ? 1 : ctas <= 2 ? 2 : ctas <= 4 ? 4 : kBookCluster; }
 
 // The copies (and, for compaction, the table) of up to kPoolsPerLaunch pools a launch.
 int copy_pools(CopyParams p, const cudallm_page_pool *pools, int64_t count, cudaStream_t stream)
@@ -169,10 +172,9 @@ int cudallm_pages_fork(const cudallm_page_book *book, const int32_t *src, const 
     p.src = src; p.dst = dst; p.n = (int)n;
     p.staged_len = static_cast<int *>(scratch);
     p.staged = p.staged_len + cdiv(n, 4) * 4;
-    cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    const dim3 grid((unsigned)std::min<int64_t>(n, 8 * kPlanSms));
-    st = rt_launch(fork_stage_kernel, grid, 256, 0, stream, p);
-    return st != CUDALLM_OK ? st : rt_launch(fork_put_kernel, grid, 256, 0, stream, p);
+    p.chunks = (int)std::max<int64_t>(1, cdiv(book->table_cols, kForkCols));
+    const int64_t ctas = cluster_for(cdiv(n * p.chunks, kBookThreads / 32));
+    return rt_launch_cluster(pages_fork_kernel, dim3((unsigned)ctas), (unsigned)ctas, kBookThreads, 0, static_cast<cudaStream_t>(stream_v), p);
 }
 
 size_t cudallm_pages_resize_scratch_bytes(const cudallm_page_book *book, int64_t n)
@@ -201,8 +203,9 @@ int cudallm_pages_resize(const cudallm_page_book *book, const cudallm_page_pool 
     p.count = w + at.count; p.src = w + at.src; p.dst = w + at.dst; p.state = w + at.state; p.start = w + at.start;
     p.fresh = w + at.fresh; p.claims = w + at.claims; p.claimer = w + at.claimer;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>(cdiv(n, kBookThreads / kEntryLanes), 64));
-    st = rt_launch(pages_resize_kernel, dim3((unsigned)ctas), kBookThreads, 0, stream, p);
+    const int64_t ctas = cluster_for(cdiv(n, kBookThreads / kEntryLanes));
+    st = rt_launch_cluster(n <= kBookThreads ? pages_resize_kernel<true> : pages_resize_kernel<false>, dim3((unsigned)ctas),
+                           (unsigned)ctas, kBookThreads, 0, stream, p);
     if (st != CUDALLM_OK || count == 0 || n == 0 || book->pages == 0) return st;
     CopyParams c{};
     c.src = p.src; c.dst = p.dst; c.count = p.count; c.n = n; c.pages = p.book.pages;

@@ -8,12 +8,13 @@
 #include <stdint.h>
 
 #include "../../include/cudallm_cache.h"
+#include "mma_sync.cuh"
 #include "ptx.cuh"
 
 namespace cudallm {
 
 struct Book {
-    int *refs, *lens, *table, *turn;
+    int *refs, *lens, *table;
     long long stride;
     int pages, rows, slots, cols, cap;         // cap: states that a row of the table holds
 };
@@ -84,68 +85,78 @@ pages_copy_kernel(const CopyParams p, const __grid_constant__ PoolList pools)
 }
 
 // --------------------------------------------------------------------- fork --
-// Two launches, since a slot may be read by one entry and overwritten by another: the sources' rows go to scratch and
-// their pages get one holder more; then the old rows are given up and the new ones put in.  One CTA an entry.
+constexpr int kBookThreads = 1024;
+constexpr int kBookCluster = 8;                // CTAs of a launch that changes a book, at most: one cluster
+
 struct ForkParams {
     Book book;
     const int *src, *dst;
     int n;
     int *staged_len;                           // n: the length that dst[i] gets, -1: entry i changes nothing
     int *staged;                               // n rows of cols page numbers
+    int chunks;                                // pieces of kForkCols columns in a row of the table
 };
-__global__ void __launch_bounds__(256)
-fork_stage_kernel(const ForkParams p)
+constexpr int kForkCols = 256;
+
+// A slot may be read by one entry and overwritten by another, so the sources' rows first go to scratch, their pages
+// getting one holder more; then, behind a barrier of the whole cluster, the old rows are given up and the
+// new ones put in.  A warp works on 256 columns of an entry at a time.
+__global__ void __launch_bounds__(kBookThreads, 1)
+pages_fork_kernel(const ForkParams p)
 {
     grid_launch_dependents();
     grid_dependency_wait();
     const Book &bk = p.book;
-    for (int i = blockIdx.x; i < p.n; i += gridDim.x) {
+    const int lane = threadIdx.x & 31, warp = (blockIdx.x * kBookThreads + threadIdx.x) >> 5, warps = gridDim.x * kBookThreads / 32;
+    const long long tasks = (long long)p.n * p.chunks;
+    for (long long k = warp; k < tasks; k += warps) {
+        const int i = (int)(k / p.chunks), c0 = (int)(k - (long long)i * p.chunks) * kForkCols;
         const int src = p.src[i], dst = p.dst[i];
-        bool live = (unsigned)src < (unsigned)bk.slots && (unsigned)dst < (unsigned)bk.slots;
-        if (live) {                                                // (the same for all threads)
-            bool first = true;
-            for (int j = threadIdx.x; j < i; j += 256) first &= !(p.dst[j] == dst && (unsigned)p.src[j] < (unsigned)bk.slots);
-            live = __syncthreads_and(first) && src != dst;
-        }
-        const int len = live ? book_len(bk, src) : -1;
-        if (threadIdx.x == 0) p.staged_len[i] = len;
+        bool live = (unsigned)src < (unsigned)bk.slots && (unsigned)dst < (unsigned)bk.slots && src != dst;
+        const int len = live ? book_len(bk, src) : -1, held = live ? pages_of(bk, len) : 0;
+        if (c0 > 0 && c0 >= held) continue;
+        for (int j = lane; j < i && live; j += 32) live = !(p.dst[j] == dst && (unsigned)p.src[j] < (unsigned)bk.slots);
+        live = __all_sync(0xffffffffu, live);
+        if (c0 == 0 && lane == 0) p.staged_len[i] = live ? len : -1;
         if (!live) continue;
-        const int held = pages_of(bk, len);
         const int *row = bk.table + src * bk.stride;
         int *to = p.staged + (long long)i * bk.cols;
-        for (int c = threadIdx.x; c < held; c += 256) {
+#pragma unroll
+        for (int m = 0; m < kForkCols / 32; ++m) {
+            const int c = c0 + m * 32 + lane;
+            if (c >= held) break;
             const int page = row[c];
             to[c] = page;
             if (is_page(bk, page)) atomicAdd(bk.refs + page, 1);
         }
     }
-}
-__global__ void __launch_bounds__(256)
-fork_put_kernel(const ForkParams p)
-{
-    grid_launch_dependents();
-    grid_dependency_wait();
-    const Book &bk = p.book;
-    for (int i = blockIdx.x; i < p.n; i += gridDim.x) {
-        const int len = p.staged_len[i];
+    cluster_sync_all();
+    for (long long k = warp; k < tasks; k += warps) {
+        const int i = (int)(k / p.chunks), c0 = (int)(k - (long long)i * p.chunks) * kForkCols;
+        const int len = __ldcg(p.staged_len + i);
         if (len < 0) continue;
         const int dst = p.dst[i], had = pages_of(bk, book_len(bk, dst)), held = pages_of(bk, len);
         int *row = bk.table + dst * bk.stride;
         const int *from = p.staged + (long long)i * bk.cols;
-        for (int c = threadIdx.x; c < max(had, held); c += 256) {
+#pragma unroll
+        for (int m = 0; m < kForkCols / 32; ++m) {
+            const int c = c0 + m * 32 + lane;
+            if (c >= max(had, held)) break;
             if (c < had) {
                 const int page = row[c];
                 if (is_page(bk, page)) atomicSub(bk.refs + page, 1);
             }
-            if (c < held) row[c] = from[c];
+            if (c < held) row[c] = __ldcg(from + c);
         }
-        __syncthreads();                                           // every thread has read the old length
-        if (threadIdx.x == 0) bk.lens[dst] = len;
+    }
+    cluster_sync_all();                                            // every warp has read the old lengths
+    for (int i = blockIdx.x * kBookThreads + threadIdx.x; i < p.n; i += gridDim.x * kBookThreads) {
+        const int len = __ldcg(p.staged_len + i);
+        if (len >= 0) bk.lens[p.dst[i]] = len;
     }
 }
 
 // -------------------------------------------------- counting within a block --
-constexpr int kBookThreads = 1024;
 // Sum of v over the threads below this one; total: over all.  All of the block's 1024 threads call it.
 __device__ __forceinline__ long long block_before(long long v, long long &total)
 {
@@ -217,104 +228,184 @@ struct ResizeParams {
 };
 constexpr int kEntryLanes = 8;                 // lanes that work on an entry together
 
-__device__ __forceinline__ int slot_at(const ResizeParams &p, int i) { return p.slot_of ? p.slot_of[i] : i; }
+struct ResizeEntry {
+    int slot, want, state;                     // (as in the scratch)
+    int tail;                                  // the page that its new tokens go into, if others hold it too; -1: none
+};
 
-// First all CTAs give back the pages of sequences that become shorter; the last of them to be done does the rest, which
+// Which of several entries with one key (a slot, a page) comes first, and how many there are: a table in shared memory for
+// the at most 1024 entries of a list that one thread each works on.
+struct KeyTable {
+    static constexpr int kSize = 2048;
+    int key[kSize], first[kSize], count[kSize];
+    __device__ __forceinline__ void clear()
+    {
+        for (int i = threadIdx.x; i < kSize; i += kBookThreads) {
+            key[i] = -1;
+            first[i] = 0x7fffffff;
+            count[i] = 0;
+        }
+    }
+    __device__ __forceinline__ int add(int k, int entry)
+    {
+        int at = (unsigned)k * 2654435761u >> 21;
+        for (;; at = (at + 1) % kSize) {                           // (half of the places stay free)
+            const int old = atomicCAS(key + at, -1, k);
+            if (old == -1 || old == k) break;
+        }
+        atomicMin(first + at, entry);
+        atomicAdd(count + at, 1);
+        return at;
+    }
+};
+
+// First all CTAs of the cluster give back the pages of sequences that become shorter; then the first does the rest, which
 // has an order: shared tails, how many pages are needed, which are free, who gets which.  If they do not suffice, it
-// takes what was given back again.
-__global__ void __launch_bounds__(kBookThreads)
+// takes what was given back again.  ONE: up to 1024 entries, a thread each, in registers and shared
+// memory; longer lists go through the scratch.
+template <bool ONE>
+__global__ void __launch_bounds__(kBookThreads, 1)
 pages_resize_kernel(const ResizeParams p)
 {
+    __shared__ KeyTable table;
+    __shared__ int s_slot[ONE ? kBookThreads : 1], s_want[ONE ? kBookThreads : 1], s_state[ONE ? kBookThreads : 1];
+    const Book &bk = p.book;
+    const int tid = threadIdx.x, sub = tid % kEntryLanes, groups = kBookThreads / kEntryLanes;
+    if constexpr (ONE) {
+        table.clear();
+        __syncthreads();
+    }
     grid_launch_dependents();
     grid_dependency_wait();
-    const Book &bk = p.book;
-    const int tid = threadIdx.x, sub = tid % kEntryLanes;
-    const int groups = kBookThreads / kEntryLanes;
-    const unsigned quad = 0xffu << (tid & 31 & ~(kEntryLanes - 1));        // the lanes of this thread's entry
-    for (int i = blockIdx.x * groups + tid / kEntryLanes; i < p.n; i += gridDim.x * groups) {
-        const int slot = slot_at(p, i), want = p.want[i];
-        int state = -1;
-        if ((unsigned)slot < (unsigned)bk.slots && want >= 0) {
-            bool first = true;
-            if (p.slot_of)
-                for (int j = sub; j < i; j += kEntryLanes) first &= !(p.slot_of[j] == slot && p.want[j] >= 0);
-            if (__all_sync(quad, first)) {
-                const int len = book_len(bk, slot);
-                state = want > bk.cap ? -2 : len;
-                if (want < len) {
-                    const int *row = bk.table + slot * bk.stride;
-                    const int had = pages_of(bk, len);
-                    for (int c = pages_of(bk, want) + sub; c < had; c += kEntryLanes)
-                        if (is_page(bk, row[c])) atomicSub(bk.refs + row[c], 1);
-                }
+    // gives back (sign -1), or takes again, the pages behind an entry's new end
+    auto give = [&](int slot, int want, int state, int sign) {
+        const int *row = bk.table + slot * bk.stride;
+        const int had = pages_of(bk, state);
+        for (int c = pages_of(bk, want) + sub; c < had; c += kEntryLanes)
+            if (is_page(bk, row[c])) atomicAdd(bk.refs + row[c], sign);
+    };
+    auto slot_at = [&](int i) { return p.slot_of ? p.slot_of[i] : i; };
+    ResizeEntry mine{-1, 0, -1, -1};
+    bool gives = false;
+    if constexpr (ONE) {
+        int place = -1;
+        if (tid < p.n) {
+            mine.slot = slot_at(tid);
+            mine.want = p.want[tid];
+            if ((unsigned)mine.slot < (unsigned)bk.slots && mine.want >= 0) {
+                mine.state = mine.want > bk.cap ? -2 : book_len(bk, mine.slot);
+                if (p.slot_of) place = table.add(mine.slot, tid);
             }
         }
-        if (sub == 0) p.state[i] = state;
+        __syncthreads();
+        if (place >= 0 && table.first[place] != tid) mine.state = -1;
+        s_slot[tid] = mine.slot;
+        s_want[tid] = mine.want;
+        s_state[tid] = mine.state;
+        gives = __syncthreads_or(mine.state > mine.want && pages_of(bk, mine.state) > pages_of(bk, mine.want));
+        table.clear();
+        if (gives)
+            for (int i = blockIdx.x * groups + tid / kEntryLanes; i < p.n; i += gridDim.x * groups)
+                if (s_state[i] > s_want[i]) give(s_slot[i], s_want[i], s_state[i], -1);
+    } else {
+        const unsigned quad = 0xffu << (tid & 31 & ~(kEntryLanes - 1));    // the lanes of this thread's entry
+        for (int i = blockIdx.x * groups + tid / kEntryLanes; i < p.n; i += gridDim.x * groups) {
+            const int slot = slot_at(i), want = p.want[i];
+            int state = -1;
+            if ((unsigned)slot < (unsigned)bk.slots && want >= 0) {
+                bool first = true;
+                if (p.slot_of)
+                    for (int j = sub; j < i; j += kEntryLanes) first &= !(p.slot_of[j] == slot && p.want[j] >= 0);
+                if (__all_sync(quad, first)) {
+                    state = want > bk.cap ? -2 : book_len(bk, slot);
+                    if (state > want) give(slot, want, state, -1);
+                }
+            }
+            if (sub == 0) p.state[i] = state;
+        }
+        gives = true;
     }
     if (gridDim.x > 1) {
-        __shared__ bool last;
         __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-            last = atomicAdd(bk.turn, 1) == (int)gridDim.x - 1;
-            if (last) *bk.turn = 0;
-            __threadfence();
-        }
-        __syncthreads();
-        if (!last) return;
-    } else {
+        cluster_sync_all();
+        if (blockIdx.x != 0) return;
+    } else if (gives) {
         __threadfence();
-        __syncthreads();
     }
+    __syncthreads();
 
-    // the tail that an entry's new tokens go into, if others hold it too; -1: none
-    auto shared_tail = [&](int i, int state) {
-        if (state <= 0 || p.want[i] <= state || state % bk.rows == 0) return -1;
-        const int page = bk.table[slot_at(p, i) * bk.stride + pages_of(bk, state) - 1];
+    auto find_tail = [&](const ResizeEntry &e) {
+        if (e.state <= 0 || e.want <= e.state || e.state % bk.rows == 0) return -1;
+        const int page = bk.table[e.slot * bk.stride + pages_of(bk, e.state) - 1];
         return is_page(bk, page) && refs_now(bk, page) > 1 ? page : -1;
     };
-    bool tails = false, too_long = false;
-    for (int i = tid; i < p.n; i += kBookThreads) {
-        const int state = __ldcg(p.state + i), page = shared_tail(i, state);
-        too_long |= state == -2;
-        if (page >= 0) {
+    auto each = [&](auto f) {
+        if constexpr (ONE) {
+            if (tid < p.n) f(tid, mine);
+        } else {
+            for (int i = tid; i < p.n; i += kBookThreads) {
+                ResizeEntry e{slot_at(i), p.want[i], __ldcg(p.state + i), -1};
+                e.tail = find_tail(e);
+                f(i, e);
+            }
+        }
+    };
+    // growing sequences that share a tail: how many, and the first of them
+    bool too_long = false, tails = false;
+    int claim = -1;                                                // (ONE: this entry's place in the table)
+    if constexpr (ONE) {
+        mine.tail = find_tail(mine);
+        too_long = mine.state == -2;
+        if (mine.tail >= 0) claim = table.add(mine.tail, tid);
+        __syncthreads();
+    } else {
+        each([&](int, ResizeEntry &e) {
+            too_long |= e.state == -2;
+            if (e.tail < 0) return;
             tails = true;
-            __stcg(p.claims + page, 0);
-            __stcg(p.claimer + page, 0x7fffffff);
+            __stcg(p.claims + e.tail, 0);
+            __stcg(p.claimer + e.tail, 0x7fffffff);
+        });
+        tails = __syncthreads_or(tails);
+        if (tails) {
+            __threadfence();
+            __syncthreads();
+            each([&](int i, ResizeEntry &e) {
+                if (e.tail < 0) return;
+                atomicAdd(p.claims + e.tail, 1);
+                atomicMin(p.claimer + e.tail, i);
+            });
+            __threadfence();
+            __syncthreads();
         }
-    }
-    tails = __syncthreads_or(tails);
-    if (tails) {
-        __threadfence();
-        __syncthreads();
-        for (int i = tid; i < p.n; i += kBookThreads) {
-            const int page = shared_tail(i, __ldcg(p.state + i));
-            if (page < 0) continue;
-            atomicAdd(p.claims + page, 1);
-            atomicMin(p.claimer + page, i);
-        }
-        __threadfence();
-        __syncthreads();
     }
     // new pages and copies of the entries before each
     long long need = 0;
+    int start = 0, copy = 0;                                       // (ONE: of this entry)
     for (int base = 0; base < p.n; base += kBookThreads) {
         const int i = base + tid;
-        int pages = 0, copy = 0, page = -1;
-        if (i < p.n) {
-            const int state = __ldcg(p.state + i);
-            page = tails ? shared_tail(i, state) : -1;
-            copy = page >= 0 && !(__ldcg(p.claims + page) == refs_now(bk, page) && __ldcg(p.claimer + page) == i);
-            if (state >= 0) pages = min(copy + max(pages_of(bk, p.want[i]) - pages_of(bk, state), 0), bk.pages + 1);
+        ResizeEntry e{-1, 0, -1, -1};
+        if constexpr (ONE) {
+            e = mine;
+        } else if (i < p.n) {
+            e = ResizeEntry{slot_at(i), p.want[i], __ldcg(p.state + i), -1};
+            if (tails) e.tail = find_tail(e);
         }
+        int pages = 0;
+        copy = 0;
+        if (e.tail >= 0) {
+            const int sharers = ONE ? table.count[claim] : __ldcg(p.claims + e.tail);
+            const int first = ONE ? table.first[claim] : __ldcg(p.claimer + e.tail);
+            copy = !(sharers == refs_now(bk, e.tail) && first == i);
+        }
+        if (e.state >= 0) pages = min(copy + max(pages_of(bk, e.want) - pages_of(bk, e.state), 0), bk.pages + 1);
         long long total;
         const long long before = need + block_before(pack2(pages, copy), total);
-        if (i < p.n) {
-            p.start[i] = (int)(low_of(before) & 0x7fffffff) | (copy ? (int)0x80000000 : 0);
-            if (copy) {                                            // (where the copy goes is filled in below)
-                p.src[high_of(before)] = page;
-                p.dst[high_of(before)] = i;
-            }
+        start = (int)(low_of(before) & 0x7fffffff);
+        if (!ONE && i < p.n) p.start[i] = start | (copy ? (int)0x80000000 : 0);
+        if (copy) {                                                // (where the copy goes is filled in below)
+            p.src[high_of(before)] = e.tail;
+            p.dst[high_of(before)] = start;
         }
         need += total;
     }
@@ -331,29 +422,26 @@ pages_resize_kernel(const ResizeParams p)
             for (; free; free &= free - 1) p.fresh[at++] = first + __ffs(free) - 1;
             found += (int)total;
         }
-    __threadfence();
-    __syncthreads();
+    __syncthreads();                                               // (this CTA reads what it has written)
     const bool done = !refused && found >= pages;
     if (tid == 0) {
         if (p.result) *p.result = refused ? -1 : done ? 0 : (int)min(pages - found, 0x7fffffffLL);
         *p.count = done ? copies : 0;
     }
-    for (int i = tid / kEntryLanes; i < p.n; i += groups) {
-        const int state = __ldcg(p.state + i);
-        if (state == -1) continue;
-        const int slot = slot_at(p, i), want = p.want[i];
-        int *row = bk.table + slot * bk.stride;
-        if (!done) {
-            if (state >= 0)
-                for (int c = pages_of(bk, want) + sub; c < pages_of(bk, state); c += kEntryLanes)
-                    if (is_page(bk, row[c])) atomicAdd(bk.refs + row[c], 1);
-            continue;
+    if (!done) {
+        for (int i = tid / kEntryLanes; i < p.n && gives; i += groups) {
+            const int state = ONE ? s_state[i] : __ldcg(p.state + i), want = ONE ? s_want[i] : p.want[i];
+            if (state >= 0) give(ONE ? s_slot[i] : slot_at(i), want, state, 1);
         }
-        const int mark = p.start[i], had = pages_of(bk, state), held = pages_of(bk, want);
-        const int copy = mark < 0, start = mark & 0x7fffffff;
+        return;
+    }
+    // Every entry's lanes put in its new pages.  (ONE: what its thread knows goes round by shuffle.)
+    auto put = [&](int slot, int want, int state, int first, int takes) {
+        int *row = bk.table + slot * bk.stride;
+        const int had = pages_of(bk, state), held = pages_of(bk, want);
         if (sub == 0) {
-            if (copy) {
-                const int page = p.fresh[start];
+            if (takes) {
+                const int page = p.fresh[first];
                 atomicSub(bk.refs + row[had - 1], 1);
                 bk.refs[page] = 1;
                 row[had - 1] = page;
@@ -361,13 +449,26 @@ pages_resize_kernel(const ResizeParams p)
             bk.lens[slot] = want;
         }
         for (int c = had + sub; c < held; c += kEntryLanes) {
-            const int page = p.fresh[start + copy + c - had];
+            const int page = p.fresh[first + takes + c - had];
             row[c] = page;
             bk.refs[page] = 1;
         }
+    };
+    if constexpr (ONE) {
+        for (int k = 0; k < kEntryLanes; ++k) {                    // entry k of this thread's group of lanes
+            const int from = (tid & 31 & ~(kEntryLanes - 1)) + k;
+            const int slot = __shfl_sync(0xffffffffu, mine.slot, from), want = __shfl_sync(0xffffffffu, mine.want, from);
+            const int state = __shfl_sync(0xffffffffu, mine.state, from), first = __shfl_sync(0xffffffffu, start, from);
+            const int takes = __shfl_sync(0xffffffffu, copy, from);
+            if (state >= 0) put(slot, want, state, first, takes);
+        }
+    } else {
+        for (int i = tid / kEntryLanes; i < p.n; i += groups) {
+            const int state = __ldcg(p.state + i), mark = p.start[i];
+            if (state >= 0) put(slot_at(i), p.want[i], state, mark & 0x7fffffff, mark < 0);
+        }
     }
-    if (done)
-        for (int k = tid; k < copies; k += kBookThreads) p.dst[k] = p.fresh[p.start[p.dst[k]] & 0x7fffffff];
+    for (int k = tid; k < copies; k += kBookThreads) p.dst[k] = p.fresh[p.dst[k]];
 }
 
 // ------------------------------------------------------------------ compact --
@@ -381,7 +482,7 @@ struct CompactParams {
 };
 // One CTA.  Which pages are held goes to shared memory as bits in one pass over refs; the k-th held one above the
 // number of pages in use and the k-th free one below it become pair k.
-__global__ void __launch_bounds__(kBookThreads)
+__global__ void __launch_bounds__(kBookThreads, 1)
 pages_compact_kernel(const CompactParams p)
 {
     extern __shared__ uint16_t held[];

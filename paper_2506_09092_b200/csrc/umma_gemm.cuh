@@ -25,6 +25,7 @@
 // dp_tiles = 0 is plain split-K; dp_tiles = tiles - tiles % grid splits only the
 // ragged last wave of a launch so that it takes about 1/split_k of a tile's time.
 #pragma once
+#include "fast_div.cuh"
 #include "ptx.cuh"
 
 namespace cudallm {
@@ -37,29 +38,6 @@ constexpr int kEpiThreads = 128;
 
 // status detail codes: (role << 8) | barrier kind
 enum : int { kRoleProducer = 1, kRoleMma = 2, kRoleEpilogue = 3 };
-
-// Division of a 32-bit unsigned number by a divisor fixed on the host (1 <= d <
-// 2^31): q = (t + ((n - t) >> sh1)) >> sh2 with t = the high half of mul * n
-// (the round-up method for invariant divisors).  Exact for every 32-bit n.
-struct FastDiv {
-    uint32_t mul;
-    uint16_t sh1, sh2;
-};
-__device__ __forceinline__ uint32_t fast_div(uint32_t n, FastDiv d)
-{
-    const uint32_t t = __umulhi(d.mul, n);
-    return (t + ((n - t) >> d.sh1)) >> d.sh2;
-}
-inline FastDiv make_fast_div(uint32_t d)
-{
-    int l = 0;
-    while ((1ull << l) < d) ++l;                         // l = ceil(log2 d)
-    FastDiv f;
-    f.mul = static_cast<uint32_t>((((1ull << 32) * ((1ull << l) - d)) / d) + 1);
-    f.sh1 = static_cast<uint16_t>(l < 1 ? l : 1);
-    f.sh2 = static_cast<uint16_t>(l ? l - 1 : 0);
-    return f;
-}
 
 struct GemmParams {
     void *C;

@@ -112,7 +112,7 @@ def test_pool_refusals():
 
 
 def c_book(**k):
-    a = dict(refs=P, lens=P, table=P, turn=P, pages=100, page_rows=8, slots=6, table_cols=9, table_stride=9)
+    a = dict(refs=P, lens=P, table=P, pages=100, page_rows=8, slots=6, table_cols=9, table_stride=9)
     a.update(k)
 
     class Book:
@@ -132,8 +132,8 @@ def book_calls(book, n=4, **k):
 
 @pytest.mark.parametrize("change,status", [
     (dict(refs=None), B.ERR_INVALID_POINTER), (dict(lens=None), B.ERR_INVALID_POINTER), (dict(table=None), B.ERR_INVALID_POINTER),
-    (dict(turn=None), B.ERR_INVALID_POINTER), (dict(refs=P + 4), B.ERR_MISALIGNED), (dict(lens=P + 2), B.ERR_MISALIGNED),
-    (dict(table=P + 2), B.ERR_MISALIGNED), (dict(turn=P + 1), B.ERR_MISALIGNED),
+    (dict(refs=P + 4), B.ERR_MISALIGNED), (dict(lens=P + 2), B.ERR_MISALIGNED),
+    (dict(table=P + 2), B.ERR_MISALIGNED),
     (dict(pages=-1), B.ERR_INVALID_DIM), (dict(pages=(1 << 20) + 1), B.ERR_INVALID_DIM), (dict(page_rows=0), B.ERR_INVALID_DIM),
     (dict(slots=-1), B.ERR_INVALID_DIM), (dict(table_cols=-1), B.ERR_INVALID_DIM),
     (dict(table_cols=1 << 28, table_stride=1 << 28), B.ERR_INVALID_DIM),
@@ -147,7 +147,7 @@ def test_book_refusals(change, status):
 
 def test_book_call_refusals():
     book = c_book()
-    assert book_calls(book, n=-1)[:2] == book_calls(book, n=65537)[:2] == (B.ERR_INVALID_DIM,) * 2
+    assert book_calls(book, n=-1)[:2] == book_calls(book, n=16385)[:2] == (B.ERR_INVALID_DIM,) * 2
     for k in (dict(scratch=None), dict(scratch=P + 8), dict(scratch_bytes=15)):
         assert set(book_calls(book, **k)) == {B.ERR_WORKSPACE}
     assert B.pages_fork(book, None, P, 1, P, 1 << 30, check=False) == B.pages_fork(book, P, None, 1, P, 1 << 30, check=False) == B.ERR_INVALID_POINTER
@@ -186,7 +186,7 @@ def test_verify_refusals(change, status):
 
 
 def test_struct_layouts():
-    assert ctypes.sizeof(B.PagedShape) == 232 and ctypes.sizeof(B.CPagePool) == 24 and ctypes.sizeof(B.CPageBook) == 72
+    assert ctypes.sizeof(B.PagedShape) == 232 and ctypes.sizeof(B.CPagePool) == 24 and ctypes.sizeof(B.CPageBook) == 64
 
 
 # ------------------------------------------------------------- the binding --
@@ -265,7 +265,7 @@ def test_pools_and_books_of_tensors(monkeypatch):
             B.page_pools(bad)
     book = B.PageBook(7, 4, 3, 5, device="cpu")
     assert book.refs.shape == (7,) and book.lens.shape == (3,) and book.table.shape == (3, 5) and not book.data.any()
-    assert (book.c.refs - book.c.turn, book.c.lens - book.c.turn, book.c.table - book.c.turn) == (16, 48, 64)
+    assert (book.c.lens - book.c.refs, book.c.table - book.c.refs, book.c.refs) == (32, 48, book.data.data_ptr())
     with pytest.raises(ValueError, match="pools of 50 pages"):
         B.pages_resize(book, both, None, P, 1, None, P, 1 << 20)
     for name, k in (("src", dict(src=torch.zeros(2))), ("dst", dict(dst=torch.zeros(1, dtype=torch.int32)))):
