@@ -8,6 +8,7 @@
 
 #include "runtime.h"
 #include "paged_attn.cuh"
+#include "paged_tile.cuh"
 
 using namespace cudallm;
 
@@ -15,6 +16,7 @@ namespace {
 
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxElems = int64_t(1) << 46;          // of an operand, strides included
+constexpr int64_t kMaxTmaStride = int64_t(1) << 39;      // elements
 constexpr int64_t kPlanSms = 148;                        // the split is planned for this many SMs
 #ifndef PA_CB
 #define PA_CB 16
@@ -79,10 +81,20 @@ int check_shape(const cudallm_paged_shape *sp)
     return st;
 }
 
+// Whether TMA can bring the pools' pages into tiles (its strides are below 2^40 bytes).
+bool tile_pages(const cudallm_paged_shape &s)
+{
+    for (const auto *st : {&s.k_stride, &s.v_stride})
+        if ((s.pages > 1 && (*st)[0] >= kMaxTmaStride) || (s.page_rows > 1 && (*st)[1] >= kMaxTmaStride)
+            || (s.kv_heads > 1 && (*st)[2] >= kMaxTmaStride))
+            return false;
+    return !no_states(s) && paged_tile_pages(s.page_rows);
+}
+
 // How an attention call runs.
 struct Plan {
     bool wide;                  // head dims above 64
-    int mt, row_tiles;          // row tiles of 16 mt rows
+    int mt, row_tiles;          // row tiles of 16 mt rows; 0: of 128, by paged_tile_kernel
     int cluster;                // CTAs a cluster; 0: equal shares
     int ctas;
     size_t part_bytes, scratch;
@@ -90,22 +102,29 @@ struct Plan {
 Plan plan_attn(const cudallm_paged_shape &s)
 {
     Plan f{};
-    const int64_t rows = (s.q_heads / s.kv_heads) * s.q_rows;
+    const int64_t rows = (s.q_heads / s.kv_heads) * s.q_rows, cap = no_states(s) ? 0 : s.table_cols * s.page_rows;
     f.wide = s.head_dim > 64;
     f.mt = (int)std::min<int64_t>(4, cdiv(rows, 16));
     f.row_tiles = (int)cdiv(rows, 16 * f.mt);
-    const int64_t items = s.batch * s.kv_heads * f.row_tiles, full = 2 * kPlanSms;
-    const int64_t blocks = std::max<int64_t>(1, cdiv(no_states(s) ? 0 : s.table_cols * s.page_rows, f.wide ? 64 : 128));
-    const int64_t fits = std::min<int64_t>({int64_t(kPaCluster), full / std::max<int64_t>(items, 1), blocks});
+    int64_t items = s.batch * s.kv_heads * f.row_tiles, blocks = std::max<int64_t>(1, cdiv(cap, f.wide ? 64 : 128));
+    const int64_t fits = std::min<int64_t>({int64_t(kPaCluster), 2 * kPlanSms / std::max<int64_t>(items, 1), blocks});
     if (items <= kPlanSms && blocks <= kClusterBlocks * fits) {
         f.cluster = (int)std::max<int64_t>(1, fits);
         f.ctas = (int)(items * f.cluster);
-    } else {
-        f.ctas = (int)std::min<int64_t>(full, items * blocks);
-        const size_t slot = (size_t)16 * f.mt * ((f.wide ? 128 : 64) + 1) * sizeof(float);
-        f.part_bytes = 2 * (size_t)f.ctas * slot;
-        f.scratch = f.part_bytes + (size_t)f.ctas * kPaDesc * sizeof(int);
+        return f;
     }
+    int64_t full = 2 * kPlanSms, tile = 16 * f.mt;
+    if (f.mt > 1 && tile_pages(s)) {
+        f.mt = 0;
+        full = kPlanSms;
+        tile = kXaRows;
+        f.row_tiles = (int)cdiv(rows, tile);
+        items = s.batch * s.kv_heads * f.row_tiles;
+        blocks = std::max<int64_t>(1, cdiv(cap, kXaRows));
+    }
+    f.ctas = (int)std::min<int64_t>(full, items * blocks);
+    f.part_bytes = 2 * (size_t)f.ctas * (size_t)tile * ((f.wide ? 128 : 64) + 1) * sizeof(float);
+    f.scratch = f.part_bytes + (size_t)f.ctas * kPaDesc * sizeof(int);
     return f;
 }
 
@@ -118,25 +137,67 @@ inline PagedStrides page_strides(const int64_t (&s)[3]) { return PagedStrides{(l
 inline XaStrides pieces(const int64_t (&s)[3]) { return XaStrides{s[0] / 8, s[1] / 8, s[2] / 8}; }
 inline PagedStrides page_pieces(const int64_t (&s)[3]) { return PagedStrides{s[0] / 8, s[1] / 8, s[2] / 8}; }
 
+// Raises a kernel's limit of dynamic shared memory, once per device.
+template <typename Kernel>
+int allow_smem(Kernel kernel, int bytes, std::atomic<bool> (&done)[kRtMaxDevices], int dev)
+{
+    if (!done[dev].load(std::memory_order_relaxed)) {
+        RT_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        done[dev].store(true, std::memory_order_relaxed);
+    }
+    return CUDALLM_OK;
+}
+
+// Equal shares leave parts of items behind, to be joined.
+template <int DP, int ROWS, typename T>
+int join(const cudallm_paged_shape &s, const Plan &f, const PagedParams &p, cudaStream_t stream)
+{
+    if (f.ctas == 1) return CUDALLM_OK;
+    const int64_t rows = std::min<int64_t>(ROWS, (int64_t)p.group * s.q_rows);
+    return rt_launch(paged_join_kernel<DP, ROWS, T>, dim3((unsigned)f.ctas, (unsigned)cdiv(rows, 128 / (DP / 8))), 128, 0, stream, p);
+}
 template <int DP, int MT, typename T>
 int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
 {
     using L = PagedSmem<DP, MT>;
     static std::atomic<bool> done[kRtMaxDevices] = {};
-    if (!done[dev].load(std::memory_order_relaxed)) {
-        RT_CUDA_TRY(cudaFuncSetAttribute(paged_attn_kernel<DP, MT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes));
-        done[dev].store(true, std::memory_order_relaxed);
-    }
-    const int st = rt_launch_cluster(paged_attn_kernel<DP, MT, T>, dim3((unsigned)f.ctas), f.cluster ? (unsigned)f.cluster : 1u,
-                                     kPaThreads, (size_t)L::kBytes, stream, p);
-    if (st != CUDALLM_OK || f.cluster || f.ctas == 1) return st;
-    const int64_t rows = std::min<int64_t>(L::kRows, (int64_t)p.group * s.q_rows);
-    return rt_launch(paged_join_kernel<DP, MT, T>, dim3((unsigned)f.ctas, (unsigned)cdiv(rows, 128 / (DP / 8))), 128, 0, stream, p);
+    int st = allow_smem(paged_attn_kernel<DP, MT, T>, L::kBytes, done, dev);
+    if (st != CUDALLM_OK) return st;
+    st = rt_launch_cluster(paged_attn_kernel<DP, MT, T>, dim3((unsigned)f.ctas), f.cluster ? (unsigned)f.cluster : 1u,
+                           kPaThreads, (size_t)L::kBytes, stream, p);
+    return st != CUDALLM_OK || f.cluster ? st : join<DP, L::kRows, T>(s, f, p, stream);
+}
+// Tensor map of a pool: 64 columns of one key head of up to 128 rows of a page.
+int encode(CUtensorMap *tm, const void *base, bool f16, const cudallm_paged_shape &s, const int64_t (&st)[3])
+{
+    const uint64_t dims[4] = {(uint64_t)s.head_dim, (uint64_t)s.kv_heads, (uint64_t)s.page_rows, (uint64_t)s.pages};
+    const uint64_t bytes[3] = {(uint64_t)(s.kv_heads > 1 ? st[2] : 8) * 2, (uint64_t)(s.page_rows > 1 ? st[1] : 8) * 2,
+                               (uint64_t)(s.pages > 1 ? st[0] : 8) * 2};
+    return rt_encode_rows(tm, base, f16, dims, bytes, (int)std::min<int64_t>(s.page_rows, kXaRows));
+}
+template <int DP, typename T>
+int run_tile(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
+{
+    using L = PagedTileSmem<DP>;
+    static std::atomic<bool> done[kRtMaxDevices] = {};
+    int st = allow_smem(paged_tile_kernel<DP, T>, L::kBytes, done, dev);
+    if (st != CUDALLM_OK) return st;
+    const bool f16 = s.dtype == CUDALLM_F16;
+    CUtensorMap tk, tv;
+    if ((st = encode(&tk, p.k, f16, s, s.k_stride)) != CUDALLM_OK || (st = encode(&tv, p.v, f16, s, s.v_stride)) != CUDALLM_OK) return st;
+    PagedTileParams t{};
+    t.a = p;
+    if ((st = rt_attention_status_word(dev, &t.status)) != CUDALLM_OK) return st;
+    t.skip_loads = rt_take_skip_loads();
+    t.wait_limit_ns = rt_wait_limit_ns();
+    st = rt_launch(paged_tile_kernel<DP, T>, dim3((unsigned)f.ctas), kPtThreads, (size_t)L::kBytes, stream, tk, tv, t);
+    return st != CUDALLM_OK ? st : join<DP, L::kRows, T>(s, f, p, stream);
 }
 template <int DP, typename T>
 int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
 {
     switch (f.mt) {
+    case 0: return run_tile<DP, T>(s, f, p, dev, stream);
     case 1: return run<DP, 1, T>(s, f, p, dev, stream);
     case 2: return run<DP, 2, T>(s, f, p, dev, stream);
     case 3: return run<DP, 3, T>(s, f, p, dev, stream);

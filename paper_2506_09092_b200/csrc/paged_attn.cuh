@@ -708,6 +708,109 @@ __device__ __forceinline__ float paged_join_parts(const PagedParams &p, const ui
     return fmaf(mx, p.scale, logf(sum));
 }
 
+// Equal shares: all blocks of keys in one line, items in order, in each the key heads, in each the row tiles; a CTA's
+// share of it in pieces (segments) that each belong to one item, key head and row tile.
+template <int ROWS, int BLOCK> struct PagedSegments {
+    const PagedParams &p;
+    long long pos, end, rem;                   // the block behind the segment, the share's end, pos counted from the item's first block
+    PagedItem it;
+    int b, kvh, rt, blk0, blk1, blocks;        // blocks: of the item, key head and row tile
+
+    __device__ __forceinline__ explicit PagedSegments(const PagedParams &p_) : p(p_) {}
+    __device__ __forceinline__ static unsigned head_blocks(const PagedParams &p, const PagedItem &x)
+    {
+        unsigned n = 0;
+        for (int r = 0; r < p.row_tiles; ++r) n += paged_blocks(x, p.group, ROWS, r, BLOCK);
+        return n;
+    }
+    __device__ __forceinline__ static long long divide(long long a, unsigned d)
+    {
+        return a >> 32 ? a / d : (long long)((unsigned)a / d);
+    }
+    // How many blocks there are in all, and which item this CTA's share begins in: the first 128 threads count, `each` items
+    // a thread.  All of the CTA's threads call it; `smem` is free again afterwards.  per: blocks of a share.
+    __device__ __forceinline__ void locate(uint8_t *smem, long long &per)
+    {
+        long long *warp_sum = reinterpret_cast<long long *>(smem), &s_rem = warp_sum[kPaWarps];
+        int &s_item = *reinterpret_cast<int *>(warp_sum + kPaWarps + 1);
+        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, each = (p.batch + kPaThreads - 1) / kPaThreads;
+        long long sum = 0, upto = 0, total = 0;
+        if (tid < kPaThreads) {
+            for (int i = 0; i < each; ++i)
+                if (tid * each + i < p.batch) sum += (long long)head_blocks(p, paged_item(p, tid * each + i)) * p.kv_heads;
+            upto = sum;                                            // blocks of all threads up to this one
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const long long v = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += v;
+            }
+            if (lane == 31) warp_sum[warp] = upto;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kPaWarps; ++w) {
+            if (w < warp) upto += warp_sum[w];
+            total += warp_sum[w];
+        }
+        per = max(divide(total + gridDim.x - 1, gridDim.x), 1LL);
+        pos = blockIdx.x * per;
+        end = min(total, pos + per);
+        if (tid == 0) p.desc[blockIdx.x * kPaDesc] = 0;
+        if (tid < kPaThreads && pos < end && pos >= upto - sum && pos < upto) {
+            long long left = pos - (upto - sum);
+            int x = tid * each;
+            if (each > 1)
+                for (;; ++x) {
+                    const long long n = (long long)head_blocks(p, paged_item(p, x)) * p.kv_heads;
+                    if (left < n) break;
+                    left -= n;
+                }
+            s_item = x;
+            s_rem = left;
+        }
+        __syncthreads();
+        b = s_item;
+        rem = s_rem;
+        __syncthreads();
+    }
+    // The next segment; false: there are no more.
+    __device__ __forceinline__ bool next()
+    {
+        if (pos >= end) return false;
+        unsigned head;
+        for (;; ++b) {
+            it = paged_item(p, b);
+            head = head_blocks(p, it);
+            if (rem < (long long)head * p.kv_heads) break;
+            rem -= (long long)head * p.kv_heads;
+        }
+        kvh = (int)divide(rem, head);
+        blk0 = (int)(rem - (long long)kvh * head);
+        for (rt = 0; blk0 >= (blocks = paged_blocks(it, p.group, ROWS, rt, BLOCK)); ++rt) blk0 -= blocks;
+        blk1 = (int)min((long long)blocks, blk0 + (end - pos));
+        pos += blk1 - blk0;
+        rem += blk1 - blk0;
+        return true;
+    }
+    __device__ __forceinline__ int rows() const { return min(it.news * p.group - rt * ROWS, ROWS); }
+    __device__ __forceinline__ int key0() const { return blk0 * BLOCK; }
+    __device__ __forceinline__ int key_end() const { return min(paged_tile_seen(it, p.group, ROWS, rt), blk1 * BLOCK); }
+    // blocks that hold keys (a row tile that sees nothing has one that holds none)
+    __device__ __forceinline__ int live() const { return max(0, (key_end() - key0() + BLOCK - 1) / BLOCK); }
+    // keys below this are seen by every row
+    __device__ __forceinline__ int seen_lo() const { return paged_seen(it, rt * ROWS / p.group); }
+    __device__ __forceinline__ bool whole() const { return blk0 == 0 && blk1 == blocks; }
+    // The first of several parts of an item, key head and row tile says how many CTAs share them.
+    __device__ __forceinline__ void describe(long long per) const
+    {
+        int *d = p.desc + blockIdx.x * kPaDesc;
+        d[0] = (int)(divide(pos - blk1 + blocks - 1, (unsigned)min(per, 0xffffffffLL)) - blockIdx.x) + 1;
+        d[1] = b;
+        d[2] = kvh;
+        d[3] = rt;
+    }
+};
+
 template <int DP, int MT, typename T>
 __global__ void __launch_bounds__(kPaThreads, 2)
 paged_attn_kernel(const PagedParams p)
@@ -715,104 +818,43 @@ paged_attn_kernel(const PagedParams p)
     using L = PagedSmem<DP, MT>;
     constexpr int kChunks = DP / 8;
     extern __shared__ __align__(128) uint8_t smem[];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x;
     grid_launch_dependents();
     grid_dependency_wait();
 
-    PagedItem it;
-    int b = 0, kvh = 0, rt = 0, blk0 = 0, blk1 = 0, blocks = 0;
-    long long pos = 0, end = 0, rem = 0, per = 0;
-    auto item_blocks = [&](const PagedItem &x) {
-        long long n = 0;
-        for (int r = 0; r < p.row_tiles; ++r) n += paged_blocks(x, p.group, L::kRows, r, L::kBlock);
-        return n * p.kv_heads;
-    };
+    PagedSegments<L::kRows, L::kBlock> seg(p);
+    long long per = 1;
     const int cta = blockIdx.x, rank = p.cluster ? cta % p.cluster : 0;
-    if (p.cluster) {
+    if (p.cluster) {                                               // one segment: an equal share of the cluster's item
         int x = cta / p.cluster;
-        rt = x % p.row_tiles;
+        seg.rt = x % p.row_tiles;
         x /= p.row_tiles;
-        kvh = x % p.kv_heads;
-        b = x / p.kv_heads;
-        it = paged_item(p, b);
-        blocks = paged_blocks(it, p.group, L::kRows, rt, L::kBlock);
-        if (blocks == 0) return;                                   // (the whole cluster)
-        blk0 = (int)((long long)blocks * rank / p.cluster);
-        blk1 = (int)((long long)blocks * (rank + 1) / p.cluster);
+        seg.kvh = x % p.kv_heads;
+        seg.b = x / p.kv_heads;
+        seg.it = paged_item(p, seg.b);
+        seg.blocks = paged_blocks(seg.it, p.group, L::kRows, seg.rt, L::kBlock);
+        if (seg.blocks == 0) return;                               // (the whole cluster)
+        seg.blk0 = (int)((long long)seg.blocks * rank / p.cluster);
+        seg.blk1 = (int)((long long)seg.blocks * (rank + 1) / p.cluster);
     } else {
-        // Equal shares.  Items in order, in each the key heads, in each the row tiles, in each the blocks of keys: how
-        // many blocks there are in all, and which item this CTA's first one lies in (thread t counts `each` items).
-        long long *warp_sum = reinterpret_cast<long long *>(smem), &s_rem = warp_sum[kPaWarps];
-        int &s_item = *reinterpret_cast<int *>(warp_sum + kPaWarps + 1);
-        const int each = (p.batch + kPaThreads - 1) / kPaThreads;
-        long long sum = 0;
-        for (int i = 0; i < each; ++i)
-            if (tid * each + i < p.batch) sum += item_blocks(paged_item(p, tid * each + i));
-        long long upto = sum;                                      // blocks of all threads up to this one
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const long long v = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += v;
-        }
-        if (lane == 31) warp_sum[warp] = upto;
-        __syncthreads();
-        long long total = 0;
-#pragma unroll
-        for (int w = 0; w < kPaWarps; ++w) {
-            if (w < warp) upto += warp_sum[w];
-            total += warp_sum[w];
-        }
-        per = max((total + gridDim.x - 1) / gridDim.x, 1LL);
-        pos = cta * per;
-        end = min(total, pos + per);
-        if (tid == 0) p.desc[cta * kPaDesc] = 0;
-        if (pos >= end) return;
-        if (pos >= upto - sum && pos < upto) {
-            long long left = pos - (upto - sum);
-            int x = tid * each;
-            for (;; ++x) {
-                const long long n = item_blocks(paged_item(p, x));
-                if (left < n) break;
-                left -= n;
-            }
-            s_item = x;
-            s_rem = left;
-        }
-        __syncthreads();
-        b = s_item;
-        rem = s_rem;
-        __syncthreads();                                           // (copies land there next)
+        seg.locate(smem, per);
+        if (!seg.next()) return;
     }
-
     for (;;) {
-        if (!p.cluster) {
-            long long all;
-            for (;; ++b) {
-                it = paged_item(p, b);
-                all = item_blocks(it);
-                if (rem < all) break;
-                rem -= all;
-            }
-            const long long head = all / p.kv_heads;
-            kvh = (int)(rem / head);
-            blk0 = (int)(rem - kvh * head);
-            for (rt = 0; blk0 >= (blocks = paged_blocks(it, p.group, L::kRows, rt, L::kBlock)); ++rt) blk0 -= blocks;
-            blk1 = (int)min((long long)blocks, blk0 + (end - pos));
-        }
-        if constexpr (MT == 1) paged_walk_narrow<DP, T>(p, smem, it, b, kvh, rt, blk0, blk1);
-        else paged_walk_wide<DP, MT, T>(p, smem, it, b, kvh, rt, blk0, blk1);
+        if constexpr (MT == 1) paged_walk_narrow<DP, T>(p, smem, seg.it, seg.b, seg.kvh, seg.rt, seg.blk0, seg.blk1);
+        else paged_walk_wide<DP, MT, T>(p, smem, seg.it, seg.b, seg.kvh, seg.rt, seg.blk0, seg.blk1);
         // whole results leave at once, parts go to the cluster's or the call's scratch
-        const bool whole = blk0 == 0 && blk1 == blocks && p.cluster <= 1;
-        const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
-        float *slot = p.cluster ? reinterpret_cast<float *>(smem + L::kShare) : p.part + (2LL * cta + (blk0 == 0)) * L::kSlot;
+        const bool whole = seg.whole() && p.cluster <= 1;
+        const int rows = seg.rows();
+        float *slot = p.cluster ? reinterpret_cast<float *>(smem + L::kShare) : p.part + (2LL * cta + (seg.blk0 == 0)) * L::kSlot;
         for (int i = tid; i < rows * kChunks; i += kPaThreads) {
             const int r = i / kChunks, c = i % kChunks;
             float acc[8];
             const float lse = paged_join_parts<DP, MT>(p, smem, r, c, acc);
             if (whole) {
-                const int row = rt * L::kRows + r, t = row / p.group, h = kvh * p.group + row - t * p.group;
-                paged_store<T>(p, b, t, h, c, acc);
-                if (c == 0) paged_store_lse(p, b, t, h, lse);
+                const int row = seg.rt * L::kRows + r, t = row / p.group, h = seg.kvh * p.group + row - t * p.group;
+                paged_store<T>(p, seg.b, t, h, c, acc);
+                if (c == 0) paged_store_lse(p, seg.b, t, h, lse);
             } else {
                 float4 *dst = reinterpret_cast<float4 *>(slot + r * DP + c * 8);
                 dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
@@ -821,23 +863,15 @@ paged_attn_kernel(const PagedParams p)
             }
         }
         if (p.cluster) break;
-        if (tid == 0 && blk0 == 0 && !whole) {                     // the first of the parts: how many CTAs share it
-            int *d = p.desc + cta * kPaDesc;
-            d[0] = (int)((pos + blocks - 1) / per) - cta + 1;
-            d[1] = b;
-            d[2] = kvh;
-            d[3] = rt;
-        }
-        pos += blk1 - blk0;
-        rem += blk1 - blk0;
-        if (pos >= end) return;
+        if (tid == 0 && seg.blk0 == 0 && !whole) seg.describe(per);
+        if (!seg.next()) return;
         __syncthreads();                                           // the joining blocks have been read
     }
     if (p.cluster == 1) return;
 
     // the cluster's CTAs each write a share of the rows' pieces, from all of their results
     cluster_sync_all();
-    const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
+    const int rows = min(seg.it.news * p.group - seg.rt * L::kRows, L::kRows);
     const uint32_t at = smem_u32(smem) + L::kShare;
     for (int i = rank * kPaThreads + tid; i < rows * kChunks; i += p.cluster * kPaThreads) {
         const int r = i / kChunks, c = i % kChunks;
@@ -860,21 +894,20 @@ paged_attn_kernel(const PagedParams p)
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] *= inv;
-        const int row = rt * L::kRows + r, t = row / p.group, h = kvh * p.group + row - t * p.group;
-        paged_store<T>(p, b, t, h, c, acc);
-        if (c == 0) paged_store_lse(p, b, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
+        const int row = seg.rt * L::kRows + r, t = row / p.group, h = seg.kvh * p.group + row - t * p.group;
+        paged_store<T>(p, seg.b, t, h, c, acc);
+        if (c == 0) paged_store_lse(p, seg.b, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
     }
     cluster_sync_all();                                            // nobody's shared memory goes while it is read
 }
 
 // The parts of an item's key head and row tile that several CTAs worked on, added up in order: the first lies in slot 1 of
 // the CTA that it began in, the others in slot 0 of those after it.  blockIdx.x: that CTA; blockIdx.y: four rows.
-template <int DP, int MT, typename T>
+template <int DP, int ROWS, typename T>
 __global__ void __launch_bounds__(128)
 paged_join_kernel(const PagedParams p)
 {
-    using L = PagedSmem<DP, MT>;
-    constexpr int kChunks = DP / 8;
+    constexpr int kChunks = DP / 8, kSlot = ROWS * (DP + 1);
     grid_launch_dependents();
     grid_dependency_wait();
     const int cta = blockIdx.x;
@@ -882,18 +915,18 @@ paged_join_kernel(const PagedParams p)
     if (d.x == 0) return;
     const int news = paged_item(p, d.y).news;
     const int r = blockIdx.y * (128 / kChunks) + threadIdx.x / kChunks, c = threadIdx.x % kChunks;
-    const int row = d.w * L::kRows + r;
-    if (r >= L::kRows || row >= news * p.group) return;
-    const float *first = p.part + (2LL * cta + 1) * L::kSlot, *next = p.part + 2LL * (cta + 1) * L::kSlot;
+    const int row = d.w * ROWS + r;
+    if (r >= ROWS || row >= news * p.group) return;
+    const float *first = p.part + (2LL * cta + 1) * kSlot, *next = p.part + 2LL * (cta + 1) * kSlot;
     float mx = -INFINITY, sum = 0.f, acc[8] = {};
     for (int s0 = 0; s0 < d.x; s0 += 8) {
         float lse[8], top = mx;
         float4 v[8][2];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const float *src = s0 + s == 0 ? first : next + 2LL * (s0 + s - 1) * L::kSlot;
+            const float *src = s0 + s == 0 ? first : next + 2LL * (s0 + s - 1) * kSlot;
             const bool live = s0 + s < d.x;
-            lse[s] = live ? src[L::kRows * DP + r] : -INFINITY;
+            lse[s] = live ? src[ROWS * DP + r] : -INFINITY;
             if (live) {
                 v[s][0] = *reinterpret_cast<const float4 *>(src + r * DP + c * 8);
                 v[s][1] = *reinterpret_cast<const float4 *>(src + r * DP + c * 8 + 4);

@@ -27,6 +27,8 @@ int rt_encode_rows(CUtensorMap *tm, const void *base, bool f16, const uint64_t (
 unsigned long long rt_wait_limit_ns();
 bool rt_take_skip_loads();             // one-shot: the next attention launch loads nothing
 
+// Where the attention kernels of device `dev` (current) report a wait that ran out.
+int rt_attention_status_word(int dev, int **out);
 // Status word of the attention kernels on device `dev` (current): read, and cleared if it was set; left alone (`host`
 // too) where none of them has been launched.  Defined in xattn.cu.
 int rt_xattn_status(int dev, int (&host)[2]);

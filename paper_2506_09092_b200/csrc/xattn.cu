@@ -161,17 +161,6 @@ int encode(CUtensorMap *tm, const void *base, const void *other, bool f16, const
 
 std::atomic<int *> g_status_at[kRtMaxDevices] = {};      // g_xattn_status of each device that has launched a kernel which writes it
 
-int status_word(int dev, int **out)
-{
-    int *p = g_status_at[dev].load(std::memory_order_relaxed);
-    if (!p) {
-        RT_CUDA_TRY(cudaGetSymbolAddress(reinterpret_cast<void **>(&p), g_xattn_status));
-        g_status_at[dev].store(p, std::memory_order_relaxed);
-    }
-    *out = p;
-    return CUDALLM_OK;
-}
-
 // Raises a kernel's limit of dynamic shared memory, once per device.
 template <typename Kernel>
 int allow_smem(Kernel kernel, int bytes, std::atomic<bool> (&done)[kRtMaxDevices], int dev)
@@ -235,7 +224,7 @@ int run_fwd(const cudallm_xattn_shape &s, const FwdPlan &f, const void *q, const
         p.q_tiles = (int)cdiv(s.q_rows, 2 * kXaRows);
         p.splits = f.splits; p.tiles_per_split = (int)f.per_split;
         p.scale = s.scale; p.scale_log2 = scale_log2(s);
-        if ((st = status_word(dev, &p.status)) != CUDALLM_OK) return st;
+        if ((st = rt_attention_status_word(dev, &p.status)) != CUDALLM_OK) return st;
         p.skip_loads = rt_take_skip_loads();
         p.wait_limit_ns = rt_wait_limit_ns();
         st = rt_launch(xattn_fwd_kernel<DP, T>, dim3((unsigned)((int64_t)p.q_tiles * s.q_heads * s.batch), (unsigned)f.splits),
@@ -273,7 +262,7 @@ int run_bwd(const cudallm_xattn_shape &s, const void *q, const void *k, const vo
     p.group = (int)(s.q_heads / s.kv_heads); p.batch = (int)s.batch; p.head_dim = (int)s.head_dim;
     p.q_tiles = (int)cdiv(s.q_rows, kXaRows); p.kv_tiles = (int)cdiv(s.kv_rows, kXaRows);
     p.scale = s.scale; p.scale_log2 = scale_log2(s);
-    if ((st = status_word(dev, &p.status)) != CUDALLM_OK) return st;
+    if ((st = rt_attention_status_word(dev, &p.status)) != CUDALLM_OK) return st;
     p.wait_limit_ns = rt_wait_limit_ns();
     p.skip_loads = rt_take_skip_loads();
     if (s.q_rows > 0) {
@@ -306,6 +295,17 @@ int run_bwd(const cudallm_xattn_shape &s, const void *q, const void *k, const vo
 }  // namespace
 
 namespace cudallm {
+
+int rt_attention_status_word(int dev, int **out)
+{
+    int *p = g_status_at[dev].load(std::memory_order_relaxed);
+    if (!p) {
+        RT_CUDA_TRY(cudaGetSymbolAddress(reinterpret_cast<void **>(&p), g_xattn_status));
+        g_status_at[dev].store(p, std::memory_order_relaxed);
+    }
+    *out = p;
+    return CUDALLM_OK;
+}
 
 int rt_xattn_status(int dev, int (&host)[2])
 {

@@ -154,6 +154,21 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c)
     return d;
 }
 
+// The largest of 32 values; a NaN among them is the result.
+__device__ __forceinline__ float xa_max32(const uint32_t (&r)[32])
+{
+    float m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = max3_nan(__uint_as_float(r[i]), __uint_as_float(r[i + 4]), __uint_as_float(r[i + 8]));
+#pragma unroll
+    for (int k = 12; k < 28; k += 8)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = max3_nan(m[i], __uint_as_float(r[k + i]), __uint_as_float(r[k + 4 + i]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m[i] = max3_nan(m[i], __uint_as_float(r[28 + i]), __uint_as_float(r[28 + i]));
+    return max3_nan(max3_nan(m[0], m[1], m[2]), m[3], m[3]);
+}
+
 // 2^x by the special-function unit (relative error ~2^-22); -inf gives 0.
 __device__ __forceinline__ float xa_exp2(float x)
 {

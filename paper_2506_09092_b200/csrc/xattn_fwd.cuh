@@ -46,20 +46,6 @@ struct XaFwdParams {
     unsigned long long wait_limit_ns;
 };
 
-__device__ __forceinline__ float xa_max32(const uint32_t (&r)[32])
-{
-    float m[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = max3_nan(__uint_as_float(r[i]), __uint_as_float(r[i + 4]), __uint_as_float(r[i + 8]));
-#pragma unroll
-    for (int k = 12; k < 28; k += 8)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = max3_nan(m[i], __uint_as_float(r[k + i]), __uint_as_float(r[k + 4 + i]));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) m[i] = max3_nan(m[i], __uint_as_float(r[28 + i]), __uint_as_float(r[28 + i]));
-    return max3_nan(max3_nan(m[0], m[1], m[2]), m[3], m[3]);
-}
-
 template <int DP> struct XaFwdSmem {
     static constexpr int kTile = DP / 64 * kXaChunkBytes;
     static constexpr int kStages = DP == 128 ? 4 : 7;

@@ -91,6 +91,9 @@ def run(c, out, lse=None, scale=None, stream=None, scratch=None):
         scratch = torch.full((n + 64,), 0xFF, dtype=torch.uint8, device="cuda")
     B.paged_attn(shape, c.q, c.k, c.v, c.table, c.lens, c.slot_of, c.new_lens, out, lse, scratch, n,
                  stream or torch.cuda.current_stream())
+    if stream is None:
+        code, detail = B.device_status(torch.cuda.current_stream())
+        assert code == B.OK, hex(detail)
     assert bool((scratch[n:] == 0xFF).all())
 
 

@@ -52,15 +52,36 @@ def test_a_prompt(rows, cols):
     check(Cache([rows, rows + 77, rows - 13], rows, 6, 2, 64, "bf16", 16, cols=cols))
 
 
-def test_pages_that_are_not_there_are_left_out():
-    for cols in (None, 2000):
-        c = Cache([100, 64, 33, 16], 2, 4, 2, 64, "bf16", 16, cols=cols)
-        absent = [range(16, 32), range(0, 64), range(32, 33), []]
-        c.table[0, 1] = -1
-        c.table[1, :4] = c.k.shape[0]
-        c.table[2, 2] = 1 << 30
-        out, lse = check(c, absent=[list(a) for a in absent])
-        assert not out[1].any() and bool((lse[1] == float("-inf")).all())
+@pytest.mark.parametrize("rows,group", [(2, 2), (2, 20), (9, 8)])
+@pytest.mark.parametrize("cols", [None, 2000])
+def test_pages_that_are_not_there_are_left_out(cols, rows, group):
+    c = Cache([100, 64, 33, 16, 300], rows, 2 * group, 2, 64, "bf16", 16, cols=cols)
+    absent = [range(16, 32), range(0, 64), range(32, 33), [], [*range(0, 128), *range(288, 300)]]
+    c.table[0, 1] = -1
+    c.table[1, :4] = c.k.shape[0]
+    c.table[2, 2] = 1 << 30
+    c.table[4, :8] = -7
+    c.table[4, 18] = -1
+    out, lse = check(c, absent=[list(a) for a in absent])
+    assert not out[1].any() and bool((lse[1] == float("-inf")).all())
+
+
+@pytest.mark.parametrize("page_rows", [8, 16, 32, 64, 128, 256, 384, 24])
+@pytest.mark.parametrize("layout", ["rows", "heads", "joint", "padded"])
+@pytest.mark.parametrize("dim", [40, 64, 128])
+def test_many_rows_on_a_key_head(dim, layout, page_rows):
+    """Pages of all sizes that fill a tile, and one that does not."""
+    lens = [1000, 127, 0, 128, 129, 5, 400, 4000]
+    check(Cache(lens, 6, 16, 2, dim, "bf16", page_rows, layout, cols=cdiv(40000, page_rows), seed=page_rows))
+
+
+@pytest.mark.parametrize("batch,rows,hq,hk,dim", [(40, 3, 16, 2, 64), (3, 5, 128, 1, 128), (300, 2, 10, 1, 64), (1, 700, 3, 1, 128), (150, 17, 2, 2, 128)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_many_rows_equal_shares(dtype, batch, rows, hq, hk, dim):
+    """Shares that begin and end anywhere in an item; several row tiles; more items than threads that count them."""
+    lens = [max(0, 2000 // (1 + batch // 20) + rows - 37 * (i % 50)) for i in range(batch)]
+    news = [(i * 7) % (rows + 1) for i in range(batch)]
+    check(Cache(lens, rows, hq, hk, dim, dtype, 16, cols=1000, seed=batch, news=news))
 
 
 def test_lengths_beyond_the_table_and_below_zero():
@@ -137,9 +158,10 @@ def test_no_lse():
 STRIDE = 1 << 23                                       # 300 pages of it: the last lies 2.5e9 elements into its buffer
 
 
+@pytest.mark.parametrize("group", [4, 20])
 @pytest.mark.parametrize("cols", [150, 3000])
-def test_more_than_32_bits_of_offset(cols):
-    c = Cache([900, 1500, 2300], 2, 8, 2, 64, "bf16", 16, cols=cols, spare=5)
+def test_more_than_32_bits_of_offset(cols, group):
+    c = Cache([900, 1500, 2300], 2, 2 * group, 2, 64, "bf16", 16, cols=cols, spare=5)
     near = torch.empty_like(c.q)
     run(c, near)
     pages = c.k.shape[0]
@@ -275,6 +297,29 @@ def test_calls_overlap_on_two_streams():
     torch.cuda.synchronize()
     for a, b in zip(outs, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_waits_that_run_out(dim):
+    """Nothing is loaded, or the limit is far too short: the call ends, the status says so, the next one is right."""
+    c = Cache([3000, 700], 4, 32, 2, dim, "bf16", 16, cols=4000)
+    want, out = torch.empty_like(c.q), torch.empty_like(c.q)
+    run(c, want)
+    stream = torch.cuda.current_stream()
+    scratch = torch.full((B.paged_attn_scratch_bytes(c.shape(out)) + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+    try:
+        B.debug_set(B.DEBUG_WAIT_LIMIT_NS, 1_000_000)
+        B.debug_set(B.DEBUG_SKIP_NEXT_XATTN_LOADS, 1)
+        run(c, out, stream=stream, scratch=scratch)
+        assert B.device_status(stream)[0] == B.ERR_DEVICE_TIMEOUT
+        B.debug_set(B.DEBUG_WAIT_LIMIT_NS, 1)
+        for _ in range(20):
+            run(c, out, stream=stream, scratch=scratch)
+            assert B.device_status(stream)[0] in (B.OK, B.ERR_DEVICE_TIMEOUT)
+    finally:
+        B.debug_set(B.DEBUG_WAIT_LIMIT_NS, 0)
+    run(c, out)
+    assert torch.equal(out, want)
 
 
 def test_strides_of_sizes_of_one_do_not_matter():
