@@ -254,6 +254,7 @@ int cudallm_paged_attn(const cudallm_paged_shape *shape, const void *q, const vo
     p.pages = (int)s.pages; p.page_rows = (int)s.page_rows; p.slots = (int)s.slots;
     p.cap = states ? (int)(s.table_cols * s.page_rows) : 0;
     p.by_page_rows = make_fast_div((uint32_t)s.page_rows);
+    p.by_group = make_fast_div((uint32_t)p.group);
     p.row_tiles = f.row_tiles;
     p.cluster = f.cluster;
     p.scale = s.scale; p.scale_log2 = scale_log2(s.scale);

@@ -38,13 +38,14 @@ struct PagedParams {
     PagedStrides sk, sv;
     long long table_stride;
     int batch, q_rows, q_heads, kv_heads, group, head_dim;
+    FastDiv by_group;
     int pages, page_rows, slots, cap;          // cap: states that a row of the table holds
     FastDiv by_page_rows;
     int row_tiles;                             // tiles of 16 or 32 rows of an item and key head at most
     int cluster;                               // CTAs per item, key head and row tile; 0: equal shares
     float scale, scale_log2;
 };
-constexpr int kPaDesc = 4;                     // parts (0: none begins here), item, key head, row tile
+constexpr int kPaDesc = 4;                     // parts (0: none begins here) and 2^16 x rows, item, key head, row tile
 
 template <int DP, int MT> struct PagedSmem {
     static constexpr int kRows = 16 * MT;
@@ -86,14 +87,15 @@ __device__ __forceinline__ PagedItem paged_item(const PagedParams &p, int b)
 // States that token t sees; states that a row tile's last token sees; its blocks of keys (at least one, so that
 // somebody writes the result; none without rows).
 __device__ __forceinline__ int paged_seen(const PagedItem &it, int t) { return max(it.len - it.news + t + 1, 0); }
-__device__ __forceinline__ int paged_tile_seen(const PagedItem &it, int group, int rows, int rt)
+__device__ __forceinline__ int paged_token(const PagedParams &p, int row) { return (int)fast_div((uint32_t)row, p.by_group); }
+__device__ __forceinline__ int paged_tile_seen(const PagedParams &p, const PagedItem &it, int rows, int rt)
 {
-    return paged_seen(it, (min(it.news * group, (rt + 1) * rows) - 1) / group);
+    return paged_seen(it, paged_token(p, min(it.news * p.group, (rt + 1) * rows) - 1));
 }
-__device__ __forceinline__ int paged_blocks(const PagedItem &it, int group, int rows, int rt, int block)
+__device__ __forceinline__ int paged_blocks(const PagedParams &p, const PagedItem &it, int rows, int rt, int block)
 {
-    if (rt * rows >= it.news * group) return 0;
-    return max(1, (paged_tile_seen(it, group, rows, rt) + block - 1) / block);
+    if (rt * rows >= it.news * p.group) return 0;
+    return max(1, (int)((unsigned)(paged_tile_seen(p, it, rows, rt) + block - 1) / (unsigned)block));
 }
 
 // (as an instruction: a choice among registers must not become an address into a copy of them in local memory)
@@ -219,7 +221,7 @@ template <int DP, int MT, typename T> struct PagedLoader {
 template <typename T>
 __device__ __forceinline__ const T *paged_q_row(const PagedParams &p, int b, int kvh, int row)
 {
-    const int t = row / p.group, h = row - t * p.group;
+    const int t = paged_token(p, row), h = row - t * p.group;
     return static_cast<const T *>(p.q) + b * p.sq.b + t * p.sq.r + (long long)(kvh * p.group + h) * p.sq.h;
 }
 // The A operands of 16 rows from `row` on (up to `rows`): rows g and g + 8, columns 2 q, 2 q + 1 and + 8 of every 16.
@@ -254,8 +256,8 @@ __device__ __forceinline__ void paged_walk_narrow(const PagedParams &p, uint8_t 
     constexpr int kChunks = DP / 8, kKeys = L::kKeys, kN = kKeys / 8;      // kN: tiles of eight keys
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
-    const int seen_lo = paged_seen(it, rt * L::kRows / p.group);
-    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(it, p.group, L::kRows, rt), blk1 * L::kBlock);
+    const int seen_lo = paged_seen(it, paged_token(p, rt * L::kRows));
+    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(p, it, L::kRows, rt), blk1 * L::kBlock);
     const int ntiles = key_end > key0 ? (key_end - key0 + kKeys - 1) / kKeys : 0;
     const int mine = ntiles > warp ? (ntiles - warp + kPaWarps - 1) / kPaWarps : 0;         // tiles warp, warp + 4, ...
     const uint32_t ring = smem_u32(smem) + warp * L::kWarp;
@@ -274,7 +276,7 @@ __device__ __forceinline__ void paged_walk_narrow(const PagedParams &p, uint8_t 
     float o[DP / 8][4];
 #pragma unroll
     for (int half = 0; half < 2; ++half)
-        seen[half] = g + 8 * half < rows ? paged_seen(it, (rt * L::kRows + g + 8 * half) / p.group) : 0x7fffffff;
+        seen[half] = g + 8 * half < rows ? paged_seen(it, paged_token(p, rt * L::kRows + g + 8 * half)) : 0x7fffffff;
 #pragma unroll
     for (int n = 0; n < DP / 8; ++n)
 #pragma unroll
@@ -435,8 +437,8 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
     static_assert(L::kRows * kProb <= kAllTile, "where the keys were");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
-    const int seen_lo = paged_seen(it, rt * L::kRows / p.group);
-    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(it, p.group, L::kRows, rt), blk1 * L::kBlock);
+    const int seen_lo = paged_seen(it, paged_token(p, rt * L::kRows));
+    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(p, it, L::kRows, rt), blk1 * L::kBlock);
     const int tiles = key_end > key0 ? (key_end - key0 + L::kBlock - 1) / L::kBlock : 0;
     const uint32_t ring = smem_u32(smem), maxima = ring + L::kMax;
     Loader ld(p, it, kvh, ring + warp * L::kTile, key0 + warp * kKeys, key_end, tiles);
@@ -469,7 +471,7 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             const int r = i * 16 + g + 8 * half;
-            seen[i][half] = r < rows ? paged_seen(it, (rt * L::kRows + r) / p.group) : 0x7fffffff;
+            seen[i][half] = r < rows ? paged_seen(it, paged_token(p, rt * L::kRows + r)) : 0x7fffffff;
             m[i][half] = -INFINITY;
             l[i][half] = 0.f;
             any[i][half] = false;
@@ -720,7 +722,7 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     __device__ __forceinline__ static unsigned head_blocks(const PagedParams &p, const PagedItem &x)
     {
         unsigned n = 0;
-        for (int r = 0; r < p.row_tiles; ++r) n += paged_blocks(x, p.group, ROWS, r, BLOCK);
+        for (int r = 0; r < p.row_tiles; ++r) n += paged_blocks(p, x, ROWS, r, BLOCK);
         return n;
     }
     __device__ __forceinline__ static long long divide(long long a, unsigned d)
@@ -786,7 +788,7 @@ template <int ROWS, int BLOCK> struct PagedSegments {
         }
         kvh = (int)divide(rem, head);
         blk0 = (int)(rem - (long long)kvh * head);
-        for (rt = 0; blk0 >= (blocks = paged_blocks(it, p.group, ROWS, rt, BLOCK)); ++rt) blk0 -= blocks;
+        for (rt = 0; blk0 >= (blocks = paged_blocks(p, it, ROWS, rt, BLOCK)); ++rt) blk0 -= blocks;
         blk1 = (int)min((long long)blocks, blk0 + (end - pos));
         pos += blk1 - blk0;
         rem += blk1 - blk0;
@@ -794,17 +796,17 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     }
     __device__ __forceinline__ int rows() const { return min(it.news * p.group - rt * ROWS, ROWS); }
     __device__ __forceinline__ int key0() const { return blk0 * BLOCK; }
-    __device__ __forceinline__ int key_end() const { return min(paged_tile_seen(it, p.group, ROWS, rt), blk1 * BLOCK); }
+    __device__ __forceinline__ int key_end() const { return min(paged_tile_seen(p, it, ROWS, rt), blk1 * BLOCK); }
     // blocks that hold keys (a row tile that sees nothing has one that holds none)
-    __device__ __forceinline__ int live() const { return max(0, (key_end() - key0() + BLOCK - 1) / BLOCK); }
+    __device__ __forceinline__ int live() const { return (int)((unsigned)max(0, key_end() - key0() + BLOCK - 1) / (unsigned)BLOCK); }
     // keys below this are seen by every row
-    __device__ __forceinline__ int seen_lo() const { return paged_seen(it, rt * ROWS / p.group); }
+    __device__ __forceinline__ int seen_lo() const { return paged_seen(it, paged_token(p, rt * ROWS)); }
     __device__ __forceinline__ bool whole() const { return blk0 == 0 && blk1 == blocks; }
     // The first of several parts of an item, key head and row tile says how many CTAs share them.
     __device__ __forceinline__ void describe(long long per) const
     {
         int *d = p.desc + blockIdx.x * kPaDesc;
-        d[0] = (int)(divide(pos - blk1 + blocks - 1, (unsigned)min(per, 0xffffffffLL)) - blockIdx.x) + 1;
+        d[0] = ((int)(divide(pos - blk1 + blocks - 1, (unsigned)min(per, 0xffffffffLL)) - blockIdx.x) + 1) | rows() << 16;
         d[1] = b;
         d[2] = kvh;
         d[3] = rt;
@@ -832,7 +834,7 @@ paged_attn_kernel(const PagedParams p)
         seg.kvh = x % p.kv_heads;
         seg.b = x / p.kv_heads;
         seg.it = paged_item(p, seg.b);
-        seg.blocks = paged_blocks(seg.it, p.group, L::kRows, seg.rt, L::kBlock);
+        seg.blocks = paged_blocks(p, seg.it, L::kRows, seg.rt, L::kBlock);
         if (seg.blocks == 0) return;                               // (the whole cluster)
         seg.blk0 = (int)((long long)seg.blocks * rank / p.cluster);
         seg.blk1 = (int)((long long)seg.blocks * (rank + 1) / p.cluster);
@@ -852,7 +854,7 @@ paged_attn_kernel(const PagedParams p)
             float acc[8];
             const float lse = paged_join_parts<DP, MT>(p, smem, r, c, acc);
             if (whole) {
-                const int row = seg.rt * L::kRows + r, t = row / p.group, h = seg.kvh * p.group + row - t * p.group;
+                const int row = seg.rt * L::kRows + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
                 paged_store<T>(p, seg.b, t, h, c, acc);
                 if (c == 0) paged_store_lse(p, seg.b, t, h, lse);
             } else {
@@ -894,7 +896,7 @@ paged_attn_kernel(const PagedParams p)
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] *= inv;
-        const int row = seg.rt * L::kRows + r, t = row / p.group, h = seg.kvh * p.group + row - t * p.group;
+        const int row = seg.rt * L::kRows + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
         paged_store<T>(p, seg.b, t, h, c, acc);
         if (c == 0) paged_store_lse(p, seg.b, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
     }
@@ -913,19 +915,19 @@ paged_join_kernel(const PagedParams p)
     const int cta = blockIdx.x;
     const int4 d = *reinterpret_cast<const int4 *>(p.desc + cta * kPaDesc);
     if (d.x == 0) return;
-    const int news = paged_item(p, d.y).news;
+    const int parts = d.x & 0xffff, rows = d.x >> 16;
     const int r = blockIdx.y * (128 / kChunks) + threadIdx.x / kChunks, c = threadIdx.x % kChunks;
     const int row = d.w * ROWS + r;
-    if (r >= ROWS || row >= news * p.group) return;
+    if (r >= rows) return;
     const float *first = p.part + (2LL * cta + 1) * kSlot, *next = p.part + 2LL * (cta + 1) * kSlot;
     float mx = -INFINITY, sum = 0.f, acc[8] = {};
-    for (int s0 = 0; s0 < d.x; s0 += 8) {
+    for (int s0 = 0; s0 < parts; s0 += 8) {
         float lse[8], top = mx;
         float4 v[8][2];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             const float *src = s0 + s == 0 ? first : next + 2LL * (s0 + s - 1) * kSlot;
-            const bool live = s0 + s < d.x;
+            const bool live = s0 + s < parts;
             lse[s] = live ? src[ROWS * DP + r] : -INFINITY;
             if (live) {
                 v[s][0] = *reinterpret_cast<const float4 *>(src + r * DP + c * 8);
@@ -954,7 +956,7 @@ paged_join_kernel(const PagedParams p)
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= inv;
-    const int t = row / p.group, h = d.z * p.group + row - t * p.group;
+    const int t = paged_token(p, row), h = d.z * p.group + row - t * p.group;
     paged_store<T>(p, d.y, t, h, c, acc);
     if (c == 0) paged_store_lse(p, d.y, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
 }

@@ -156,27 +156,26 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     bool ok = true;
 
     if (warp >= kPtQueryWarp) {
-        constexpr int kOwn = kXaRows / kPtQueryWarps;
-        const int r0 = (warp - kPtQueryWarp) * kOwn;
         while (ok && seg.next()) {
             const int rows = seg.rows();
             if (seg.live() == 0) continue;
             if (segments > 0) ok = wait(q_empty, segments - 1);     // the segment before has formed its last scores
             if (!ok) break;
             // (rows that do not exist are the tensor core's own affair: they reach no other row's result)
-            constexpr int kBatch = 8, kRowStep = 32 / kChunks;     // loads in flight; rows that an instruction covers
-            const int c = lane % kChunks;
-            for (int r = r0 + lane / kChunks; r < min(rows, r0 + kOwn); r += kBatch * kRowStep) {
+            constexpr int kBatch = 8, kRowStep = 32 / kChunks * kPtQueryWarps;     // loads in flight; rows that both warps cover with one
+            const int c = lane % kChunks, row0 = seg.rt * L::kRows;
+            for (int r = lane / kChunks * kPtQueryWarps + warp - kPtQueryWarp; r < rows; r += kBatch * kRowStep) {
                 uint4 w[kBatch];
 #pragma unroll
                 for (int n = 0; n < kBatch; ++n) {
                     w[n] = make_uint4(0, 0, 0, 0);
                     if (r + n * kRowStep < rows && c * 8 < p.head_dim)
-                        w[n] = *reinterpret_cast<const uint4 *>(paged_q_row<T>(p, seg.b, seg.kvh, seg.rt * L::kRows + r + n * kRowStep) + c * 8);
+                        w[n] = *reinterpret_cast<const uint4 *>(paged_q_row<T>(p, seg.b, seg.kvh, row0 + r + n * kRowStep) + c * 8);
                 }
 #pragma unroll
                 for (int n = 0; n < kBatch; ++n)
-                    st_shared_v4_b32(sbase + tile_piece(r + n * kRowStep, c), w[n].x, w[n].y, w[n].z, w[n].w);
+                    if (r + n * kRowStep < rows)
+                        st_shared_v4_b32(sbase + tile_piece(r + n * kRowStep, c), w[n].x, w[n].y, w[n].z, w[n].w);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -277,9 +276,9 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         float *xch = reinterpret_cast<float *>(smem + L::kXch);
         while (ok && seg.next()) {
             const int blocks = seg.live(), rows = seg.rows(), key0 = seg.key0(), seen_lo = seg.seen_lo();
-            const int row = seg.rt * L::kRows + t, token = row / p.group, h = seg.kvh * p.group + row - token * p.group;
+            const int row = seg.rt * L::kRows + t, token = paged_token(p, row), h = seg.kvh * p.group + row - token * p.group;
             const bool mine = t < rows, warp_rows = (warp & 3) * 32 < rows;
-            const int seen = mine ? paged_seen(seg.it, token) : 0;
+            const int seen = mine ? paged_seen(seg.it, token) : 0x7fffffff;       // (rows that do not exist may see anything)
             float m = -INFINITY, l = 0.f;
             bool any = false;
             for (int i = 0; i < blocks; ++i, ++block) {
