@@ -44,7 +44,7 @@ __device__ __forceinline__ double cluster_ld_f64(uint32_t addr)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kVerifyThreads, 4)
+__global__ void __launch_bounds__(kVerifyThreads, 2)
 draft_verify_kernel(const VerifyParams p)
 {
     __shared__ double masses[kVerifyChunks], sums[kVerifyChunks], cta_sum;     // of each chunk; up to and with each; of all
@@ -59,22 +59,23 @@ draft_verify_kernel(const VerifyParams p)
     const int *drafts = p.drafts + (long long)b * p.n;
     const float *u = p.u + (long long)b * (p.n + 1);
     const int m = p.draft_lens ? min(max(p.draft_lens[b], 0), p.n) : p.n;
+    const double draw = (double)u[p.n];
     if (warp == 0) {
         int a = m;
-        for (int t0 = 0; t0 < m; t0 += 32) {
+        for (int t0 = 0; t0 < p.n; t0 += 32) {                     // (m is not waited for: the drafts behind it are looked at, too)
             const int t = t0 + lane;
-            bool good = true;
-            if (t < m) {
+            bool good = false;
+            if (t < p.n) {
                 const int x = drafts[t];
-                good = false;
+                const float ut = u[t];
                 if ((unsigned)x < (unsigned)p.vocab) {
                     const double qx = qq ? elem_to_double(qq[t * p.ldq + x]) : 1.0;
-                    good = (double)u[t] * qx < elem_to_double(pp[t * p.ldp + x]);
+                    good = (double)ut * qx < elem_to_double(pp[t * p.ldp + x]);
                 }
             }
             const uint32_t bad = __ballot_sync(0xffffffffu, !good);
             if (bad) {
-                a = t0 + __ffs(bad) - 1;
+                a = min(m, t0 + __ffs(bad) - 1);
                 break;
             }
         }
@@ -91,45 +92,55 @@ draft_verify_kernel(const VerifyParams p)
         return x > y && x < INFINITY && y > -INFINITY ? (double)x - (double)y : 0.0;
     };
     const T zero = elem_from_float<T>(0.f), one = elem_from_float<T>(1.f);
-    // element v of the row, v anywhere
-    auto mass_at = [&](long long v) {
-        return v < p.vocab ? mass(prow[v], v == certain ? one : qrow ? qrow[v] : zero) : 0.0;
-    };
-    // this lane's sum over 512 elements from `from` on
-    auto sum_of = [&](long long from) {
-        double s[4] = {};
-        if (from + kVerifyChunk <= p.vocab && !(certain >= from && certain < from + kVerifyChunk)) {
-            T pv[16], qv[16];
-            const T *ps = prow + from + lane;
+    // rows of 32 elements from `from` on, this lane's of each; the certain draft's probability is put in
+    auto load = [&](long long from, auto &pv, auto &qv) {
+        constexpr int kRows = sizeof pv / sizeof pv[0];
+        const T *ps = prow + from + lane, *qs = qrow + from + lane;
+        if (from + 32 * kRows <= p.vocab) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) pv[i] = ps[i * 32];
-            if (qrow) {
-                const T *qs = qrow + from + lane;
+            for (int i = 0; i < kRows; ++i) pv[i] = ps[i * 32];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) qv[i] = qs[i * 32];
-            } else {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) qv[i] = zero;
-            }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[i % 4] += mass(pv[i], qv[i]);
+            for (int i = 0; i < kRows; ++i) qv[i] = qrow ? qs[i * 32] : zero;
         } else {
+            const int left = (int)max(p.vocab - from, 0LL) - lane;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i % 4] += mass_at(from + i * 32 + lane);
+            for (int i = 0; i < kRows; ++i) pv[i] = i * 32 < left ? ps[i * 32] : zero;
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) qv[i] = qrow && i * 32 < left ? qs[i * 32] : zero;
         }
-        return (s[0] + s[1]) + (s[2] + s[3]);
+        if (certain >= from && certain < from + 32 * kRows) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+                if (from + i * 32 + lane == certain) qv[i] = one;
+        }
     };
 
-    const double draw = (double)u[p.n];
     double point, before;                                          // where in the sum of all; the sum of the CTAs before this one
     int owner;                                                     // the CTA that holds the point
     for (int pass = 0;; ++pass) {
-        for (int c = warp; c < p.chunks; c += kVerifyWarps) {
-            double s = 0.0;
-            for (int part = 0; part < p.chunk; part += kVerifyChunk) s += sum_of(((long long)rank * p.chunks + c) * p.chunk + part);
+        // a warp's chunks, each in parts of 512 elements; the next part is asked for before one is summed up
+        const int parts = p.chunk / kVerifyChunk, mine = p.chunks > warp ? ((p.chunks - warp - 1) / kVerifyWarps + 1) * parts : 0;
+        auto at = [&](int k) { return ((long long)rank * p.chunks + warp + k / parts * kVerifyWarps) * p.chunk + k % parts * kVerifyChunk; };
+        T pv[2][16], qv[2][16];
+        double s = 0.0;
+        if (mine > 0) load(at(0), pv[0], qv[0]);
+        for (int k0 = 0; k0 < mine; k0 += 2) {
 #pragma unroll
-            for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
-            if (lane == 0) masses[c] = s;
+            for (int h = 0; h < 2; ++h) {
+                const int k = k0 + h;
+                if (k + 1 < mine) load(at(k + 1), pv[h ^ 1], qv[h ^ 1]);
+                if (k >= mine) break;
+                double part[4] = {};
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[i % 4] += mass(pv[h][i], qv[h][i]);
+                s += (part[0] + part[1]) + (part[2] + part[3]);
+                if (k % parts == parts - 1) {
+#pragma unroll
+                    for (int d = 16; d; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+                    if (lane == 0) masses[warp + k / parts * kVerifyWarps] = s;
+                    s = 0.0;
+                }
+            }
         }
         __syncthreads();
         if (warp == 0) {
@@ -198,10 +209,12 @@ draft_verify_kernel(const VerifyParams p)
     constexpr int kRows = 8;
     bool found = false;
     for (int part = 0; part < p.chunk && !found; part += 32 * kRows) {
-        const long long from = ((long long)rank * p.chunks + c) * p.chunk + part + lane;
+        const long long from = ((long long)rank * p.chunks + c) * p.chunk + part;
+        T pv[kRows], qv[kRows];
+        load(from, pv, qv);
         double own[kRows], row[kRows];
 #pragma unroll
-        for (int i = 0; i < kRows; ++i) row[i] = own[i] = mass_at(from + i * 32);
+        for (int i = 0; i < kRows; ++i) row[i] = own[i] = mass(pv[i], qv[i]);
         // the sums of eight rows of 32, side by side; then the scan of the one that holds the point, or else the last with mass
         uint32_t there = 0;
 #pragma unroll
@@ -233,7 +246,7 @@ draft_verify_kernel(const VerifyParams p)
             if (lane >= d) s += x;
         }
         const uint32_t some = __ballot_sync(0xffffffffu, r > 0.0), over = __ballot_sync(0xffffffffu, r > 0.0 && below + s > point);
-        token = from - lane + pick * 32 + (over ? __ffs(over) - 1 : 31 - __clz(some));
+        token = from + pick * 32 + (over ? __ffs(over) - 1 : 31 - __clz(some));
     }
     if (lane == 0) out[a] = (int)token;
 }

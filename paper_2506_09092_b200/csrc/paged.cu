@@ -285,12 +285,15 @@ int cudallm_cache_append(const cudallm_paged_shape *shape, const void *k_new, co
     p.skn = pieces(s.kn_stride); p.svn = pieces(s.vn_stride);
     p.sk = page_pieces(s.k_stride); p.sv = page_pieces(s.v_stride);
     p.table_stride = s.table_stride;
-    p.total = (unsigned)(s.batch * s.q_rows * s.kv_heads * (s.head_dim / 8));        // (below 2^31: see check_shape)
-    p.chunks = (int)(s.head_dim / 8); p.kv_heads = (int)s.kv_heads; p.q_rows = (int)s.q_rows; p.page_rows = (int)s.page_rows;
-    p.by_chunks = make_fast_div((uint32_t)p.chunks); p.by_heads = make_fast_div((uint32_t)p.kv_heads);
-    p.by_rows = make_fast_div((uint32_t)p.q_rows); p.by_page_rows = make_fast_div((uint32_t)p.page_rows);
+    p.chunks = (int)(s.head_dim / 8); p.q_rows = (int)s.q_rows; p.page_rows = (int)s.page_rows;
+    p.tokens = (int)(s.batch * s.q_rows); p.pieces = (int)(s.kv_heads * p.chunks);           // (their product is below 2^31: see check_shape)
+    p.by_chunks = make_fast_div((uint32_t)p.chunks); p.by_rows = make_fast_div((uint32_t)p.q_rows);
+    p.by_page_rows = make_fast_div((uint32_t)p.page_rows);
     p.pages = (int)s.pages; p.slots = (int)s.slots; p.cap = (int)(s.table_cols * s.page_rows);
-    return rt_launch(cache_append_kernel, dim3((unsigned)cdiv(p.total, kAppendPieces * kAppendThreads)), kAppendThreads, 0,
+    // a warp a token, or a part of one where the token's pieces do not fill it
+    for (p.lanes = 1; p.lanes < 32 && p.lanes < p.pieces; p.lanes *= 2) {}
+    const int64_t threads = (int64_t)p.tokens * p.lanes;
+    return rt_launch(cache_append_kernel, dim3((unsigned)cdiv(threads, kAppendThreads)), kAppendThreads, 0,
                      static_cast<cudaStream_t>(stream), p);
 }
 

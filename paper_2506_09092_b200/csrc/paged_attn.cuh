@@ -969,44 +969,49 @@ struct AppendParams {
     XaStrides skn, svn;
     PagedStrides sk, sv;
     long long table_stride;
-    unsigned total;                            // pieces of the new keys
-    FastDiv by_chunks, by_heads, by_rows, by_page_rows;
-    int chunks, kv_heads, q_rows, page_rows, pages, slots, cap;
+    FastDiv by_chunks, by_rows, by_page_rows;
+    int tokens, pieces, chunks, q_rows, page_rows, pages, slots, cap;      // pieces: of a token's keys; chunks: of a head's
+    int lanes;                                 // lanes of a token: a power of two
 };
 constexpr int kAppendThreads = 256, kAppendPieces = 4;
 
-// A thread moves four 16-byte pieces of keys and four of values.  What it waits for is the chain slot -> length -> page, so
-// the four go side by side.
+// `lanes` neighbouring lanes move a token's keys and values, four 16-byte pieces of each side by side.  First where they go:
+// slot -> length -> page is what a token waits for, and one that is not there is not read.
 __global__ void __launch_bounds__(kAppendThreads)
 cache_append_kernel(const AppendParams p)
 {
     grid_launch_dependents();
     grid_dependency_wait();
-    uint4 key[kAppendPieces], value[kAppendPieces];
-    long long to_k[kAppendPieces], to_v[kAppendPieces];
+    const unsigned thread = blockIdx.x * kAppendThreads + threadIdx.x, token = thread / (unsigned)p.lanes;
+    if (token >= (unsigned)p.tokens) return;
+    const int b = (int)fast_div(token, p.by_rows), t = (int)token - b * p.q_rows;
+    const PagedItem it = paged_item(p.table, p.table_stride, p.lens, p.slot_of, p.new_lens, b, p.slots, p.cap, p.q_rows);
+    const int pos = it.len - it.news + t;
+    if (t >= it.news || pos < 0) return;
+    const int col = (int)fast_div((uint32_t)pos, p.by_page_rows), page = it.row[col], in_page = pos - col * p.page_rows;
+    if ((unsigned)page >= (unsigned)p.pages) return;
+    const uint4 *k_new = p.k_new + b * p.skn.b + t * p.skn.r, *v_new = p.v_new + b * p.svn.b + t * p.svn.r;
+    uint4 *k = p.k + page * p.sk.page + in_page * p.sk.row, *v = p.v + page * p.sv.page + in_page * p.sv.row;
+    for (int first = (int)(thread % (unsigned)p.lanes); first < p.pieces; first += kAppendPieces * p.lanes) {
+        uint4 key[kAppendPieces], value[kAppendPieces];
+        int h[kAppendPieces], c[kAppendPieces];
 #pragma unroll
-    for (int n = 0; n < kAppendPieces; ++n) {
-        const unsigned i = (blockIdx.x * kAppendPieces + n) * kAppendThreads + threadIdx.x;
-        to_k[n] = -1;
-        if (i >= p.total) continue;
-        const uint32_t rest = fast_div(i, p.by_chunks), c = i - rest * p.chunks, token = fast_div(rest, p.by_heads), h = rest - token * p.kv_heads;
-        const int b = (int)fast_div(token, p.by_rows), t = (int)token - b * p.q_rows;
-        key[n] = p.k_new[b * p.skn.b + t * p.skn.r + h * p.skn.h + c];
-        value[n] = p.v_new[b * p.svn.b + t * p.svn.r + h * p.svn.h + c];
-        const PagedItem it = paged_item(p.table, p.table_stride, p.lens, p.slot_of, p.new_lens, b, p.slots, p.cap, p.q_rows);
-        const int pos = it.len - it.news + t;
-        if (t >= it.news || pos < 0) continue;
-        const int col = (int)fast_div((uint32_t)pos, p.by_page_rows), page = it.row[col], in_page = pos - col * p.page_rows;
-        if ((unsigned)page >= (unsigned)p.pages) continue;
-        to_k[n] = page * p.sk.page + in_page * p.sk.row + h * p.sk.head + c;
-        to_v[n] = page * p.sv.page + in_page * p.sv.row + h * p.sv.head + c;
-    }
-#pragma unroll
-    for (int n = 0; n < kAppendPieces; ++n)
-        if (to_k[n] >= 0) {
-            p.k[to_k[n]] = key[n];
-            p.v[to_v[n]] = value[n];
+        for (int n = 0; n < kAppendPieces; ++n) {
+            const int i = first + n * p.lanes;
+            h[n] = (int)fast_div((uint32_t)i, p.by_chunks);
+            c[n] = i - h[n] * p.chunks;
+            if (i < p.pieces) {
+                key[n] = k_new[h[n] * p.skn.h + c[n]];
+                value[n] = v_new[h[n] * p.svn.h + c[n]];
+            }
         }
+#pragma unroll
+        for (int n = 0; n < kAppendPieces; ++n)
+            if (first + n * p.lanes < p.pieces) {
+                k[h[n] * p.sk.head + c[n]] = key[n];
+                v[h[n] * p.sv.head + c[n]] = value[n];
+            }
+    }
 }
 
 }  // namespace cudallm

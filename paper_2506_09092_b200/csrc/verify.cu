@@ -39,8 +39,8 @@ extern "C" int cudallm_draft_verify(const void *p, const void *q, const int32_t 
     VerifyParams v{};
     v.p = p; v.q = n > 0 ? q : nullptr; v.drafts = drafts; v.draft_lens = draft_lens; v.u = u; v.tokens = tokens; v.accepted = accepted;
     v.ldp = ldp; v.ldq = ldq; v.n = (int)n; v.vocab = (int)vocab;
-    // CTAs of a sequence: four an SM in all, at least eight chunks (a warp's worth each) for one
-    const int64_t want = std::min<int64_t>({int64_t(kVerifyCluster), 4 * kPlanSms / batch, vocab / (kVerifyWarps * kVerifyChunk)});
+    // CTAs of a sequence: two an SM in all, at least eight chunks (a warp's worth each) for one
+    const int64_t want = std::min<int64_t>({int64_t(kVerifyCluster), 2 * kPlanSms / batch, vocab / (kVerifyWarps * kVerifyChunk)});
     v.cluster = (int)std::max<int64_t>(want, 1);
     v.chunk = (int)(kVerifyChunk * cdiv(vocab, (int64_t)kVerifyChunk * kVerifyChunks * v.cluster));
     v.chunks = (int)cdiv(cdiv(vocab, v.chunk), v.cluster);
