@@ -274,6 +274,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const int half = warp >> 2, t = (warp & 3) * 32 + lane;    // half of a block's keys; row of the tile = lane of tensor memory
         const uint32_t t_lane = static_cast<uint32_t>((warp & 3) * 32) << 16, t_o = tmem + L::kTmemO + half * (DP / 2) + t_lane;
         float *xch = reinterpret_cast<float *>(smem + L::kXch);
+        // the two warps that share rows meet at a barrier of their own, and agree there on whether to go on
+        auto meet = [&]() { ok = named_bar_all(1 + (warp & 3), 64, ok); };
         while (ok && seg.next()) {
             const int blocks = seg.live(), rows = seg.rows(), key0 = seg.key0(), seen_lo = seg.seen_lo();
             const int row = seg.rt * L::kRows + t, token = paged_token(p, row), h = seg.kvh * p.group + row - token * p.group;
@@ -308,10 +310,9 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                     }
                     bm = max3_nan(xa_max32(r[0]), xa_max32(r[1]), -INFINITY);
                 }
-                // the other half of the row; a wait that failed for one warp ends the loop for all, so that
-                // none is missing at a later barrier
+                // the other half of the row
                 xch[((block & 1) * 2 + half) * kXaRows + t] = bm;
-                ok = named_bar_all(1, 32 * kPtSoftmaxWarps, ok);
+                meet();
                 if (!ok) break;
                 if (warp_rows) {
                     bm = max3_nan(bm, xch[((block & 1) * 2 + (half ^ 1)) * kXaRows + t], bm);
@@ -381,22 +382,25 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                     }
                     if (lane == 0) bads[block % kPtMaskSlots * kPtWords + warp] = aside;
                 }
+                // The product of the block before is over before this one's may start: so a wait for it, here and at the
+                // segment's end, is never for a phase two behind (whose parity would pass for the one that is meant).
+                if (i > 0) ok = ok && wait(pv_done, block - 1);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full + 8 * (block & 1));
             }
-            // The row's result: the halves' sums join, each thread has half of the columns.  (A wait that failed for one warp
-            // in the last block is all warps' here.)
+            // The row's result: the halves' sums join, each thread has half of the columns.  (A wait that failed for one of the
+            // two warps in the last block is both's here.)
             if (blocks > 0) {
                 ok = ok && wait(pv_done, block - 1);
                 // scores of -inf alone are not the same as no scores
                 if (any && m == -INFINITY) l = __int_as_float(0x7fc00000);
                 xch[((block & 1) * 2 + half) * kXaRows + t] = l;
-                ok = named_bar_all(1, 32 * kPtSoftmaxWarps, ok);
+                meet();
                 if (!ok) break;
                 tc_fence_after();
                 l += xch[((block & 1) * 2 + (half ^ 1)) * kXaRows + t];
-                ok = named_bar_all(1, 32 * kPtSoftmaxWarps, ok);   // (the next segment's first maxima go to the same place)
+                meet();                                            // (the next segment's first maxima go to the same place)
             }
             if (blocks > 0 && warp_rows)
                 add_set_aside<DP, T>(p, seg.it.row, seg.b, seg.kvh, row, seen, m, half * (DP / 2), t_o, bads, key0, block, blocks,
