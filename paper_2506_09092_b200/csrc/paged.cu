@@ -18,10 +18,7 @@ constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxElems = int64_t(1) << 46;          // of an operand, strides included
 constexpr int64_t kMaxTmaStride = int64_t(1) << 39;      // elements
 constexpr int64_t kPlanSms = 148;                        // the split is planned for this many SMs
-#ifndef PA_CB
-#define PA_CB 16
-#endif
-constexpr int64_t kClusterBlocks = PA_CB;                   // blocks of keys that a CTA of a cluster may get at most
+constexpr int64_t kClusterBlocks = 16;                   // blocks of keys that a CTA of a cluster may get at most
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool off(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
@@ -96,7 +93,7 @@ struct Plan {
     bool wide;                  // head dims above 64
     int mt, row_tiles;          // row tiles of 16 mt rows; 0: of 128, by paged_tile_kernel
     int cluster;                // CTAs a cluster; 0: equal shares
-    int ctas;
+    int shares, ctas;           // equal shares of a key head; CTAs in all
     size_t part_bytes, scratch;
 };
 Plan plan_attn(const cudallm_paged_shape &s)
@@ -104,26 +101,24 @@ Plan plan_attn(const cudallm_paged_shape &s)
     Plan f{};
     const int64_t rows = (s.q_heads / s.kv_heads) * s.q_rows, cap = no_states(s) ? 0 : s.table_cols * s.page_rows;
     f.wide = s.head_dim > 64;
-    f.mt = (int)std::min<int64_t>(4, cdiv(rows, 16));
-    f.row_tiles = (int)cdiv(rows, 16 * f.mt);
-    int64_t items = s.batch * s.kv_heads * f.row_tiles, blocks = std::max<int64_t>(1, cdiv(cap, f.wide ? 64 : 128));
+    // More than 16 rows on a key head: by tiles of 128 on tcgen05 where TMA can bring the pages.  (Up to 32 rows and 1024
+    // states a cluster of mma.sync CTAs is as fast or faster: 32 rows x 8 key heads of 128: 9.6 against 10.2 us at 120 states,
+    // 10.8 against 11.8 at 500, 12.4 both at 1000, 20.6 against 17.0 at 4000; 64 rows: 14.3 against 10.9 at 120.)
+    const bool tile = rows > 16 && tile_pages(s) && !(rows <= 32 && cap <= 1024);
+    f.mt = tile ? 0 : (int)std::min<int64_t>(4, cdiv(rows, 16));
+    const int64_t tile_rows = tile ? kXaRows : 16 * f.mt, block = tile ? kXaRows : f.wide ? 64 : 128;
+    f.row_tiles = (int)cdiv(rows, tile_rows);
+    const int64_t items = s.batch * s.kv_heads * f.row_tiles, blocks = std::max<int64_t>(1, cdiv(cap, block));
     const int64_t fits = std::min<int64_t>({int64_t(kPaCluster), 2 * kPlanSms / std::max<int64_t>(items, 1), blocks});
-    if (items <= kPlanSms && blocks <= kClusterBlocks * fits) {
+    if (!tile && items <= kPlanSms && blocks <= kClusterBlocks * fits) {
         f.cluster = (int)std::max<int64_t>(1, fits);
         f.ctas = (int)(items * f.cluster);
         return f;
     }
-    int64_t full = 2 * kPlanSms, tile = 16 * f.mt;
-    if (f.mt > 1 && tile_pages(s)) {
-        f.mt = 0;
-        full = kPlanSms;
-        tile = kXaRows;
-        f.row_tiles = (int)cdiv(rows, tile);
-        items = s.batch * s.kv_heads * f.row_tiles;
-        blocks = std::max<int64_t>(1, cdiv(cap, kXaRows));
-    }
-    f.ctas = (int)std::min<int64_t>(full, items * blocks);
-    f.part_bytes = 2 * (size_t)f.ctas * (size_t)tile * ((f.wide ? 128 : 64) + 1) * sizeof(float);
+    // as many shares of every key head as fit at once, but no more than there are blocks
+    f.shares = (int)std::max<int64_t>(1, std::min<int64_t>((tile ? 1 : 2) * kPlanSms / s.kv_heads, s.batch * f.row_tiles * blocks));
+    f.ctas = (int)(f.shares * s.kv_heads);
+    f.part_bytes = 2 * (size_t)f.ctas * (size_t)tile_rows * ((f.wide ? 128 : 64) + 1) * sizeof(float);
     f.scratch = f.part_bytes + (size_t)f.ctas * kPaDesc * sizeof(int);
     return f;
 }
@@ -152,7 +147,7 @@ int allow_smem(Kernel kernel, int bytes, std::atomic<bool> (&done)[kRtMaxDevices
 template <int DP, int ROWS, typename T>
 int join(const cudallm_paged_shape &s, const Plan &f, const PagedParams &p, cudaStream_t stream)
 {
-    if (f.ctas == 1) return CUDALLM_OK;
+    if (f.shares == 1) return CUDALLM_OK;
     const int64_t rows = std::min<int64_t>(ROWS, (int64_t)p.group * s.q_rows);
     return rt_launch(paged_join_kernel<DP, ROWS, T>, dim3((unsigned)f.ctas, (unsigned)cdiv(rows, 128 / (DP / 8))), 128, 0, stream, p);
 }
@@ -257,6 +252,7 @@ int cudallm_paged_attn(const cudallm_paged_shape *shape, const void *q, const vo
     p.by_group = make_fast_div((uint32_t)p.group);
     p.row_tiles = f.row_tiles;
     p.cluster = f.cluster;
+    p.shares = f.shares;
     p.scale = s.scale; p.scale_log2 = scale_log2(s.scale);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     return s.dtype == CUDALLM_BF16 ? run<__nv_bfloat16>(s, f, p, dev, cs) : run<__half>(s, f, p, dev, cs);

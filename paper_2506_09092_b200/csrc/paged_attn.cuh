@@ -11,9 +11,11 @@
 // Only the device knows the lengths, so the split is made there, in one of two ways:
 //  * a cluster of CTAs per (item, key head, row tile), each with an equal share of its keys; they join
 //    through each other's shared memory.  One launch, but as long as the longest sequence takes.
-//  * equal shares: all blocks of keys of all items in one line, cut into as many equal pieces as CTAs fit.
-//    A CTA's piece may begin and end inside an item; such parts go to scratch (two slots a CTA) and
-//    paged_join_kernel adds them up in order.
+//  * equal shares: all blocks of keys of all items in one line, cut into equal pieces, as many as CTAs fit for
+//    every key head.  Neighbouring CTAs have the same piece for the different heads: where the heads of a token lie side by
+//    side they read the same DRAM pages at the same time (32 x 64000 keys of 64, a CTA's piece in a line that
+//    ran through the heads, too: 101 us).  A piece may begin and end inside an item; such parts go to scratch
+//    (two slots a CTA) and paged_join_kernel adds them up in order.
 #pragma once
 #include "fast_div.cuh"
 #include "mma_sync.cuh"
@@ -43,6 +45,7 @@ struct PagedParams {
     FastDiv by_page_rows;
     int row_tiles;                             // tiles of 16 or 32 rows of an item and key head at most
     int cluster;                               // CTAs per item, key head and row tile; 0: equal shares
+    int shares;                                // of a key head; CTA = share * kv_heads + key head
     float scale, scale_log2;
 };
 constexpr int kPaDesc = 4;                     // parts (0: none begins here) and 2^16 x rows, item, key head, row tile
@@ -710,16 +713,16 @@ __device__ __forceinline__ float paged_join_parts(const PagedParams &p, const ui
     return fmaf(mx, p.scale, logf(sum));
 }
 
-// Equal shares: all blocks of keys in one line, items in order, in each the key heads, in each the row tiles; a CTA's
-// share of it in pieces (segments) that each belong to one item, key head and row tile.
+// Equal shares: for each key head all blocks of keys in one line, items in order, in each the row tiles; a CTA's share of it in
+// pieces (segments) that each belong to one item and row tile.
 template <int ROWS, int BLOCK> struct PagedSegments {
     const PagedParams &p;
     long long pos, end, rem;                   // the block behind the segment, the share's end, pos counted from the item's first block
     PagedItem it;
-    int b, kvh, rt, blk0, blk1, blocks;        // blocks: of the item, key head and row tile
+    int b, kvh, rt, blk0, blk1, blocks;        // blocks: of the item and row tile
 
     __device__ __forceinline__ explicit PagedSegments(const PagedParams &p_) : p(p_) {}
-    __device__ __forceinline__ static unsigned head_blocks(const PagedParams &p, const PagedItem &x)
+    __device__ __forceinline__ static unsigned item_blocks(const PagedParams &p, const PagedItem &x)
     {
         unsigned n = 0;
         for (int r = 0; r < p.row_tiles; ++r) n += paged_blocks(p, x, ROWS, r, BLOCK);
@@ -729,17 +732,42 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     {
         return a >> 32 ? a / d : (long long)((unsigned)a / d);
     }
-    // How many blocks there are in all, and which item this CTA's share begins in: the first 128 threads count, `each` items
-    // a thread.  All of the CTA's threads call it; `smem` is free again afterwards.  per: blocks of a share.
-    __device__ __forceinline__ void locate(uint8_t *smem, long long &per)
+    // Where in its item, which has `all` blocks, the next segment lies.
+    __device__ __forceinline__ void place(unsigned all)
     {
-        long long *warp_sum = reinterpret_cast<long long *>(smem), &s_rem = warp_sum[kPaWarps];
-        int &s_item = *reinterpret_cast<int *>(warp_sum + kPaWarps + 1);
+        blk0 = (int)rem;
+        if (p.row_tiles == 1) {
+            rt = 0;
+            blocks = (int)all;
+        } else {
+            for (rt = 0; blk0 >= (blocks = paged_blocks(p, it, ROWS, rt, BLOCK)); ++rt) blk0 -= blocks;
+        }
+        blk1 = (int)min((long long)blocks, blk0 + (end - pos));
+        pos += blk1 - blk0;
+        rem += blk1 - blk0;
+    }
+    // How many blocks there are in all, and where this CTA's share begins: the first 128 threads count, `each` items a
+    // thread, and the one that has found the place makes out the first segment (and whether there is one, which it
+    // returns).  All of the CTA's threads call it; `smem` is free again afterwards.  per: blocks of a share.
+    __device__ __forceinline__ bool locate(uint8_t *smem, long long &per)
+    {
+        struct Found {
+            long long pos, end, rem, per;
+            PagedItem it;
+            int b, rt, blk0, blk1, blocks;
+        };
+        long long *warp_sum = reinterpret_cast<long long *>(smem);
+        Found &found = *reinterpret_cast<Found *>(warp_sum + kPaWarps);
         const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, each = (p.batch + kPaThreads - 1) / kPaThreads;
-        long long sum = 0, upto = 0, total = 0;
+        long long sum = 0, upto = 0;
+        unsigned all = 0;
         if (tid < kPaThreads) {
             for (int i = 0; i < each; ++i)
-                if (tid * each + i < p.batch) sum += (long long)head_blocks(p, paged_item(p, tid * each + i)) * p.kv_heads;
+                if (tid * each + i < p.batch) {
+                    it = paged_item(p, tid * each + i);
+                    all = item_blocks(p, it);
+                    sum += all;
+                }
             upto = sum;                                            // blocks of all threads up to this one
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
@@ -748,51 +776,64 @@ template <int ROWS, int BLOCK> struct PagedSegments {
             }
             if (lane == 31) warp_sum[warp] = upto;
         }
+        if (tid == 0) {
+            found.pos = found.end = 0;                             // (nobody's, unless one of the threads finds its place)
+            p.desc[blockIdx.x * kPaDesc] = 0;
+        }
         __syncthreads();
+        if (tid < kPaThreads) {
+            long long total = 0;
 #pragma unroll
-        for (int w = 0; w < kPaWarps; ++w) {
-            if (w < warp) upto += warp_sum[w];
-            total += warp_sum[w];
-        }
-        per = max(divide(total + gridDim.x - 1, gridDim.x), 1LL);
-        pos = blockIdx.x * per;
-        end = min(total, pos + per);
-        if (tid == 0) p.desc[blockIdx.x * kPaDesc] = 0;
-        if (tid < kPaThreads && pos < end && pos >= upto - sum && pos < upto) {
-            long long left = pos - (upto - sum);
-            int x = tid * each;
-            if (each > 1)
-                for (;; ++x) {
-                    const long long n = (long long)head_blocks(p, paged_item(p, x)) * p.kv_heads;
-                    if (left < n) break;
-                    left -= n;
-                }
-            s_item = x;
-            s_rem = left;
+            for (int w = 0; w < kPaWarps; ++w) {
+                if (w < warp) upto += warp_sum[w];
+                total += warp_sum[w];
+            }
+            per = max(divide(total + p.shares - 1, (unsigned)p.shares), 1LL);
+            pos = (blockIdx.x / (unsigned)p.kv_heads) * per;
+            end = min(total, pos + per);
+            rem = pos - (upto - sum);
+            if (pos < end && rem >= 0 && rem < sum) {
+                b = tid * each;
+                if (each > 1)
+                    for (;; ++b) {
+                        it = paged_item(p, b);
+                        all = item_blocks(p, it);
+                        if (rem < (long long)all) break;
+                        rem -= all;
+                    }
+                place(all);
+                found = Found{pos, end, rem, per, it, b, rt, blk0, blk1, blocks};
+            }
         }
         __syncthreads();
-        b = s_item;
-        rem = s_rem;
+        const Found f = found;
+        pos = f.pos;
+        end = f.end;
+        rem = f.rem;
+        per = f.per;
+        it = f.it;
+        b = f.b;
+        kvh = (int)(blockIdx.x % (unsigned)p.kv_heads);
+        rt = f.rt;
+        blk0 = f.blk0;
+        blk1 = f.blk1;
+        blocks = f.blocks;
         __syncthreads();
+        return pos > 0;
     }
     // The next segment; false: there are no more.
     __device__ __forceinline__ bool next()
     {
         if (pos >= end) return false;
-        unsigned head;
         for (;; ++b) {
             it = paged_item(p, b);
-            head = head_blocks(p, it);
-            if (rem < (long long)head * p.kv_heads) break;
-            rem -= (long long)head * p.kv_heads;
+            const unsigned all = item_blocks(p, it);
+            if (rem < (long long)all) {
+                place(all);
+                return true;
+            }
+            rem -= all;
         }
-        kvh = (int)divide(rem, head);
-        blk0 = (int)(rem - (long long)kvh * head);
-        for (rt = 0; blk0 >= (blocks = paged_blocks(p, it, ROWS, rt, BLOCK)); ++rt) blk0 -= blocks;
-        blk1 = (int)min((long long)blocks, blk0 + (end - pos));
-        pos += blk1 - blk0;
-        rem += blk1 - blk0;
-        return true;
     }
     __device__ __forceinline__ int rows() const { return min(it.news * p.group - rt * ROWS, ROWS); }
     __device__ __forceinline__ int key0() const { return blk0 * BLOCK; }
@@ -802,11 +843,11 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     // keys below this are seen by every row
     __device__ __forceinline__ int seen_lo() const { return paged_seen(it, paged_token(p, rt * ROWS)); }
     __device__ __forceinline__ bool whole() const { return blk0 == 0 && blk1 == blocks; }
-    // The first of several parts of an item, key head and row tile says how many CTAs share them.
+    // The first of several parts of an item, key head and row tile says how many CTAs share them: every kv_heads-th from here.
     __device__ __forceinline__ void describe(long long per) const
     {
         int *d = p.desc + blockIdx.x * kPaDesc;
-        d[0] = ((int)(divide(pos - blk1 + blocks - 1, (unsigned)min(per, 0xffffffffLL)) - blockIdx.x) + 1) | rows() << 16;
+        d[0] = ((int)divide(pos - blk1 + blocks - 1, (unsigned)min(per, 0xffffffffLL)) - (int)(blockIdx.x / (unsigned)p.kv_heads) + 1) | rows() << 16;
         d[1] = b;
         d[2] = kvh;
         d[3] = rt;
@@ -839,8 +880,7 @@ paged_attn_kernel(const PagedParams p)
         seg.blk0 = (int)((long long)seg.blocks * rank / p.cluster);
         seg.blk1 = (int)((long long)seg.blocks * (rank + 1) / p.cluster);
     } else {
-        seg.locate(smem, per);
-        if (!seg.next()) return;
+        if (!seg.locate(smem, per)) return;
     }
     for (;;) {
         if constexpr (MT == 1) paged_walk_narrow<DP, T>(p, smem, seg.it, seg.b, seg.kvh, seg.rt, seg.blk0, seg.blk1);
@@ -904,7 +944,7 @@ paged_attn_kernel(const PagedParams p)
 }
 
 // The parts of an item's key head and row tile that several CTAs worked on, added up in order: the first lies in slot 1 of
-// the CTA that it began in, the others in slot 0 of those after it.  blockIdx.x: that CTA; blockIdx.y: four rows.
+// the CTA that it began in, the others in slot 0 of the next CTAs of the key head.  blockIdx.x: that CTA; blockIdx.y: four rows.
 template <int DP, int ROWS, typename T>
 __global__ void __launch_bounds__(128)
 paged_join_kernel(const PagedParams p)
@@ -919,14 +959,14 @@ paged_join_kernel(const PagedParams p)
     const int r = blockIdx.y * (128 / kChunks) + threadIdx.x / kChunks, c = threadIdx.x % kChunks;
     const int row = d.w * ROWS + r;
     if (r >= rows) return;
-    const float *first = p.part + (2LL * cta + 1) * kSlot, *next = p.part + 2LL * (cta + 1) * kSlot;
+    const float *first = p.part + (2LL * cta + 1) * kSlot, *next = p.part + 2LL * (cta + p.kv_heads) * kSlot;
     float mx = -INFINITY, sum = 0.f, acc[8] = {};
     for (int s0 = 0; s0 < parts; s0 += 8) {
         float lse[8], top = mx;
         float4 v[8][2];
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
-            const float *src = s0 + s == 0 ? first : next + 2LL * (s0 + s - 1) * kSlot;
+            const float *src = s0 + s == 0 ? first : next + 2LL * (s0 + s - 1) * p.kv_heads * kSlot;
             const bool live = s0 + s < parts;
             lse[s] = live ? src[ROWS * DP + r] : -INFINITY;
             if (live) {

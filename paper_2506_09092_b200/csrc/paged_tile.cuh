@@ -6,9 +6,10 @@
 //   warps 0-7    softmax: 128 rows are the lanes of tensor memory, a row's 128 scores are shared by two
 //                threads; then the rows' results
 //   warp 8       the tensor core: S = Q K^T into one of two places in tensor memory, O += P V with P written over S
-//   warp 9       TMA: the pages of a block of K and of V into a ring of tiles, a lane a page; needs pages of 8, 16, 32,
+//   warps 9, 10  TMA: the pages of a block of K, and those of V, into a ring of tiles, a lane a page (a TMA instruction
+//                takes its warp some 120 clocks: one warp for both was the bound with pages of 16 rows); needs pages of 8, 16, 32,
 //                64 or a multiple of 128 rows, so that they fill a tile and begin on a swizzle's boundary
-//   warps 10, 11 the queries of a segment
+//   warp 11      the queries of a segment
 // While the softmax of one block runs, the scores of the next are formed; the copies run ahead by the ring, into
 // the next segment too.  tcgen05 has 128 rows whether they are used or not, but the products of a block take a
 // third of the time that its bytes take from HBM, no registers and no issue slots of the other warps; mma.sync
@@ -18,8 +19,8 @@
 
 namespace cudallm {
 
-constexpr int kPtSoftmaxWarps = 8, kPtMmaWarp = 8, kPtLoadWarp = 9, kPtQueryWarp = 10, kPtQueryWarps = 2;
-constexpr int kPtThreads = 32 * (kPtQueryWarp + kPtQueryWarps);        // 12 warps: three to a quarter of the SM, 168 registers each
+constexpr int kPtSoftmaxWarps = 8, kPtMmaWarp = 8, kPtLoadWarp = 9, kPtQueryWarp = 11;
+constexpr int kPtThreads = 32 * (kPtQueryWarp + 1);        // 12 warps: three to a quarter of the SM, 168 registers each
 constexpr int kPtMaskSlots = 8;                // blocks whose masks are kept: more than the copies can be ahead of the softmax
 constexpr int kPtWords = kXaRows / 32;         // masks of a block: a bit a key
 
@@ -28,7 +29,7 @@ enum : int { kXaRolePagedLoad = 0x40, kXaRolePagedMma = 0x41, kXaRolePagedSoftma
 template <int DP> struct PagedTileSmem {
     static constexpr int kRows = kXaRows, kBlock = kXaRows;
     static constexpr int kTile = DP / 64 * kXaChunkBytes;          // 128 rows of Q, K or V
-    static constexpr int kStages = DP == 128 ? 6 : 12;
+    static constexpr int kStages = DP == 128 ? 6 : 12;             // (even: K and V each have every second)
     static constexpr int kRing = kTile;                            // behind the queries
     static constexpr int kBars = kRing + kStages * kTile;
     // q_full, q_empty, pv_done, drain, s_full[2], p_full[2], full[kStages], empty[kStages]
@@ -123,9 +124,9 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
     if (tid == 0) *abort_flag = 0;
     if (warp == 0) {
-        // arrivals: the query warps at q_full, the softmax warps at p_full, one at the others
+        // arrivals: the softmax warps at p_full, one at the others
         static_assert(L::kNumBars <= 32, "barriers");
-        if (lane < L::kNumBars) mbar_init(bars + 8 * lane, lane == 0 ? kPtQueryWarps : lane == 6 || lane == 7 ? kPtSoftmaxWarps : 1);
+        if (lane < L::kNumBars) mbar_init(bars + 8 * lane, lane == 6 || lane == 7 ? kPtSoftmaxWarps : 1);
         fence_mbar_init();
     }
     if (warp == kPtMmaWarp) {
@@ -146,7 +147,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
     long long per;
     PagedSegments<L::kRows, L::kBlock> seg(p);
-    seg.locate(smem, per);
+    const bool some = seg.locate(smem, per);
     const int cta = blockIdx.x;
     // (a whole warp waits; what fails for one lane ends it for all)
     auto wait = [&](uint32_t bar, int parity) {
@@ -155,40 +156,33 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     int segments = 0, block = 0;                                   // of this CTA so far, those without keys not counted
     bool ok = true;
 
-    if (warp >= kPtQueryWarp) {
-        while (ok && seg.next()) {
+    if (warp == kPtQueryWarp) {
+        for (bool more = some; ok && more; more = seg.next()) {
             const int rows = seg.rows();
             if (seg.live() == 0) continue;
             if (segments > 0) ok = wait(q_empty, segments - 1);     // the segment before has formed its last scores
             if (!ok) break;
             // (rows that do not exist are the tensor core's own affair: they reach no other row's result)
-            constexpr int kBatch = 8, kRowStep = 32 / kChunks * kPtQueryWarps;     // loads in flight; rows that both warps cover with one
+            constexpr int kRowStep = 32 / kChunks;                 // rows that an instruction covers
             const int c = lane % kChunks, row0 = seg.rt * L::kRows;
-            for (int r = lane / kChunks * kPtQueryWarps + warp - kPtQueryWarp; r < rows; r += kBatch * kRowStep) {
-                uint4 w[kBatch];
-#pragma unroll
-                for (int n = 0; n < kBatch; ++n) {
-                    w[n] = make_uint4(0, 0, 0, 0);
-                    if (r + n * kRowStep < rows && c * 8 < p.head_dim)
-                        w[n] = *reinterpret_cast<const uint4 *>(paged_q_row<T>(p, seg.b, seg.kvh, row0 + r + n * kRowStep) + c * 8);
-                }
-#pragma unroll
-                for (int n = 0; n < kBatch; ++n)
-                    if (r + n * kRowStep < rows)
-                        st_shared_v4_b32(sbase + tile_piece(r + n * kRowStep, c), w[n].x, w[n].y, w[n].z, w[n].w);
-            }
+            const bool live = c * 8 < p.head_dim;
+#pragma unroll 2
+            for (int r = lane / kChunks; r < rows; r += kRowStep)
+                cp_async_16_cg(sbase + tile_piece(r, c), paged_q_row<T>(p, seg.b, seg.kvh, row0 + r) + (live ? c * 8 : 0), live ? 16 : 0);
+            cp_async_wait_all();
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
             ++segments;
         }
         if (!ok && lane == 0) xa_report(tp.status, kXaRolePagedQuery, 1);
-    } else if (warp == kPtLoadWarp) {
+    } else if (warp > kPtMmaWarp) {
         // the pages of a block: lane j has the j-th, up to 16 of them; of larger ones the part that the block is
         const int box = min(p.page_rows, L::kBlock), pages = L::kBlock / box;
-        int tile = 0;
+        const int kv = warp - kPtLoadWarp;
+        const CUtensorMap *tm = kv ? &tm_v : &tm_k;
         ok = !tp.skip_loads;
-        while (ok && seg.next()) {
+        for (bool more = some; ok && more; more = seg.next()) {
             const int blocks = seg.live(), key0 = seg.key0(), key_end = seg.key_end();
             int page = -1, in_page = 0;                            // this lane's page of the next block
             auto look_up = [&](int i) {
@@ -206,32 +200,34 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 const bool there = (unsigned)at < (unsigned)p.pages;
                 const uint32_t have = __ballot_sync(0xffffffffu, there);
                 look_up(i + 1);
-                for (int kv = 0; kv < 2 && ok; ++kv, ++tile) {
-                    const int stage = tile % L::kStages, use = tile / L::kStages;
-                    if (use > 0) ok = wait(empty + 8 * stage, use - 1);
-                    if (!ok) break;
-                    if (kv == 0) {
+                const int tile = 2 * block + kv, stage = tile % L::kStages, use = tile / L::kStages;
+                if (use > 0) ok = wait(empty + 8 * stage, use - 1);
+                if (!ok) break;
+                if (kv == 0) {
 #pragma unroll
-                        for (int w = 0; w < kPtWords; ++w) {
-                            const int r = w * 32 + lane;
-                            const uint32_t word = __ballot_sync(0xffffffffu, (have >> (r / box) & 1) && key0 + i * L::kBlock + r < key_end);
-                            if (lane == 0) masks[block % kPtMaskSlots * kPtWords + w] = word;
-                        }
+                    for (int w = 0; w < kPtWords; ++w) {
+                        const int r = w * 32 + lane;
+                        const uint32_t word = __ballot_sync(0xffffffffu, (have >> (r / box) & 1) && key0 + i * L::kBlock + r < key_end);
+                        if (lane == 0) masks[block % kPtMaskSlots * kPtWords + w] = word;
                     }
-                    if (lane == 0) mbar_expect_tx(full + 8 * stage, __popc(have) * box * (DP / 64) * 128);
                     __syncwarp();
-                    if (there) {
-                        const uint32_t dst = sbase + L::kRing + stage * L::kTile + lane * box * 128;
+                }
+                // (the pages go round by shuffle and one lane asks for all of them: their addresses are uniform values then)
+                if (lane == 0) mbar_expect_tx(full + 8 * stage, __popc(have) * box * (DP / 64) * 128);
+                __syncwarp();
+                uint32_t dst = sbase + L::kRing + stage * L::kTile;
+                for (int j = 0; j < pages; ++j, dst += box * 128) {
+                    const int pg = __shfl_sync(0xffffffffu, at, j), row = __shfl_sync(0xffffffffu, from, j);
+                    if ((have >> j & 1) && elect_one()) {
 #pragma unroll
                         for (int c = 0; c < DP / 64; ++c)
-                            paged_load_box(kv ? &tm_v : &tm_k, dst + c * kXaChunkBytes, full + 8 * stage, c, seg.kvh, from, at);
+                            paged_load_box(tm, dst + c * kXaChunkBytes, full + 8 * stage, c, seg.kvh, row, pg);
                     }
                     __syncwarp();
                 }
             }
         }
         if (!ok && lane == 0 && !tp.skip_loads) xa_report(tp.status, kXaRolePagedLoad, 1);
-        segments = tile;                                           // (tiles asked for: see the end)
     } else if (warp == kPtMmaWarp) {
         constexpr uint32_t idesc_s = xa_idesc<T>(kXaRows, 0), idesc_o = xa_idesc<T>(DP, 1);
         const uint32_t t0 = __shfl_sync(0xffffffffu, tmem, 0);
@@ -250,7 +246,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             }
             __syncwarp();
         };
-        while (ok && seg.next()) {
+        for (bool more = some; ok && more; more = seg.next()) {
             const int blocks = seg.live();
             if (blocks == 0) continue;
             ok = wait(q_full, segments);
@@ -276,7 +272,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         float *xch = reinterpret_cast<float *>(smem + L::kXch);
         // the two warps that share rows meet at a barrier of their own, and agree there on whether to go on
         auto meet = [&]() { ok = named_bar_all(1 + (warp & 3), 64, ok); };
-        while (ok && seg.next()) {
+        for (bool more = some; ok && more; more = seg.next()) {
             const int blocks = seg.live(), rows = seg.rows(), key0 = seg.key0(), seen_lo = seg.seen_lo();
             const int row = seg.rt * L::kRows + t, token = paged_token(p, row), h = seg.kvh * p.group + row - token * p.group;
             const bool mine = t < rows, warp_rows = (warp & 3) * 32 < rows;
@@ -450,9 +446,14 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // before shared and tensor memory are another CTA's.
     tc_fence_before();
     __syncthreads();
-    if (*abort_flag && warp == kPtLoadWarp && lane == 0 && segments > 0) {
+    if (*abort_flag && (warp == kPtLoadWarp || warp == kPtLoadWarp + 1) && lane == 0) {
+        // the last copy into each stage of this warp's: every second one
         volatile int never = 0;
-        xa_ring_landed<L::kStages>(full, segments, &never);
+        constexpr int kOwn = L::kStages / 2;
+        for (int s = 0; s < kOwn; ++s) {
+            const int uses = (block - s + kOwn - 1) / kOwn;
+            if (uses > 0) mbar_wait(full + 8 * (2 * s + warp - kPtLoadWarp), (uses - 1) & 1, &never);
+        }
     }
     if (warp == kPtMmaWarp) {
         tc_fence_after();
