@@ -8,6 +8,7 @@
 
 #include "runtime.h"
 #include "paged_attn.cuh"
+#include "paged_narrow.cuh"
 #include "paged_tile.cuh"
 
 using namespace cudallm;
@@ -151,16 +152,15 @@ int join(const cudallm_paged_shape &s, const Plan &f, const PagedParams &p, cuda
     const int64_t rows = std::min<int64_t>(ROWS, (int64_t)p.group * s.q_rows);
     return rt_launch(paged_join_kernel<DP, ROWS, T>, dim3((unsigned)f.ctas, (unsigned)cdiv(rows, 128 / (DP / 8))), 128, 0, stream, p);
 }
-template <int DP, int MT, typename T>
-int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cudaStream_t stream)
+// The mma.sync kernels: ROWS rows of a key head a CTA.
+template <int DP, int ROWS, typename T, typename Kernel>
+int run_mma(Kernel kernel, int bytes, const cudallm_paged_shape &s, const Plan &f, const PagedParams &p, int dev, cudaStream_t stream)
 {
-    using L = PagedSmem<DP, MT>;
     static std::atomic<bool> done[kRtMaxDevices] = {};
-    int st = allow_smem(paged_attn_kernel<DP, MT, T>, L::kBytes, done, dev);
+    int st = allow_smem(kernel, bytes, done, dev);
     if (st != CUDALLM_OK) return st;
-    st = rt_launch_cluster(paged_attn_kernel<DP, MT, T>, dim3((unsigned)f.ctas), f.cluster ? (unsigned)f.cluster : 1u,
-                           kPaThreads, (size_t)L::kBytes, stream, p);
-    return st != CUDALLM_OK || f.cluster ? st : join<DP, L::kRows, T>(s, f, p, stream);
+    st = rt_launch_cluster(kernel, dim3((unsigned)f.ctas), f.cluster ? (unsigned)f.cluster : 1u, kPaThreads, (size_t)bytes, stream, p);
+    return st != CUDALLM_OK || f.cluster ? st : join<DP, ROWS, T>(s, f, p, stream);
 }
 // Tensor map of a pool: 64 columns of one key head of up to 128 rows of a page.
 int encode(CUtensorMap *tm, const void *base, bool f16, const cudallm_paged_shape &s, const int64_t (&st)[3])
@@ -193,10 +193,10 @@ int run(const cudallm_paged_shape &s, const Plan &f, PagedParams &p, int dev, cu
 {
     switch (f.mt) {
     case 0: return run_tile<DP, T>(s, f, p, dev, stream);
-    case 1: return run<DP, 1, T>(s, f, p, dev, stream);
-    case 2: return run<DP, 2, T>(s, f, p, dev, stream);
-    case 3: return run<DP, 3, T>(s, f, p, dev, stream);
-    default: return run<DP, 4, T>(s, f, p, dev, stream);
+    case 1: return run_mma<DP, 16, T>(paged_narrow_kernel<DP, T>, PagedNarrowSmem<DP>::kBytes, s, f, p, dev, stream);
+    case 2: return run_mma<DP, 32, T>(paged_wide_kernel<DP, 2, T>, PagedSmem<DP, 2>::kBytes, s, f, p, dev, stream);
+    case 3: return run_mma<DP, 48, T>(paged_wide_kernel<DP, 3, T>, PagedSmem<DP, 3>::kBytes, s, f, p, dev, stream);
+    default: return run_mma<DP, 64, T>(paged_wide_kernel<DP, 4, T>, PagedSmem<DP, 4>::kBytes, s, f, p, dev, stream);
     }
 }
 template <typename T>

@@ -50,26 +50,27 @@ struct PagedParams {
 };
 constexpr int kPaDesc = 4;                     // parts (0: none begins here) and 2^16 x rows, item, key head, row tile
 
-template <int DP, int MT> struct PagedSmem {
-    static constexpr int kRows = 16 * MT;
+template <int DP> struct PagedSizes {
     static constexpr int kKeys = DP == 128 ? 16 : 32;              // of a stage and warp
     static constexpr int kBlock = kKeys * kPaWarps;                // of a round of the four warps: unit of the split
     static constexpr int kStages = 3;                              // 96 KiB a CTA: two on an SM
     static constexpr int kTile = kKeys * DP * 2;                   // a warp's one of K, V
-    static constexpr int kWarp = kStages * 2 * kTile;              // (one row tile: each warp has its own ring)
-    static constexpr int kRing = kPaWarps * kWarp;
-    // results of the walk: blocks of [row][DP] fp32, the rows' maxima, their sums; one a warp where each has keys of its own
-    static constexpr int kParts = MT == 1 ? kPaWarps : 1;
+    static constexpr int kRing = kPaWarps * kStages * 2 * kTile;
+};
+// Two to four row tiles.
+template <int DP, int MT> struct PagedSmem : PagedSizes<DP> {
+    using S = PagedSizes<DP>;
+    static constexpr int kRows = 16 * MT;
+    // the result of the walk: [row][DP] fp32, the rows' maxima, their sums
     static constexpr int kPitch = DP + 4;                          // floats per row
     static constexpr int kPart = (kRows * kPitch + 2 * kRows) * 4;
     // a CTA's result for its cluster: [row][DP] fp32, then the rows' lse
-    static constexpr int kShare = (kParts * kPart + 127) / 128 * 128;
-    static_assert(kShare + kRows * (DP + 1) * 4 <= kRing, "behind the results");
+    static constexpr int kShare = (kPart + 127) / 128 * 128;
+    static_assert(kShare + kRows * (DP + 1) * 4 <= S::kRing, "behind the result");
     static constexpr bool kQInSmem = MT > 3;                       // queries of four row tiles do not fit into registers
-    static constexpr int kMax = kRing + (kQInSmem ? kRows * DP * 2 : 0);   // warps' maxima of each row (several row tiles)
-    static constexpr int kBytes = kMax + (MT > 1 ? kRows * kPaWarps * 4 : 0);
+    static constexpr int kMax = S::kRing + (kQInSmem ? kRows * DP * 2 : 0);    // warps' maxima of each row
+    static constexpr int kBytes = kMax + kRows * kPaWarps * 4;
     static_assert(2 * (kBytes + 1024) <= 228 * 1024, "two CTAs on an SM");
-    static constexpr int kSlot = kRows * (DP + 1);                 // floats of a part's result
 };
 
 // An item: its row of the table, its states, its new tokens (0: none, or the item is not there).
@@ -163,8 +164,8 @@ __device__ __forceinline__ void paged_store_lse(const PagedParams &p, int b, int
 
 // A warp's rows of the stages of a ring: pages looked up one tile ahead, copies past L1.  The pieces of a row go to
 // neighbouring lanes, piece c of row r to position c ^ (r & 7) (conflict-free ldmatrix).
-template <int DP, int MT, typename T> struct PagedLoader {
-    using L = PagedSmem<DP, MT>;
+template <int DP, typename T> struct PagedLoader {
+    using L = PagedSizes<DP>;
     static constexpr int kChunks = DP / 8, kRowStep = 32 / kChunks;        // 16-byte pieces of a row; rows that a copy instruction covers
     static constexpr uint32_t kAll = L::kKeys == 32 ? 0xffffffffu : (1u << L::kKeys) - 1;
     const PagedParams &p;
@@ -174,11 +175,16 @@ template <int DP, int MT, typename T> struct PagedLoader {
     int first, key_end, tiles, lane;           // the warp's tile t begins at key first + t * kBlock
     int page = -1, in_page = 0;                // this lane's row of the next tile
 
-    __device__ __forceinline__ PagedLoader(const PagedParams &p_, const PagedItem &it, int kvh, uint32_t to_, int first_, int key_end_,
-                                           int tiles_)
-        : p(p_), kbase(static_cast<const T *>(p_.k) + kvh * p_.sk.head), vbase(static_cast<const T *>(p_.v) + kvh * p_.sv.head),
-          row(it.row), to(to_), first(first_), key_end(key_end_), tiles(tiles_), lane(threadIdx.x & 31)
+    __device__ __forceinline__ PagedLoader(const PagedParams &p_, uint32_t to_) : p(p_), to(to_), lane(threadIdx.x & 31) {}
+    // From now on the warp's tiles of these keys; no page has been looked up.
+    __device__ __forceinline__ void set(const PagedItem &it, int kvh, int first_, int key_end_, int tiles_)
     {
+        kbase = static_cast<const T *>(p.k) + kvh * p.sk.head;
+        vbase = static_cast<const T *>(p.v) + kvh * p.sv.head;
+        row = it.row;
+        first = first_;
+        key_end = key_end_;
+        tiles = tiles_;
     }
     __device__ __forceinline__ void look_up(int t)
     {
@@ -245,184 +251,10 @@ __device__ __forceinline__ void paged_load_q(const PagedParams &p, int b, int kv
     }
 }
 
-// Blocks blk0 .. blk1 - 1 of an item's keys for one key head and row tile.  Leaves sums, not yet normalised, in the
-// parts' places: rows x DP, then the rows' maxima (of the scores), then the sums of exponentials.  A row that has
+// Blocks blk0 .. blk1 - 1 of an item's keys for one key head and row tile.  Leaves sums, not yet normalised, at the start of
+// shared memory: rows x DP, then the rows' maxima (of the scores), then the sums of exponentials.  A row that has
 // seen no state has maximum -inf and sum 0.
 //
-// One row tile: each warp has tiles of its own and sums of its own.
-template <int DP, typename T>
-__device__ __forceinline__ void paged_walk_narrow(const PagedParams &p, uint8_t *smem, const PagedItem &it, int b, int kvh, int rt,
-                                                  int blk0, int blk1)
-{
-    using L = PagedSmem<DP, 1>;
-    using Loader = PagedLoader<DP, 1, T>;
-    constexpr int kChunks = DP / 8, kKeys = L::kKeys, kN = kKeys / 8;      // kN: tiles of eight keys
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int rows = min(it.news * p.group - rt * L::kRows, L::kRows);
-    const int seen_lo = paged_seen(it, paged_token(p, rt * L::kRows));
-    const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(p, it, L::kRows, rt), blk1 * L::kBlock);
-    const int ntiles = key_end > key0 ? (key_end - key0 + kKeys - 1) / kKeys : 0;
-    const int mine = ntiles > warp ? (ntiles - warp + kPaWarps - 1) / kPaWarps : 0;         // tiles warp, warp + 4, ...
-    const uint32_t ring = smem_u32(smem) + warp * L::kWarp;
-    Loader ld(p, it, kvh, ring, key0 + warp * kKeys, key_end, mine);
-    ld.look_up(0);
-    uint32_t there[L::kStages - 1];                                // of tiles t, t + 1
-#pragma unroll
-    for (int t = 0; t < L::kStages - 1; ++t) there[t] = ld.load(t, t * 2 * L::kTile, L::kTile);
-
-    const int g = lane >> 2, q4 = lane & 3;
-    uint32_t qa[DP / 16][4];
-    paged_load_q<DP, T>(p, b, kvh, rt * L::kRows, rows, qa);
-    int seen[2];                                                   // keys that a row sees lie below this
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    bool any[2] = {false, false};
-    float o[DP / 8][4];
-#pragma unroll
-    for (int half = 0; half < 2; ++half)
-        seen[half] = g + 8 * half < rows ? paged_seen(it, paged_token(p, rt * L::kRows + g + 8 * half)) : 0x7fffffff;
-#pragma unroll
-    for (int n = 0; n < DP / 8; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-
-    for (int t = 0; t < mine; ++t) {
-        cp_async_wait_group<L::kStages - 2>();
-        __syncwarp();                                              // every lane's copies of stage t have landed
-        const uint32_t mask = there[0];
-#pragma unroll
-        for (int i = 0; i + 1 < L::kStages - 1; ++i) there[i] = there[i + 1];
-        const int next = t + L::kStages - 1;
-        there[L::kStages - 2] = ld.load(next, next % L::kStages * 2 * L::kTile, L::kTile);  // (read in round t - 1)
-        const uint32_t sk = ring + (t % L::kStages) * 2 * L::kTile, sv = sk + L::kTile;
-        float s[kN][4] = {};
-        {
-            const int idx = lane >> 3, kr = (idx >> 1) * 8 + (lane & 7);
-#pragma unroll
-            for (int k = 0; k < DP / 16; ++k)
-#pragma unroll
-                for (int n = 0; n < kN; n += 2) {
-                    uint32_t bf[4];
-                    ldmatrix_x4(bf, sk + (n * 8 + kr) * DP * 2 + (((2 * k + (idx & 1)) ^ (kr & 7)) << 4));
-                    mma_16x8x16<T>(s[n], qa[k], bf[0], bf[1]);
-                    mma_16x8x16<T>(s[n + 1], qa[k], bf[2], bf[3]);
-                }
-        }
-        const int pos0 = ld.first + t * L::kBlock;
-        const bool full = mask == Loader::kAll && pos0 + kKeys <= seen_lo;     // every row sees every key
-        if (!full) {
-#pragma unroll
-            for (int n = 0; n < kN; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int key = n * 8 + q4 * 2 + (e & 1);
-                    if (!(mask >> key & 1) || pos0 + key >= seen[e >> 1]) s[n][e] = -INFINITY;
-                }
-        }
-        float bm[2];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            float v = fmaxf(s[0][2 * half], s[0][2 * half + 1]);
-#pragma unroll
-            for (int n = 1; n < kN; ++n) v = fmaxf(v, fmaxf(s[n][2 * half], s[n][2 * half + 1]));
-            v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 1));
-            bm[half] = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 2));
-            any[half] |= full || (mask & low_bits(seen[half] - pos0)) != 0;
-        }
-        if (__any_sync(0xffffffffu, bm[0] > m[0] || bm[1] > m[1])) {
-            float alpha[2];
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const float nm = fmaxf(m[half], bm[half]);
-                alpha[half] = nm == m[half] ? 1.f : xa_exp2((m[half] - nm) * p.scale_log2);
-                m[half] = nm;
-                l[half] *= alpha[half];
-            }
-#pragma unroll
-            for (int n = 0; n < DP / 8; ++n) {
-                o[n][0] *= alpha[0];
-                o[n][1] *= alpha[0];
-                o[n][2] *= alpha[1];
-                o[n][3] *= alpha[1];
-            }
-        }
-        // (a row that has seen nothing yet: all its scores are -inf, and so are their differences to 0)
-        const float neg[2] = {m[0] == -INFINITY ? 0.f : -m[0] * p.scale_log2, m[1] == -INFINITY ? 0.f : -m[1] * p.scale_log2};
-#pragma unroll
-        for (int n = 0; n < kN; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[n][e] = xa_exp2(fmaf(s[n][e], p.scale_log2, neg[e >> 1]));
-                l[e >> 1] += s[n][e];
-            }
-        // Keys that some of the rows do not see: 0 x a value that is not finite would reach those rows through
-        // the product, so such a value's rows are added by hand and it becomes zero.
-        uint32_t partly = full ? 0u : mask & ~low_bits(seen_lo - pos0);
-        while (partly) {
-            const int j = __ffs(partly) - 1;
-            partly &= partly - 1;
-            const uint32_t row = sv + j * DP * 2;
-            const bool bad = lane < kChunks && any_not_finite<T>(ld_shared_v4(row + ((lane ^ (j & 7)) << 4)));
-            if (!__any_sync(0xffffffffu, bad)) continue;
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                float w = 0.f;
-#pragma unroll
-                for (int n = 0; n < kN; ++n)
-                    w = select(n == j >> 3, select(j & 1, s[n][2 * half + 1], s[n][2 * half]), w);
-                w = __shfl_sync(0xffffffffu, w, (lane & ~3) | ((j & 7) >> 1));
-                if (pos0 + j < seen[half]) {
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n) {
-                        const float2 f = unpack2<T>(ld_shared_u32(row + ((n ^ (j & 7)) << 4) + q4 * 4));
-                        o[n][2 * half] = fmaf(w, f.x, o[n][2 * half]);
-                        o[n][2 * half + 1] = fmaf(w, f.y, o[n][2 * half + 1]);
-                    }
-                }
-            }
-            __syncwarp();
-            if (lane < kChunks) st_shared_v4_b32(row + (lane << 4), 0, 0, 0, 0);
-            __syncwarp();
-        }
-        {
-            const int idx = lane >> 3, kr = (idx & 1) * 8 + (lane & 7);
-#pragma unroll
-            for (int h = 0; h < kN; h += 2) {
-                const uint32_t pa[4] = {XaElem<T>::pack(s[h][0], s[h][1]), XaElem<T>::pack(s[h][2], s[h][3]),
-                                        XaElem<T>::pack(s[h + 1][0], s[h + 1][1]), XaElem<T>::pack(s[h + 1][2], s[h + 1][3])};
-#pragma unroll
-                for (int n = 0; n < DP / 16; ++n) {
-                    uint32_t bf[4];
-                    ldmatrix_x4_trans(bf, sv + (h * 8 + kr) * DP * 2 + (((2 * n + (idx >> 1)) ^ (kr & 7)) << 4));
-                    mma_16x8x16<T>(o[2 * n], pa, bf[0], bf[1]);
-                    mma_16x8x16<T>(o[2 * n + 1], pa, bf[2], bf[3]);
-                }
-            }
-        }
-        __syncwarp();                                              // stage t has been read by every lane
-    }
-    cp_async_wait_group<0>();
-    __syncthreads();                                               // the rings are free
-    float *jo = reinterpret_cast<float *>(smem) + warp * (L::kPart / 4);
-    float *jm = jo + L::kRows * L::kPitch, *jl = jm + L::kRows;
-#pragma unroll
-    for (int n = 0; n < DP / 8; ++n) {
-        *reinterpret_cast<float2 *>(jo + g * L::kPitch + n * 8 + q4 * 2) = make_float2(o[n][0], o[n][1]);
-        *reinterpret_cast<float2 *>(jo + (g + 8) * L::kPitch + n * 8 + q4 * 2) = make_float2(o[n][2], o[n][3]);
-    }
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
-        l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
-        // scores of -inf alone are not the same as no scores
-        if (any[half] && m[half] == -INFINITY) l[half] = __int_as_float(0x7fc00000);
-        if (q4 == 0) {
-            jm[g + 8 * half] = m[half];
-            jl[g + 8 * half] = l[half];
-        }
-    }
-    __syncthreads();
-}
-
 // Two to four row tiles: registers do not hold a whole result per warp, so the warps share a stage.  Each takes its
 // own keys' scores for all rows (S = Q K^T), they agree on the rows' maxima, the probabilities go to shared memory (where the
 // stage's keys were), and each multiplies all of them with its own quarter of the columns of V.  Two
@@ -432,7 +264,7 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
                                                 int blk0, int blk1)
 {
     using L = PagedSmem<DP, MT>;
-    using Loader = PagedLoader<DP, MT, T>;
+    using Loader = PagedLoader<DP, T>;
     constexpr int kKeys = L::kKeys, kN = kKeys / 8, kChunks = DP / 8;
     constexpr int kAllTile = kPaWarps * L::kTile, kStage = 2 * kAllTile;   // a stage: all warps' keys, all warps' values
     constexpr int kProb = L::kBlock * 2;                           // bytes of a row of probabilities
@@ -444,7 +276,8 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
     const int key0 = blk0 * L::kBlock, key_end = min(paged_tile_seen(p, it, L::kRows, rt), blk1 * L::kBlock);
     const int tiles = key_end > key0 ? (key_end - key0 + L::kBlock - 1) / L::kBlock : 0;
     const uint32_t ring = smem_u32(smem), maxima = ring + L::kMax;
-    Loader ld(p, it, kvh, ring + warp * L::kTile, key0 + warp * kKeys, key_end, tiles);
+    Loader ld(p, ring + warp * L::kTile);
+    ld.set(it, kvh, key0 + warp * kKeys, key_end, tiles);
     ld.look_up(0);
     uint32_t there[L::kStages - 1];
 #pragma unroll
@@ -681,38 +514,6 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
     __syncthreads();
 }
 
-// Eight columns (c) of row r: the parts' sums, weighted to the common maximum, normalised; returns lse
-// (-inf: no states, and zeros).
-template <int DP, int MT>
-__device__ __forceinline__ float paged_join_parts(const PagedParams &p, const uint8_t *smem, int r, int c, float (&acc)[8])
-{
-    using L = PagedSmem<DP, MT>;
-    const float *base = reinterpret_cast<const float *>(smem);
-    constexpr int kStep = L::kPart / 4;
-    float wm[L::kParts], wl[L::kParts], mx = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < L::kParts; ++w) {
-        wm[w] = base[w * kStep + L::kRows * L::kPitch + r];
-        wl[w] = base[w * kStep + L::kRows * L::kPitch + L::kRows + r];
-        mx = fmaxf(mx, wm[w]);
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-#pragma unroll
-    for (int w = 0; w < L::kParts; ++w) {
-        if (wl[w] == 0.f) continue;                                // a part without keys
-        const float a = xa_exp2((wm[w] - mx) * p.scale_log2);
-        sum = fmaf(a, wl[w], sum);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = fmaf(a, base[w * kStep + r * L::kPitch + c * 8 + e], acc[e]);
-    }
-    if (sum == 0.f) return -INFINITY;
-    const float inv = 1.f / sum;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] *= inv;
-    return fmaf(mx, p.scale, logf(sum));
-}
-
 // Equal shares: for each key head all blocks of keys in one line, items in order, in each the row tiles; a CTA's share of it in
 // pieces (segments) that each belong to one item and row tile.
 template <int ROWS, int BLOCK> struct PagedSegments {
@@ -722,6 +523,14 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     int b, kvh, rt, blk0, blk1, blocks;        // blocks: of the item and row tile
 
     __device__ __forceinline__ explicit PagedSegments(const PagedParams &p_) : p(p_) {}
+    PagedSegments(const PagedSegments &) = default;
+    __device__ __forceinline__ PagedSegments &operator=(const PagedSegments &s)        // (of the same call)
+    {
+        pos = s.pos; end = s.end; rem = s.rem;
+        it = s.it;
+        b = s.b; kvh = s.kvh; rt = s.rt; blk0 = s.blk0; blk1 = s.blk1; blocks = s.blocks;
+        return *this;
+    }
     __device__ __forceinline__ static unsigned item_blocks(const PagedParams &p, const PagedItem &x)
     {
         unsigned n = 0;
@@ -854,73 +663,44 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     }
 };
 
-template <int DP, int MT, typename T>
-__global__ void __launch_bounds__(kPaThreads, 2)
-paged_attn_kernel(const PagedParams p)
+// A row's eight columns (c), normalised, as a part of the result: row r of [row][DP] fp32 and, behind them, lse.
+template <int DP, int ROWS>
+__device__ __forceinline__ void paged_store_part(float *slot, int r, int c, const float (&v)[8], float lse)
 {
-    using L = PagedSmem<DP, MT>;
+    float4 *dst = reinterpret_cast<float4 *>(slot + r * DP + c * 8);
+    dst[0] = make_float4(v[0], v[1], v[2], v[3]);
+    dst[1] = make_float4(v[4], v[5], v[6], v[7]);
+    if (c == 0) slot[ROWS * DP + r] = lse;
+}
+// The segment of a CTA of a cluster: an equal share of the blocks of the cluster's item, key head and row tile.  false: there is
+// nothing to do (for the whole cluster).
+template <int ROWS, int BLOCK>
+__device__ __forceinline__ bool paged_cluster_segment(const PagedParams &p, PagedSegments<ROWS, BLOCK> &seg, int rank)
+{
+    int x = blockIdx.x / p.cluster;
+    seg.rt = x % p.row_tiles;
+    x /= p.row_tiles;
+    seg.kvh = x % p.kv_heads;
+    seg.b = x / p.kv_heads;
+    seg.it = paged_item(p, seg.b);
+    seg.blocks = paged_blocks(p, seg.it, ROWS, seg.rt, BLOCK);
+    seg.blk0 = (int)((long long)seg.blocks * rank / p.cluster);
+    seg.blk1 = (int)((long long)seg.blocks * (rank + 1) / p.cluster);
+    return seg.blocks > 0;
+}
+// The cluster's CTAs each write a share of the rows' pieces, from the parts that all of them hold at `at` in shared memory.
+template <int DP, int ROWS, int BLOCK, typename T>
+__device__ __forceinline__ void paged_join_cluster(const PagedParams &p, const PagedSegments<ROWS, BLOCK> &seg, uint32_t at, int rank)
+{
     constexpr int kChunks = DP / 8;
-    extern __shared__ __align__(128) uint8_t smem[];
-    const int tid = threadIdx.x;
-    grid_launch_dependents();
-    grid_dependency_wait();
-
-    PagedSegments<L::kRows, L::kBlock> seg(p);
-    long long per = 1;
-    const int cta = blockIdx.x, rank = p.cluster ? cta % p.cluster : 0;
-    if (p.cluster) {                                               // one segment: an equal share of the cluster's item
-        int x = cta / p.cluster;
-        seg.rt = x % p.row_tiles;
-        x /= p.row_tiles;
-        seg.kvh = x % p.kv_heads;
-        seg.b = x / p.kv_heads;
-        seg.it = paged_item(p, seg.b);
-        seg.blocks = paged_blocks(p, seg.it, L::kRows, seg.rt, L::kBlock);
-        if (seg.blocks == 0) return;                               // (the whole cluster)
-        seg.blk0 = (int)((long long)seg.blocks * rank / p.cluster);
-        seg.blk1 = (int)((long long)seg.blocks * (rank + 1) / p.cluster);
-    } else {
-        if (!seg.locate(smem, per)) return;
-    }
-    for (;;) {
-        if constexpr (MT == 1) paged_walk_narrow<DP, T>(p, smem, seg.it, seg.b, seg.kvh, seg.rt, seg.blk0, seg.blk1);
-        else paged_walk_wide<DP, MT, T>(p, smem, seg.it, seg.b, seg.kvh, seg.rt, seg.blk0, seg.blk1);
-        // whole results leave at once, parts go to the cluster's or the call's scratch
-        const bool whole = seg.whole() && p.cluster <= 1;
-        const int rows = seg.rows();
-        float *slot = p.cluster ? reinterpret_cast<float *>(smem + L::kShare) : p.part + (2LL * cta + (seg.blk0 == 0)) * L::kSlot;
-        for (int i = tid; i < rows * kChunks; i += kPaThreads) {
-            const int r = i / kChunks, c = i % kChunks;
-            float acc[8];
-            const float lse = paged_join_parts<DP, MT>(p, smem, r, c, acc);
-            if (whole) {
-                const int row = seg.rt * L::kRows + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
-                paged_store<T>(p, seg.b, t, h, c, acc);
-                if (c == 0) paged_store_lse(p, seg.b, t, h, lse);
-            } else {
-                float4 *dst = reinterpret_cast<float4 *>(slot + r * DP + c * 8);
-                dst[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-                dst[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-                if (c == 0) slot[L::kRows * DP + r] = lse;
-            }
-        }
-        if (p.cluster) break;
-        if (tid == 0 && seg.blk0 == 0 && !whole) seg.describe(per);
-        if (!seg.next()) return;
-        __syncthreads();                                           // the joining blocks have been read
-    }
-    if (p.cluster == 1) return;
-
-    // the cluster's CTAs each write a share of the rows' pieces, from all of their results
     cluster_sync_all();
-    const int rows = min(seg.it.news * p.group - seg.rt * L::kRows, L::kRows);
-    const uint32_t at = smem_u32(smem) + L::kShare;
-    for (int i = rank * kPaThreads + tid; i < rows * kChunks; i += p.cluster * kPaThreads) {
+    const int rows = seg.rows();
+    for (int i = rank * kPaThreads + threadIdx.x; i < rows * kChunks; i += p.cluster * kPaThreads) {
         const int r = i / kChunks, c = i % kChunks;
         float part[kPaCluster], mx = -INFINITY, sum = 0.f, acc[8] = {};
 #pragma unroll
         for (int s = 0; s < kPaCluster; ++s) {
-            part[s] = s < p.cluster ? cluster_ld(cluster_map(at + (L::kRows * DP + r) * 4, s)) : -INFINITY;
+            part[s] = s < p.cluster ? cluster_ld(cluster_map(at + (ROWS * DP + r) * 4, s)) : -INFINITY;
             mx = fmaxf(mx, part[s]);
         }
 #pragma unroll
@@ -936,11 +716,55 @@ paged_attn_kernel(const PagedParams p)
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] *= inv;
-        const int row = seg.rt * L::kRows + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
+        const int row = seg.rt * ROWS + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
         paged_store<T>(p, seg.b, t, h, c, acc);
         if (c == 0) paged_store_lse(p, seg.b, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
     }
     cluster_sync_all();                                            // nobody's shared memory goes while it is read
+}
+
+template <int DP, int MT, typename T>
+__global__ void __launch_bounds__(kPaThreads, 2)
+paged_wide_kernel(const PagedParams p)
+{
+    using L = PagedSmem<DP, MT>;
+    constexpr int kChunks = DP / 8, kRows = L::kRows;
+    extern __shared__ __align__(128) uint8_t smem[];
+    const int tid = threadIdx.x;
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    PagedSegments<kRows, L::kBlock> seg(p);
+    long long per = 1;
+    const int cta = blockIdx.x, rank = p.cluster ? cta % p.cluster : 0;
+    if (!(p.cluster ? paged_cluster_segment(p, seg, rank) : seg.locate(smem, per))) return;
+    for (;;) {
+        paged_walk_wide<DP, MT, T>(p, smem, seg.it, seg.b, seg.kvh, seg.rt, seg.blk0, seg.blk1);
+        // whole results leave at once, parts go to the cluster's or the call's scratch
+        const bool whole = seg.whole() && p.cluster <= 1;
+        const int rows = seg.rows();
+        const float *o = reinterpret_cast<const float *>(smem), *m = o + kRows * L::kPitch, *l = m + kRows;
+        float *slot = p.cluster ? reinterpret_cast<float *>(smem + L::kShare) : p.part + (2LL * cta + (seg.blk0 == 0)) * kRows * (DP + 1);
+        for (int i = tid; i < rows * kChunks; i += kPaThreads) {
+            const int r = i / kChunks, c = i % kChunks;
+            const float sum = l[r], inv = sum == 0.f ? 0.f : 1.f / sum, lse = sum == 0.f ? -INFINITY : fmaf(m[r], p.scale, logf(sum));
+            float acc[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = o[r * L::kPitch + c * 8 + e] * inv;
+            if (whole) {
+                const int row = seg.rt * kRows + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
+                paged_store<T>(p, seg.b, t, h, c, acc);
+                if (c == 0) paged_store_lse(p, seg.b, t, h, lse);
+            } else {
+                paged_store_part<DP, kRows>(slot, r, c, acc, lse);
+            }
+        }
+        if (p.cluster) break;
+        if (tid == 0 && seg.blk0 == 0 && !whole) seg.describe(per);
+        if (!seg.next()) return;
+        __syncthreads();                                           // the result has been read
+    }
+    if (p.cluster > 1) paged_join_cluster<DP, kRows, L::kBlock, T>(p, seg, smem_u32(smem) + L::kShare, rank);
 }
 
 // The parts of an item's key head and row tile that several CTAs worked on, added up in order: the first lies in slot 1 of
