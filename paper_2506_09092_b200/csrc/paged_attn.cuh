@@ -515,10 +515,13 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
 }
 
 // Equal shares: for each key head all blocks of keys in one line, items in order, in each the row tiles; a CTA's share of it in
-// pieces (segments) that each belong to one item and row tile.
+// pieces (segments) that each belong to one item and row tile.  Every row tile has kPaStart units in the line before its
+// blocks: what beginning and ending a segment costs, in blocks (128 sequences of 250 to 1000 states, 8 key heads of
+// 128: 70.2 us with 0, 67.8, 64.2 and 63.1 us with 1, 2 and 3; 48 of 1024 to 4096: 86.0 and 83.8 us with 0 and 3).
+constexpr int kPaStart = 3;
 template <int ROWS, int BLOCK> struct PagedSegments {
     const PagedParams &p;
-    long long pos, end, rem;                   // the block behind the segment, the share's end, pos counted from the item's first block
+    long long pos, end, rem;                   // the unit behind the segment, the share's end, pos counted from the item's first unit
     PagedItem it;
     int b, kvh, rt, blk0, blk1, blocks;        // blocks: of the item and row tile
 
@@ -531,39 +534,41 @@ template <int ROWS, int BLOCK> struct PagedSegments {
         b = s.b; kvh = s.kvh; rt = s.rt; blk0 = s.blk0; blk1 = s.blk1; blocks = s.blocks;
         return *this;
     }
-    __device__ __forceinline__ static unsigned item_blocks(const PagedParams &p, const PagedItem &x)
+    __device__ __forceinline__ static unsigned units(int blocks) { return blocks > 0 ? blocks + kPaStart : 0; }
+    __device__ __forceinline__ static unsigned item_units(const PagedParams &p, const PagedItem &x)
     {
         unsigned n = 0;
-        for (int r = 0; r < p.row_tiles; ++r) n += paged_blocks(p, x, ROWS, r, BLOCK);
+        for (int r = 0; r < p.row_tiles; ++r) n += units(paged_blocks(p, x, ROWS, r, BLOCK));
         return n;
     }
     __device__ __forceinline__ static long long divide(long long a, unsigned d)
     {
         return a >> 32 ? a / d : (long long)((unsigned)a / d);
     }
-    // Where in its item, which has `all` blocks, the next segment lies.
-    __device__ __forceinline__ void place(unsigned all)
+    // The next segment in this item, which has `all` units, rem of them behind us; false: the share has none of its blocks.
+    __device__ __forceinline__ bool place(unsigned all)
     {
-        blk0 = (int)rem;
-        if (p.row_tiles == 1) {
-            rt = 0;
-            blocks = (int)all;
-        } else {
-            for (rt = 0; blk0 >= (blocks = paged_blocks(p, it, ROWS, rt, BLOCK)); ++rt) blk0 -= blocks;
+        while (pos < end && rem < (long long)all) {
+            unsigned at = (unsigned)rem, own;
+            for (rt = 0; at >= (own = units(blocks = paged_blocks(p, it, ROWS, rt, BLOCK))); ++rt) at -= own;
+            const unsigned upto = (unsigned)min((long long)own, at + (end - pos));
+            pos += upto - at;
+            rem += upto - at;
+            blk0 = max((int)at - kPaStart, 0);
+            blk1 = max((int)upto - kPaStart, 0);
+            if (blk1 > blk0) return true;
         }
-        blk1 = (int)min((long long)blocks, blk0 + (end - pos));
-        pos += blk1 - blk0;
-        rem += blk1 - blk0;
+        return false;
     }
-    // How many blocks there are in all, and where this CTA's share begins: the first 128 threads count, `each` items a
+    // How many units there are in all, and where this CTA's share begins: the first 128 threads count, `each` items a
     // thread, and the one that has found the place makes out the first segment (and whether there is one, which it
-    // returns).  All of the CTA's threads call it; `smem` is free again afterwards.  per: blocks of a share.
+    // returns).  All of the CTA's threads call it; `smem` is free again afterwards.  per: units of a share.
     __device__ __forceinline__ bool locate(uint8_t *smem, long long &per)
     {
         struct Found {
             long long pos, end, rem, per;
             PagedItem it;
-            int b, rt, blk0, blk1, blocks;
+            int b, rt, blk0, blk1, blocks, some;
         };
         long long *warp_sum = reinterpret_cast<long long *>(smem);
         Found &found = *reinterpret_cast<Found *>(warp_sum + kPaWarps);
@@ -574,10 +579,10 @@ template <int ROWS, int BLOCK> struct PagedSegments {
             for (int i = 0; i < each; ++i)
                 if (tid * each + i < p.batch) {
                     it = paged_item(p, tid * each + i);
-                    all = item_blocks(p, it);
+                    all = item_units(p, it);
                     sum += all;
                 }
-            upto = sum;                                            // blocks of all threads up to this one
+            upto = sum;                                            // units of all threads up to this one
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
                 const long long v = __shfl_up_sync(0xffffffffu, upto, d);
@@ -586,7 +591,7 @@ template <int ROWS, int BLOCK> struct PagedSegments {
             if (lane == 31) warp_sum[warp] = upto;
         }
         if (tid == 0) {
-            found.pos = found.end = 0;                             // (nobody's, unless one of the threads finds its place)
+            found.some = 0;                                        // (unless one of the threads finds its place)
             p.desc[blockIdx.x * kPaDesc] = 0;
         }
         __syncthreads();
@@ -606,12 +611,12 @@ template <int ROWS, int BLOCK> struct PagedSegments {
                 if (each > 1)
                     for (;; ++b) {
                         it = paged_item(p, b);
-                        all = item_blocks(p, it);
+                        all = item_units(p, it);
                         if (rem < (long long)all) break;
                         rem -= all;
                     }
-                place(all);
-                found = Found{pos, end, rem, per, it, b, rt, blk0, blk1, blocks};
+                const bool some = place(all) || next();
+                found = Found{pos, end, rem, per, it, b, rt, blk0, blk1, blocks, some};
             }
         }
         __syncthreads();
@@ -628,21 +633,19 @@ template <int ROWS, int BLOCK> struct PagedSegments {
         blk1 = f.blk1;
         blocks = f.blocks;
         __syncthreads();
-        return pos > 0;
+        return f.some;
     }
     // The next segment; false: there are no more.
     __device__ __forceinline__ bool next()
     {
-        if (pos >= end) return false;
-        for (;; ++b) {
+        for (; pos < end; ++b) {
             it = paged_item(p, b);
-            const unsigned all = item_blocks(p, it);
-            if (rem < (long long)all) {
-                place(all);
-                return true;
-            }
+            const unsigned all = item_units(p, it);
+            if (rem < (long long)all && place(all)) return true;
+            if (pos >= end) break;
             rem -= all;
         }
+        return false;
     }
     __device__ __forceinline__ int rows() const { return min(it.news * p.group - rt * ROWS, ROWS); }
     __device__ __forceinline__ int key0() const { return blk0 * BLOCK; }
@@ -689,7 +692,7 @@ __device__ __forceinline__ bool paged_cluster_segment(const PagedParams &p, Page
     return seg.blocks > 0;
 }
 // The cluster's CTAs each write a share of the rows' pieces, from the parts that all of them hold at `at` in shared memory.
-template <int DP, int ROWS, int BLOCK, typename T>
+template <int DP, typename T, int ROWS, int BLOCK>
 __device__ __forceinline__ void paged_join_cluster(const PagedParams &p, const PagedSegments<ROWS, BLOCK> &seg, uint32_t at, int rank)
 {
     constexpr int kChunks = DP / 8;
@@ -764,7 +767,7 @@ paged_wide_kernel(const PagedParams p)
         if (!seg.next()) return;
         __syncthreads();                                           // the result has been read
     }
-    if (p.cluster > 1) paged_join_cluster<DP, kRows, L::kBlock, T>(p, seg, smem_u32(smem) + L::kShare, rank);
+    if (p.cluster > 1) paged_join_cluster<DP, T>(p, seg, smem_u32(smem) + L::kShare, rank);
 }
 
 // The parts of an item's key head and row tile that several CTAs worked on, added up in order: the first lies in slot 1 of
