@@ -517,15 +517,19 @@ def _main(argv=None):
     ap.add_argument("--table", default=None, help="with --search: JSON file to record the winner in")
     ap.add_argument("--dispatch", default=None,
                     help="a table file, or 'packaged': enter its records into the library's dispatch table first")
-    ap.add_argument("--task", default=None, choices=["transpose", "sum", "dot", "layernorm", "attention", "tf32", "f32", *LAYER_TASKS],
+    ap.add_argument("--task", default=None, choices=["transpose", "sum", "dot", "layernorm", "attention", "tf32", "f32", *LAYER_TASKS, *CACHE_TASKS],
                     help="time one of the other tasks (8, 14, 15, 4, 6; tf32 / f32: Task 2 with float32 operands "
-                         "through cudallm_gemm_tf32 / cudallm_gemm_f32; ln-rows ... xattn-bwd: the layer operators) "
+                         "through cudallm_gemm_tf32 / cudallm_gemm_f32; ln-rows ... xattn-bwd: the layer operators; "
+                         "paged-attn ... draft-verify: those of a paged cache) "
                          "instead of a GEMM configuration")
     ap.add_argument("--size", type=int, default=None,
                     help="with --task: N (transpose: N x N; sum, dot: N elements; layernorm: (16, 4, N, N); "
                          "attention: N queries and keys; tf32, f32: A (N x 4096) x B (4096 x 2048); ln-rows, ln-rows-bwd: "
                          "bf16 N x 4096; grad-clip: N bf16 gradients in 48 tensors; xattn, xattn-bwd: N queries x 2 N "
-                         "states, 16 heads of 128; xattn-token: 8 tokens x N states, 32 heads on 8 key heads of 128)")
+                         "states, 16 heads of 128; xattn-token: 8 tokens x N states, 32 heads on 8 key heads of 128; "
+                         "paged-attn: 16 sequences of N states, a new token each; paged-drafts: five each, under 8 heads a key "
+                         "head; cache-append: N tokens each of 8 sequences; pages-copy: N pages of 32 KiB in 16 pools; "
+                         "draft-verify: 64 sequences, 5 drafts, N tokens to choose from)")
     ap.add_argument("--layernorm-kernels", default="auto", choices=["auto", "two", "persistent"],
                     help="with --task layernorm: let the library choose by size, or force the two plain "
                          "kernels / the persistent kernel (cudallm_debug_set)")
@@ -638,6 +642,55 @@ def layer_problem(task: str, size: int, nsets: int | None = None):
                                   dv[i % n], scratch, need, st)), 2 * bytes_, what
 
 
+CACHE_TASKS = ("paged-attn", "paged-drafts", "cache-append", "pages-copy", "draft-verify")
+
+
+def cache_problem(task: str, size: int, nsets: int | None = None):
+    """The same for the operators of include/cudallm_cache.h (``CACHE_TASKS``)."""
+    import torch
+    from . import binding as B
+
+    st = torch.cuda.current_stream()
+    gen = torch.Generator(device="cuda").manual_seed(901)
+
+    def sets(bytes_):
+        return nsets or max(1, min(8, (400 << 20) // max(bytes_, 1) + 1))
+
+    def normal(*shape):
+        return torch.empty(*shape, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+
+    if task == "draft-verify":
+        batch, drafts = 64, 5
+        p, q = (torch.softmax(torch.randn(batch, drafts + i, size, generator=gen, device="cuda") * 2, 2) for i in (1, 0))
+        x = torch.multinomial(q.view(batch * drafts, size), 1, generator=gen).int()
+        u = torch.rand(batch, drafts + 1, generator=gen, device="cuda")
+        tokens, accepted = torch.empty(batch, drafts + 1, dtype=torch.int32, device="cuda"), torch.empty(batch, dtype=torch.int32, device="cuda")
+        return (lambda i: B.draft_verify(p, q, x, None, u, tokens, accepted, batch, drafts, size, size, size, B.F32, st)), \
+            2 * 4 * batch * size, f"{batch} sequences, {drafts} drafts, {size} tokens, float32"
+    if task == "pages-copy":
+        pools = normal(16, 2 * size, 16384)
+        table = B.page_pools(list(pools))
+        src, dst = torch.randperm(2 * size, generator=gen, device="cuda").int().chunk(2)
+        return (lambda i: B.pages_copy(table, src, dst, size, st)), 2 * 32768 * 16 * size, f"{size} pages of 32 KiB in 16 pools"
+    rows, hk, hq, batch = {"paged-attn": (1, 8, 32, 16), "paged-drafts": (5, 4, 32, 16), "cache-append": (size, 8, 32, 8)}[task]
+    cols = (size + 15) // 16
+    bytes_ = 2 * 2 * 128 * hk * batch * size * (2 if task == "cache-append" else 1)
+    n = sets(bytes_)
+    k, v = ([normal(batch * cols, 16, hk, 128) for _ in range(n)] for _ in range(2))
+    table = torch.randperm(batch * cols, generator=gen, device="cuda").int().view(batch, cols)
+    lens = torch.full((batch,), size, dtype=torch.int32, device="cuda")
+    qkv = normal(batch, rows, hq + 2 * hk, 128)
+    q, k_new, v_new = qkv[:, :, :hq], qkv[:, :, hq:hq + hk], qkv[:, :, hq + hk:]
+    o = torch.empty(batch, rows, hq, 128, dtype=torch.bfloat16, device="cuda")
+    shape = B.PagedShape.of(q, k[0], v[0], o, table, k_new, v_new)
+    what = f"{batch} sequences of {size} states in pages of 16, {rows} new tokens, {hq} heads on {hk} key heads of 128, bf16"
+    if task == "cache-append":
+        return (lambda i: B.cache_append(shape, k_new, v_new, k[i % n], v[i % n], table, lens, None, None, st)), bytes_, what
+    need = B.paged_attn_scratch_bytes(shape)
+    scratch = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    return (lambda i: B.paged_attn(shape, q, k[i % n], v[i % n], table, lens, None, None, o, None, scratch, need, st)), bytes_, what
+
+
 def task_problem(task: str, size: int, nsets: int | None = None):
     """(launch(i), algorithmic bytes per call, description) for one task on seeded device
     inputs, with enough rotating buffer sets to exceed L2 (at most 8)."""
@@ -705,11 +758,12 @@ def _task_main(args):
 
     default = {"transpose": 8192, "sum": 1 << 28, "dot": 1 << 27, "layernorm": 512, "attention": 512,
                "tf32": 1 << 14, "f32": 1 << 14, "ln-rows": 16384, "ln-rows-bwd": 16384, "grad-clip": 1 << 28, "xattn": 2048,
-               "xattn-token": 16384, "xattn-bwd": 2048}
+               "xattn-token": 16384, "xattn-bwd": 2048, "paged-attn": 16384, "paged-drafts": 16384, "cache-append": 2048,
+               "pages-copy": 1024, "draft-verify": 128000}
     size = args.size or default[args.task]
     if args.task == "layernorm":
         B.debug_set(B.DEBUG_LAYERNORM_PATH, {"auto": 0, "two": 1, "persistent": 2}[args.layernorm_kernels])
-    problem = layer_problem if args.task in LAYER_TASKS else task_problem
+    problem = layer_problem if args.task in LAYER_TASKS else cache_problem if args.task in CACHE_TASKS else task_problem
     launch, bytes_, what = problem(args.task, size, args.sets)
     t = performance_profiler(launch, iters=args.iters, warmup=args.warmup)
     code, detail = B.device_status(torch.cuda.current_stream())
