@@ -119,7 +119,7 @@ Plan plan_attn(const cudallm_paged_shape &s)
     // as many shares of every key head as fit at once, but no more than there are blocks
     f.shares = (int)std::max<int64_t>(1, std::min<int64_t>((tile ? 1 : 2) * kPlanSms / s.kv_heads, s.batch * f.row_tiles * blocks));
     f.ctas = (int)(f.shares * s.kv_heads);
-    f.part_bytes = 2 * (size_t)f.ctas * (size_t)tile_rows * ((f.wide ? 128 : 64) + 1) * sizeof(float);
+    f.part_bytes = f.shares == 1 ? 0 : 2 * (size_t)f.ctas * (size_t)tile_rows * ((f.wide ? 128 : 64) + 1) * sizeof(float);
     f.scratch = f.part_bytes + (size_t)f.ctas * kPaDesc * sizeof(int);
     return f;
 }

@@ -521,7 +521,8 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
 constexpr int kPaStart = 3;
 template <int ROWS, int BLOCK> struct PagedSegments {
     const PagedParams &p;
-    long long pos, end, rem;                   // the unit behind the segment, the share's end, pos counted from the item's first unit
+    long long pos, end;                        // in units: behind the segment, the share's end
+    int at;                                    // behind the segment, of its row tile
     PagedItem it;
     int b, kvh, rt, blk0, blk1, blocks;        // blocks: of the item and row tile
 
@@ -529,58 +530,69 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     PagedSegments(const PagedSegments &) = default;
     __device__ __forceinline__ PagedSegments &operator=(const PagedSegments &s)        // (of the same call)
     {
-        pos = s.pos; end = s.end; rem = s.rem;
+        pos = s.pos; end = s.end; at = s.at;
         it = s.it;
         b = s.b; kvh = s.kvh; rt = s.rt; blk0 = s.blk0; blk1 = s.blk1; blocks = s.blocks;
         return *this;
     }
-    __device__ __forceinline__ static unsigned units(int blocks) { return blocks > 0 ? blocks + kPaStart : 0; }
-    __device__ __forceinline__ static unsigned item_units(const PagedParams &p, const PagedItem &x)
+    __device__ __forceinline__ static int units(int blocks) { return blocks > 0 ? blocks + kPaStart : 0; }
+    __device__ __forceinline__ void enter(int b_, int rt_)
     {
-        unsigned n = 0;
-        for (int r = 0; r < p.row_tiles; ++r) n += units(paged_blocks(p, x, ROWS, r, BLOCK));
-        return n;
+        if (b_ != b) it = paged_item(p, b_);
+        b = b_;
+        rt = rt_;
+        at = 0;
+        blocks = paged_blocks(p, it, ROWS, rt, BLOCK);
     }
-    __device__ __forceinline__ static long long divide(long long a, unsigned d)
+    __device__ __forceinline__ static long long divide(long long a, long long d)
     {
-        return a >> 32 ? a / d : (long long)((unsigned)a / d);
+        return (a | d) >> 32 ? a / d : (long long)((unsigned)a / (unsigned)d);
     }
-    // The next segment in this item, which has `all` units, rem of them behind us; false: the share has none of its blocks.
-    __device__ __forceinline__ bool place(unsigned all)
+    // The next segment; false: there are no more.
+    __device__ __forceinline__ bool next()
     {
-        while (pos < end && rem < (long long)all) {
-            unsigned at = (unsigned)rem, own;
-            for (rt = 0; at >= (own = units(blocks = paged_blocks(p, it, ROWS, rt, BLOCK))); ++rt) at -= own;
-            const unsigned upto = (unsigned)min((long long)own, at + (end - pos));
-            pos += upto - at;
-            rem += upto - at;
-            blk0 = max((int)at - kPaStart, 0);
-            blk1 = max((int)upto - kPaStart, 0);
-            if (blk1 > blk0) return true;
+        while (pos < end) {
+            const int own = units(blocks);
+            if (at < own) {
+                const int upto = (int)min((long long)own, at + (end - pos));
+                blk0 = max(at - kPaStart, 0);
+                blk1 = max(upto - kPaStart, 0);
+                pos += upto - at;
+                at = upto;
+                if (blk1 > blk0) return true;
+            } else if (rt + 1 < p.row_tiles && blocks > 0) {
+                enter(b, rt + 1);
+            } else {
+                enter(b + 1, 0);                                   // (there is one: the share has units left)
+            }
         }
         return false;
     }
-    // How many units there are in all, and where this CTA's share begins: the first 128 threads count, `each` items a
-    // thread, and the one that has found the place makes out the first segment (and whether there is one, which it
-    // returns).  All of the CTA's threads call it; `smem` is free again afterwards.  per: units of a share.
+    // How many units there are in all, and where this CTA's share begins: each of the first 128 threads counts the row tiles of
+    // some items, or some of the row tiles of one, and the one that has found the place makes out the first segment (and
+    // whether there is one, which it returns).  All of the CTA's threads call it; `smem` is free again afterwards.
+    // per: units of a share.
     __device__ __forceinline__ bool locate(uint8_t *smem, long long &per)
     {
         struct Found {
-            long long pos, end, rem, per;
+            long long pos, end, per;
             PagedItem it;
-            int b, rt, blk0, blk1, blocks, some;
+            int at, b, rt, blk0, blk1, blocks, some;
         };
         long long *warp_sum = reinterpret_cast<long long *>(smem);
         Found &found = *reinterpret_cast<Found *>(warp_sum + kPaWarps);
-        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, each = (p.batch + kPaThreads - 1) / kPaThreads;
+        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+        const int each = (p.batch + kPaThreads - 1) / kPaThreads;  // items a thread
+        const int sharing = p.row_tiles > 1 ? max(1, kPaThreads / p.batch) : 1;            // threads an item, if there are fewer
+        const int tiles = (p.row_tiles + sharing - 1) / sharing, b0 = tid / sharing * each, rt0 = tid % sharing * tiles;
         long long sum = 0, upto = 0;
-        unsigned all = 0;
+        b = -1;
         if (tid < kPaThreads) {
-            for (int i = 0; i < each; ++i)
-                if (tid * each + i < p.batch) {
-                    it = paged_item(p, tid * each + i);
-                    all = item_units(p, it);
-                    sum += all;
+            for (int i = b0; i < min(b0 + each, p.batch); ++i)
+                for (int r = rt0; r < min(rt0 + tiles, p.row_tiles); ++r) {
+                    enter(i, r);
+                    if (blocks == 0) break;
+                    sum += units(blocks);
                 }
             upto = sum;                                            // units of all threads up to this one
 #pragma unroll
@@ -602,28 +614,27 @@ template <int ROWS, int BLOCK> struct PagedSegments {
                 if (w < warp) upto += warp_sum[w];
                 total += warp_sum[w];
             }
-            per = max(divide(total + p.shares - 1, (unsigned)p.shares), 1LL);
+            per = max(divide(total + p.shares - 1, p.shares), 1LL);
             pos = (blockIdx.x / (unsigned)p.kv_heads) * per;
             end = min(total, pos + per);
-            rem = pos - (upto - sum);
+            long long rem = pos - (upto - sum);
             if (pos < end && rem >= 0 && rem < sum) {
-                b = tid * each;
-                if (each > 1)
-                    for (;; ++b) {
-                        it = paged_item(p, b);
-                        all = item_units(p, it);
-                        if (rem < (long long)all) break;
-                        rem -= all;
+                if (each > 1 || tiles > 1)                         // (else it has entered its only one)
+                    for (enter(b0, rt0); rem >= units(blocks);) {
+                        rem -= units(blocks);
+                        if (rt + 1 < min(rt0 + tiles, p.row_tiles) && blocks > 0) enter(b, rt + 1);
+                        else enter(b + 1, rt0);
                     }
-                const bool some = place(all) || next();
-                found = Found{pos, end, rem, per, it, b, rt, blk0, blk1, blocks, some};
+                at = (int)rem;
+                const bool some = next();
+                found = Found{pos, end, per, it, at, b, rt, blk0, blk1, blocks, some};
             }
         }
         __syncthreads();
         const Found f = found;
         pos = f.pos;
         end = f.end;
-        rem = f.rem;
+        at = f.at;
         per = f.per;
         it = f.it;
         b = f.b;
@@ -634,18 +645,6 @@ template <int ROWS, int BLOCK> struct PagedSegments {
         blocks = f.blocks;
         __syncthreads();
         return f.some;
-    }
-    // The next segment; false: there are no more.
-    __device__ __forceinline__ bool next()
-    {
-        for (; pos < end; ++b) {
-            it = paged_item(p, b);
-            const unsigned all = item_units(p, it);
-            if (rem < (long long)all && place(all)) return true;
-            if (pos >= end) break;
-            rem -= all;
-        }
-        return false;
     }
     __device__ __forceinline__ int rows() const { return min(it.news * p.group - rt * ROWS, ROWS); }
     __device__ __forceinline__ int key0() const { return blk0 * BLOCK; }
@@ -659,7 +658,7 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     __device__ __forceinline__ void describe(long long per) const
     {
         int *d = p.desc + blockIdx.x * kPaDesc;
-        d[0] = ((int)divide(pos - blk1 + blocks - 1, (unsigned)min(per, 0xffffffffLL)) - (int)(blockIdx.x / (unsigned)p.kv_heads) + 1) | rows() << 16;
+        d[0] = ((int)divide(pos - blk1 + blocks - 1, per) - (int)(blockIdx.x / (unsigned)p.kv_heads) + 1) | rows() << 16;
         d[1] = b;
         d[2] = kvh;
         d[3] = rt;
