@@ -19,7 +19,8 @@ constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxElems = int64_t(1) << 46;          // of an operand, strides included
 constexpr int64_t kMaxTmaStride = int64_t(1) << 39;      // elements
 constexpr int64_t kPlanSms = 148;                        // the split is planned for this many SMs
-constexpr int64_t kClusterBlocks = 16;                   // blocks of keys that a CTA of a cluster may get at most
+constexpr int64_t kClusterBlocks = 16;                   // blocks of keys that a CTA of a cluster may get at most,
+constexpr int64_t kClusterMore = 4;                      // and how many more than an equal share would have
 
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool off(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
@@ -111,7 +112,13 @@ Plan plan_attn(const cudallm_paged_shape &s)
     f.row_tiles = (int)cdiv(rows, tile_rows);
     const int64_t items = s.batch * s.kv_heads * f.row_tiles, blocks = std::max<int64_t>(1, cdiv(cap, block));
     const int64_t fits = std::min<int64_t>({int64_t(kPaCluster), 2 * kPlanSms / std::max<int64_t>(items, 1), blocks});
-    if (!tile && items <= kPlanSms && blocks <= kClusterBlocks * fits) {
+    // A cluster per item needs no second launch, but takes as long as the longest item and may leave SMs idle: blocks / fits against
+    // blocks x items / (two CTAs an SM) blocks, one of them about a microsecond, and the launch that joins costs about four.
+    // (Heads of 128, 4 rows, clusters against equal shares, us: one item of 1000, 2000, 4000 states 8.3 / 9.6, 10.0 / 9.9, 14.0 / 10.0;
+    // 8 items of 2000, 4000: 10.4 / 11.2, 14.5 / 11.6; 32 items of 4000, 8000: 16.4 / 18.4, 27.9 / 30.2; 64 items of 4000: 27.1 /
+    // 29.6, of 1000 to 4000: 23.5 / 20.1.)
+    if (!tile && items <= kPlanSms && blocks <= kClusterBlocks * fits
+        && blocks * (2 * kPlanSms - fits * items) <= kClusterMore * 2 * kPlanSms * fits) {
         f.cluster = (int)std::max<int64_t>(1, fits);
         f.ctas = (int)(items * f.cluster);
         return f;
@@ -144,13 +151,21 @@ int allow_smem(Kernel kernel, int bytes, std::atomic<bool> (&done)[kRtMaxDevices
     return CUDALLM_OK;
 }
 
+constexpr int64_t kJoinCtas = 16 * kPlanSms;             // of 128 threads: a full machine
 // Equal shares leave parts of items behind, to be joined.
 template <int DP, int ROWS, typename T>
 int join(const cudallm_paged_shape &s, const Plan &f, const PagedParams &p, cudaStream_t stream)
 {
     if (f.shares == 1) return CUDALLM_OK;
+    constexpr int64_t kMaxGroups = kPaJoinThreads / (DP / 8);
     const int64_t rows = std::min<int64_t>(ROWS, (int64_t)p.group * s.q_rows);
-    return rt_launch(paged_join_kernel<DP, ROWS, T>, dim3((unsigned)f.ctas, (unsigned)cdiv(rows, 128 / (DP / 8))), 128, 0, stream, p);
+    // threads for every eight or so of the parts that an item has on average; all CTAs that may have one to join run at once
+    const int64_t parts = cdiv(f.shares, s.batch * f.row_tiles) + 1;
+    int64_t groups = 1;
+    while (groups < kMaxGroups && parts > 8 * groups) groups *= 2;
+    const int64_t y = cdiv(rows, kMaxGroups / groups);
+    return rt_launch(paged_join_kernel<DP, ROWS, T>, dim3((unsigned)f.ctas, (unsigned)std::min<int64_t>(y, std::max<int64_t>(1, kJoinCtas / f.ctas))),
+                     kPaJoinThreads, 0, stream, p, (int)groups);
 }
 // The mma.sync kernels: ROWS rows of a key head a CTA.
 template <int DP, int ROWS, typename T, typename Kernel>
