@@ -161,11 +161,11 @@ int join(const cudallm_paged_shape &s, const Plan &f, const PagedParams &p, cuda
     const int64_t rows = std::min<int64_t>(ROWS, (int64_t)p.group * s.q_rows);
     // threads for every eight or so of the parts that an item has on average; all CTAs that may have one to join run at once
     const int64_t parts = cdiv(f.shares, s.batch * f.row_tiles) + 1;
-    int64_t groups = 1;
-    while (groups < kMaxGroups && parts > 8 * groups) groups *= 2;
-    const int64_t y = cdiv(rows, kMaxGroups / groups);
+    int shift = 0;
+    while (1 << shift < kMaxGroups && parts > 8 << shift) ++shift;
+    const int64_t y = cdiv(rows, kMaxGroups >> shift);
     return rt_launch(paged_join_kernel<DP, ROWS, T>, dim3((unsigned)f.ctas, (unsigned)std::min<int64_t>(y, std::max<int64_t>(1, kJoinCtas / f.ctas))),
-                     kPaJoinThreads, 0, stream, p, (int)groups);
+                     kPaJoinThreads, 0, stream, p, shift);
 }
 // The mma.sync kernels: ROWS rows of a key head a CTA.
 template <int DP, int ROWS, typename T, typename Kernel>
@@ -268,6 +268,11 @@ int cudallm_paged_attn(const cudallm_paged_shape *shape, const void *q, const vo
     p.row_tiles = f.row_tiles;
     p.cluster = f.cluster;
     p.shares = f.shares;
+    // 128 threads count the units of all row tiles: some items each, or (more row tiles than one, few items) some each of an item's
+    p.count_items = (int)cdiv(s.batch, kPaThreads);
+    if (f.row_tiles > 1)
+        while (s.batch << (p.count_shift + 1) <= kPaThreads) ++p.count_shift;
+    p.count_tiles = (int)cdiv(f.row_tiles, int64_t(1) << p.count_shift);
     p.scale = s.scale; p.scale_log2 = scale_log2(s.scale);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     return s.dtype == CUDALLM_BF16 ? run<__nv_bfloat16>(s, f, p, dev, cs) : run<__half>(s, f, p, dev, cs);

@@ -46,6 +46,8 @@ struct PagedParams {
     int row_tiles;                             // tiles of 16 or 32 rows of an item and key head at most
     int cluster;                               // CTAs per item, key head and row tile; 0: equal shares
     int shares;                                // of a key head; CTA = share * kv_heads + key head
+    // who counts what (locate): items a thread, or 2^count_shift threads an item, count_tiles row tiles each
+    int count_items, count_shift, count_tiles;
     float scale, scale_log2;
 };
 constexpr int kPaDesc = 4;                     // parts (0: none begins here) and 2^16 x rows, item, key head, row tile
@@ -581,10 +583,8 @@ template <int ROWS, int BLOCK> struct PagedSegments {
         };
         long long *warp_sum = reinterpret_cast<long long *>(smem);
         Found &found = *reinterpret_cast<Found *>(warp_sum + kPaWarps);
-        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-        const int each = (p.batch + kPaThreads - 1) / kPaThreads;  // items a thread
-        const int sharing = p.row_tiles > 1 ? max(1, kPaThreads / p.batch) : 1;            // threads an item, if there are fewer
-        const int tiles = (p.row_tiles + sharing - 1) / sharing, b0 = tid / sharing * each, rt0 = tid % sharing * tiles;
+        const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, each = p.count_items, tiles = p.count_tiles;
+        const int b0 = (tid >> p.count_shift) * each, rt0 = (tid & ((1 << p.count_shift) - 1)) * tiles;
         long long sum = 0, upto = 0;
         b = -1;
         if (tid < kPaThreads) {
@@ -771,25 +771,25 @@ paged_wide_kernel(const PagedParams p)
 
 // The parts of an item's key head and row tile that several CTAs worked on, added up in order: the first lies in slot 1 of
 // the CTA that it began in, the others in slot 0 of the next CTAs of the key head.  blockIdx.x: that CTA.  Where an item may
-// have many parts (few items over many CTAs), `groups` threads take every groups-th part of a row's eight columns and join at
+// have many parts (few items over many CTAs), 2^group_shift threads share a row's eight columns, part by part in turn, and join at
 // the end (16000 and 64000 states of one key head of 128, some 250 parts: 12.3 and 17.5 us the whole call, 23.1 and 39.7 with one).
 constexpr int kPaJoinThreads = 128;
 template <int DP, int ROWS, typename T>
 __global__ void __launch_bounds__(kPaJoinThreads)
-paged_join_kernel(const PagedParams p, const int groups)
+paged_join_kernel(const PagedParams p, const int group_shift)
 {
     constexpr int kChunks = DP / 8, kSlot = ROWS * (DP + 1);
     __shared__ float shared[kPaJoinThreads][11];               // of each thread: the maximum, the sum, eight columns
     grid_launch_dependents();
     grid_dependency_wait();
-    const int cta = blockIdx.x;
+    const int cta = blockIdx.x, groups = 1 << group_shift;
     const int4 d = *reinterpret_cast<const int4 *>(p.desc + cta * kPaDesc);
     if (d.x == 0) return;
     const int parts = d.x & 0xffff, rows = d.x >> 16;
-    const int c = threadIdx.x % kChunks, g = threadIdx.x / kChunks % groups, each = kPaJoinThreads / kChunks / groups;
+    const int c = threadIdx.x % kChunks, g = threadIdx.x / kChunks & (groups - 1), each = kPaJoinThreads / kChunks >> group_shift;
     const float *first = p.part + (2LL * cta + 1) * kSlot, *next = p.part + 2LL * (cta + p.kv_heads) * kSlot;
     for (int r0 = blockIdx.y * each; r0 < rows; r0 += gridDim.y * each) {
-        const int r = r0 + threadIdx.x / (kChunks * groups);
+        const int r = r0 + (threadIdx.x / kChunks >> group_shift);
         float mx = -INFINITY, sum = 0.f, acc[8] = {};
         for (int s0 = g; s0 < parts && r < rows; s0 += 8 * groups) {
             float lse[8], top = mx;
