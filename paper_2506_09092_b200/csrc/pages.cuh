@@ -115,7 +115,10 @@ pages_fork_kernel(const ForkParams p)
         bool live = (unsigned)src < (unsigned)bk.slots && (unsigned)dst < (unsigned)bk.slots && src != dst;
         const int len = live ? book_len(bk, src) : -1, held = live ? pages_of(bk, len) : 0;
         if (c0 > 0 && c0 >= held) continue;
-        for (int j = lane; j < i && live; j += 32) live = !(p.dst[j] == dst && (unsigned)p.src[j] < (unsigned)bk.slots);
+        bool taken = false;                                        // (no early end: the loads of several rounds run side by side)
+#pragma unroll 4
+        for (int j = lane; j < i; j += 32) taken |= p.dst[j] == dst & (unsigned)p.src[j] < (unsigned)bk.slots;
+        live &= !taken;
         live = __all_sync(0xffffffffu, live);
         if (c0 == 0 && lane == 0) p.staged_len[i] = live ? len : -1;
         if (!live) continue;
@@ -227,6 +230,7 @@ struct ResizeParams {
     int *claims, *claimer;                     // pages: growing sequences that share a tail, the first of them
 };
 constexpr int kEntryLanes = 8;                 // lanes that work on an entry together
+constexpr int kFreshShared = 2048;             // up to so many new pages pass through shared memory
 
 struct ResizeEntry {
     int slot, want, state;                     // (as in the scratch)
@@ -268,6 +272,7 @@ __global__ void __launch_bounds__(kBookThreads, 1)
 pages_resize_kernel(const ResizeParams p)
 {
     __shared__ KeyTable table;
+    __shared__ int s_fresh[kFreshShared];
     __shared__ int s_slot[ONE ? kBookThreads : 1], s_want[ONE ? kBookThreads : 1], s_state[ONE ? kBookThreads : 1];
     const Book &bk = p.book;
     const int tid = threadIdx.x, sub = tid % kEntryLanes, groups = kBookThreads / kEntryLanes;
@@ -287,11 +292,15 @@ pages_resize_kernel(const ResizeParams p)
     auto slot_at = [&](int i) { return p.slot_of ? p.slot_of[i] : i; };
     ResizeEntry mine{-1, 0, -1, -1};
     bool gives = false;
+    uint32_t early = 0xffff;                                       // the first pages: asked for beside the list
     if constexpr (ONE) {
         int place = -1;
         if (tid < p.n) {
             mine.slot = slot_at(tid);
             mine.want = p.want[tid];
+        }
+        if (tid * 16 < bk.pages) early = held16(bk, tid * 16);
+        if (tid < p.n) {
             if ((unsigned)mine.slot < (unsigned)bk.slots && mine.want >= 0) {
                 mine.state = mine.want > bk.cap ? -2 : book_len(bk, mine.slot);
                 if (p.slot_of) place = table.add(mine.slot, tid);
@@ -412,14 +421,15 @@ pages_resize_kernel(const ResizeParams p)
     const long long pages = low_of(need);
     const int copies = high_of(need);
     int found = 0;
+    int *const fresh = pages <= kFreshShared ? s_fresh : p.fresh;
     const bool refused = __syncthreads_or(too_long);
     if (!refused)                                                  // (more than there are need not be found to be refused)
         for (int base = 0; base < bk.pages && found < pages; base += kBookThreads * 16) {
             const int first = base + tid * 16;
-            uint32_t free = first < bk.pages ? ~held16(bk, first) & 0xffff : 0;
+            uint32_t free = first < bk.pages ? ~(ONE && !gives && base == 0 ? early : held16(bk, first)) & 0xffff : 0;
             long long total;
             int at = found + (int)block_before(__popc(free), total);
-            for (; free; free &= free - 1) p.fresh[at++] = first + __ffs(free) - 1;
+            for (; free && at < pages; free &= free - 1) fresh[at++] = first + __ffs(free) - 1;
             found += (int)total;
         }
     __syncthreads();                                               // (this CTA reads what it has written)
@@ -441,7 +451,7 @@ pages_resize_kernel(const ResizeParams p)
         const int had = pages_of(bk, state), held = pages_of(bk, want);
         if (sub == 0) {
             if (takes) {
-                const int page = p.fresh[first];
+                const int page = fresh[first];
                 atomicSub(bk.refs + row[had - 1], 1);
                 bk.refs[page] = 1;
                 row[had - 1] = page;
@@ -449,7 +459,7 @@ pages_resize_kernel(const ResizeParams p)
             bk.lens[slot] = want;
         }
         for (int c = had + sub; c < held; c += kEntryLanes) {
-            const int page = p.fresh[first + takes + c - had];
+            const int page = fresh[first + takes + c - had];
             row[c] = page;
             bk.refs[page] = 1;
         }
@@ -468,7 +478,7 @@ pages_resize_kernel(const ResizeParams p)
             if (state >= 0) put(slot_at(i), p.want[i], state, mark & 0x7fffffff, mark < 0);
         }
     }
-    for (int k = tid; k < copies; k += kBookThreads) p.dst[k] = p.fresh[p.dst[k]];
+    for (int k = tid; k < copies; k += kBookThreads) p.dst[k] = fresh[p.dst[k]];
 }
 
 // ------------------------------------------------------------------ compact --
