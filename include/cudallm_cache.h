@@ -100,10 +100,12 @@ int cudallm_cache_append(const cudallm_paged_shape *shape, const void *k_new, co
  * Products on the tensor cores with fp32 accumulation; maxima and sums in fp32; the
  * probabilities, relative to a maximum, are rounded to dtype for the second product
  * (2^-8 or 2^-11 of themselves; fp16 also 2^-25 of the maximum); O is rounded once.
- * Made for few new tokens: 32 rows (query heads of a key head x tokens) share one reading of K
- * and V, more of them read the states again (correct for any q_rows, a prompt's included).
- * The work is dealt out by the lengths on the device, so neither table_cols nor unequal
- * lengths cost time.
+ * K and V are read once for every 128 rows (query heads of a key head x tokens) where page_rows is 8,
+ * 16, 32, 64 or a multiple of 128, else for every 64: single tokens, drafts and prompts (whole, or in pieces) alike.
+ * The work is dealt out by the lengths on the device, so that unequal lengths cost no time (small shapes, in
+ * which every SM has room for the longest sequence's share, are split by table_cols * page_rows).
+ * Where K and V come in tiles of 128 rows the kernel's waits have a limit in time; if one runs out, it gives up
+ * (o and lse are then not valid) and cudallm_device_status reports it, as for cudallm_xattn_fwd.
  * Empty sizes: as append (q_heads too); with no pages, slots or columns every token that is there has no
  * states, or its item is not there (slots == 0).
  * Errors: as append; WORKSPACE.
@@ -130,7 +132,7 @@ typedef struct cudallm_page_pool {
  *              nor the src of one and the dst of another.
  * n, count or pages == 0: success, nothing copied.
  * Errors: INVALID_POINTER, INVALID_DIM (negative; n > 2^31 - 1024, pages > 2^31 - 1024,
- * count > 65536, a pool of 2^46 bytes or more), INVALID_LD (stride < bytes), UNSUPPORTED_SHAPE (off 16 bytes),
+ * count > 65536, a page of more than 2^37 bytes, a pool of more than 2^46), INVALID_LD (stride < bytes), UNSUPPORTED_SHAPE (off 16 bytes),
  * MISALIGNED (src, dst), UNSUPPORTED_DEVICE, CUDA.
  */
 int cudallm_pages_copy(const cudallm_page_pool *pools, int64_t count, int64_t pages, const int32_t *src, const int32_t *dst,
@@ -221,7 +223,8 @@ size_t cudallm_pages_compact_scratch_bytes(const cudallm_page_book *book);
  *   dtype      : CUDALLM_F32, _BF16 or _F16
  * Comparisons and sums are in 64 bits (the product and the difference are exact).  Probabilities need not add up
  * to one; values of r that are not positive and finite count as zero.  Where p_a has no mass
- * either, the token drawn is -1.  n may be 0 (a token is drawn from p_0).
+ * either, the token drawn is -1.  n may be 0 (a token is drawn from p_0).  Drafts behind m, and their
+ * probabilities, are read but change nothing.  tokens and accepted must not overlap what is read.
  * Errors: INVALID_DTYPE, INVALID_DIM (negative; vocab 0; batch * (n + 1) or vocab > 2^31 - 1024), INVALID_LD,
  * INVALID_POINTER, MISALIGNED, UNSUPPORTED_DEVICE, CUDA.
  */

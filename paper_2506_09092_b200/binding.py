@@ -623,14 +623,10 @@ class PageBook:
         return self.c
 
 
-def _pool_array(pools):
-    return (None, 0) if pools is None else (pools.array, pools.count)
-
-
 def _pools_of(book, pools):
     if pools is not None and pools.count and pools.pages != book.c.pages:
         raise ValueError(f"pools of {pools.pages} pages, a book of {book.c.pages}")
-    return _pool_array(pools)
+    return (None, 0) if pools is None else (pools.array, pools.count)
 
 
 def pages_copy(pools, src, dst, n, stream=None, check=True):

@@ -13,6 +13,8 @@ namespace {
 
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxBytes = int64_t(1) << 46;
+constexpr int64_t kMaxPage = int64_t(1) << 37;           // bytes: the chunks of a launch's pools are counted in 31 bits
+static_assert(kMaxPage / kCopyChunk * kPoolsPerLaunch < kMaxDim, "chunks");
 constexpr int64_t kMaxBook = int64_t(1) << 20;           // pages of a book
 constexpr int64_t kMaxList = int64_t(1) << 14;           // entries of a list
 constexpr int64_t kMaxPools = 65536;
@@ -28,7 +30,7 @@ int check_pools(const cudallm_page_pool *pools, int64_t count, int64_t pages)
     if (!pools) return CUDALLM_ERR_INVALID_POINTER;
     for (int64_t i = 0; i < count; ++i) {
         const cudallm_page_pool &p = pools[i];
-        if (p.bytes < 0 || p.bytes > kMaxBytes) return CUDALLM_ERR_INVALID_DIM;
+        if (p.bytes < 0 || p.bytes > kMaxPage) return CUDALLM_ERR_INVALID_DIM;
         if (p.bytes == 0 || pages == 0) continue;
         if (!p.data) return CUDALLM_ERR_INVALID_POINTER;
         if (pages > 1 && p.stride < p.bytes) return CUDALLM_ERR_INVALID_LD;
@@ -118,7 +120,6 @@ int copy_pools(CopyParams p, const cudallm_page_pool *pools, int64_t count, cuda
             }
         if (p.pools == 0 && !p.remap) return CUDALLM_OK;
         const int64_t chunks = std::max<int64_t>(1, cdiv(largest, kCopyChunk));
-        if (chunks * p.pools > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
         p.chunks = (int)chunks;
         int64_t want = p.pools > 0 ? (p.n > kMaxDim / (chunks * p.pools) ? kMaxDim : p.n * chunks * p.pools) : 0;
         if (p.remap) want = std::max<int64_t>(want, p.book.slots);
