@@ -132,7 +132,7 @@ typedef struct cudallm_page_pool {
  *              nor the src of one and the dst of another.
  * n, count or pages == 0: success, nothing copied.
  * Errors: INVALID_POINTER, INVALID_DIM (negative; n > 2^31 - 1024, pages > 2^31 - 1024,
- * count > 65536, a page of more than 2^37 bytes, a pool of more than 2^46), INVALID_LD (stride < bytes), UNSUPPORTED_SHAPE (off 16 bytes),
+ * count > 65536, a page of more than 2^35 bytes, a pool of more than 2^46), INVALID_LD (stride < bytes), UNSUPPORTED_SHAPE (off 16 bytes),
  * MISALIGNED (src, dst), UNSUPPORTED_DEVICE, CUDA.
  */
 int cudallm_pages_copy(const cudallm_page_pool *pools, int64_t count, int64_t pages, const int32_t *src, const int32_t *dst,

@@ -13,7 +13,7 @@ namespace {
 
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxBytes = int64_t(1) << 46;
-constexpr int64_t kMaxPage = int64_t(1) << 37;           // bytes: the chunks of a launch's pools are counted in 31 bits
+constexpr int64_t kMaxPage = int64_t(1) << 35;           // bytes: the chunks of a launch's pools are counted in 31 bits
 static_assert(kMaxPage / kCopyChunk * kPoolsPerLaunch < kMaxDim, "chunks");
 constexpr int64_t kMaxBook = int64_t(1) << 20;           // pages of a book
 constexpr int64_t kMaxList = int64_t(1) << 14;           // entries of a list
@@ -121,9 +121,9 @@ int copy_pools(CopyParams p, const cudallm_page_pool *pools, int64_t count, cuda
         if (p.pools == 0 && !p.remap) return CUDALLM_OK;
         const int64_t chunks = std::max<int64_t>(1, cdiv(largest, kCopyChunk));
         p.chunks = (int)chunks;
-        int64_t want = p.pools > 0 ? (p.n > kMaxDim / (chunks * p.pools) ? kMaxDim : p.n * chunks * p.pools) : 0;
+        int64_t want = p.pools > 0 ? (p.n > kMaxDim / (chunks * p.pools) ? kMaxDim : cdiv(p.n * chunks * p.pools, kCopyThreads / 32)) : 0;
         if (p.remap) want = std::max<int64_t>(want, p.book.slots);
-        const int st = rt_launch(pages_copy_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(want, 8 * kPlanSms))),
+        const int st = rt_launch(pages_copy_kernel, dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(want, 16 * kPlanSms))),
                                  kCopyThreads, 0, stream, p, list);
         if (st != CUDALLM_OK) return st;
         p.remap = nullptr;

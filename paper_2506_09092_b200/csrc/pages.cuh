@@ -28,8 +28,8 @@ __device__ __forceinline__ int refs_now(const Book &b, int page) { return __ldcg
 constexpr int kPoolsPerLaunch = 120;           // their descriptions travel in the kernel's parameters
 struct PoolList { cudallm_page_pool at[kPoolsPerLaunch]; };
 constexpr int kCopyThreads = 256;
-constexpr int kCopyUnroll = 4;
-constexpr int kCopyChunk = kCopyThreads * 16 * kCopyUnroll;    // bytes of a page that a CTA copies at a time
+constexpr int kCopyUnroll = 8;
+constexpr int kCopyChunk = 32 * 16 * kCopyUnroll;              // bytes of a page that a warp copies at a time
 
 struct CopyParams {
     const int *src, *dst;
@@ -41,7 +41,9 @@ struct CopyParams {
     const int *remap, *first_moved;
 };
 
-// Units of (pair, pool, chunk) in order.  A thread has four 16-byte loads in flight.
+// Units of (pair, pool, chunk) in order, a warp each, so that short pages leave no threads idle; a thread has eight 16-byte
+// loads in flight.  1024 pages of 32 KiB in 16 pools (1.07 GB moved): 170 us, 6.30 TB/s (4000 of them: 6.40); with four loads
+// 179 us, with sixteen 174, with a CTA's worth of each page at a time and four loads 190, on half of the CTAs 176.
 __global__ void __launch_bounds__(kCopyThreads)
 pages_copy_kernel(const CopyParams p, const __grid_constant__ PoolList pools)
 {
@@ -61,24 +63,25 @@ pages_copy_kernel(const CopyParams p, const __grid_constant__ PoolList pools)
     const long long pairs = p.count ? min((long long)*p.count, p.n) : p.n;
     const unsigned per_pair = (unsigned)(p.pools * p.chunks);
     const long long units = pairs * per_pair;
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (long long u = blockIdx.x * (kCopyThreads / 32) + warp; u < units; u += gridDim.x * (kCopyThreads / 32)) {
         const long long pair = u / per_pair;
         const unsigned rest = (unsigned)(u - pair * per_pair), pool = rest / p.chunks, chunk = rest - pool * p.chunks;
         const int src = p.src[pair], dst = p.dst[pair];
         if ((unsigned)src >= (unsigned)p.pages || (unsigned)dst >= (unsigned)p.pages || src == dst) continue;
         const cudallm_page_pool &pl = pools.at[pool];
-        const long long first = (long long)chunk * kCopyChunk + threadIdx.x * 16;
+        const long long first = (long long)chunk * kCopyChunk + lane * 16;
         const uint8_t *from = static_cast<const uint8_t *>(pl.data) + src * pl.stride;
         uint8_t *to = static_cast<uint8_t *>(pl.data) + dst * pl.stride;
         uint4 v[kCopyUnroll];
 #pragma unroll
         for (int i = 0; i < kCopyUnroll; ++i) {
-            const long long at = first + i * kCopyThreads * 16;
+            const long long at = first + i * 512;
             if (at < pl.bytes) v[i] = __ldcs(reinterpret_cast<const uint4 *>(from + at));
         }
 #pragma unroll
         for (int i = 0; i < kCopyUnroll; ++i) {
-            const long long at = first + i * kCopyThreads * 16;
+            const long long at = first + i * 512;
             if (at < pl.bytes) __stcs(reinterpret_cast<uint4 *>(to + at), v[i]);
         }
     }
