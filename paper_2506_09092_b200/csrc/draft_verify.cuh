@@ -43,7 +43,66 @@ __device__ __forceinline__ double cluster_ld_f64(uint32_t addr)
     return v;
 }
 
-template <typename T>
+// What an element adds to the row that the token is drawn from: p - q where that is positive and finite, in 64 bits.  (fp32 says
+// so exactly: a difference of two values is zero there only if they are equal.  As two choices under one predicate: a
+// branch for each element costs more than its sum, 24 us instead of 16 for 64 rows of 128000.)
+template <typename T> __device__ __forceinline__ double mass(T p, T q)
+{
+    float x = elem_to_float(p), y = elem_to_float(q);
+    asm("{\n\t.reg .pred p;\n\tsetp.gt.f32 p, %2, 0f00000000;\n\tsetp.lt.and.f32 p, %2, 0f7F800000, p;\n\t"
+        "selp.f32 %0, %0, 0f00000000, p;\n\tselp.f32 %1, %1, 0f00000000, p;\n\t}"
+        : "+f"(x), "+f"(y) : "f"(x - y));
+    return (double)x - (double)y;
+}
+
+// N elements a lane of the 32 N from `from` on, zeros behind the end; `certain`: the one place where q is one.  VEC elements lie side
+// by side in 16 bytes (rows that begin there), else neighbouring lanes have neighbouring elements.
+template <int VEC, typename T, int N>
+__device__ __forceinline__ void verify_load(const T *prow, const T *qrow, long long from, int vocab, int certain, T (&pv)[N], T (&qv)[N])
+{
+    const int lane = threadIdx.x & 31;
+    const T zero = elem_from_float<T>(0.f), one = elem_from_float<T>(1.f);
+    const int left = (int)min((long long)vocab - from, 32LL * N);  // (may be negative)
+    int mine = -1;                                                 // the certain one's place among this lane's
+    const long long at = certain - from;
+    const bool here = certain >= 0 && at >= 0 && at < 32 * N;
+    if (VEC > 1 && left == 32 * N) {
+        union Piece {
+            uint4 w;
+            T e[VEC];
+            __device__ Piece() {}
+        };
+#pragma unroll
+        for (int i = 0; i < N; i += VEC) {
+            Piece x;
+            x.w = *reinterpret_cast<const uint4 *>(prow + from + i * 32 + lane * VEC);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) pv[i + e] = x.e[e];
+        }
+#pragma unroll
+        for (int i = 0; i < N; i += VEC) {
+            Piece x;
+            if (qrow) x.w = *reinterpret_cast<const uint4 *>(qrow + from + i * 32 + lane * VEC);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) qv[i + e] = qrow ? x.e[e] : zero;
+        }
+        if (here && (int)at / VEC % 32 == lane) mine = (int)at / (32 * VEC) * VEC + (int)at % VEC;
+    } else {
+        const T *ps = prow + from + lane, *qs = qrow + from + lane;
+#pragma unroll
+        for (int i = 0; i < N; ++i) pv[i] = i * 32 + lane < left ? ps[i * 32] : zero;
+#pragma unroll
+        for (int i = 0; i < N; ++i) qv[i] = qrow && i * 32 + lane < left ? qs[i * 32] : zero;
+        if (here && (int)at % 32 == lane) mine = (int)at / 32;
+    }
+    if (here) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i == mine) qv[i] = one;
+    }
+}
+
+template <typename T, int VEC>
 __global__ void __launch_bounds__(kVerifyThreads, 2)
 draft_verify_kernel(const VerifyParams p)
 {
@@ -86,35 +145,6 @@ draft_verify_kernel(const VerifyParams p)
     // what is drawn from: max(p_a - q_a, 0) while drafts are left, q_a being a row or 1 at `certain`; else p_a
     const T *prow = pp + a * p.ldp, *qrow = a < m && qq ? qq + a * p.ldq : nullptr;
     int certain = a < m && !qq ? drafts[a] : -1;
-    // (compared in 32 bits, where p > q says exactly that p - q > 0; only then subtracted)
-    auto mass = [&](T pv, T qv) {
-        const float x = elem_to_float(pv), y = elem_to_float(qv);
-        return x > y && x < INFINITY && y > -INFINITY ? (double)x - (double)y : 0.0;
-    };
-    const T zero = elem_from_float<T>(0.f), one = elem_from_float<T>(1.f);
-    // rows of 32 elements from `from` on, this lane's of each; the certain draft's probability is put in
-    auto load = [&](long long from, auto &pv, auto &qv) {
-        constexpr int kRows = sizeof pv / sizeof pv[0];
-        const T *ps = prow + from + lane, *qs = qrow + from + lane;
-        if (from + 32 * kRows <= p.vocab) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) pv[i] = ps[i * 32];
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) qv[i] = qrow ? qs[i * 32] : zero;
-        } else {
-            const int left = (int)max(p.vocab - from, 0LL) - lane;
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) pv[i] = i * 32 < left ? ps[i * 32] : zero;
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) qv[i] = qrow && i * 32 < left ? qs[i * 32] : zero;
-        }
-        if (certain >= from && certain < from + 32 * kRows) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i)
-                if (from + i * 32 + lane == certain) qv[i] = one;
-        }
-    };
-
     double point, before;                                          // where in the sum of all; the sum of the CTAs before this one
     int owner;                                                     // the CTA that holds the point
     for (int pass = 0;; ++pass) {
@@ -123,12 +153,12 @@ draft_verify_kernel(const VerifyParams p)
         auto at = [&](int k) { return ((long long)rank * p.chunks + warp + k / parts * kVerifyWarps) * p.chunk + k % parts * kVerifyChunk; };
         T pv[2][16], qv[2][16];
         double s = 0.0;
-        if (mine > 0) load(at(0), pv[0], qv[0]);
+        if (mine > 0) verify_load<VEC>(prow, qrow, at(0), p.vocab, certain, pv[0], qv[0]);
         for (int k0 = 0; k0 < mine; k0 += 2) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int k = k0 + h;
-                if (k + 1 < mine) load(at(k + 1), pv[h ^ 1], qv[h ^ 1]);
+                if (k + 1 < mine) verify_load<VEC>(prow, qrow, at(k + 1), p.vocab, certain, pv[h ^ 1], qv[h ^ 1]);
                 if (k >= mine) break;
                 double part[4] = {};
 #pragma unroll
@@ -211,7 +241,7 @@ draft_verify_kernel(const VerifyParams p)
     for (int part = 0; part < p.chunk && !found; part += 32 * kRows) {
         const long long from = ((long long)rank * p.chunks + c) * p.chunk + part;
         T pv[kRows], qv[kRows];
-        load(from, pv, qv);
+        verify_load<1>(prow, qrow, from, p.vocab, certain, pv, qv);
         double own[kRows], row[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) row[i] = own[i] = mass(pv[i], qv[i]);

@@ -17,6 +17,13 @@ constexpr int64_t kPlanSms = 148;
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool off(const void *p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) != 0; }
 
+// wide: all rows begin on 16 bytes
+template <typename T> int launch(const VerifyParams &v, bool wide, dim3 grid, cudaStream_t stream)
+{
+    return rt_launch_cluster(wide ? draft_verify_kernel<T, 16 / (int)sizeof(T)> : draft_verify_kernel<T, 1>, grid, (unsigned)v.cluster,
+                             kVerifyThreads, 0, stream, v);
+}
+
 }  // namespace
 
 extern "C" int cudallm_draft_verify(const void *p, const void *q, const int32_t *drafts, const int32_t *draft_lens, const float *u,
@@ -47,8 +54,7 @@ extern "C" int cudallm_draft_verify(const void *p, const void *q, const int32_t 
     if (batch * v.cluster > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
     const dim3 grid((unsigned)(batch * v.cluster));
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
-    if (dtype == CUDALLM_F32) return rt_launch_cluster(draft_verify_kernel<float>, grid, (unsigned)v.cluster, kVerifyThreads, 0, stream, v);
-    if (dtype == CUDALLM_BF16)
-        return rt_launch_cluster(draft_verify_kernel<__nv_bfloat16>, grid, (unsigned)v.cluster, kVerifyThreads, 0, stream, v);
-    return rt_launch_cluster(draft_verify_kernel<__half>, grid, (unsigned)v.cluster, kVerifyThreads, 0, stream, v);
+    const bool wide = !off(p, 16) && !off(v.q, 16) && ldp * es % 16 == 0 && (!v.q || ldq * es % 16 == 0);
+    if (dtype == CUDALLM_F32) return launch<float>(v, wide, grid, stream);
+    return dtype == CUDALLM_BF16 ? launch<__nv_bfloat16>(v, wide, grid, stream) : launch<__half>(v, wide, grid, stream);
 }
