@@ -376,8 +376,8 @@ int cudallm_shutdown(void);
  *   CUDALLM_DEBUG_LAYERNORM_PATH         value = 0: cudallm_layernorm_f32 picks its
  *       kernel by size; 1: always the two-kernel path; 2: the one-pass kernel
  *       whenever the samples fit in shared memory, however small.
- *   CUDALLM_DEBUG_SKIP_NEXT_XATTN_LOADS  value != 0: the next cudallm_xattn_fwd or
- *       cudallm_xattn_bwd kernel with in-kernel waits (not the one for single tokens)
+ *   CUDALLM_DEBUG_SKIP_NEXT_XATTN_LOADS  value != 0: the next cudallm_xattn_fwd,
+ *       cudallm_xattn_bwd or cudallm_paged_attn kernel with in-kernel waits (not those for single tokens)
  *       loads nothing, so its waits run out after the limit; as above it returns
  *       normally with unspecified output, and the status says so.  One launch only.
  * Returns CUDALLM_ERR_INVALID_VARIANT for an unknown `what` or value.

@@ -1,20 +1,27 @@
 // Attention of the newest tokens of each sequence over its pages, and writing their keys and values there.
 //
+// O = softmax(scale Q K^T) V with a running maximum m, a sum l of exponentials and an unnormalised O per row: one pass over the keys,
+// o <- o 2^((m - m') s) + P V.  Parts of the keys join by their lse.
+//
 // Bound: HBM (K and V of every sequence are read once; 16 or 32 rows of arithmetic per key are far below
-// any pipe's rate), so what matters is bytes in flight and an even split.  A CTA has four warps; each walks
-// its own tiles of 32 keys (16 at head dims above 64) through its own ring of cp.async stages, no barrier
-// between warps.  A lane looks up the page of "its" row of the next tile one tile ahead, and the rows'
-// offsets go round by shuffle, so pages may have any number of rows.  The rows that share a key head
-// (query heads x new tokens) are the M of mma.sync.m16n8k16, one or two tiles of 16: a tcgen05 tile would be 128
-// rows, most of them empty, and 16 rows need a tenth of mma.sync's rate at the full speed of HBM.
+// any pipe's rate), so what matters is bytes in flight and an even split.  The rows that share a key head (query heads x new
+// tokens) share its reading.  Up to 16 of them are one tile of mma.sync.m16n8k16 (paged_narrow.cuh: 4 sequences of 64000 states,
+// 8 key heads of 128, 4 rows: 160 us for 1.05 GB, at the copy rate; 16 rows need a tenth of mma.sync's rate at the full speed of
+// HBM, and a tcgen05 tile would be 128 rows, most of them empty).  More are tiles of 128 on tcgen05 (paged_tile.cuh) if TMA can
+// bring the pages, else two to four tiles of 16 that share their stages (paged_wide_kernel, here).
+//
+// The mma.sync kernels' CTAs have four warps, each with its own tiles of 32 keys (16 at head dims above 64) in a ring of
+// cp.async stages, 96 KiB a CTA and two CTAs an SM.  A lane looks up the page of "its" row of the next tile one tile ahead, and
+// the rows' offsets go round by shuffle, so pages may have any number of rows.
 //
 // Only the device knows the lengths, so the split is made there, in one of two ways:
 //  * a cluster of CTAs per (item, key head, row tile), each with an equal share of its keys; they join
-//    through each other's shared memory.  One launch, but as long as the longest sequence takes.
+//    through each other's shared memory.  One launch, but as long as the longest sequence takes (plan_attn has
+//    the rule and both sides' times).
 //  * equal shares: all blocks of keys of all items in one line, cut into equal pieces, as many as CTAs fit for
 //    every key head.  Neighbouring CTAs have the same piece for the different heads: where the heads of a token lie side by
 //    side they read the same DRAM pages at the same time (32 x 64000 keys of 64, a CTA's piece in a line that
-//    ran through the heads, too: 101 us).  A piece may begin and end inside an item; such parts go to scratch
+//    ran through the heads, too: 101 us against 86).  A piece may begin and end inside an item; such parts go to scratch
 //    (two slots a CTA) and paged_join_kernel adds them up in order.
 #pragma once
 #include "fast_div.cuh"
@@ -260,7 +267,8 @@ __device__ __forceinline__ void paged_load_q(const PagedParams &p, int b, int kv
 // Two to four row tiles: registers do not hold a whole result per warp, so the warps share a stage.  Each takes its
 // own keys' scores for all rows (S = Q K^T), they agree on the rows' maxima, the probabilities go to shared memory (where the
 // stage's keys were), and each multiplies all of them with its own quarter of the columns of V.  Two
-// barriers a stage.
+// barriers a stage.  Bound by issue slots and those barriers (16 sequences of 16000 states, 4 key heads of 128, 40 rows: 132 us where
+// the tcgen05 kernel takes 98), so it serves pages that TMA cannot bring into tiles, and short tables of up to 32 rows.
 template <int DP, int MT, typename T>
 __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *smem, const PagedItem &it, int b, int kvh, int rt,
                                                 int blk0, int blk1)
@@ -872,7 +880,9 @@ struct AppendParams {
 constexpr int kAppendThreads = 256, kAppendPieces = 4;
 
 // `lanes` neighbouring lanes move a token's keys and values, four 16-byte pieces of each side by side.  First where they go:
-// slot -> length -> page is what a token waits for, and one that is not there is not read.
+// slot -> length -> page is what a token waits for, and one that is not there is not read.  Bound: HBM for prompts (8 x 2048 tokens,
+// 8 key heads of 128: 134 MB moved in 25.7 us, 5.2 TB/s, the launch and the chain among them), that chain for
+// single tokens (64 of them: 3.0 us).
 __global__ void __launch_bounds__(kAppendThreads)
 cache_append_kernel(const AppendParams p)
 {

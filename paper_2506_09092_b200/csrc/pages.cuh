@@ -103,7 +103,8 @@ constexpr int kForkCols = 256;
 
 // A slot may be read by one entry and overwritten by another, so the sources' rows first go to scratch, their pages
 // getting one holder more; then, behind a barrier of the whole cluster, the old rows are given up and the
-// new ones put in.  A warp works on 256 columns of an entry at a time.
+// new ones put in.  A warp works on 256 columns of an entry at a time.  Bound: the latency of four dependent reads and two cluster
+// barriers; 256 sequences of 11 pages: 7.8 us under a profiler on eight CTAs (8 sequences on one: 5.5).
 __global__ void __launch_bounds__(kBookThreads, 1)
 pages_fork_kernel(const ForkParams p)
 {
@@ -269,7 +270,8 @@ struct KeyTable {
 // First all CTAs of the cluster give back the pages of sequences that become shorter; then the first does the rest, which
 // has an order: shared tails, how many pages are needed, which are free, who gets which.  If they do not suffice, it
 // takes what was given back again.  ONE: up to 1024 entries, a thread each, in registers and shared
-// memory; longer lists go through the scratch.
+// memory; longer lists go through the scratch.  Bound: latency (list -> length -> last page -> its holders, then the counting
+// within a block, twice): 256 sequences, 256 new pages: 11.0 us under a profiler, 8 sequences 10.2, of which the launch is four.
 template <bool ONE>
 __global__ void __launch_bounds__(kBookThreads, 1)
 pages_resize_kernel(const ResizeParams p)
@@ -493,7 +495,7 @@ struct CompactParams {
     int *src, *dst;                            // pages each
     int *remap;                                // pages: where a page from first_moved on goes
 };
-// One CTA.  Which pages are held goes to shared memory as bits in one pass over refs; the k-th held one above the
+// One CTA (3000 pages: 7.7 us under a profiler, 4 of them the launch).  Which pages are held goes to shared memory as bits in one pass over refs; the k-th held one above the
 // number of pages in use and the k-th free one below it become pair k.
 __global__ void __launch_bounds__(kBookThreads, 1)
 pages_compact_kernel(const CompactParams p)

@@ -46,8 +46,9 @@ extern "C" int cudallm_draft_verify(const void *p, const void *q, const int32_t 
     VerifyParams v{};
     v.p = p; v.q = n > 0 ? q : nullptr; v.drafts = drafts; v.draft_lens = draft_lens; v.u = u; v.tokens = tokens; v.accepted = accepted;
     v.ldp = ldp; v.ldq = ldq; v.n = (int)n; v.vocab = (int)vocab;
-    // CTAs of a sequence: two an SM in all, at least eight chunks (a warp's worth each) for one
-    const int64_t want = std::min<int64_t>({int64_t(kVerifyCluster), 2 * kPlanSms / batch, vocab / (kVerifyWarps * kVerifyChunk)});
+    // CTAs of a sequence: two an SM in all, and four chunks of 512 at least for one.  (One row of 4000, 16000, 32000, 128000 fp32
+    // values on one CTA 5.5, 7.1, 11.5, 29.1 us, on eight 6.3, 5.5, 6.8, 8.4; 64 rows of 128000 on 1, 2, 4, 8: 33.8, 24.1, 16.4, 21.1.)
+    const int64_t want = std::min<int64_t>({int64_t(kVerifyCluster), 2 * kPlanSms / batch, vocab / (4 * kVerifyChunk)});
     v.cluster = (int)std::max<int64_t>(want, 1);
     v.chunk = (int)(kVerifyChunk * cdiv(vocab, (int64_t)kVerifyChunk * kVerifyChunks * v.cluster));
     v.chunks = (int)cdiv(cdiv(vocab, v.chunk), v.cluster);
