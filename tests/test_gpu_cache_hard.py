@@ -173,3 +173,43 @@ print("as captured")
 def test_first_calls_of_a_process_are_captured():
     p = subprocess.run([sys.executable, "-c", FIRST.format(repo=REPO)], capture_output=True, text=True, timeout=300)
     assert p.returncode == 0 and "as captured" in p.stdout, p.stderr[-2000:]
+
+
+@pytest.mark.parametrize("rows,group,hk,dim", [(1, 1, 400, 64), (3, 8, 200, 64), (2, 10, 160, 128), (1, 30, 300, 40)])
+def test_more_key_heads_than_shares(rows, group, hk, dim):
+    """Each CTA takes all of a key head's keys: nothing is left in parts, and no room is asked for them."""
+    c = Cache([700, 0, 33, 130, 1], rows, group * hk, hk, dim, "bf16", 16, cols=3000)
+    assert B.paged_attn_scratch_bytes(c.shape(torch.empty_like(c.q))) <= 16 * hk
+    check(c)
+
+
+@pytest.mark.parametrize("rows,group", [(1, 4), (6, 8)])
+def test_the_same_slot_twice(rows, group):
+    """Items may look at one sequence side by side: its states are read, nothing of it is written."""
+    c = Cache([500, 90, 33], rows, 2 * group, 2, 64, "bf16", 16)
+    q = torch.cat([c.q, c.q.flip(0)])
+    slot_of = torch.tensor([0, 1, 2, 0, 1, 0], dtype=torch.int32, device="cuda")
+    out = torch.empty_like(q)
+    shape = B.PagedShape.of(q, c.k, c.v, out, c.table)
+    n = B.paged_attn_scratch_bytes(shape)
+    scratch = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    B.paged_attn(shape, q, c.k, c.v, c.table, c.lens, slot_of, None, out, None, scratch, n, torch.cuda.current_stream())
+    alone = torch.empty_like(q)
+    for i, w in enumerate(slot_of.tolist()):
+        one, at = q[i:i + 1], slot_of[i:i + 1]
+        shape = B.PagedShape.of(one, c.k, c.v, alone[i:i + 1], c.table)
+        n = B.paged_attn_scratch_bytes(shape)
+        scratch = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+        B.paged_attn(shape, one, c.k, c.v, c.table, c.lens, at, None, alone[i:i + 1], None, scratch, n, torch.cuda.current_stream())
+        a, b = out[i].float(), alone[i].float()                # (the split may differ: each within h (|O| + sum p |v|))
+        assert bool(((a - b).abs() <= 2 * 1.1 * 2.0 ** -8 * (b.abs() + c.values[w].float().abs().max())).all())
+
+
+@pytest.mark.parametrize("values", [8, 40, 5000])
+def test_one_page_copied_to_several(values):
+    pool = torch.randn(9, values, device="cuda").bfloat16()
+    want = pool.clone()
+    src, dst = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in ([5, 5, 5, 2], [1, 8, 0, 3]))
+    want[[1, 8, 0]], want[3] = pool[5].clone(), pool[2].clone()
+    B.pages_copy(B.page_pools([pool]), src, dst, 4, torch.cuda.current_stream())
+    assert torch.equal(pool, want)
