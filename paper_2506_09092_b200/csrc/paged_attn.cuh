@@ -50,7 +50,7 @@ struct PagedParams {
     FastDiv by_group;
     int pages, page_rows, slots, cap;          // cap: states that a row of the table holds
     FastDiv by_page_rows;
-    int row_tiles;                             // tiles of 16 or 32 rows of an item and key head at most
+    int row_tiles;                             // tiles of 16 to 128 rows of an item and key head at most
     int cluster;                               // CTAs per item, key head and row tile; 0: equal shares
     int shares;                                // of a key head; CTA = share * kv_heads + key head
     // who counts what (locate): items a thread, or 2^count_shift threads an item, count_tiles row tiles each
