@@ -65,7 +65,8 @@ __device__ __forceinline__ uint32_t tile_piece(int r, int c)
 }
 
 // Values that were set aside (see the softmax), of keys in the blocks from `aside` on: added to this row's half of the columns of
-// O in tensor memory, from scores taken anew.  A warp's lanes together; `block`: the number behind the segment's last.
+// O in tensor memory, from scores taken anew.  A warp's lanes together, those without a row of their own among them: such a lane sees
+// nothing (seen = 0), so that no query is read for it.  `block`: the number behind the segment's last.
 template <int DP, typename T>
 __device__ __noinline__ void add_set_aside(const PagedParams &p, const int *pages, int b, int kvh, int row, int seen, float m, int d0,
                                            uint32_t t_o, volatile uint32_t *bads, int key0, int block, int blocks, int aside)
@@ -404,7 +405,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 meet();                                            // (the next segment's first maxima go to the same place)
             }
             if (blocks > 0 && warp_rows)
-                add_set_aside<DP, T>(p, seg.it.row, seg.b, seg.kvh, row, seen, m, half * (DP / 2), t_o, bads, key0, block, blocks,
+                add_set_aside<DP, T>(p, seg.it.row, seg.b, seg.kvh, row, mine ? seen : 0, m, half * (DP / 2), t_o, bads, key0, block, blocks,
                                      min(blocks, max(0, seen_lo - key0) / L::kBlock));
             const float inv = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
             const bool whole = seg.whole();
