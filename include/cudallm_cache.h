@@ -185,8 +185,8 @@ size_t cudallm_pages_fork_scratch_bytes(const cudallm_page_book *book, int64_t n
  *              negative lengths are passed over; of several entries with the same slot the first of the others counts.
  *   new_lens : int32, n elements
  *   pools    : HOST array of `count` pools that the copies are made in (0: a book without data)
- *   result   : int32, one word, or NULL: 0 done; > 0: so many pages are missing; -1: a length
- *              beyond the table
+ *   result   : int32, one word, or NULL: 0 done; > 0: so many pages are missing (at most 2^31 - 1 is said);
+ *              -1: a length beyond the table
  * Errors: as cudallm_pages_fork and cudallm_pages_copy.
  */
 int cudallm_pages_resize(const cudallm_page_book *book, const cudallm_page_pool *pools, int64_t count, const int32_t *slot_of,

@@ -194,8 +194,9 @@ __device__ __forceinline__ long long block_before(long long v, long long &total)
     __syncthreads();                                               // (it may be called again at once)
     return before;
 }
-// Two counts in one word: at most 2^16 entries that need at most 2^20 + 1 pages each, and at most 2^20 of the other.
-constexpr int kLowBits = 42;
+// Two counts in one word: at most 2^14 entries that need fewer than 2^31 pages each, and at most 2^14 copies (or, in a compaction,
+// at most 2^20 of either).
+constexpr int kLowBits = 45;
 __device__ __forceinline__ long long pack2(int lo, int hi) { return (long long)hi << kLowBits | lo; }
 __device__ __forceinline__ long long low_of(long long v) { return v & ((1LL << kLowBits) - 1); }
 __device__ __forceinline__ int high_of(long long v) { return (int)(v >> kLowBits); }
@@ -412,7 +413,7 @@ pages_resize_kernel(const ResizeParams p)
             const int first = ONE ? table.first[claim] : __ldcg(p.claimer + e.tail);
             copy = !(sharers == refs_now(bk, e.tail) && first == i);
         }
-        if (e.state >= 0) pages = min(copy + max(pages_of(bk, e.want) - pages_of(bk, e.state), 0), bk.pages + 1);
+        if (e.state >= 0) pages = copy + max(pages_of(bk, e.want) - pages_of(bk, e.state), 0);
         long long total;
         const long long before = need + block_before(pack2(pages, copy), total);
         start = (int)(low_of(before) & 0x7fffffff);
