@@ -237,12 +237,11 @@ int cudallm_pages_compact(const cudallm_page_book *book, const cudallm_page_pool
     p.src = w + at.src; p.dst = w + at.dst; p.remap = w + at.remap;
     cudaStream_t stream = static_cast<cudaStream_t>(stream_v);
     const int smem = (int)(cdiv(book->pages, 16) * 2);             // 128 KiB for 2^20 pages
-    if (smem > 48 * 1024) {
-        static std::atomic<bool> done[kRtMaxDevices] = {};
-        if (!done[dev].load(std::memory_order_relaxed)) {
-            RT_CUDA_TRY(cudaFuncSetAttribute(pages_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kMaxBook / 8)));
-            done[dev].store(true, std::memory_order_relaxed);
-        }
+    // (the kernel's own shared memory counts in the 48 KiB that a launch may have unasked, so it is asked for whatever the size)
+    static std::atomic<bool> done[kRtMaxDevices] = {};
+    if (!done[dev].load(std::memory_order_relaxed)) {
+        RT_CUDA_TRY(cudaFuncSetAttribute(pages_compact_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(kMaxBook / 8)));
+        done[dev].store(true, std::memory_order_relaxed);
     }
     st = rt_launch(pages_compact_kernel, dim3(1), kBookThreads, (size_t)smem, stream, p);
     if (st != CUDALLM_OK) return st;
