@@ -94,9 +94,10 @@ int cudallm_cache_append(const cudallm_paged_shape *shape, const void *k_new, co
  *   lse      : fp32, contiguous [batch][q_heads][q_rows], or NULL
  * Rows of o and lse of tokens from n on, and of items that are not there, stay as they
  * are.  States on pages that are not there are left out, as if masked.  A token that sees no state
- * gives O = 0, lse = -inf.  A state, query or value that is not finite makes the
- * tokens that see it not finite, and no others; what lies in pages behind a sequence's
- * end does not matter, whatever it is.
+ * gives O = 0, lse = -inf.  What is not finite reaches the tokens that see it, as the formulas
+ * say, and no others: a score of NaN or +inf makes its row (O and lse) NaN, one of -inf is a weight of zero unless the
+ * row has no other (then NaN), a value that is not finite makes its column of O not finite.  What lies in
+ * pages behind a sequence's end does not matter, whatever it is.
  * Products on the tensor cores with fp32 accumulation; maxima and sums in fp32; the
  * probabilities, relative to a maximum, are rounded to dtype for the second product
  * (2^-8 or 2^-11 of themselves; fp16 also 2^-25 of the maximum); O is rounded once.

@@ -1,7 +1,9 @@
 // Attention of the newest tokens of each sequence over its pages, and writing their keys and values there.
 //
 // O = softmax(scale Q K^T) V with a running maximum m, a sum l of exponentials and an unnormalised O per row: one pass over the keys,
-// o <- o 2^((m - m') s) + P V.  Parts of the keys join by their lse.
+// o <- o 2^((m - m') s) + P V.  Parts of the keys join by their lse: -inf for a part without keys, kPaOnlyInf for one
+// whose scores are all -inf.  Its weight beside any other part is zero, too, but if there are only such parts the row is no number
+// (0 / 0), where a row without keys is zero.
 //
 // Bound: HBM (K and V of every sequence are read once; 16 or 32 rows of arithmetic per key are far below
 // any pipe's rate), so what matters is bytes in flight and an even split.  The rows that share a key head (query heads x new
@@ -33,6 +35,7 @@ namespace cudallm {
 constexpr int kPaWarps = 4;
 constexpr int kPaThreads = 32 * kPaWarps;
 constexpr int kPaCluster = 8;
+constexpr float kPaOnlyInf = -3.402823466e38f;         // the lowest number: e to its power is zero, its difference to itself not
 
 struct PagedStrides { long long page, row, head; };
 
@@ -262,7 +265,7 @@ __device__ __forceinline__ void paged_load_q(const PagedParams &p, int b, int kv
 
 // Blocks blk0 .. blk1 - 1 of an item's keys for one key head and row tile.  Leaves sums, not yet normalised, at the start of
 // shared memory: rows x DP, then the rows' maxima (of the scores), then the sums of exponentials.  A row that has
-// seen no state has maximum -inf and sum 0.
+// seen no state has maximum -inf and sum 0, one whose scores are all -inf the maximum kPaOnlyInf.
 //
 // Two to four row tiles: registers do not hold a whole result per warp, so the warps share a stage.  Each takes its
 // own keys' scores for all rows (S = Q K^T), they agree on the rows' maxima, the probabilities go to shared memory (where the
@@ -509,8 +512,8 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
         for (int half = 0; half < 2; ++half) {
             l[i][half] += __shfl_xor_sync(0xffffffffu, l[i][half], 1);
             l[i][half] += __shfl_xor_sync(0xffffffffu, l[i][half], 2);
-            // scores of -inf alone are not the same as no scores
-            if (any[i][half] && m[i][half] == -INFINITY) l[i][half] = __int_as_float(0x7fc00000);
+            // scores of -inf alone are not the same as no scores: a mark that no sum is
+            if (any[i][half] && m[i][half] == -INFINITY && l[i][half] == 0.f) l[i][half] = -1.f;
             if (q4 == 0)
                 asm volatile("st.shared.f32 [%0], %1;" ::"r"(maxima + (i * 16 + g + 8 * half) * 16 + warp * 4), "f"(l[i][half]) : "memory");
             if (q4 == 0 && warp == 0) jm[i * 16 + g + 8 * half] = m[i][half];
@@ -519,7 +522,9 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
     __syncthreads();
     if (tid < L::kRows) {
         const uint4 w = ld_shared_v4(maxima + tid * 16);
-        jl[tid] = (__uint_as_float(w.x) + __uint_as_float(w.y)) + (__uint_as_float(w.z) + __uint_as_float(w.w));
+        const float sum = (__uint_as_float(w.x) + __uint_as_float(w.y)) + (__uint_as_float(w.z) + __uint_as_float(w.w));
+        jl[tid] = sum < 0.f ? 0.f : sum;                           // (marks: the maximum is the CTA's, so the other warps' sums are 0)
+        if (sum < 0.f) jm[tid] = kPaOnlyInf;
     }
     __syncthreads();
 }
@@ -673,6 +678,25 @@ template <int ROWS, int BLOCK> struct PagedSegments {
     }
 };
 
+// 1 / sum and lse of a row, or of a part of it.
+struct PagedNorm { float inv, lse; };
+__device__ __forceinline__ PagedNorm paged_norm(float m, float sum, float scale)
+{
+    if (sum != 0.f) return PagedNorm{1.f / sum, fmaf(m, scale, logf(sum))};
+    return PagedNorm{0.f, m == kPaOnlyInf ? kPaOnlyInf : -INFINITY};
+}
+// ... of a whole row: scores of -inf alone are no number.
+__device__ __forceinline__ PagedNorm paged_whole(PagedNorm n)
+{
+    const float nan = __int_as_float(0x7fc00000);
+    return n.lse == kPaOnlyInf ? PagedNorm{nan, nan} : n;
+}
+// ... of a row joined from parts, of which `mx` is the largest lse and `sum` the sum of their weights.
+__device__ __forceinline__ PagedNorm paged_joined(float mx, float sum)
+{
+    return sum == 0.f ? PagedNorm{0.f, -INFINITY} : paged_whole(PagedNorm{1.f / sum, mx == kPaOnlyInf ? kPaOnlyInf : mx + logf(sum)});
+}
+
 // A row's eight columns (c), normalised, as a part of the result: row r of [row][DP] fp32 and, behind them, lse.
 template <int DP, int ROWS>
 __device__ __forceinline__ void paged_store_part(float *slot, int r, int c, const float (&v)[8], float lse)
@@ -723,12 +747,12 @@ __device__ __forceinline__ void paged_join_cluster(const PagedParams &p, const P
             acc[0] = fmaf(w, a.x, acc[0]); acc[1] = fmaf(w, a.y, acc[1]); acc[2] = fmaf(w, a.z, acc[2]); acc[3] = fmaf(w, a.w, acc[3]);
             acc[4] = fmaf(w, b4.x, acc[4]); acc[5] = fmaf(w, b4.y, acc[5]); acc[6] = fmaf(w, b4.z, acc[6]); acc[7] = fmaf(w, b4.w, acc[7]);
         }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const PagedNorm norm = paged_joined(mx, sum);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] *= inv;
+        for (int e = 0; e < 8; ++e) acc[e] *= norm.inv;
         const int row = seg.rt * ROWS + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
         paged_store<T>(p, seg.b, t, h, c, acc);
-        if (c == 0) paged_store_lse(p, seg.b, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
+        if (c == 0) paged_store_lse(p, seg.b, t, h, norm.lse);
     }
     cluster_sync_all();                                            // nobody's shared memory goes while it is read
 }
@@ -757,16 +781,17 @@ paged_wide_kernel(const PagedParams p)
         float *slot = p.cluster ? reinterpret_cast<float *>(smem + L::kShare) : p.part + (2LL * cta + (seg.blk0 == 0)) * kRows * (DP + 1);
         for (int i = tid; i < rows * kChunks; i += kPaThreads) {
             const int r = i / kChunks, c = i % kChunks;
-            const float sum = l[r], inv = sum == 0.f ? 0.f : 1.f / sum, lse = sum == 0.f ? -INFINITY : fmaf(m[r], p.scale, logf(sum));
+            PagedNorm norm = paged_norm(m[r], l[r], p.scale);
+            if (whole) norm = paged_whole(norm);
             float acc[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] = o[r * L::kPitch + c * 8 + e] * inv;
+            for (int e = 0; e < 8; ++e) acc[e] = o[r * L::kPitch + c * 8 + e] * norm.inv;
             if (whole) {
                 const int row = seg.rt * kRows + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
                 paged_store<T>(p, seg.b, t, h, c, acc);
-                if (c == 0) paged_store_lse(p, seg.b, t, h, lse);
+                if (c == 0) paged_store_lse(p, seg.b, t, h, norm.lse);
             } else {
-                paged_store_part<DP, kRows>(slot, r, c, acc, lse);
+                paged_store_part<DP, kRows>(slot, r, c, acc, norm.lse);
             }
         }
         if (p.cluster) break;
@@ -856,12 +881,12 @@ paged_join_kernel(const PagedParams p, const int group_shift)
             __syncthreads();
         }
         if (g != 0 || r >= rows) continue;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const PagedNorm norm = paged_joined(mx, sum);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] *= inv;
+        for (int e = 0; e < 8; ++e) acc[e] *= norm.inv;
         const int row = d.w * ROWS + r, t = paged_token(p, row), h = d.z * p.group + row - t * p.group;
         paged_store<T>(p, d.y, t, h, c, acc);
-        if (c == 0) paged_store_lse(p, d.y, t, h, sum == 0.f ? -INFINITY : mx + logf(sum));
+        if (c == 0) paged_store_lse(p, d.y, t, h, norm.lse);
     }
 }
 

@@ -229,8 +229,7 @@ paged_narrow_kernel(const PagedParams p)
         for (int half = 0; half < 2; ++half) {
             l[half] += __shfl_xor_sync(0xffffffffu, l[half], 1);
             l[half] += __shfl_xor_sync(0xffffffffu, l[half], 2);
-            // scores of -inf alone are not the same as no scores
-            if (any[half] && m[half] == -INFINITY) l[half] = __int_as_float(0x7fc00000);
+            if (any[half] && m[half] == -INFINITY && l[half] == 0.f) m[half] = kPaOnlyInf;
             if (q4 == 0) {
                 stats[warp * 2 * L::kRows + g + 8 * half] = m[half];
                 stats[warp * 2 * L::kRows + L::kRows + g + 8 * half] = l[half];
@@ -252,7 +251,7 @@ paged_narrow_kernel(const PagedParams p)
             }
 #pragma unroll
             for (int w = 0; w < kPaWarps; ++w) {
-                if (wl[w] == 0.f) continue;                        // a warp without keys
+                if (wl[w] == 0.f && wm[w] == -INFINITY) continue;  // a warp without keys
                 const float a = xa_exp2((wm[w] - mx) * p.scale_log2);
                 sum = fmaf(a, wl[w], sum);
                 const float *src = reinterpret_cast<const float *>(smem + w * L::kWarp + stage_at(joint));
@@ -261,15 +260,16 @@ paged_narrow_kernel(const PagedParams p)
                 acc[0] = fmaf(a, x.x, acc[0]); acc[1] = fmaf(a, x.y, acc[1]); acc[2] = fmaf(a, x.z, acc[2]); acc[3] = fmaf(a, x.w, acc[3]);
                 acc[4] = fmaf(a, y.x, acc[4]); acc[5] = fmaf(a, y.y, acc[5]); acc[6] = fmaf(a, y.z, acc[6]); acc[7] = fmaf(a, y.w, acc[7]);
             }
-            const float inv = sum == 0.f ? 0.f : 1.f / sum, lse = sum == 0.f ? -INFINITY : fmaf(mx, p.scale, logf(sum));
+            PagedNorm norm = paged_norm(mx, sum, p.scale);
+            if (whole) norm = paged_whole(norm);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[e] *= inv;
+            for (int e = 0; e < 8; ++e) acc[e] *= norm.inv;
             if (whole) {
                 const int row = seg.rt * L::kRows + r, t = paged_token(p, row), h = seg.kvh * p.group + row - t * p.group;
                 paged_store<T>(p, seg.b, t, h, c, acc);
-                if (c == 0) paged_store_lse(p, seg.b, t, h, lse);
+                if (c == 0) paged_store_lse(p, seg.b, t, h, norm.lse);
             } else {
-                paged_store_part<DP, L::kRows>(slot, r, c, acc, lse);
+                paged_store_part<DP, L::kRows>(slot, r, c, acc, norm.lse);
             }
         }
         if (tid == 0 && !p.cluster && seg.blk0 == 0 && !whole) seg.describe(per);

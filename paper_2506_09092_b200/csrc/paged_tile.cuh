@@ -85,7 +85,7 @@ __device__ __noinline__ void add_set_aside(const PagedParams &p, const int *page
                     const T *q = paged_q_row<T>(p, b, kvh, row);
                     float s = 0.f;
                     for (int d = 0; d < p.head_dim; ++d) s = fmaf(elem_to_float(q[d]), elem_to_float(k[d]), s);
-                    weight = xa_exp2((s - m) * p.scale_log2);
+                    weight = m == -INFINITY ? 0.f : xa_exp2((s - m) * p.scale_log2);       // (all its scores are -inf)
                 }
                 for (int c = 0; c < DP / 2; c += 16) {
                     uint32_t o[16];
@@ -395,8 +395,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             // two warps in the last block is both's here.)
             if (blocks > 0) {
                 ok = ok && wait(pv_done, block - 1);
-                // scores of -inf alone are not the same as no scores
-                if (any && m == -INFINITY) l = __int_as_float(0x7fc00000);
+                // scores of -inf alone are not the same as no scores: a mark that no sum is
+                if (any && m == -INFINITY && l == 0.f) l = -1.f;
                 xch[((block & 1) * 2 + half) * kXaRows + t] = l;
                 meet();
                 if (!ok) break;
@@ -407,8 +407,10 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             if (blocks > 0 && warp_rows)
                 add_set_aside<DP, T>(p, seg.it.row, seg.b, seg.kvh, row, mine ? seen : 0, m, half * (DP / 2), t_o, bads, key0, block, blocks,
                                      min(blocks, max(0, seen_lo - key0) / L::kBlock));
-            const float inv = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
             const bool whole = seg.whole();
+            // (a mark: the maximum is both halves', so the other's sum is 0 or a mark, too)
+            PagedNorm norm = paged_norm(l < 0.f ? kPaOnlyInf : m, l < 0.f ? 0.f : l, p.scale);
+            if (whole) norm = paged_whole(norm);
             float *part = p.part + (2LL * cta + (seg.blk0 == 0)) * L::kSlot;
             if (warp_rows) {
 #pragma unroll
@@ -427,7 +429,7 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                         for (int g = 0; g < 4; ++g) {
                             float v[8];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[8 * g + k]) * inv;
+                            for (int k = 0; k < 8; ++k) v[k] = __uint_as_float(r[8 * g + k]) * norm.inv;
                             if (whole) {
                                 paged_store<T>(p, seg.b, token, h, d0 / 8 + g, v);
                             } else {
@@ -439,8 +441,8 @@ paged_tile_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                     }
                 }
                 if (mine && half == 0) {
-                    if (whole) paged_store_lse(p, seg.b, token, h, lse);
-                    else part[L::kRows * DP + t] = lse;
+                    if (whole) paged_store_lse(p, seg.b, token, h, norm.lse);
+                    else part[L::kRows * DP + t] = norm.lse;
                 }
             }
             if (tid == 0 && seg.blk0 == 0 && !whole) seg.describe(per);
