@@ -48,7 +48,7 @@ extern "C" {
  *   strides  : multiples of 8 for dimensions larger than 1, no two elements in one place
  *              (kn_stride and vn_stride count for append only, q_stride and o_stride for attention only)
  *   dtype    : CUDALLM_BF16 or CUDALLM_F16, of everything but lse
- *   scale    : finite, >= 0 (usually 1 / sqrt(head_dim))
+ *   scale    : 0 to 2e38 (usually 1 / sqrt(head_dim))
  */
 typedef struct cudallm_paged_shape {
     int64_t batch, q_rows, q_heads, kv_heads, head_dim;

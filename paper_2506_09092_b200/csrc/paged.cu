@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <limits>
 
 #include "runtime.h"
 #include "paged_attn.cuh"
@@ -18,6 +19,7 @@ namespace {
 constexpr int64_t kMaxDim = (int64_t(1) << 31) - 1024;
 constexpr int64_t kMaxElems = int64_t(1) << 46;          // of an operand, strides included
 constexpr int64_t kMaxTmaStride = int64_t(1) << 39;      // elements
+constexpr float kMaxScale = 2.0e38f;                     // (times log2 e it is still a number)
 constexpr int64_t kPlanSms = 148;                        // the split is planned for this many SMs
 constexpr int64_t kClusterBlocks = 16;                   // blocks of keys that a CTA of a cluster may get at most,
 constexpr int64_t kClusterMore = 4;                      // and how many more than an equal share would have
@@ -66,7 +68,7 @@ int check_shape(const cudallm_paged_shape *sp)
     for (int64_t v : {s.batch, s.q_rows, s.q_heads, s.kv_heads, s.head_dim, s.pages, s.slots, s.table_cols})
         if (v < 0 || v > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
     if (s.page_rows < 1 || s.page_rows > kMaxDim) return CUDALLM_ERR_INVALID_DIM;
-    if (!(s.scale >= 0.f) || !(s.scale <= 3.0e38f)) return CUDALLM_ERR_INVALID_DIM;
+    if (!(s.scale >= 0.f) || !(s.scale <= kMaxScale)) return CUDALLM_ERR_INVALID_DIM;
     if (s.q_heads > 0 && (s.kv_heads == 0 || s.q_heads % s.kv_heads)) return CUDALLM_ERR_INVALID_DIM;
     if (s.table_cols > kMaxDim / s.page_rows) return CUDALLM_ERR_INVALID_DIM;
     if (s.slots > 1 && s.table_stride < s.table_cols) return CUDALLM_ERR_INVALID_LD;
@@ -131,9 +133,13 @@ Plan plan_attn(const cudallm_paged_shape &s)
     return f;
 }
 
-// Factor of the exponentials' arguments.  Masked scores are -inf, and -inf x 0 is no number, so a
-// scale of 0 enters as 1e-30: every finite score then gives exp2(0) = 1 all the same.
-inline float scale_log2(float scale) { return std::max(scale, 1e-30f) * 1.4426950408889634f; }
+// Factor of the exponentials' arguments.  Masked scores are -inf, and -inf x 0 is no number, so a scale that leaves nothing enters as
+// the smallest number, 2^-149: finite scores differ by less than 2^129, so their exponents by less than 2^-20, and their
+// exponentials are 1 to within that.  Other scales are taken as they are, however small.
+inline float scale_log2(float scale)
+{
+    return std::max(scale * 1.4426950408889634f, std::numeric_limits<float>::denorm_min());
+}
 
 inline XaStrides strides(const int64_t (&s)[3]) { return XaStrides{(long long)s[0], (long long)s[1], (long long)s[2]}; }
 inline PagedStrides page_strides(const int64_t (&s)[3]) { return PagedStrides{(long long)s[0], (long long)s[1], (long long)s[2]}; }
