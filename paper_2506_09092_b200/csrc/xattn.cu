@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <limits>
 
 #include "runtime.h"
 #include "xattn_fwd.cuh"
@@ -110,9 +111,13 @@ FwdPlan plan_fwd(const cudallm_xattn_shape &s)
     return f;
 }
 
-// Factor of the exponentials' arguments.  Masked scores are -inf, and -inf x 0 is no number, so a
-// scale of 0 enters as 1e-30: every finite score then gives exp2(0) = 1 all the same.
-inline float scale_log2(const cudallm_xattn_shape &s) { return std::max(s.scale, 1e-30f) * 1.4426950408889634f; }
+// Factor of the exponentials' arguments.  Masked scores are -inf, and -inf x 0 is no number, so a scale that leaves nothing enters as
+// the smallest number, 2^-149: finite scores differ by less than 2^129, so their exponents by less than 2^-20, and their
+// exponentials are 1 to within that.  Other scales are taken as they are, however small.
+inline float scale_log2(const cudallm_xattn_shape &s)
+{
+    return std::max(s.scale * 1.4426950408889634f, std::numeric_limits<float>::denorm_min());
+}
 
 // The backward call's parts (see xattn_bwd.cuh), planned for kPlanSms SMs, and where they lie in the scratch.
 struct BwdPlan {
