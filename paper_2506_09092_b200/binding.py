@@ -686,22 +686,47 @@ def _probabilities(t, dtype):
     return _PROBABILITIES.get(dtype, t.dtype) is t.dtype
 
 
+def _check_rows(name, t, batch, per, vocab, ld):
+    """Refuses a tensor whose rows do not lie where a call looks for them: batch * per rows of vocab values, one every ld elements."""
+    rows = batch * per
+    if rows <= 0:
+        return
+    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    if (1 + sum((s - 1) * d for s, d in zip(t.shape, t.stride())) if t.numel() else 0) < (rows - 1) * ld + vocab:
+        raise ValueError(f"{name}: {tuple(t.shape)} ends before {rows} rows of pitch {ld} do")
+    if rows == 1 or t.dim() < 2:                                   # (a flat buffer is taken as it is)
+        return
+    size, stride = list(t.shape), t.stride()
+    width = size.pop()
+    while size and width < vocab and stride[len(size) - 1] == width:   # several dimensions of a row's values
+        width *= size.pop()
+    good, at = width >= vocab and (width <= ld or width % ld == 0), max(width, ld)
+    for s, d in zip(reversed(size), reversed(stride[:len(size)])):
+        good = good and (s == 1 or d == at)
+        at *= s
+    if not good:
+        raise ValueError(f"{name} has sizes {tuple(t.shape)} and strides {stride}: not {rows} rows of {vocab}, one every {ld}")
+    if t.dim() > 2 and t.shape[0] == batch > 1 and t.shape[1] > per:
+        raise ValueError(f"{name}: {tuple(t.shape)} has more than {per} rows for each of {batch}")
+
+
 def draft_verify(p, q, drafts, draft_lens, u, tokens, accepted, batch, n, vocab, ldp, ldq, dtype, stream=None, check=True):
     """Drafted tokens against the target's probabilities p (batch * (n + 1) rows) and the draft's q (batch * n rows, or
-    None: the drafts were certain), by the random numbers u: tokens (batch, n + 1) and accepted (batch) are written."""
+    None: the drafts were certain), by the random numbers u: tokens (batch, n + 1) and accepted (batch) are written.  The rows
+    of p and q lie ldp and ldq elements apart, all of them: ``p[:, :n + 1]`` of a tensor with more rows a sequence is refused."""
     rows = batch * (n + 1)
     _vectors(("drafts", drafts, batch * n), ("draft_lens", draft_lens, batch), ("u", u, rows), ("tokens", tokens, rows),
              ("accepted", accepted, batch))
-    for name, t, r, ld in (("p", p, rows, ldp), ("q", q, batch * n, ldq)):
+    for name, t, per in (("drafts", drafts, n), ("u", u, n + 1), ("tokens", tokens, n + 1)):
+        if t is not None and t.__class__ is not int and t.dim() > 1 and t.shape[0] == batch > 1 and t.shape[1] > per:
+            raise ValueError(f"{name}: {tuple(t.shape)} has more than {per} for each of {batch}")
+    for name, t, per, ld in (("p", p, n + 1, ldp), ("q", q, n, ldq)):
         if t is not None and t.__class__ is not int:
-            if (t.is_contiguous() and t.numel() >= r * ld or r <= 0) and _probabilities(t, dtype):
-                continue
             if not _probabilities(t, dtype):
                 raise TypeError(f"{name} has to be of the type that dtype says, not {t.dtype}")
-            if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
-                raise ValueError(f"{name}: the last dimension must be contiguous")
-            if (1 + sum((s - 1) * d for s, d in zip(t.shape, t.stride())) if t.numel() else 0) < (r - 1) * ld + vocab:
-                raise ValueError(f"{name}: {tuple(t.shape)} ends before {r} rows of pitch {ld} do")
+            if not (t.shape == (batch, per, ld) and t.is_contiguous()):
+                _check_rows(name, t, batch, per, vocab, ld)
     st = lib().cudallm_draft_verify(*_d(p, q, drafts, draft_lens, u, tokens, accepted), batch, n, vocab, ldp, ldq, dtype,
                                     _s(stream))
     return _check(st, "cudallm_draft_verify", check)
