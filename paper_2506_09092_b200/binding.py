@@ -569,7 +569,7 @@ def paged_attn(shape, q, k, v, table, lens, slot_of, new_lens, o, lse, scratch, 
 
 class PagePools:
     """The tensors that hold a cache's pages (every layer's keys and values), as the C calls take them: a host array of
-    ``cudallm_page_pool``.  Built once; holds references to the tensors."""
+    ``cudallm_page_pool``.  Built once; holds references to the tensors.  Every call asks whether their device is the current one."""
 
     def __init__(self, tensors):
         tensors = list(tensors)
@@ -592,6 +592,10 @@ class PagePools:
         for a, b in zip(spans, spans[1:]):
             if b[0] < a[1] and not (a[2] == b[2] and (b[0] - a[0]) % a[2] >= a[3] and (b[0] - a[0]) % a[2] + b[3] <= a[2]):
                 raise ValueError("two pools overlap")
+
+    def _here(self):
+        _d(*self._keep[:1])                            # (all are on the device that was current when the table was built)
+        return self.array
 
 
 def page_pools(tensors) -> PagePools:
@@ -626,13 +630,13 @@ class PageBook:
 def _pools_of(book, pools):
     if pools is not None and pools.count and pools.pages != book.c.pages:
         raise ValueError(f"pools of {pools.pages} pages, a book of {book.c.pages}")
-    return (None, 0) if pools is None else (pools.array, pools.count)
+    return (None, 0) if pools is None else (pools._here(), pools.count)
 
 
 def pages_copy(pools, src, dst, n, stream=None, check=True):
     """Page src[i] to page dst[i] in every pool, i < n (int32 on the device)."""
     _vectors(("src", src, n), ("dst", dst, n))
-    st = lib().cudallm_pages_copy(pools.array, pools.count, pools.pages, *_d(src, dst), n, _s(stream))
+    st = lib().cudallm_pages_copy(pools._here(), pools.count, pools.pages, *_d(src, dst), n, _s(stream))
     return _check(st, "cudallm_pages_copy", check)
 
 

@@ -5,7 +5,7 @@ import torch
 
 from paper_2506_09092_b200 import binding as B
 from paper_2506_09092_b200 import build as libbuild
-from test_cache_host import append, attn, shape
+from test_cache_host import P, append, attn, shape
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -72,3 +72,40 @@ def test_vectors_with_more_than_a_sequence_has(addresses):
         with pytest.raises(ValueError, match=f"^{name}"):
             verify(**{name: bad})
     assert verify(u=torch.zeros(50), drafts=torch.zeros(7, dtype=torch.int32), tokens=torch.zeros(2, 9, dtype=torch.int32)) == B.OK
+
+
+class _OnDevice(torch.Tensor):
+    """A host tensor that says it is on a device."""
+    device_index = 0
+
+    def get_device(self):
+        return self.device_index
+
+
+def on(index, *size, dtype=torch.bfloat16):
+    t = torch.zeros(*size, dtype=dtype).as_subclass(_OnDevice)
+    t.device_index = index
+    return t
+
+
+def test_pools_of_another_device_than_the_current_one(monkeypatch):
+    """A table of pools was built under one device and a call is made under another: its addresses mean nothing there."""
+    monkeypatch.setattr(B, "lib", lambda: _Nothing())
+    monkeypatch.setattr(B, "_get_device", lambda: 0)
+    pools = B.page_pools([on(0, 50, 64), on(0, 50, 64)])
+    with pytest.raises(ValueError, match="device 1, the current device is 0"):
+        B.page_pools([on(1, 50, 64)])
+    with pytest.raises(ValueError, match="device 1, the current device is 0"):
+        B.page_pools([on(0, 50, 64), on(1, 50, 64)])
+    assert B.pages_copy(pools, P, P, 2) == B.OK
+    book, scratch = B.PageBook(50, 4, 3, 5, device="cpu"), 1 << 20
+    book.data = on(0, 80, dtype=torch.int32)
+    calls = (lambda: B.pages_resize(book, pools, None, P, 1, None, P, scratch), lambda: B.pages_compact(book, pools, None, P, scratch))
+    assert all(c() == B.OK for c in calls)
+    monkeypatch.setattr(B, "_get_device", lambda: 1)
+    book.data = on(1, 80, dtype=torch.int32)
+    for call in (lambda: B.pages_copy(pools, P, P, 2), *calls):
+        with pytest.raises(ValueError, match="device 0, the current device is 1"):
+            call()
+    assert B.pages_resize(book, None, None, P, 1, None, P, scratch) == B.OK
+    assert B.pages_copy(B.page_pools([]), P, P, 2) == B.OK
