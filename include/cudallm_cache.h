@@ -178,6 +178,8 @@ size_t cudallm_pages_fork_scratch_bytes(const cudallm_page_book *book, int64_t n
  *    shared, the new tokens would be written into another sequence's page: it gets a copy
  *    of its own instead, in all pools, unless all that share it grow in this call, in which case the first
  *    of them keeps it.
+ * With pools the copies are a launch of their own behind the book's, also where none turn out to be needed (only the
+ * device knows).  A step in which no sequence that grows shares its last page may pass count == 0 and save it.
  * New pages are the lowest free ones (those given back in this call among them), dealt out in the order
  * of the list, a sequence's copy first.
  * All or nothing: where there are not enough pages, or a length exceeds table_cols *
@@ -223,7 +225,7 @@ size_t cudallm_pages_compact_scratch_bytes(const cudallm_page_book *book);
  *   accepted   : int32, `batch` elements: a
  *   dtype      : CUDALLM_F32, _BF16 or _F16
  * Comparisons and sums are in 64 bits (the product and the difference are exact).  Probabilities need not add up
- * to one; values of r that are not positive and finite count as zero.  Where p_a has no mass
+ * to one; values of r that are not positive and finite, as fp32 has them, count as zero.  Where p_a has no mass
  * either, the token drawn is -1.  n may be 0 (a token is drawn from p_0).  Drafts behind m, and their
  * probabilities, are read but change nothing.  tokens and accepted must not overlap what is read.
  * Errors: INVALID_DTYPE, INVALID_DIM (negative; vocab 0; batch * (n + 1) or vocab > 2^31 - 1024), INVALID_LD,

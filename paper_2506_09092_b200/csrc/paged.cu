@@ -105,9 +105,13 @@ Plan plan_attn(const cudallm_paged_shape &s)
     Plan f{};
     const int64_t rows = (s.q_heads / s.kv_heads) * s.q_rows, cap = no_states(s) ? 0 : s.table_cols * s.page_rows;
     f.wide = s.head_dim > 64;
-    // More than 16 rows on a key head: by tiles of 128 on tcgen05 where TMA can bring the pages.  (Up to 32 rows and 1024
-    // states a cluster of mma.sync CTAs is as fast or faster: 32 rows x 8 key heads of 128: 9.6 against 10.2 us at 120 states,
-    // 10.8 against 11.8 at 500, 12.4 both at 1000, 20.6 against 17.0 at 4000; 64 rows: 14.3 against 10.9 at 120.)
+    // More than 16 rows on a key head: by tiles of 128 on tcgen05 where TMA can bring the pages.  Up to 32 rows and 1024
+    // states by mma.sync, in clusters or equal shares: a tile costs the same however few its rows and keys are.  (mma.sync against
+    // tiles, us.  Clusters, 32 rows x 8 key heads of 128: 9.6 / 10.2 at 120 states, 10.8 / 11.8 at 500, 12.4 / 12.4 at 1000, 20.6 /
+    // 17.0 at 4000; 64 rows: 14.3 / 10.9 at 120.  16 sequences of 8 key heads at 250 and 500 states: 20 rows 12.4 / 12.3, 15.9 / 14.9, 32
+    // rows 13.7 / 12.0, 17.0 / 14.5, of a quarter to all of 500 16.2 / 18.2; heads of 64, 32 rows 9.6 / 11.2, 11.6 / 13.6.  Equal
+    // shares, 64 sequences at 100, 250, 500: 20 rows 21.1 / 24.1, 29.7 / 32.9, 44.4 / 50.3, 32 rows 23.4 / 24.4, 32.9 / 32.4,
+    // 48.5 / 47.9, of a quarter to all of 500 34.4 / 43.1; heads of 64, 20 rows 14.5 / 21.6, 19.7 / 29.9, 27.6 / 40.6.)
     const bool tile = rows > 16 && tile_pages(s) && !(rows <= 32 && cap <= 1024);
     f.mt = tile ? 0 : (int)std::min<int64_t>(4, cdiv(rows, 16));
     const int64_t tile_rows = tile ? kXaRows : 16 * f.mt, block = tile ? kXaRows : f.wide ? 64 : 128;
@@ -125,7 +129,9 @@ Plan plan_attn(const cudallm_paged_shape &s)
         f.ctas = (int)(items * f.cluster);
         return f;
     }
-    // as many shares of every key head as fit at once, but no more than there are blocks
+    // As many shares of every key head as fit at once, but no more than there are blocks.  A whole number for each: neighbouring CTAs
+    // take the same share for the different heads (see paged_attn.cuh), at the cost of the rest of the SMs where their number
+    // is no multiple of kv_heads (40 key heads on tiles: 120 of 148).
     f.shares = (int)std::max<int64_t>(1, std::min<int64_t>((tile ? 1 : 2) * kPlanSms / s.kv_heads, s.batch * f.row_tiles * blocks));
     f.ctas = (int)(f.shares * s.kv_heads);
     f.part_bytes = f.shares == 1 ? 0 : 2 * (size_t)f.ctas * (size_t)tile_rows * ((f.wide ? 128 : 64) + 1) * sizeof(float);

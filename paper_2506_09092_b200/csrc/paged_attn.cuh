@@ -5,6 +5,10 @@
 // whose scores are all -inf.  Its weight beside any other part is zero, too, but if there are only such parts the row is no number
 // (0 / 0), where a row without keys is zero.
 //
+// Scores, maxima, sums and O are fp32 throughout.  The probabilities alone are rounded to the operands' 16 bits, since the tensor core
+// multiplies them with V: half a step each, relative to themselves, which an average over many keys mostly evens out (48 sequences, bf16:
+// O is off by 2.2e-3 of itself against 64 bits, 1.7e-3 of it its own rounding; fp16, 16 sequences: 2.9e-4 and 2.1e-4).
+//
 // Bound: HBM (K and V of every sequence are read once; 16 or 32 rows of arithmetic per key are far below
 // any pipe's rate), so what matters is bytes in flight and an even split.  The rows that share a key head (query heads x new
 // tokens) share its reading.  Up to 16 of them are one tile of mma.sync.m16n8k16 (paged_narrow.cuh: 4 sequences of 64000 states,
@@ -531,8 +535,11 @@ __device__ __forceinline__ void paged_walk_wide(const PagedParams &p, uint8_t *s
 
 // Equal shares: for each key head all blocks of keys in one line, items in order, in each the row tiles; a CTA's share of it in
 // pieces (segments) that each belong to one item and row tile.  Every row tile has kPaStart units in the line before its
-// blocks: what beginning and ending a segment costs, in blocks (128 sequences of 250 to 1000 states, 8 key heads of
-// 128: 70.2 us with 0, 67.8, 64.2 and 63.1 us with 1, 2 and 3; 48 of 1024 to 4096: 86.0 and 83.8 us with 0 and 3).
+// blocks: what beginning and ending a segment costs, in blocks.  One number for all kernels, although their blocks differ (us with
+// 0, 1, 2, 3.  One new token on 8 key heads, 128 sequences of 250 to 1000 states: heads of 128 70.0, 66.8, 63.1, 62.4, of 64
+// 45.2, 41.4, 39.8, 39.6; 48 of 1024 to 4096: 87.5, 87.8, 83.8, 83.4 and 50.5, 48.3, 48.4, 48.4.  Tiles, 40 rows on 4 key heads, 128 of
+// 300 to 1200: heads of 128 67.4, 62.8, 61.6, 60.4, of 64 57.4, 52.5, 52.9, 53.4; 48 of 1024 to 4096: 60.8, 59.1, 58.6, 58.1 and 53.0,
+// 51.9, 53.2, 53.1).
 constexpr int kPaStart = 3;
 template <int ROWS, int BLOCK> struct PagedSegments {
     const PagedParams &p;
